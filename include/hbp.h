@@ -300,6 +300,101 @@ hbp_status hbp_selftest_gate_math(const double* v, double* out, int64_t n, void*
  * for them.  HBP_ERR_UNSUPPORTED: there is no such split, the cell runs one launch per step. */
 hbp_status hbp_recurrence_plan(const hbp_config* cfg, int32_t backward, const int32_t* at_once, int64_t* plan, size_t* pack_bytes);
 
+/* ---------------------------------------------------------------- a decoder's step on its own
+ * Operators beside the decoder block of hbp_forward / hbp_backward, for callers that run layers of their own (hbp_iterate) or
+ * other shapes of attention: rotary positions, attention over ragged batches with grouped heads and its backward pass, and
+ * activations kept in 8 bits with their use in GELU's backward pass.  They keep no state and allocate nothing; calls on
+ * different streams are independent as long as their buffers are.  All can be captured into a CUDA graph.
+ *
+ * A tensor [rows][heads][head_dim]: element (row, head, c) lies at x + row * row_stride + head * head_stride + c, strides in
+ * elements, so that queries, keys and values may be parts of one buffer.  Pointers 16-byte aligned, strides multiples of
+ * 16 bytes. */
+typedef struct {
+  void* x;
+  int64_t row_stride, head_stride;
+} hbp_heads;
+
+/* Rotary positions.  The first rotary_dim channels of every head turn in pairs, pair i by the angle pos * f_i with
+ * f_i = base^(-2 i / rotary_dim):  (a, b) -> amplitude * (a cos - b sin, b cos + a sin).  The other channels are copied.
+ *  layout    HALF: pair i is channels (i, i + rotary_dim / 2); INTERLEAVED: channels (2 i, 2 i + 1).
+ *  scaling   for contexts longer than the trained ones: NONE; LINEAR: f_i / factor; BY_PARTS: with
+ *            w = clamp((trained_length * f_i / 2 pi - slow) / (fast - slow), 0, 1), f_i * (w + (1 - w) / factor): channels that turn
+ *            at least `fast` times over the trained length are kept, those that turn at most `slow` times are slowed down.
+ *  amplitude times cosine and sine (1 = a pure rotation). */
+typedef enum { HBP_ROTARY_HALF = 0, HBP_ROTARY_INTERLEAVED = 1 } hbp_rotary_layout;
+typedef enum { HBP_ROTARY_NONE = 0, HBP_ROTARY_LINEAR = 1, HBP_ROTARY_BY_PARTS = 2 } hbp_rotary_scaling;
+typedef struct {
+  int32_t layout, scaling;
+  int32_t rotary_dim; /* even, 2 .. head_dim */
+  float base;         /* > 1 */
+  float factor;       /* >= 1; LINEAR, BY_PARTS */
+  float trained_length, fast, slow; /* BY_PARTS; fast > slow */
+  float amplitude;
+} hbp_rotary_spec;
+
+/* Turns q_heads heads of q into q_out and kv_heads heads of k into k_out (kv_heads may be 0; k and k_out are then ignored),
+ * `rows` rows each, in one launch.  inverse != 0: by the opposite angles, which is the gradient (same amplitude).  An output
+ * may be its input (same pointer and strides); otherwise they must not overlap.
+ * The position of a row: positions[row] (device, int32 if position_bytes is 4, int64 if 8), or, where positions is NULL,
+ * first + row % period (period 0: first + row).  Angles are formed in double (|positions| up to 2^53 / rotary turns), the
+ * rotation in float, and rounded once to dtype.  head_dim up to 256. */
+hbp_status hbp_rotary(const hbp_rotary_spec* spec, int32_t inverse, int32_t dtype, int64_t rows, int32_t q_heads, int32_t kv_heads,
+                      int32_t head_dim, const void* positions, int32_t position_bytes, int64_t first, int64_t period,
+                      const hbp_heads* q, const hbp_heads* q_out, const hbp_heads* k, const hbp_heads* k_out, void* cuda_stream);
+
+/* Attention over `sequences` pairs of sequences: the queries of sequence b attend to its keys, o = softmax(scale * q k^T) v.
+ *  heads     query head h reads key / value head h / (q_heads / kv_heads); q_heads is a multiple of kv_heads.
+ *  offsets   device int32 [sequences + 1]: sequence b is rows offsets[b] .. offsets[b + 1] - 1 of the tensors; q_len (kv_len) is then
+ *            the longest of them.  NULL: all sequences are q_len (kv_len) long, one after the other.  Empty sequences are
+ *            allowed.  Rows of q_rows (kv_rows) in no sequence are neither read nor written.
+ *  causal    query i of n sees keys 0 .. i + (kv_n - n): the last query sees the last key.
+ * A query that sees no key has output 0, log-sum-exp -infinity and gradient 0.  A sequence whose offsets decrease, leave the tensor or
+ * span more than q_len (kv_len) rows is skipped, and *status (device int32, may be NULL; zeroed by the caller) becomes
+ * HBP_ERR_INVALID_ARG; a bounded wait that runs out makes it HBP_ERR_TIMEOUT and leaves outputs incomplete.
+ * head_dim up to 128, a multiple of 16 bytes. */
+typedef struct {
+  int32_t dtype, causal;
+  int32_t sequences, q_heads, kv_heads, head_dim;
+  int32_t q_len, kv_len;
+  int64_t q_rows, kv_rows;
+  const int32_t *q_offsets, *kv_offsets;
+  float scale;
+  int32_t* status;
+} hbp_attention;
+
+/* o [q_rows][q_heads][head_dim] and lse [q_heads][q_rows] (float, natural logarithm), which the backward pass reads. */
+hbp_status hbp_attention_forward(const hbp_attention* a, const hbp_heads* q, const hbp_heads* k, const hbp_heads* v,
+                                 const hbp_heads* o, float* lse, void* cuda_stream);
+
+/* Gradients of q, k and v (OVERWRITTEN) from that of o.  The probabilities are formed again from q, k and lse; nothing of
+ * the size of q_len x kv_len is stored.  Every output element is summed by one thread block in a fixed order: runs agree bit for bit.
+ * scratch: device memory of hbp_attention_scratch_bytes bytes, 16-byte aligned, not shared by calls that may overlap. */
+hbp_status hbp_attention_scratch_bytes(const hbp_attention* a, size_t* bytes);
+hbp_status hbp_attention_backward(const hbp_attention* a, const hbp_heads* d_o, const hbp_heads* q, const hbp_heads* k,
+                                  const hbp_heads* v, const hbp_heads* o, const float* lse, const hbp_heads* dq, const hbp_heads* dk,
+                                  const hbp_heads* dv, void* scratch, size_t scratch_bytes, void* cuda_stream);
+
+/* Activations in 8 bits.  Highway-BP's all-layer VJPs need the activations of every layer at once; kept like this they take 1.03
+ * bytes a value.  Of every row each 32 consecutive channels (the last group may be shorter) share a power of two 2^e, the smallest
+ * (e >= -126) with max |x| <= 127 * 2^e; codes [rows][d] (int8) are x / 2^e rounded to the nearest whole number (ties to even),
+ * scales [rows][(d + 31) / 32] (uint8) are e + 127.  Every stored value is a bf16 number: reading it back is exact in both dtypes,
+ * and is off by at most 2^(e-1) from x (2^e where x is 63.5 * 2^122 or more: 2^128 is no float).  A group that holds an infinity or a NaN has scale 255 and is read back as NaN throughout.
+ * ld* are elements between rows of the dtype tensors (>= d, multiples of 16 bytes); codes and scales have none.  codes 16-byte
+ * aligned.  rows may be 0.
+ *  store          codes, scales of x
+ *  load           x of codes, scales
+ *  gelu           act = gelu(z) from z itself (act may be z), and z's codes and scales
+ *  gelu_backward  dz = d_act * gelu'(z8) (dz may be d_act) and, where act is given, gelu(z8), z8 being the stored values */
+hbp_status hbp_checkpoint_store(int32_t dtype, int64_t rows, int32_t d, const void* x, int64_t ldx, int8_t* codes, uint8_t* scales,
+                                void* cuda_stream);
+hbp_status hbp_checkpoint_load(int32_t dtype, int64_t rows, int32_t d, const int8_t* codes, const uint8_t* scales, void* x, int64_t ldx,
+                               void* cuda_stream);
+hbp_status hbp_checkpoint_gelu(int32_t dtype, int64_t rows, int32_t d, const void* z, int64_t ldz, void* act, int64_t lda,
+                               int8_t* codes, uint8_t* scales, void* cuda_stream);
+hbp_status hbp_checkpoint_gelu_backward(int32_t dtype, int64_t rows, int32_t d, const int8_t* codes, const uint8_t* scales,
+                                        const void* d_act, int64_t ldd, void* dz, int64_t ldz, void* act, int64_t lda,
+                                        void* cuda_stream);
+
 const char* hbp_status_string(hbp_status s);
 void hbp_destroy(hbp_ctx* ctx);
 

@@ -25,6 +25,8 @@ EXPORTS = ["hbp_workspace_bytes", "hbp_create", "hbp_forward", "hbp_backward", "
            "hbp_context_modes", "hbp_selftest_wait_timeout", "hbp_selftest_gate_math", "hbp_recurrence_plan",
            "hbp_profile_enable", "hbp_profile_read", "hbp_cumsumprod_static", "hbp_cumsumprod_static_max_bytes",
            "hbp_compare_scratch_bytes", "hbp_compare", "hbp_iterate", "hbp_add_carry", "hbp_param_grads",
+           "hbp_rotary", "hbp_attention_forward", "hbp_attention_scratch_bytes", "hbp_attention_backward",
+           "hbp_checkpoint_store", "hbp_checkpoint_load", "hbp_checkpoint_gelu", "hbp_checkpoint_gelu_backward",
            "hbp_status_string", "hbp_destroy"]
 
 
@@ -47,6 +49,26 @@ class hbp_params(C.Structure):
 
 class hbp_grads(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("dW1", "dW2", "dW", "dU", "dWq", "dWk", "dWv", "dWo", "da")]
+
+
+class hbp_heads(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class hbp_rotary_spec(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("scaling", C.c_int32), ("rotary_dim", C.c_int32), ("base", C.c_float), ("factor", C.c_float),
+                ("trained_length", C.c_float), ("fast", C.c_float), ("slow", C.c_float), ("amplitude", C.c_float)]
+
+
+class hbp_attention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("causal", C.c_int32), ("sequences", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("q_len", C.c_int32), ("kv_len", C.c_int32), ("q_rows", C.c_int64), ("kv_rows", C.c_int64),
+                ("q_offsets", C.c_void_p), ("kv_offsets", C.c_void_p), ("scale", C.c_float), ("status", C.c_void_p)]
+
+
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "by_parts": 2}
+CHECKPOINT_GROUP = 32
 
 
 def _load():
@@ -75,6 +97,15 @@ def _load():
     lib.hbp_param_grads.argtypes = [vp, C.POINTER(hbp_params), vp, vp, vp, C.POINTER(hbp_grads), vp]
     lib.hbp_compare_scratch_bytes.argtypes = [i32]
     lib.hbp_compare.argtypes = [i32, i32, i64, vp, vp, vp, vp, sz, vp]
+    heads = C.POINTER(hbp_heads)
+    lib.hbp_rotary.argtypes = [C.POINTER(hbp_rotary_spec), i32, i32, i64, i32, i32, i32, vp, i32, i64, i64, heads, heads, heads, heads, vp]
+    lib.hbp_attention_forward.argtypes = [C.POINTER(hbp_attention), heads, heads, heads, heads, vp, vp]
+    lib.hbp_attention_scratch_bytes.argtypes = [C.POINTER(hbp_attention), C.POINTER(sz)]
+    lib.hbp_attention_backward.argtypes = [C.POINTER(hbp_attention)] + [heads] * 5 + [vp] + [heads] * 3 + [vp, sz, vp]
+    lib.hbp_checkpoint_store.argtypes = [i32, i64, i32, vp, i64, vp, vp, vp]
+    lib.hbp_checkpoint_load.argtypes = [i32, i64, i32, vp, vp, vp, i64, vp]
+    lib.hbp_checkpoint_gelu.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, vp, vp]
+    lib.hbp_checkpoint_gelu_backward.argtypes = [i32, i64, i32, vp, vp, vp, i64, vp, i64, vp, i64, vp]
     lib.hbp_sync_status.argtypes = [vp, vp]
     lib.hbp_profile_enable.argtypes = [vp, i32]
     lib.hbp_profile_read.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(i64)]
@@ -370,3 +401,194 @@ def compare(a, b, segments=1):
     _check(lib.hbp_compare(_dtype_code(a.dtype), segments, a.numel() // segments, _ptr(a), _ptr(b), _ptr(out),
                            _ptr(scratch), need, _stream()), "hbp_compare")
     return out
+
+
+# ---- a decoder's step on its own: rotary positions, attention over ragged batches, activations in 8 bits --------------------
+def _here(name, *tensors):
+    """Refuses tensors of another device than the current one: the library launches on the current device's stream."""
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != at):
+            raise HbpError(1, f"{name}: a tensor is on {t.device}, the current device is cuda:{at}")
+
+
+def _shape(ok, name, what):
+    if not ok:
+        raise HbpError(2, f"{name}: {what}")
+
+
+def _heads(t, name):
+    """hbp_heads of a tensor [rows, heads, head_dim] whose channels are contiguous (any other strides)."""
+    _shape(t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] == 1), name, "wanted [rows, heads, head_dim] with contiguous channels")
+    # (torch gives dimensions of one element any stride)
+    return hbp_heads(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _matrix(t, name):
+    _shape(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), name, "wanted [rows, channels] with contiguous channels")
+    # (a single row has no stride of its own)
+    return _ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def rotary_spec(rotary_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained_length=0.0, fast=32.0, slow=1.0,
+                amplitude=1.0) -> hbp_rotary_spec:
+    if layout not in ROTARY_LAYOUTS or scaling not in ROTARY_SCALINGS:
+        raise HbpError(6, f"rotary layout {layout!r}, scaling {scaling!r}")
+    return hbp_rotary_spec(ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], rotary_dim, base, factor, trained_length, fast, slow, amplitude)
+
+
+def rotary(q, k=None, positions=None, first=0, period=0, rotary_dim=None, base=10000.0, layout="half", scaling="none", factor=1.0,
+           trained_length=0.0, fast=32.0, slow=1.0, amplitude=1.0, inverse=False, q_out=None, k_out=None):
+    """Rotary positions on q [rows, heads, head_dim] and, in the same launch, k [rows, kv_heads, head_dim]: see hbp_rotary.
+    Returns (q_out, k_out), new tensors unless given (they may be q and k themselves); ``inverse`` is the gradient.
+    ``positions``: int32 or int64 [rows] on the device, or None for first + row % period (period 0: first + row)."""
+    _here("rotary", q, k, positions, q_out, k_out)
+    rows, q_heads, head_dim = q.shape
+    spec = rotary_spec(head_dim if rotary_dim is None else rotary_dim, base, layout, scaling, factor, trained_length, fast, slow, amplitude)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    _shape(q_out.shape == q.shape and q_out.dtype == q.dtype, "rotary", "q_out is not like q")
+    kv_heads, kh, ko = 0, None, None
+    if k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+        _shape(k.dim() == 3 and k.shape[0] == rows and k.shape[2] == head_dim and k.dtype == q.dtype, "rotary", "k is not like q")
+        _shape(k_out.shape == k.shape and k_out.dtype == k.dtype, "rotary", "k_out is not like k")
+        kv_heads, kh, ko = k.shape[1], C.byref(_heads(k, "rotary k")), C.byref(_heads(k_out, "rotary k_out"))
+    size = 0
+    if positions is not None:
+        _shape(positions.shape == (rows,) and positions.is_contiguous() and positions.dtype in (torch.int32, torch.int64), "rotary",
+               "positions: wanted int32 or int64 [rows]")
+        size = positions.element_size()
+    _check(lib.hbp_rotary(C.byref(spec), int(inverse), _dtype_code(q.dtype), rows, q_heads, kv_heads, head_dim, _ptr(positions), size,
+                          first, period, C.byref(_heads(q, "rotary q")), C.byref(_heads(q_out, "rotary q_out")), kh, ko, _stream()), "hbp_rotary")
+    return q_out, k_out
+
+
+def _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status):
+    _shape(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.shape[2] == q.shape[2], name, "q, k and v do not belong together")
+    _shape(q.dtype == k.dtype == v.dtype, name, "q, k and v differ in type")
+    for off in (q_offsets, kv_offsets):
+        if off is None:
+            continue
+        _shape(off.dim() == 1 and off.is_contiguous() and off.dtype == torch.int32 and off.numel() >= 1, name, "offsets: wanted int32 [sequences + 1]")
+        _shape(sequences is None or sequences == off.numel() - 1, name, "offsets of another number of sequences")
+        sequences = off.numel() - 1
+    if sequences is None:
+        sequences = 1
+    if q_len is None:
+        _shape(q_offsets is None, name, "q_len, the longest of the sequences, has to be given with q_offsets")
+        q_len = q.shape[0] // sequences if sequences else 0
+    if kv_len is None:
+        _shape(kv_offsets is None, name, "kv_len, the longest of the sequences, has to be given with kv_offsets")
+        kv_len = k.shape[0] // sequences if sequences else 0
+    _shape(status is None or (status.dtype == torch.int32 and status.numel() >= 1), name, "status: wanted an int32 tensor")
+    return hbp_attention(_dtype_code(q.dtype), int(causal), sequences, q.shape[1], k.shape[1], q.shape[2], q_len, kv_len, q.shape[0], k.shape[0],
+                         _ptr(q_offsets), _ptr(kv_offsets), q.shape[2] ** -0.5 if scale is None else scale, _ptr(status))
+
+
+def attention_forward(q, k, v, sequences=None, q_len=None, kv_len=None, q_offsets=None, kv_offsets=None, causal=True, scale=None,
+                      o=None, lse=None, status=None):
+    """softmax(scale q k^T) v over pairs of sequences: see hbp_attention_forward.  q [q_rows, q_heads, head_dim], k and v
+    [kv_rows, kv_heads, head_dim]; returns o like q and lse [q_heads, q_rows] (float).  Without offsets the rows are ``sequences``
+    sequences of equal length; with them (int32 [sequences + 1], on the device) q_len / kv_len are the longest ones'."""
+    _here("attention_forward", q, k, v, q_offsets, kv_offsets, o, lse, status)
+    a = _attention("attention_forward", q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
+    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if o is None else o
+    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device) if lse is None else lse
+    _shape(o.shape == q.shape and o.dtype == q.dtype, "attention_forward", "o is not like q")
+    _shape(lse.shape == (q.shape[1], q.shape[0]) and lse.is_contiguous() and lse.dtype == torch.float32, "attention_forward", "lse: wanted float [q_heads, q_rows]")
+    _check(lib.hbp_attention_forward(C.byref(a), C.byref(_heads(q, "q")), C.byref(_heads(k, "k")), C.byref(_heads(v, "v")),
+                                     C.byref(_heads(o, "o")), _ptr(lse), _stream()), "hbp_attention_forward")
+    return o, lse
+
+
+def attention_backward(d_o, q, k, v, o, lse, sequences=None, q_len=None, kv_len=None, q_offsets=None, kv_offsets=None, causal=True,
+                       scale=None, dq=None, dk=None, dv=None, scratch=None, status=None):
+    """The gradients (dq, dk, dv) of attention_forward's q, k and v from that of its output: see hbp_attention_backward."""
+    _here("attention_backward", d_o, q, k, v, o, lse, q_offsets, kv_offsets, dq, dk, dv, scratch, status)
+    a = _attention("attention_backward", q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
+    for t, like in ((d_o, q), (o, q), (dq, q), (dk, k), (dv, v)):
+        _shape(t.shape == like.shape and t.dtype == like.dtype, "attention_backward", "a gradient is not like its tensor")
+    _shape(lse.shape == (q.shape[1], q.shape[0]) and lse.is_contiguous() and lse.dtype == torch.float32, "attention_backward", "lse: wanted float [q_heads, q_rows]")
+    need = 4 * lse.numel()
+    if scratch is None:
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib.hbp_attention_backward(C.byref(a), C.byref(_heads(d_o, "d_o")), C.byref(_heads(q, "q")), C.byref(_heads(k, "k")),
+                                      C.byref(_heads(v, "v")), C.byref(_heads(o, "o")), _ptr(lse), C.byref(_heads(dq, "dq")),
+                                      C.byref(_heads(dk, "dk")), C.byref(_heads(dv, "dv")), _ptr(scratch),
+                                      scratch.numel() * scratch.element_size(), _stream()), "hbp_attention_backward")
+    return dq, dk, dv
+
+
+def attention_scratch_bytes(q_heads, q_rows) -> int:
+    """Bytes of the scratch of attention_backward."""
+    a = hbp_attention(HBP_F32, 0, 0, q_heads, q_heads, 4, 0, 0, q_rows, 0, None, None, 1.0, None)
+    n = C.c_size_t(0)
+    _check(lib.hbp_attention_scratch_bytes(C.byref(a), C.byref(n)), "hbp_attention_scratch_bytes")
+    return n.value
+
+
+def _kept(rows, d, codes, scales, device, name):
+    groups = (d + CHECKPOINT_GROUP - 1) // CHECKPOINT_GROUP
+    codes = torch.empty((rows, d), dtype=torch.int8, device=device) if codes is None else codes
+    scales = torch.empty((rows, groups), dtype=torch.uint8, device=device) if scales is None else scales
+    _shape(codes.shape == (rows, d) and codes.is_contiguous() and codes.dtype == torch.int8, name, "codes: wanted int8 [rows, channels]")
+    _shape(scales.shape == (rows, groups) and scales.is_contiguous() and scales.dtype == torch.uint8, name, "scales: wanted uint8 [rows, channels / 32 rounded up]")
+    return codes, scales
+
+
+def checkpoint_store(x, codes=None, scales=None):
+    """x [rows, channels] in 8 bits: (codes int8 like x, scales uint8 [rows, channels / 32 rounded up]); see hbp_checkpoint_store."""
+    _here("checkpoint_store", x, codes, scales)
+    px, ld = _matrix(x, "checkpoint_store")
+    rows, d = x.shape
+    codes, scales = _kept(rows, d, codes, scales, x.device, "checkpoint_store")
+    _check(lib.hbp_checkpoint_store(_dtype_code(x.dtype), rows, d, px, ld, _ptr(codes), _ptr(scales), _stream()), "hbp_checkpoint_store")
+    return codes, scales
+
+
+def checkpoint_load(codes, scales, dtype=torch.bfloat16, out=None):
+    """The values that checkpoint_store kept, exactly, in dtype."""
+    _here("checkpoint_load", codes, scales, out)
+    _shape(codes.dim() == 2, "checkpoint_load", "codes: wanted int8 [rows, channels]")
+    rows, d = codes.shape
+    codes, scales = _kept(rows, d, codes, scales, codes.device, "checkpoint_load")
+    out = torch.empty((rows, d), dtype=dtype, device=codes.device) if out is None else out
+    _shape(out.shape == codes.shape, "checkpoint_load", "out is not like codes")
+    px, ld = _matrix(out, "checkpoint_load")
+    _check(lib.hbp_checkpoint_load(_dtype_code(out.dtype), rows, d, _ptr(codes), _ptr(scales), px, ld, _stream()), "hbp_checkpoint_load")
+    return out
+
+
+def checkpoint_gelu(z, act=None, codes=None, scales=None):
+    """(gelu(z), codes, scales): GELU of z [rows, channels] (``act`` may be z itself), and z in 8 bits for the backward pass."""
+    _here("checkpoint_gelu", z, act, codes, scales)
+    pz, ldz = _matrix(z, "checkpoint_gelu")
+    rows, d = z.shape
+    codes, scales = _kept(rows, d, codes, scales, z.device, "checkpoint_gelu")
+    act = torch.empty((rows, d), dtype=z.dtype, device=z.device) if act is None else act
+    _shape(act.shape == z.shape and act.dtype == z.dtype, "checkpoint_gelu", "act is not like z")
+    pa, lda = _matrix(act, "checkpoint_gelu")
+    _check(lib.hbp_checkpoint_gelu(_dtype_code(z.dtype), rows, d, pz, ldz, pa, lda, _ptr(codes), _ptr(scales), _stream()), "hbp_checkpoint_gelu")
+    return act, codes, scales
+
+
+def checkpoint_gelu_backward(d_act, codes, scales, with_act=False, dz=None, act=None):
+    """dz = d_act * gelu'(z8) (``dz`` may be d_act itself) from the z that checkpoint_gelu kept, and with ``with_act`` (or
+    ``act`` given) gelu(z8) too, the operand of the following product's weight gradient: dz, or (dz, act)."""
+    _here("checkpoint_gelu_backward", d_act, codes, scales, dz, act)
+    pd, ldd = _matrix(d_act, "checkpoint_gelu_backward")
+    rows, d = d_act.shape
+    codes, scales = _kept(rows, d, codes, scales, d_act.device, "checkpoint_gelu_backward")
+    dz = torch.empty((rows, d), dtype=d_act.dtype, device=d_act.device) if dz is None else dz
+    if with_act and act is None:
+        act = torch.empty((rows, d), dtype=d_act.dtype, device=d_act.device)
+    for t in (dz, act):
+        _shape(t is None or (t.shape == d_act.shape and t.dtype == d_act.dtype), "checkpoint_gelu_backward", "an output is not like d_act")
+    pz, ldz = _matrix(dz, "checkpoint_gelu_backward")
+    pa, lda = (None, 0) if act is None else _matrix(act, "checkpoint_gelu_backward")
+    _check(lib.hbp_checkpoint_gelu_backward(_dtype_code(d_act.dtype), rows, d, _ptr(codes), _ptr(scales), pd, ldd, pz, ldz, pa, lda, _stream()),
+           "hbp_checkpoint_gelu_backward")
+    return dz if act is None else (dz, act)

@@ -1,0 +1,469 @@
+// Attention over ragged batches with grouped heads (hbp_attention_forward / _backward): argument checks, and the CUDA-core
+// kernels, which are those of float tensors.
+//
+// With s_ij = scale * q_i . k_j over the keys j that query i sees:
+//   forward    o_i = sum_j p_ij v_j,  p_ij = exp(s_ij - lse_i), lse_i = log sum_j exp(s_ij): one pass over the keys with a
+//              running maximum and sum; what was summed before is scaled down when the maximum grows.
+//   backward   p_ij again from q, k and lse; D_i = d_o_i . o_i; ds_ij = p_ij (d_o_i . v_j - D_i);
+//              dv_j = sum_i p_ij d_o_i, dk_j = scale sum_i ds_ij q_i, dq_i = scale sum_j ds_ij k_j.
+// Blocks own 64 queries (forward, dq) or 64 keys of a key head (dk, dv: all query heads of its group), so that every sum
+// has one owner and one order.  Tiles of 64 rows lie in shared memory row by row, 16 bytes between rows more than they need, which
+// keeps the 16-byte reads of neighbouring rows in different banks; a thread forms 4 x 4 products of a score tile, or 4 rows times
+// every 16th vector of an output.  Bound by the FFMA pipe and the shared-memory reads that feed it (one 16-byte read per 8
+// FFMA in the scores).
+#include <cmath>
+
+#include "attention_ragged.cuh"
+
+namespace hbp {
+
+namespace {
+
+constexpr int TILE = 64, THREADS = 256;
+constexpr int PS = TILE + 4;  // floats between rows of a score tile
+
+template <int HD>
+constexpr int kStride = HD + 4;
+
+// `TILE` rows of a tensor from row r0 of a sequence of n rows on into shared memory as float, zeros behind the sequence's end and
+// behind channel `width`.  base: the sequence's first row of one head.
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p) {
+  const uint2 raw = *reinterpret_cast<const uint2*>(p);
+  const T* e = reinterpret_cast<const T*>(&raw);
+  return make_float4(to_f(e[0]), to_f(e[1]), to_f(e[2]), to_f(e[3]));
+}
+template <>
+__device__ __forceinline__ float4 load4<float>(const float* p) {
+  return *reinterpret_cast<const float4*>(p);
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
+  const T e[4] = {from_f<T>(a), from_f<T>(b), from_f<T>(c), from_f<T>(d)};
+  *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(e);
+}
+template <>
+__device__ __forceinline__ void store4<float>(float* p, float a, float b, float c, float d) {
+  *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
+template <typename T, int HD>
+__device__ __forceinline__ void load_tile(float* __restrict__ dst, const T* __restrict__ base, int64_t row_stride, int r0, int n, int width) {
+  constexpr int VECS = HD / 4;
+  for (int i = threadIdx.x; i < TILE * VECS; i += THREADS) {
+    const int r = i / VECS, c = (i % VECS) * 4;
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (r0 + r < n && c < width) v = load4<T>(base + (int64_t)(r0 + r) * row_stride + c);
+    *reinterpret_cast<float4*>(dst + r * kStride<HD> + c) = v;
+  }
+}
+
+// s[r][c] = sum over channels of A[ty * 4 + r] * B[tx + 16 * c]
+template <int HD>
+__device__ __forceinline__ void score_tile(const float* __restrict__ A, const float* __restrict__ B, int ty, int tx, float (&s)[4][4]) {
+  constexpr int LD = kStride<HD>;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) s[r][c] = 0.0f;
+#pragma unroll 4
+  for (int k = 0; k < HD; k += 4) {
+    float4 a[4], b[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) a[r] = *reinterpret_cast<const float4*>(A + (ty * 4 + r) * LD + k);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) b[c] = *reinterpret_cast<const float4*>(B + (tx + 16 * c) * LD + k);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[r][c] = fmaf(a[r].x, b[c].x, fmaf(a[r].y, b[c].y, fmaf(a[r].z, b[c].z, fmaf(a[r].w, b[c].w, s[r][c]))));
+  }
+}
+
+// acc[r][4 v + e] += sum over rows j of W[j][ty * 4 + r] * X[j][(tx + 16 v) * 4 + e]; W has PS floats a row
+template <int HD>
+__device__ __forceinline__ void add_product(const float* __restrict__ W, const float* __restrict__ X, int ty, int tx, float (&acc)[4][HD / 16]) {
+  constexpr int LD = kStride<HD>;
+#pragma unroll 4
+  for (int j = 0; j < TILE; ++j) {
+    const float4 w = *reinterpret_cast<const float4*>(W + j * PS + ty * 4);
+    const float wr[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int v = 0; v < HD / 64; ++v) {
+      const float4 x = *reinterpret_cast<const float4*>(X + j * LD + (tx + 16 * v) * 4);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        acc[r][4 * v] = fmaf(wr[r], x.x, acc[r][4 * v]);
+        acc[r][4 * v + 1] = fmaf(wr[r], x.y, acc[r][4 * v + 1]);
+        acc[r][4 * v + 2] = fmaf(wr[r], x.z, acc[r][4 * v + 2]);
+        acc[r][4 * v + 3] = fmaf(wr[r], x.w, acc[r][4 * v + 3]);
+      }
+    }
+  }
+}
+
+template <typename T, int HD>
+__device__ __forceinline__ void store_rows(T* __restrict__ base, int64_t row_stride, int r0, int n, int width, int ty, int tx, float mul,
+                                           const float (&acc)[4][HD / 16]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = r0 + ty * 4 + r;
+    if (row >= n) continue;
+#pragma unroll
+    for (int v = 0; v < HD / 64; ++v) {
+      const int c = (tx + 16 * v) * 4;
+      if (c < width)
+        store4<T>(base + (int64_t)row * row_stride + c, mul * acc[r][4 * v], mul * acc[r][4 * v + 1], mul * acc[r][4 * v + 2], mul * acc[r][4 * v + 3]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------- forward
+template <typename T, int HD>
+__global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_constant__ RaggedAttn p) {
+  extern __shared__ float4 smem4[];
+  constexpr int LD = kStride<HD>;
+  float* sQ = reinterpret_cast<float*>(smem4);
+  float* sK = sQ + TILE * LD;
+  float* sV = sK + TILE * LD;
+  float* sPt = sV + TILE * LD;  // [key][query]
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const BlockOf w = block_of(p.a.q_len, TILE, p.a.q_heads, true);
+  const SeqPair sq = sequence_pair(p.a, w.b);
+  const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
+  if (q0 >= sq.nq) return;
+  const T* q = (const T*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride;
+  const T* k = (const T*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
+  const T* v = (const T*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
+  const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;  // query i sees keys 0 .. i + shift (capped by nk)
+  const int seen = min(sq.nk, p.a.causal ? min(q0 + TILE, sq.nq) + shift : sq.nk);
+  load_tile<T, HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+  float acc[4][HD / 16], m[4], l[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < HD / 16; ++e) acc[r][e] = 0.0f;
+  }
+  for (int k0 = 0; k0 < seen; k0 += TILE) {
+    __syncthreads();
+    load_tile<T, HD>(sK, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    load_tile<T, HD>(sV, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+    __syncthreads();
+    float s[4][4];
+    score_tile<HD>(sQ, sK, ty, tx, s);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int last = min(sq.nk - 1, p.a.causal ? q0 + ty * 4 + r + shift : sq.nk - 1);  // the last key this query sees
+      float top = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[r][c] = k0 + tx + 16 * c <= last ? s[r][c] * p.a.scale : -INFINITY;
+        top = fmaxf(top, s[r][c]);
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float mn = fmaxf(m[r], top), ref = mn == -INFINITY ? 0.0f : mn;  // (a row that has seen nothing yet)
+      const float keep = expf(m[r] - ref);
+      m[r] = mn;
+      float sum = 0.0f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[r][c] = expf(s[r][c] - ref);
+        sum += s[r][c];
+      }
+      l[r] = l[r] * keep + sum;
+#pragma unroll
+      for (int e = 0; e < HD / 16; ++e) acc[r][e] *= keep;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<float4*>(sPt + (tx + 16 * c) * PS + ty * 4) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
+    __syncthreads();
+    add_product<HD>(sPt, sV, ty, tx, acc);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
+    const float inv = l[r] > 0.0f ? 1.0f / l[r] : l[r];  // nothing seen: zeros (a sum that is NaN stays NaN)
+#pragma unroll
+    for (int e = 0; e < HD / 16; ++e) acc[r][e] *= inv;
+    const int row = q0 + ty * 4 + r;
+    if (tx == 0 && row < sq.nq) p.lse[w.h * p.a.q_rows + sq.q0 + row] = l[r] == 0.0f ? -INFINITY : m[r] + logf(l[r]);
+  }
+  store_rows<T, HD>((T*)p.o.x + sq.q0 * p.o.row_stride + w.h * p.o.head_stride, p.o.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, 1.0f, acc);
+}
+
+// ------------------------------------------------------------------------------------------- backward
+// p and ds of one 64 x 64 tile; rows are queries.  lse, dd: those of this thread's four queries.
+template <int HD>
+__device__ __forceinline__ void probabilities(const float* sQ, const float* sK, const float* sG, const float* sV, int ty, int tx, int q0, int k0,
+                                              const SeqPair& sq, const RaggedAttn& p, int shift, const float (&lse)[4], const float (&dd)[4],
+                                              float (&pr)[4][4], float (&ds)[4][4]) {
+  score_tile<HD>(sQ, sK, ty, tx, pr);
+  score_tile<HD>(sG, sV, ty, tx, ds);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = q0 + ty * 4 + r, last = row < sq.nq ? min(sq.nk - 1, p.a.causal ? row + shift : sq.nk - 1) : -1;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const bool vis = k0 + tx + 16 * c <= last;
+      pr[r][c] = vis ? expf(pr[r][c] * p.a.scale - lse[r]) : 0.0f;
+      ds[r][c] = vis ? pr[r][c] * (ds[r][c] - dd[r]) : 0.0f;
+    }
+  }
+}
+__device__ __forceinline__ void row_statistics(const RaggedAttn& p, const SeqPair& sq, int h, int q0, int ty, float (&lse)[4], float (&dd)[4]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = q0 + ty * 4 + r;
+    const int64_t at = h * p.a.q_rows + sq.q0 + row;
+    lse[r] = row < sq.nq ? p.lse[at] : 0.0f;
+    dd[r] = row < sq.nq ? p.drow[at] : 0.0f;
+  }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(THREADS) ragged_dq_kernel(const __grid_constant__ RaggedAttn p) {
+  extern __shared__ float4 smem4[];
+  constexpr int LD = kStride<HD>;
+  float* sQ = reinterpret_cast<float*>(smem4);
+  float* sG = sQ + TILE * LD;
+  float* sK = sG + TILE * LD;
+  float* sV = sK + TILE * LD;
+  float* sSt = sV + TILE * LD;  // [key][query]
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const BlockOf w = block_of(p.a.q_len, TILE, p.a.q_heads, true);
+  const SeqPair sq = sequence_pair(p.a, w.b);
+  const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
+  if (q0 >= sq.nq) return;
+  const T* k = (const T*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
+  const T* v = (const T*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
+  const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
+  const int seen = min(sq.nk, p.a.causal ? min(q0 + TILE, sq.nq) + shift : sq.nk);
+  load_tile<T, HD>(sQ, (const T*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+  load_tile<T, HD>(sG, (const T*)p.d_o.x + sq.q0 * p.d_o.row_stride + w.h * p.d_o.head_stride, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
+  float lse[4], dd[4], acc[4][HD / 16] = {};
+  row_statistics(p, sq, w.h, q0, ty, lse, dd);
+  for (int k0 = 0; k0 < seen; k0 += TILE) {
+    __syncthreads();
+    load_tile<T, HD>(sK, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    load_tile<T, HD>(sV, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+    __syncthreads();
+    float pr[4][4], ds[4][4];
+    probabilities<HD>(sQ, sK, sG, sV, ty, tx, q0, k0, sq, p, shift, lse, dd, pr, ds);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<float4*>(sSt + (tx + 16 * c) * PS + ty * 4) = make_float4(ds[0][c], ds[1][c], ds[2][c], ds[3][c]);
+    __syncthreads();
+    add_product<HD>(sSt, sK, ty, tx, acc);
+  }
+  store_rows<T, HD>((T*)p.dq.x + sq.q0 * p.dq.row_stride + w.h * p.dq.head_stride, p.dq.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, p.a.scale, acc);
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(THREADS) ragged_dkv_kernel(const __grid_constant__ RaggedAttn p) {
+  extern __shared__ float4 smem4[];
+  constexpr int LD = kStride<HD>;
+  float* sK = reinterpret_cast<float*>(smem4);
+  float* sV = sK + TILE * LD;
+  float* sQ = sV + TILE * LD;
+  float* sG = sQ + TILE * LD;
+  float* sP = sG + TILE * LD;  // [query][key]
+  float* sS = sP + TILE * PS;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const BlockOf w = block_of(p.a.kv_len, TILE, p.a.kv_heads, false);
+  const SeqPair sq = sequence_pair(p.a, w.b);
+  const int k0 = w.blk * TILE, group = p.a.q_heads / p.a.kv_heads;
+  if (k0 >= sq.nk) return;
+  const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
+  const int first = p.a.causal ? max(0, k0 - shift) / TILE * TILE : 0;  // the first block of queries that sees key k0
+  load_tile<T, HD>(sK, (const T*)p.k.x + sq.k0 * p.k.row_stride + w.h * p.k.head_stride, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+  load_tile<T, HD>(sV, (const T*)p.v.x + sq.k0 * p.v.row_stride + w.h * p.v.head_stride, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+  float dk[4][HD / 16] = {}, dv[4][HD / 16] = {};
+  for (int h = w.h * group; h < (w.h + 1) * group; ++h) {
+    const T* q = (const T*)p.q.x + sq.q0 * p.q.row_stride + h * p.q.head_stride;
+    const T* g = (const T*)p.d_o.x + sq.q0 * p.d_o.row_stride + h * p.d_o.head_stride;
+    for (int q0 = first; q0 < sq.nq; q0 += TILE) {
+      __syncthreads();
+      load_tile<T, HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+      load_tile<T, HD>(sG, g, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
+      float lse[4], dd[4];
+      row_statistics(p, sq, h, q0, ty, lse, dd);
+      __syncthreads();
+      float pr[4][4], ds[4][4];
+      probabilities<HD>(sQ, sK, sG, sV, ty, tx, q0, k0, sq, p, shift, lse, dd, pr, ds);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          sP[(ty * 4 + r) * PS + tx + 16 * c] = pr[r][c];
+          sS[(ty * 4 + r) * PS + tx + 16 * c] = ds[r][c];
+        }
+      __syncthreads();
+      add_product<HD>(sP, sG, ty, tx, dv);
+      add_product<HD>(sS, sQ, ty, tx, dk);
+    }
+  }
+  store_rows<T, HD>((T*)p.dk.x + sq.k0 * p.dk.row_stride + w.h * p.dk.head_stride, p.dk.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, p.a.scale, dk);
+  store_rows<T, HD>((T*)p.dv.x + sq.k0 * p.dv.row_stride + w.h * p.dv.head_stride, p.dv.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, 1.0f, dv);
+}
+
+// drow[h][row] = sum over channels of d_o * o, `lanes` (a power of two, 16 bytes each) to a row of a head; neighbouring lanes take neighbouring
+// heads of a row.
+template <typename T>
+__global__ void __launch_bounds__(256) row_dot_kernel(const __grid_constant__ RaggedAttn p, int lanes) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
+  const int lane = threadIdx.x & (lanes - 1);
+  const int64_t row = i / p.a.q_heads;
+  const int h = (int)(i - row * p.a.q_heads);
+  float s = 0.0f;
+  if (row < p.a.q_rows && lane * V < p.a.head_dim) {
+    const uint4 g4 = *reinterpret_cast<const uint4*>((const T*)p.d_o.x + row * p.d_o.row_stride + h * p.d_o.head_stride + lane * V);
+    const uint4 o4 = *reinterpret_cast<const uint4*>((const T*)p.o.x + row * p.o.row_stride + h * p.o.head_stride + lane * V);
+    const T *g = reinterpret_cast<const T*>(&g4), *o = reinterpret_cast<const T*>(&o4);
+#pragma unroll
+    for (int e = 0; e < V; ++e) s = fmaf(to_f(g[e]), to_f(o[e]), s);
+  }
+  for (int o = lanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (row < p.a.q_rows && lane == 0) p.drow[h * p.a.q_rows + row] = s;
+}
+
+template <int HD>
+constexpr int smem_of(int tiles, int scores) {
+  return (tiles * TILE * kStride<HD> + scores * TILE * PS) * 4;
+}
+
+template <typename K>
+bool launch(Launcher& lc, K kernel, int64_t blocks, int smem, const RaggedAttn& r) {
+  if (blocks == 0) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+    lc.check();
+    return false;
+  }
+  kernel<<<(unsigned)blocks, THREADS, smem, lc.stream>>>(r);
+  lc.count();
+  lc.check();
+  return true;
+}
+
+template <typename T, int HD>
+void forward_simt(Launcher& lc, const RaggedAttn& r) {
+  launch(lc, ragged_fwd_kernel<T, HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(3, 1), r);
+}
+template <typename T, int HD>
+void backward_simt(Launcher& lc, const RaggedAttn& r) {
+  launch(lc, ragged_dkv_kernel<T, HD>, blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences), smem_of<HD>(4, 2), r);
+  launch(lc, ragged_dq_kernel<T, HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(4, 1), r);
+}
+
+void row_dots(Launcher& lc, const RaggedAttn& r) {
+  if (r.a.q_rows == 0) return;
+  const int v = r.a.dtype == HBP_F32 ? 4 : 8;
+  int lanes = 1;
+  while (lanes * v < r.a.head_dim) lanes *= 2;
+  const int64_t blocks = (r.a.q_rows * r.a.q_heads * lanes + 255) / 256;
+  if (r.a.dtype == HBP_F32) row_dot_kernel<float><<<(unsigned)blocks, 256, 0, lc.stream>>>(r, lanes);
+  else row_dot_kernel<bf16><<<(unsigned)blocks, 256, 0, lc.stream>>>(r, lanes);
+  lc.count();
+  lc.check();
+}
+
+hbp_status check_attention(const hbp_attention* a) {
+  if (!a) return HBP_ERR_INVALID_ARG;
+  if (a->dtype != HBP_F32 && a->dtype != HBP_BF16) return HBP_ERR_DTYPE;
+  if (a->sequences < 0 || a->q_heads <= 0 || a->kv_heads <= 0 || a->q_heads % a->kv_heads || a->q_heads > 65535) return HBP_ERR_SHAPE;
+  if (a->head_dim <= 0 || a->head_dim > 128 || a->head_dim % (a->dtype == HBP_F32 ? 4 : 8)) return HBP_ERR_SHAPE;
+  if (a->q_len < 0 || a->kv_len < 0 || a->q_rows < 0 || a->kv_rows < 0 || a->q_rows > INT32_MAX || a->kv_rows > INT32_MAX) return HBP_ERR_SHAPE;
+  if (!a->q_offsets && (int64_t)a->sequences * a->q_len > a->q_rows) return HBP_ERR_SHAPE;
+  if (!a->kv_offsets && (int64_t)a->sequences * a->kv_len > a->kv_rows) return HBP_ERR_SHAPE;
+  if (a->q_len > a->q_rows || a->kv_len > a->kv_rows) return HBP_ERR_SHAPE;
+  if (!std::isfinite(a->scale)) return HBP_ERR_INVALID_ARG;
+  if (((uintptr_t)a->q_offsets | (uintptr_t)a->kv_offsets | (uintptr_t)a->status) & 3u) return HBP_ERR_SHAPE;
+  // (as many blocks of 64 rows as one grid holds)
+  if (blocks_of(a->q_len, TILE, a->q_heads, a->sequences) > INT32_MAX / 2 || blocks_of(a->kv_len, TILE, a->kv_heads, a->sequences) > INT32_MAX / 2 ||
+      a->q_rows * a->q_heads > (int64_t)INT32_MAX * 8)
+    return HBP_ERR_SHAPE;
+  return HBP_OK;
+}
+
+hbp_status check_heads(const hbp_attention& a, const hbp_heads* const* t, int n) {
+  const int v = a.dtype == HBP_F32 ? 4 : 8;
+  for (int i = 0; i < n; ++i) {
+    if (!t[i] || !t[i]->x) return HBP_ERR_INVALID_ARG;
+    if (((uintptr_t)t[i]->x & 15u) || t[i]->row_stride % v || t[i]->head_stride % v || t[i]->row_stride < 0 || t[i]->head_stride < 0) return HBP_ERR_SHAPE;
+  }
+  return HBP_OK;
+}
+
+}  // namespace
+
+}  // namespace hbp
+
+using namespace hbp;
+
+extern "C" {
+
+hbp_status hbp_attention_forward(const hbp_attention* a, const hbp_heads* q, const hbp_heads* k, const hbp_heads* v, const hbp_heads* o,
+                                 float* lse, void* cuda_stream) {
+  hbp_status st = check_attention(a);
+  if (st != HBP_OK) return st;
+  if (a->sequences == 0 || a->q_len == 0) return HBP_OK;
+  const hbp_heads* const qt[4] = {q, o, k, v};
+  st = check_heads(*a, qt, a->kv_len ? 4 : 2);  // (no keys at all: their tensors may be empty)
+  if (st != HBP_OK) return st;
+  if (!lse) return HBP_ERR_INVALID_ARG;
+  if ((uintptr_t)lse & 3u) return HBP_ERR_SHAPE;
+  Launcher lc;
+  lc.stream = (cudaStream_t)cuda_stream;
+  RaggedAttn r = {};
+  r.a = *a;
+  r.q = *q; r.o = *o; r.lse = lse;
+  if (a->kv_len) { r.k = *k; r.v = *v; }
+  const bool f32 = a->dtype == HBP_F32;
+  if (a->head_dim <= 64) f32 ? forward_simt<float, 64>(lc, r) : forward_simt<bf16, 64>(lc, r);
+  else f32 ? forward_simt<float, 128>(lc, r) : forward_simt<bf16, 128>(lc, r);
+  return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
+}
+
+hbp_status hbp_attention_scratch_bytes(const hbp_attention* a, size_t* bytes) {
+  if (!bytes) return HBP_ERR_INVALID_ARG;
+  const hbp_status st = check_attention(a);
+  if (st != HBP_OK) return st;
+  *bytes = (size_t)a->q_heads * a->q_rows * sizeof(float);
+  return HBP_OK;
+}
+
+hbp_status hbp_attention_backward(const hbp_attention* a, const hbp_heads* d_o, const hbp_heads* q, const hbp_heads* k, const hbp_heads* v,
+                                  const hbp_heads* o, const float* lse, const hbp_heads* dq, const hbp_heads* dk, const hbp_heads* dv,
+                                  void* scratch, size_t scratch_bytes, void* cuda_stream) {
+  hbp_status st = check_attention(a);
+  if (st != HBP_OK) return st;
+  if (a->sequences == 0 || (a->q_len == 0 && a->kv_len == 0)) return HBP_OK;
+  const hbp_heads* const qt[4] = {d_o, q, o, dq};
+  const hbp_heads* const kt[4] = {k, v, dk, dv};
+  if (a->q_len && (st = check_heads(*a, qt, 4)) != HBP_OK) return st;
+  if (a->kv_len && (st = check_heads(*a, kt, 4)) != HBP_OK) return st;
+  RaggedAttn r = {};
+  r.a = *a;
+  if (a->q_len) {
+    if (!lse) return HBP_ERR_INVALID_ARG;
+    if (!scratch || ((uintptr_t)scratch & 15u) || scratch_bytes < (size_t)a->q_heads * a->q_rows * sizeof(float)) return HBP_ERR_WORKSPACE;
+    if ((uintptr_t)lse & 3u) return HBP_ERR_SHAPE;
+    r.q = *q; r.o = *o; r.d_o = *d_o; r.dq = *dq;
+    r.lse = const_cast<float*>(lse);
+    r.drow = (float*)scratch;
+  }
+  if (a->kv_len) { r.k = *k; r.v = *v; r.dk = *dk; r.dv = *dv; }
+  Launcher lc;
+  lc.stream = (cudaStream_t)cuda_stream;
+  if (a->q_len) row_dots(lc, r);
+  const bool f32 = a->dtype == HBP_F32;
+  if (a->head_dim <= 64) f32 ? backward_simt<float, 64>(lc, r) : backward_simt<bf16, 64>(lc, r);
+  else f32 ? backward_simt<float, 128>(lc, r) : backward_simt<bf16, 128>(lc, r);
+  return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -345,6 +345,20 @@ bool attention_bwd_tc(Launcher& lc, const AttnArgs& a, int* status_word);
 // Tensor-core forward (attention_tc.cu), same conditions.
 bool attention_fwd_tc(Launcher& lc, const AttnArgs& a, int* status_word);
 
+// ---------------------------------------------------------------- a decoder's step on its own
+// hbp_rotary (rotary.cu); the arguments have been checked.
+hbp_status check_rotary_spec(const hbp_rotary_spec* spec, int head_dim);
+void rotary(Launcher& lc, const hbp_rotary_spec& spec, bool inverse, int dtype, int64_t rows, int q_heads, int kv_heads, int head_dim,
+            const void* positions, int position_bytes, int64_t first, int64_t period, const hbp_heads& q, const hbp_heads& q_out,
+            const hbp_heads& k, const hbp_heads& k_out);
+// hbp_attention_forward / _backward (attention_ragged.cu); the arguments have been checked.
+struct RaggedAttn {
+  hbp_attention a;
+  hbp_heads q, k, v, o, d_o, dq, dk, dv;
+  float* lse;   // [q_heads][q_rows]
+  float* drow;  // [q_heads][q_rows]: sum of d_o * o
+};
+
 // ---------------------------------------------------------------- device math
 // Sum over `splits` partial sums, `stride` apart from p on, of one element per lane of a block of 256: each warp adds an eighth of them
 // in double, the first one the eighths (all in fixed order).  The sum is that warp's.  From kManySplits on this is faster than a thread
