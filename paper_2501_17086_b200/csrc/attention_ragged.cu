@@ -27,32 +27,13 @@ constexpr int kStride = HD + 4;
 
 // `TILE` rows of a tensor from row r0 of a sequence of n rows on into shared memory as float, zeros behind the sequence's end and
 // behind channel `width`.  base: the sequence's first row of one head.
-template <typename T>
-__device__ __forceinline__ float4 load4(const T* p) {
-  const uint2 raw = *reinterpret_cast<const uint2*>(p);
-  const T* e = reinterpret_cast<const T*>(&raw);
-  return make_float4(to_f(e[0]), to_f(e[1]), to_f(e[2]), to_f(e[3]));
-}
-template <>
-__device__ __forceinline__ float4 load4<float>(const float* p) {
-  return *reinterpret_cast<const float4*>(p);
-}
-template <typename T>
-__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d) {
-  const T e[4] = {from_f<T>(a), from_f<T>(b), from_f<T>(c), from_f<T>(d)};
-  *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(e);
-}
-template <>
-__device__ __forceinline__ void store4<float>(float* p, float a, float b, float c, float d) {
-  *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
-}
-template <typename T, int HD>
-__device__ __forceinline__ void load_tile(float* __restrict__ dst, const T* __restrict__ base, int64_t row_stride, int r0, int n, int width) {
+template <int HD>
+__device__ __forceinline__ void load_tile(float* __restrict__ dst, const float* __restrict__ base, int64_t row_stride, int r0, int n, int width) {
   constexpr int VECS = HD / 4;
   for (int i = threadIdx.x; i < TILE * VECS; i += THREADS) {
     const int r = i / VECS, c = (i % VECS) * 4;
     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (r0 + r < n && c < width) v = load4<T>(base + (int64_t)(r0 + r) * row_stride + c);
+    if (r0 + r < n && c < width) v = *reinterpret_cast<const float4*>(base + (int64_t)(r0 + r) * row_stride + c);
     *reinterpret_cast<float4*>(dst + r * kStride<HD> + c) = v;
   }
 }
@@ -101,8 +82,8 @@ __device__ __forceinline__ void add_product(const float* __restrict__ W, const f
   }
 }
 
-template <typename T, int HD>
-__device__ __forceinline__ void store_rows(T* __restrict__ base, int64_t row_stride, int r0, int n, int width, int ty, int tx, float mul,
+template <int HD>
+__device__ __forceinline__ void store_rows(float* __restrict__ base, int64_t row_stride, int r0, int n, int width, int ty, int tx, float mul,
                                            const float (&acc)[4][HD / 16]) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -112,13 +93,14 @@ __device__ __forceinline__ void store_rows(T* __restrict__ base, int64_t row_str
     for (int v = 0; v < HD / 64; ++v) {
       const int c = (tx + 16 * v) * 4;
       if (c < width)
-        store4<T>(base + (int64_t)row * row_stride + c, mul * acc[r][4 * v], mul * acc[r][4 * v + 1], mul * acc[r][4 * v + 2], mul * acc[r][4 * v + 3]);
+        *reinterpret_cast<float4*>(base + (int64_t)row * row_stride + c) =
+            make_float4(mul * acc[r][4 * v], mul * acc[r][4 * v + 1], mul * acc[r][4 * v + 2], mul * acc[r][4 * v + 3]);
     }
   }
 }
 
 // ------------------------------------------------------------------------------------------- forward
-template <typename T, int HD>
+template <int HD>
 __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_constant__ RaggedAttn p) {
   extern __shared__ float4 smem4[];
   constexpr int LD = kStride<HD>;
@@ -131,12 +113,12 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
   const SeqPair sq = sequence_pair(p.a, w.b);
   const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
   if (q0 >= sq.nq) return;
-  const T* q = (const T*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride;
-  const T* k = (const T*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
-  const T* v = (const T*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
+  const float* q = (const float*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride;
+  const float* k = (const float*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
+  const float* v = (const float*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;  // query i sees keys 0 .. i + shift (capped by nk)
   const int seen = min(sq.nk, p.a.causal ? min(q0 + TILE, sq.nq) + shift : sq.nk);
-  load_tile<T, HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+  load_tile<HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
   float acc[4][HD / 16], m[4], l[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -147,8 +129,8 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
   }
   for (int k0 = 0; k0 < seen; k0 += TILE) {
     __syncthreads();
-    load_tile<T, HD>(sK, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
-    load_tile<T, HD>(sV, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+    load_tile<HD>(sK, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    load_tile<HD>(sV, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
     __syncthreads();
     float s[4][4];
     score_tile<HD>(sQ, sK, ty, tx, s);
@@ -192,7 +174,7 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
     const int row = q0 + ty * 4 + r;
     if (tx == 0 && row < sq.nq) p.lse[w.h * p.a.q_rows + sq.q0 + row] = l[r] == 0.0f ? -INFINITY : m[r] + logf(l[r]);
   }
-  store_rows<T, HD>((T*)p.o.x + sq.q0 * p.o.row_stride + w.h * p.o.head_stride, p.o.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, 1.0f, acc);
+  store_rows<HD>((float*)p.o.x + sq.q0 * p.o.row_stride + w.h * p.o.head_stride, p.o.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, 1.0f, acc);
 }
 
 // ------------------------------------------------------------------------------------------- backward
@@ -224,7 +206,7 @@ __device__ __forceinline__ void row_statistics(const RaggedAttn& p, const SeqPai
   }
 }
 
-template <typename T, int HD>
+template <int HD>
 __global__ void __launch_bounds__(THREADS) ragged_dq_kernel(const __grid_constant__ RaggedAttn p) {
   extern __shared__ float4 smem4[];
   constexpr int LD = kStride<HD>;
@@ -238,18 +220,18 @@ __global__ void __launch_bounds__(THREADS) ragged_dq_kernel(const __grid_constan
   const SeqPair sq = sequence_pair(p.a, w.b);
   const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
   if (q0 >= sq.nq) return;
-  const T* k = (const T*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
-  const T* v = (const T*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
+  const float* k = (const float*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
+  const float* v = (const float*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
   const int seen = min(sq.nk, p.a.causal ? min(q0 + TILE, sq.nq) + shift : sq.nk);
-  load_tile<T, HD>(sQ, (const T*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride, p.q.row_stride, q0, sq.nq, p.a.head_dim);
-  load_tile<T, HD>(sG, (const T*)p.d_o.x + sq.q0 * p.d_o.row_stride + w.h * p.d_o.head_stride, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
+  load_tile<HD>(sQ, (const float*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+  load_tile<HD>(sG, (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + w.h * p.d_o.head_stride, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
   float lse[4], dd[4], acc[4][HD / 16] = {};
   row_statistics(p, sq, w.h, q0, ty, lse, dd);
   for (int k0 = 0; k0 < seen; k0 += TILE) {
     __syncthreads();
-    load_tile<T, HD>(sK, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
-    load_tile<T, HD>(sV, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+    load_tile<HD>(sK, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    load_tile<HD>(sV, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
     __syncthreads();
     float pr[4][4], ds[4][4];
     probabilities<HD>(sQ, sK, sG, sV, ty, tx, q0, k0, sq, p, shift, lse, dd, pr, ds);
@@ -259,10 +241,10 @@ __global__ void __launch_bounds__(THREADS) ragged_dq_kernel(const __grid_constan
     __syncthreads();
     add_product<HD>(sSt, sK, ty, tx, acc);
   }
-  store_rows<T, HD>((T*)p.dq.x + sq.q0 * p.dq.row_stride + w.h * p.dq.head_stride, p.dq.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, p.a.scale, acc);
+  store_rows<HD>((float*)p.dq.x + sq.q0 * p.dq.row_stride + w.h * p.dq.head_stride, p.dq.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, p.a.scale, acc);
 }
 
-template <typename T, int HD>
+template <int HD>
 __global__ void __launch_bounds__(THREADS) ragged_dkv_kernel(const __grid_constant__ RaggedAttn p) {
   extern __shared__ float4 smem4[];
   constexpr int LD = kStride<HD>;
@@ -279,16 +261,16 @@ __global__ void __launch_bounds__(THREADS) ragged_dkv_kernel(const __grid_consta
   if (k0 >= sq.nk) return;
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
   const int first = p.a.causal ? max(0, k0 - shift) / TILE * TILE : 0;  // the first block of queries that sees key k0
-  load_tile<T, HD>(sK, (const T*)p.k.x + sq.k0 * p.k.row_stride + w.h * p.k.head_stride, p.k.row_stride, k0, sq.nk, p.a.head_dim);
-  load_tile<T, HD>(sV, (const T*)p.v.x + sq.k0 * p.v.row_stride + w.h * p.v.head_stride, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+  load_tile<HD>(sK, (const float*)p.k.x + sq.k0 * p.k.row_stride + w.h * p.k.head_stride, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+  load_tile<HD>(sV, (const float*)p.v.x + sq.k0 * p.v.row_stride + w.h * p.v.head_stride, p.v.row_stride, k0, sq.nk, p.a.head_dim);
   float dk[4][HD / 16] = {}, dv[4][HD / 16] = {};
   for (int h = w.h * group; h < (w.h + 1) * group; ++h) {
-    const T* q = (const T*)p.q.x + sq.q0 * p.q.row_stride + h * p.q.head_stride;
-    const T* g = (const T*)p.d_o.x + sq.q0 * p.d_o.row_stride + h * p.d_o.head_stride;
+    const float* q = (const float*)p.q.x + sq.q0 * p.q.row_stride + h * p.q.head_stride;
+    const float* g = (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + h * p.d_o.head_stride;
     for (int q0 = first; q0 < sq.nq; q0 += TILE) {
       __syncthreads();
-      load_tile<T, HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
-      load_tile<T, HD>(sG, g, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
+      load_tile<HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+      load_tile<HD>(sG, g, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
       float lse[4], dd[4];
       row_statistics(p, sq, h, q0, ty, lse, dd);
       __syncthreads();
@@ -306,8 +288,8 @@ __global__ void __launch_bounds__(THREADS) ragged_dkv_kernel(const __grid_consta
       add_product<HD>(sS, sQ, ty, tx, dk);
     }
   }
-  store_rows<T, HD>((T*)p.dk.x + sq.k0 * p.dk.row_stride + w.h * p.dk.head_stride, p.dk.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, p.a.scale, dk);
-  store_rows<T, HD>((T*)p.dv.x + sq.k0 * p.dv.row_stride + w.h * p.dv.head_stride, p.dv.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, 1.0f, dv);
+  store_rows<HD>((float*)p.dk.x + sq.k0 * p.dk.row_stride + w.h * p.dk.head_stride, p.dk.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, p.a.scale, dk);
+  store_rows<HD>((float*)p.dv.x + sq.k0 * p.dv.row_stride + w.h * p.dv.head_stride, p.dv.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, 1.0f, dv);
 }
 
 // drow[h][row] = sum over channels of d_o * o, `lanes` (a power of two, 16 bytes each) to a row of a head; neighbouring lanes take neighbouring
@@ -349,14 +331,14 @@ bool launch(Launcher& lc, K kernel, int64_t blocks, int smem, const RaggedAttn& 
   return true;
 }
 
-template <typename T, int HD>
-void forward_simt(Launcher& lc, const RaggedAttn& r) {
-  launch(lc, ragged_fwd_kernel<T, HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(3, 1), r);
+template <int HD>
+void forward_f32(Launcher& lc, const RaggedAttn& r) {
+  launch(lc, ragged_fwd_kernel<HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(3, 1), r);
 }
-template <typename T, int HD>
-void backward_simt(Launcher& lc, const RaggedAttn& r) {
-  launch(lc, ragged_dkv_kernel<T, HD>, blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences), smem_of<HD>(4, 2), r);
-  launch(lc, ragged_dq_kernel<T, HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(4, 1), r);
+template <int HD>
+void backward_f32(Launcher& lc, const RaggedAttn& r) {
+  launch(lc, ragged_dkv_kernel<HD>, blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences), smem_of<HD>(4, 2), r);
+  launch(lc, ragged_dq_kernel<HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(4, 1), r);
 }
 
 void row_dots(Launcher& lc, const RaggedAttn& r) {
@@ -422,9 +404,13 @@ hbp_status hbp_attention_forward(const hbp_attention* a, const hbp_heads* q, con
   r.a = *a;
   r.q = *q; r.o = *o; r.lse = lse;
   if (a->kv_len) { r.k = *k; r.v = *v; }
-  const bool f32 = a->dtype == HBP_F32;
-  if (a->head_dim <= 64) f32 ? forward_simt<float, 64>(lc, r) : forward_simt<bf16, 64>(lc, r);
-  else f32 ? forward_simt<float, 128>(lc, r) : forward_simt<bf16, 128>(lc, r);
+  if (a->dtype == HBP_BF16) {
+    if (!ragged_forward_tc(lc, r)) return lc.err == cudaSuccess ? HBP_ERR_UNSUPPORTED : HBP_ERR_CUDA;
+  } else if (a->head_dim <= 64) {
+    forward_f32<64>(lc, r);
+  } else {
+    forward_f32<128>(lc, r);
+  }
   return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
 }
 
@@ -460,9 +446,13 @@ hbp_status hbp_attention_backward(const hbp_attention* a, const hbp_heads* d_o, 
   Launcher lc;
   lc.stream = (cudaStream_t)cuda_stream;
   if (a->q_len) row_dots(lc, r);
-  const bool f32 = a->dtype == HBP_F32;
-  if (a->head_dim <= 64) f32 ? backward_simt<float, 64>(lc, r) : backward_simt<bf16, 64>(lc, r);
-  else f32 ? backward_simt<float, 128>(lc, r) : backward_simt<bf16, 128>(lc, r);
+  if (a->dtype == HBP_BF16) {
+    if (!ragged_backward_tc(lc, r)) return lc.err == cudaSuccess ? HBP_ERR_UNSUPPORTED : HBP_ERR_CUDA;
+  } else if (a->head_dim <= 64) {
+    backward_f32<64>(lc, r);
+  } else {
+    backward_f32<128>(lc, r);
+  }
   return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
 }
 

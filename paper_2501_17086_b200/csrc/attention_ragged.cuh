@@ -55,4 +55,9 @@ __device__ __forceinline__ SeqPair sequence_pair(const hbp_attention& a, int b) 
   return s;
 }
 
+// bf16 on the tensor cores (attention_ragged_tc.cu); false if a tensor's strides or address are not such as tile copies take, in which case
+// nothing was launched.
+bool ragged_forward_tc(Launcher& lc, const RaggedAttn& r);
+bool ragged_backward_tc(Launcher& lc, const RaggedAttn& r);
+
 }  // namespace hbp

@@ -1,0 +1,671 @@
+// Attention over ragged batches on the tensor cores (bf16, heads up to 128 wide): the formulas are those of attention_ragged.cu.
+//
+// Heads are padded to HD = 64 or 128 channels: a tensor map is head_dim channels wide and its boxes 64, so that the missing ones
+// arrive as zeros.  Tiles are rows of 128 bytes (64 channels) under the 128-byte swizzle, 64 channels after the other; the same tile is a
+// K-major operand (contraction over channels) and an MN-major one (contraction over its rows).  A tile that reaches past
+// its sequence holds rows of the next one, which may be anything: where rows are contracted over, the copying warp waits for such a
+// tile and overwrites those rows with zeros before it hands the tile on (0 * NaN is not 0).
+//
+// Scores come from shared memory into tensor memory; the softmax warps turn them into bf16 probabilities that go back into the columns
+// the scores came from and are the A operand of the next product there: they never pass through shared memory, whose bandwidth
+// the products need (M = 128, N = 64, K = 16 reads 6 KB in the 32 clocks that it takes at the tensor cores' rate).
+//
+// Forward: a block owns 128 queries and walks over tiles of 128 keys with a running maximum and sum, one row per thread of four
+// warps.  The output stays in tensor memory; it is scaled down only when a row's maximum has grown by more than 2^8
+// since the last time, which is rare (sums are float: 2^8 costs no precision).  Two blocks share an SM, so that the exponentials of
+// one run under the products of the other.
+//
+// Backward: two kinds of block in one launch, so that every output has one owner and one order of its sums:
+//   dK, dV   128 keys of a key head; walks over tiles of 64 queries of all query heads of its group
+//            S^T = K Q^T, dP^T = V dO^T;  P^T = exp(S^T - lse), dS^T = P^T (dP^T - D);  dV += P^T dO, dK += dS^T Q
+//   dQ       128 queries; walks over tiles of 64 keys:  S = Q K^T, dP = dO V^T;  dQ += dS K
+// That is seven products where five would do with sums in memory that blocks add to in no fixed order.  HD = 128 takes all of tensor memory:
+// two buffers of scores, whose products run one tile ahead of the softmax warps; HD = 64 runs two blocks an SM instead.
+// All waits are bounded.
+#include "attention_ragged.cuh"
+#include "ring_drain.cuh"
+
+namespace hbp {
+
+using namespace tc;
+
+namespace {
+
+constexpr int BIG = 128;     // rows of a block; keys of a forward tile
+constexpr int SMALL = 64;    // rows of a backward tile, and of every copy
+constexpr int SUB = 64;      // channels of a run of tile rows (128 bytes)
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float kGrowth = 8.0f;  // log2 of how far a row's maximum may grow before what was summed is scaled
+
+struct RaggedMaps {
+  CUtensorMap q, k, v, d_o;
+};
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float ld_early(const float* p) {  // a load that is not moved down to its first use
+  float v;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t is_leader;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(is_leader));
+  return is_leader != 0;
+}
+__device__ __forceinline__ uint64_t desc_add(uint64_t d, uint32_t bytes) { return d + (uint64_t)(bytes >> 4); }
+
+// bf16 x bf16 -> float, M = 128, A K-major (or in tensor memory)
+template <int N, int kBmn>
+constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)kBmn << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(BIG >> 4) << 24);
+// A in tensor memory: 128 lanes, K = 16 in 8 columns
+__device__ __forceinline__ void tc_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accum)
+      : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tc_st32(uint32_t taddr, const float* v) {
+  const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
+  tc_st16(taddr, r);
+  tc_st16(taddr + 16, r + 16);
+}
+__device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+
+// 64 rows from row `row` of head `head` on, all HD channels, into a tile of `tile_rows` rows a run of channels
+template <int HD>
+__device__ __forceinline__ void copy_rows(uint32_t dst, int tile_rows, const CUtensorMap* tm, uint32_t bar, int head, int row) {
+#pragma unroll
+  for (int c = 0; c < HD / SUB; ++c) tma_load_3d(dst + c * tile_rows * 128, tm, bar, c * SUB, head, row);
+}
+// rows [from, rows) of a tile become zeros; the whole warp
+template <int HD>
+__device__ __forceinline__ void clear_rows(uint32_t tile, int rows, int from, int lane) {
+  for (int i = lane; i < (rows - from) * 8 * (HD / SUB); i += 32) {
+    const int c = i / ((rows - from) * 8), r = i - c * (rows - from) * 8;
+    st_shared16(tile + c * rows * 128 + (from + (r >> 3)) * 128 + (r & 7) * 16, make_uint4(0, 0, 0, 0));
+  }
+}
+// A wait of the whole warp: all lanes go on or none does.
+__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
+}
+// The end of a block: after a wait that gave up, every copy and product is outlasted first.
+__device__ __forceinline__ void leave(int warp, uint32_t tmem, uint32_t columns, volatile int* abort_flag) {
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) outlast_copies();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+  }
+}
+// Rows of a staged tile (this warp's 32 rows from `row0` on, kUnits 16-byte units from unit `unit0` on) to memory, neighbouring lanes
+// along a row; rows behind the sequence and channels behind the head are left alone.
+template <int kUnits>
+__device__ __forceinline__ void store_staged(uint32_t tile, int row0, int unit0, bf16* base, int64_t row_stride, int rows_there, int head_dim, int lane) {
+  constexpr int kRows = 32 / kUnits;
+  const int u = unit0 + lane % kUnits;
+#pragma unroll
+  for (int r = lane / kUnits; r < 32; r += kRows) {
+    const int row = row0 + r;
+    if (row < rows_there && u * 8 < head_dim)
+      *reinterpret_cast<uint4*>(base + (int64_t)row * row_stride + u * 8) = ld_shared16(swz(tile + (u >> 3) * BIG * 128, row, u & 7));
+  }
+}
+
+// ------------------------------------------------------------------------------------------- forward
+constexpr int FWD_THREADS = 192;  // warp 0 copies, warp 1 issues the products, warps 2..5 softmax (TMEM lane quarter = warp & 3)
+template <int HD>
+struct Fwd {
+  static constexpr int kStages = HD == 64 ? 2 : 1;  // (a key tile comes while the softmax of the one before runs)
+  static constexpr int kTile = BIG * HD * 2;
+  static constexpr int kSmem = kTile * (1 + 2 * kStages) + 256 + 1024;
+};
+
+template <int HD>
+__global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p) {
+  using C = Fwd<HD>;
+  constexpr int NS = C::kStages;
+  const BlockOf w = block_of(p.a.q_len, BIG, p.a.q_heads, true);
+  const SeqPair sq = sequence_pair(p.a, w.b);
+  const int q0 = w.blk * BIG;
+  if (q0 >= sq.nq) return;
+  const int kh = w.h / (p.a.q_heads / p.a.kv_heads);
+  const int shift = sq.nk - sq.nq;  // causal: query i sees keys 0 .. i + shift
+  const int seen = p.a.causal ? min(sq.nk, min(q0 + BIG, sq.nq) + shift) : sq.nk;
+  const int n_it = seen > 0 ? (seen + BIG - 1) / BIG : 0;
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* aligned = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t sQ = base, sK = base + C::kTile, sV = sK + NS * C::kTile;
+  uint64_t* bar_mem = reinterpret_cast<uint64_t*>(aligned + C::kTile * (1 + 2 * NS));
+  const uint32_t bars = smem_u32(bar_mem);
+  const uint32_t bQ = bars, bScores = bars + 8, bProbs = bars + 16, bDone = bars + 24, bTail = bars + 32;
+  auto bKFull = [&](int s) { return bars + 40 + 8 * s; };
+  auto bKFree = [&](int s) { return bars + 40 + 8 * (NS + s); };
+  auto bVFull = [&](int s) { return bars + 40 + 8 * (2 * NS + s); };
+  auto bVFree = [&](int s) { return bars + 40 + 8 * (3 * NS + s); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_mem + 5 + 4 * NS);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 5 + 4 * NS; ++i) mbar_init(bars + 8 * i, i == 2 ? 4 : 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(256) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot, tS = tmem, tO = tmem + BIG;
+
+  if (warp == 0) {
+    bool ok = n_it > 0;
+    if (ok && lane == 0) {
+      mbar_expect_tx(bQ, C::kTile);
+      for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sQ + r * 128, BIG, &m.q, bQ, w.h, (int)sq.q0 + q0 + r);
+    }
+    for (int it = 0; it < n_it && ok; ++it) {
+      const int s = it % NS;
+      const uint32_t free_parity = ((uint32_t)(it / NS) & 1u) ^ 1u;
+      const int row = (int)sq.k0 + it * BIG;
+      if (!wait_all(bKFree(s), free_parity, abort_flag, p.a.status)) { ok = false; break; }
+      if (lane == 0) {
+        mbar_expect_tx(bKFull(s), C::kTile);
+        for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sK + s * C::kTile + r * 128, BIG, &m.k, bKFull(s), kh, row + r);
+      }
+      if (!wait_all(bVFree(s), free_parity, abort_flag, p.a.status)) { ok = false; break; }
+      const int there = sq.nk - it * BIG;  // rows of the sequence in this tile
+      const uint32_t bar = there < BIG ? bTail : bVFull(s);
+      if (lane == 0) {
+        mbar_expect_tx(bar, C::kTile);
+        for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sV + s * C::kTile + r * 128, BIG, &m.v, bar, kh, row + r);
+      }
+      if (there < BIG) {  // the last tile: what is behind the sequence becomes zeros
+        if (!wait_all(bTail, 0, abort_flag, p.a.status)) { ok = false; break; }
+        clear_rows<HD>(sV + s * C::kTile, BIG, there, lane);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bVFull(s));
+      }
+    }
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    const uint64_t dQ = make_desc(sQ, 16, 1024), dK = make_desc(sK, 16, 1024), dV = make_desc(sV, BIG * 128, 1024);
+    bool ok = n_it == 0 || wait_all(bQ, 0, abort_flag, p.a.status);
+    for (int it = 0; it < n_it && ok; ++it) {
+      const int s = it % NS;
+      const uint32_t full_parity = (uint32_t)(it / NS) & 1u, off = (uint32_t)s * C::kTile;
+      if (!wait_all(bKFull(s), full_parity, abort_flag, p.a.status)) { ok = false; break; }
+      tc_fence_after();
+      if (leader) {  // (in order behind the product that read the probabilities in these columns)
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k)
+          tc_mma(tS, desc_add(dQ, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dK, off + (k / 4) * BIG * 128 + 32 * (k % 4)), kIdesc<BIG, 0>, k != 0);
+        tc_commit(bScores);
+        tc_commit(bKFree(s));
+      }
+      if (!wait_all(bVFull(s), full_parity, abort_flag, p.a.status) || !wait_all(bProbs, (uint32_t)it & 1u, abort_flag, p.a.status)) { ok = false; break; }
+      tc_fence_after();
+      if (leader) {
+#pragma unroll
+        for (int k = 0; k < BIG / 16; ++k) tc_mma_ts(tO, tS + 8 * k, desc_add(dV, off + 2048 * k), kIdesc<HD, 1>, (it | k) != 0);
+        tc_commit(bVFree(s));
+      }
+    }
+    if (leader) tc_commit(bDone);
+  } else {
+    const int quarter = warp & 3, row = quarter * 32 + lane, qrow = q0 + row;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const float sign = p.a.scale < 0.0f ? -1.0f : 1.0f, scale2 = fabsf(p.a.scale) * LOG2E;
+    float top = -INFINITY, total = 0.0f;  // the reference of the sums, in units of log2; the sum
+    bool ok = true;
+    for (int it = 0; it < n_it; ++it) {
+      if (!wait_all(bScores, (uint32_t)it & 1u, abort_flag, p.a.status)) { ok = false; break; }
+      tc_fence_after();
+      const int c0 = it * BIG;
+      const int last = p.a.causal ? min(sq.nk - 1, qrow + shift) : sq.nk - 1;         // the last key this row sees
+      const bool full = c0 + BIG <= sq.nk && (!p.a.causal || c0 + BIG - 1 <= q0 + shift);  // ... and every row of the block sees the whole tile
+      float most = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < BIG; c += 32) {
+        float sc[32];
+        tc_ld32(tS + lanes + c, sc);
+        if (sign < 0.0f) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sc[i] = -sc[i];
+        }
+        if (full) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) most = fmaxf(most, sc[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) most = c0 + c + i <= last ? fmaxf(most, sc[i]) : most;
+        }
+      }
+      most = most == -INFINITY ? most : most * scale2;  // (a scale of 0 times nothing is not a maximum)
+      if (it == 0) {
+        top = most;
+      } else {
+        const bool grown = most > top + kGrowth;
+        if (__any_sync(0xffffffffu, grown)) {  // scale what was summed down to the new reference
+          const float keep = grown ? fast_exp2(top - most) : 1.0f;
+          if (grown) top = most;
+          total *= keep;
+          if (!wait_all(bVFree((it - 1) % NS), (uint32_t)((it - 1) / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int c = 0; c < HD; c += 32) {
+            float o[32];
+            tc_ld32(tO + lanes + c, o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] *= keep;
+            tc_st32(tO + lanes + c, o);
+          }
+          tc_st_wait();
+        }
+      }
+      const float ref = top == -INFINITY ? 0.0f : top, mul = sign * scale2;
+#pragma unroll
+      for (int c = 0; c < BIG; c += 32) {
+        float sc[32];
+        tc_ld32(tS + lanes + c, sc);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sc[i] = fast_exp2(fmaf(sc[i], mul, -ref));
+        if (!full) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) sc[i] = c0 + c + i <= last ? sc[i] : 0.0f;
+        }
+        float s0 = 0.0f, s1 = 0.0f;
+        uint32_t packed[16];
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          s0 += sc[i];
+          s1 += sc[i + 1];
+          packed[i / 2] = pack2(sc[i], sc[i + 1]);
+        }
+        total += s0 + s1;
+        tc_st16(tS + lanes + c / 2, packed);  // (columns whose scores this thread has read)
+      }
+      tc_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bProbs);
+    }
+    ok = ok && wait_all(bDone, 0, abort_flag, p.a.status);
+    if (ok) {
+      tc_fence_after();
+      const float inv = total > 0.0f ? 1.0f / total : total;  // nothing seen: 0 (a sum that is NaN stays NaN)
+#pragma unroll 1
+      for (int c = 0; c < HD; c += 32) {
+        float o[32];
+        if (n_it > 0) tc_ld32(tO + lanes + c, o);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = total == 0.0f ? 0.0f : o[i] * inv;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) st_shared16(swz(sQ + (c / SUB) * BIG * 128, row, (c % SUB) / 8 + u), pack8(o + 8 * u));
+      }
+      __syncwarp();
+      store_staged<HD / 8>(sQ, quarter * 32, 0, (bf16*)p.o.x + (sq.q0 + q0) * p.o.row_stride + w.h * p.o.head_stride, p.o.row_stride, sq.nq - q0, p.a.head_dim, lane);
+      if (qrow < sq.nq) p.lse[w.h * p.a.q_rows + sq.q0 + qrow] = total == 0.0f ? -INFINITY : (top + __log2f(total)) * LN2;
+    }
+  }
+  leave(warp, tmem, 256, abort_flag);
+}
+
+// ------------------------------------------------------------------------------------------- backward
+constexpr int BWD_THREADS = 320;  // warp 0 copies, warp 1 issues the products, warps 2..9 softmax, two to a TMEM lane quarter
+template <int HD>
+struct Bwd {
+  static constexpr int kBuffers = HD == 64 ? 1 : 2;  // of scores
+  static constexpr int kStages = 3;
+  static constexpr int kBig = BIG * HD * 2, kSmall = SMALL * HD * 2;
+  static constexpr int kStats = 2 * SMALL * 4;  // log-sum-exp and D of a tile's queries (dK, dV)
+  static constexpr int kStage = 2 * kSmall;
+  static constexpr int kSmem = 2 * kBig + kStages * (kStage + kStats) + 256 + 1024;
+  static constexpr uint32_t kColumns = HD == 64 ? 256 : 512;
+  static constexpr int kBlocksAnSm = HD == 64 ? 2 : 1;
+};
+
+template <int HD, bool kDKV>
+__device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const RaggedAttn& p, const BlockOf w) {
+  using C = Bwd<HD>;
+  constexpr int NB = C::kBuffers, NS = C::kStages;
+  const SeqPair sq = sequence_pair(p.a, w.b);
+  const int big0 = w.blk * BIG, n_big = kDKV ? sq.nk : sq.nq, n_small = kDKV ? sq.nq : sq.nk;
+  if (big0 >= n_big) return;
+  const int group = p.a.q_heads / p.a.kv_heads;
+  const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;  // query i sees keys 0 .. i + shift (capped by nk)
+  // tiles of the other side: queries from the first that sees key big0 on; keys up to the last that the block's last query sees
+  const int t_beg = kDKV && p.a.causal ? max(0, big0 - shift) / SMALL : 0;
+  const int t_rows = kDKV ? n_small : p.a.causal ? min(n_small, min(big0 + BIG, n_big) + shift) : n_small;
+  const int tiles = max(0, (max(t_rows, 0) + SMALL - 1) / SMALL - t_beg);
+  const int n_it = kDKV ? tiles * group : tiles;
+  const int q_head0 = kDKV ? w.h * group : w.h, k_head = kDKV ? w.h : w.h / group;
+
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* aligned = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t sBig0 = base, sBig1 = base + C::kBig, sSmall = base + 2 * C::kBig;
+  float* stats = reinterpret_cast<float*>(aligned + 2 * C::kBig + NS * C::kStage);  // [stage][log-sum-exp, D][64]
+  uint64_t* bar_mem = reinterpret_cast<uint64_t*>(aligned + 2 * C::kBig + NS * (C::kStage + C::kStats));
+  const uint32_t bars = smem_u32(bar_mem);
+  const uint32_t bBig = bars, bDone = bars + 8, bTail = bars + 16;
+  auto bProbs = [&](int b) { return bars + 24 + 8 * b; };
+  auto bScores = [&](int b) { return bars + 24 + 8 * (NB + b); };
+  auto bFull = [&](int s) { return bars + 24 + 8 * (2 * NB + s); };
+  auto bFree = [&](int s) { return bars + 24 + 8 * (2 * NB + NS + s); };
+  constexpr int kBars = 3 + 2 * NB + 2 * NS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_mem + kBars);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    // (probabilities: eight warps; full: the copies, and what the copying warp adds itself)
+    for (int i = 0; i < kBars; ++i) mbar_init(bars + 8 * i, i >= 3 && i < 3 + NB ? 8 : i >= 3 + 2 * NB && i < 3 + 2 * NB + NS ? 2 : 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::kColumns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  // columns of buffer b: scores 128 b .., dP 128 b + 64 ..; probabilities of the first 32 rows of a tile in the first 16 of them, those of the
+  // others 32 columns on (a warp writes only where it has read)
+  const uint32_t tAcc0 = tmem + 128 * NB, tAcc1 = tAcc0 + HD;
+
+  if (warp == 0) {
+    bool ok = n_it > 0;
+    int tails = 0;
+    if (ok && lane == 0) {
+      mbar_expect_tx(bBig, 2 * C::kBig);
+      for (int r = 0; r < BIG; r += SMALL) {
+        const int row = (int)(kDKV ? sq.k0 : sq.q0) + big0 + r;
+        copy_rows<HD>(sBig0 + r * 128, BIG, kDKV ? &m.k : &m.q, bBig, w.h, row);
+        copy_rows<HD>(sBig1 + r * 128, BIG, kDKV ? &m.v : &m.d_o, bBig, w.h, row);
+      }
+    }
+    for (int it = 0; it < n_it && ok; ++it) {
+      const int s = it % NS, r0 = (t_beg + it % tiles) * SMALL, head = kDKV ? q_head0 + it / tiles : k_head;
+      const uint32_t tile = sSmall + s * C::kStage;
+      if (!wait_all(bFree(s), ((uint32_t)(it / NS) & 1u) ^ 1u, abort_flag, p.a.status)) { ok = false; break; }
+      const int there = n_small - r0;
+      const bool tail = there < SMALL;
+      const uint32_t bar = tail ? bTail : bFull(s);
+      if (lane == 0) {
+        const int row = (int)(kDKV ? sq.q0 : sq.k0) + r0;
+        mbar_expect_tx(bar, 2 * C::kSmall);
+        copy_rows<HD>(tile, SMALL, kDKV ? &m.q : &m.k, bar, head, row);
+        copy_rows<HD>(tile + C::kSmall, SMALL, kDKV ? &m.d_o : &m.v, bar, head, row);
+      }
+      if (kDKV) {
+        float* st = stats + s * 2 * SMALL;
+        const int64_t at = (int64_t)head * p.a.q_rows + sq.q0 + r0;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = i * 32 + lane;
+          v[i] = r < there ? ld_early(p.lse + at + r) : -INFINITY;
+          v[2 + i] = r < there ? ld_early(p.drow + at + r) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {  // a query that sees nothing, or is none, has probabilities of 0: exp2(s - infinity)
+          st[i * 32 + lane] = v[i] == -INFINITY ? INFINITY : v[i] * LOG2E;
+          st[SMALL + i * 32 + lane] = v[2 + i];
+        }
+      }
+      if (tail) {
+        if (!wait_all(bTail, (uint32_t)tails & 1u, abort_flag, p.a.status)) { ok = false; break; }
+        ++tails;
+        clear_rows<HD>(tile, SMALL, there, lane);
+        clear_rows<HD>(tile + C::kSmall, SMALL, there, lane);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bFull(s));
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bFull(s));
+    }
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    const uint64_t dB0 = make_desc(sBig0, 16, 1024), dB1 = make_desc(sBig1, 16, 1024);
+    const uint64_t dS0 = make_desc(sSmall, 16, 1024), dS1 = make_desc(sSmall + C::kSmall, 16, 1024);
+    const uint64_t dS0mn = make_desc(sSmall, SMALL * 128, 1024), dS1mn = make_desc(sSmall + C::kSmall, SMALL * 128, 1024);
+    auto scores = [&](int it) {  // both contract over channels
+      const uint32_t off = (uint32_t)(it % NS) * C::kStage, t = tmem + 128 * (it % NB);
+      if (leader) {
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k)
+          tc_mma(t, desc_add(dB0, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS0, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k)
+          tc_mma(t + 64, desc_add(dB1, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS1, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+        tc_commit(bScores(it % NB));
+      }
+    };
+    bool ok = n_it == 0 || wait_all(bBig, 0, abort_flag, p.a.status);
+    for (int it = 0; it < NB && it < n_it && ok; ++it) {
+      ok = wait_all(bFull(it % NS), 0, abort_flag, p.a.status);
+      tc_fence_after();
+      if (ok) scores(it);
+    }
+    for (int it = 0; it < n_it && ok; ++it) {
+      if (!wait_all(bProbs(it % NB), (uint32_t)(it / NB) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t off = (uint32_t)(it % NS) * C::kStage, t = tmem + 128 * (it % NB);
+      if (leader) {  // contraction over the tile's rows
+        if (kDKV) {
+#pragma unroll
+          for (int k = 0; k < SMALL / 16; ++k)  // dV += P^T dO
+            tc_mma_ts(tAcc1, t + (k / 2) * 32 + (k % 2) * 8, desc_add(dS1mn, off + 2048 * k), kIdesc<HD, 1>, (it | k) != 0);
+        }
+#pragma unroll
+        for (int k = 0; k < SMALL / 16; ++k)  // dK += dS^T Q, dQ += dS K
+          tc_mma_ts(tAcc0, t + 64 + (k / 2) * 32 + (k % 2) * 8, desc_add(dS0mn, off + 2048 * k), kIdesc<HD, 1>, (it | k) != 0);
+        tc_commit(bFree(it % NS));
+      }
+      if (it + NB < n_it) {  // into the buffer that these have read (products run in order)
+        if (!wait_all(bFull((it + NB) % NS), (uint32_t)((it + NB) / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+        tc_fence_after();
+        scores(it + NB);
+      }
+    }
+    if (leader) tc_commit(bDone);
+  } else {
+    const int ch = (warp - 2) >> 2;  // which 32 rows of a tile (columns of the scores) this warp has
+    const int quarter = warp & 3, row = quarter * 32 + lane, brow = big0 + row;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const float scale2 = p.a.scale * LOG2E;
+    float my_lse = INFINITY, my_d = 0.0f;
+    if (!kDKV && brow < n_big) {
+      const int64_t at = (int64_t)w.h * p.a.q_rows + sq.q0 + brow;
+      my_lse = p.lse[at] == -INFINITY ? INFINITY : p.lse[at] * LOG2E;
+      my_d = p.drow[at];
+    }
+    bool ok = true;
+    for (int it = 0; it < n_it; ++it) {
+      if (!wait_all(bScores(it % NB), (uint32_t)(it / NB) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+      // (over since before the scores were formed: makes the statistics that the copying warp wrote visible here)
+      if (kDKV && !wait_all(bFull(it % NS), (uint32_t)(it / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+      tc_fence_after();
+      const int c0 = (t_beg + it % tiles) * SMALL;
+      const uint32_t t = tmem + lanes + 128 * (it % NB) + ch * 32;
+      float sc[32], dp[32];
+      tc_ld32_async(t, sc);
+      tc_ld32_async(t + 64, dp);
+      tc_ld_wait();
+      // does every row of the block see (is every row of the block seen by) the whole tile?
+      const bool full = kDKV ? (!p.a.causal || big0 + BIG - 1 <= c0 + shift) : (c0 + SMALL <= sq.nk && (!p.a.causal || c0 + SMALL - 1 <= big0 + shift));
+      if (kDKV) {
+        const float4* st = reinterpret_cast<const float4*>(stats + (it % NS) * 2 * SMALL + ch * 32);
+#pragma unroll
+        for (int c = 0; c < 32; c += 4) {
+          const float4 l4 = st[c / 4], d4 = st[SMALL / 4 + c / 4];
+          const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sc[c + e] = fast_exp2(fmaf(sc[c + e], scale2, -l[e]));
+            dp[c + e] = sc[c + e] * (dp[c + e] - dd[e]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          sc[c] = fast_exp2(fmaf(sc[c], scale2, -my_lse));
+          dp[c] = sc[c] * (dp[c] - my_d);
+        }
+      }
+      if (!full) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          const int col = c0 + ch * 32 + c;  // dK, dV: a query, the row a key; dQ: a key, the row a query
+          const bool vis = kDKV ? brow <= col + shift : (col <= brow + shift && col < sq.nk);
+          sc[c] = vis ? sc[c] : 0.0f;
+          dp[c] = vis ? dp[c] : 0.0f;
+        }
+      }
+      uint32_t packed[16];
+      if (kDKV) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) packed[i] = pack2(sc[2 * i], sc[2 * i + 1]);
+        tc_st16(t, packed);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) packed[i] = pack2(dp[2 * i], dp[2 * i + 1]);
+      tc_st16(t + 64, packed);
+      tc_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bProbs(it % NB));
+    }
+    ok = ok && wait_all(bDone, 0, abort_flag, p.a.status);
+    if (ok) {  // accumulators -> bf16 -> shared memory (the block's own tiles are free) -> rows
+      tc_fence_after();
+      constexpr int kHalf = HD / 2;  // channels of this warp
+#pragma unroll 1
+      for (int o = 0; o < (kDKV ? 2 : 1); ++o) {
+        const uint32_t tile = o == 0 ? sBig0 : sBig1;
+        const float mul = o == 0 ? p.a.scale : 1.0f;  // dK and dQ carry the scores' scale
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 32) {
+          float v[32];
+          const int at = ch * kHalf + c;
+          if (n_it > 0) tc_ld32((o == 0 ? tAcc0 : tAcc1) + lanes + at, v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = n_it > 0 ? v[i] * mul : 0.0f;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) st_shared16(swz(tile + (at / SUB) * BIG * 128, row, (at % SUB) / 8 + u), pack8(v + 8 * u));
+        }
+        __syncwarp();
+        const hbp_heads& out = kDKV ? (o == 0 ? p.dk : p.dv) : p.dq;
+        store_staged<kHalf / 8>(tile, quarter * 32, ch * kHalf / 8, (bf16*)out.x + ((kDKV ? sq.k0 : sq.q0) + big0) * out.row_stride + w.h * out.head_stride,
+                                out.row_stride, n_big - big0, p.a.head_dim, lane);
+      }
+    }
+  }
+  leave(warp, tmem, C::kColumns, abort_flag);
+}
+
+template <int HD>
+__global__ void __launch_bounds__(BWD_THREADS, Bwd<HD>::kBlocksAnSm)
+ragged_bwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p, const unsigned kv_blocks) {
+  if (blockIdx.x < kv_blocks) ragged_bwd_body<HD, true>(m, p, block_at(blockIdx.x, p.a.kv_len, BIG, p.a.kv_heads, false));
+  else ragged_bwd_body<HD, false>(m, p, block_at(blockIdx.x - kv_blocks, p.a.q_len, BIG, p.a.q_heads, true));
+}
+
+// Map {channel, head, row} of a [rows][heads][head_dim] tensor: boxes of 64 channels x 1 head x 64 rows.
+bool map_heads(CUtensorMap* tm, const hbp_heads& t, int64_t rows, int heads, int head_dim) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  // (the stride of a dimension of one element is never used, but is checked all the same)
+  const int64_t hs = heads > 1 ? t.head_stride : head_dim, rs = rows > 1 ? t.row_stride : head_dim;
+  cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows};
+  cuuint64_t strides[2] = {(cuuint64_t)hs * 2, (cuuint64_t)rs * 2};
+  cuuint32_t box[3] = {SUB, 1, SMALL}, estr[3] = {1, 1, 1};
+  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, t.x, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename K>
+bool allow_smem(K kernel, int bytes, bool& done) {
+  if (!done) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+      cudaGetLastError();
+      return false;
+    }
+    done = true;
+  }
+  return true;
+}
+
+template <int HD>
+bool forward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
+  static PerDevice<bool> set;
+  if (!allow_smem(ragged_fwd_tc_kernel<HD>, Fwd<HD>::kSmem, set.here())) return false;
+  const int64_t blocks = blocks_of(r.a.q_len, BIG, r.a.q_heads, r.a.sequences);
+  ragged_fwd_tc_kernel<HD><<<(unsigned)blocks, FWD_THREADS, Fwd<HD>::kSmem, lc.stream>>>(m, r);
+  lc.count();
+  lc.check();
+  return true;
+}
+
+template <int HD>
+bool backward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
+  static PerDevice<bool> set;
+  if (!allow_smem(ragged_bwd_tc_kernel<HD>, Bwd<HD>::kSmem, set.here())) return false;
+  const int64_t kv = blocks_of(r.a.kv_len, BIG, r.a.kv_heads, r.a.sequences), q = blocks_of(r.a.q_len, BIG, r.a.q_heads, r.a.sequences);
+  ragged_bwd_tc_kernel<HD><<<(unsigned)(kv + q), BWD_THREADS, Bwd<HD>::kSmem, lc.stream>>>(m, r, (unsigned)kv);
+  lc.count();
+  lc.check();
+  return true;
+}
+
+// A side without rows has no tensors: its maps are never used.
+bool maps(const RaggedAttn& r, bool back, RaggedMaps& m) {
+  const hbp_attention& a = r.a;
+  if (a.q_len && !map_heads(&m.q, r.q, a.q_rows, a.q_heads, a.head_dim)) return false;
+  if (a.q_len && back && !map_heads(&m.d_o, r.d_o, a.q_rows, a.q_heads, a.head_dim)) return false;
+  return !a.kv_len || (map_heads(&m.k, r.k, a.kv_rows, a.kv_heads, a.head_dim) && map_heads(&m.v, r.v, a.kv_rows, a.kv_heads, a.head_dim));
+}
+
+}  // namespace
+
+bool ragged_forward_tc(Launcher& lc, const RaggedAttn& r) {
+  RaggedMaps m = {};
+  if (!maps(r, false, m)) return false;
+  return r.a.head_dim <= 64 ? forward<64>(lc, r, m) : forward<128>(lc, r, m);
+}
+
+bool ragged_backward_tc(Launcher& lc, const RaggedAttn& r) {
+  RaggedMaps m = {};
+  if (!maps(r, true, m)) return false;
+  return r.a.head_dim <= 64 ? backward<64>(lc, r, m) : backward<128>(lc, r, m);
+}
+
+}  // namespace hbp
