@@ -8,6 +8,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
+import threading
 
 import torch
 
@@ -97,11 +99,11 @@ def _load():
     lib.hbp_param_grads.argtypes = [vp, C.POINTER(hbp_params), vp, vp, vp, C.POINTER(hbp_grads), vp]
     lib.hbp_compare_scratch_bytes.argtypes = [i32]
     lib.hbp_compare.argtypes = [i32, i32, i64, vp, vp, vp, vp, sz, vp]
-    heads = C.POINTER(hbp_heads)
-    lib.hbp_rotary.argtypes = [C.POINTER(hbp_rotary_spec), i32, i32, i64, i32, i32, i32, vp, i32, i64, i64, heads, heads, heads, heads, vp]
-    lib.hbp_attention_forward.argtypes = [C.POINTER(hbp_attention), heads, heads, heads, heads, vp, vp]
-    lib.hbp_attention_scratch_bytes.argtypes = [C.POINTER(hbp_attention), C.POINTER(sz)]
-    lib.hbp_attention_backward.argtypes = [C.POINTER(hbp_attention)] + [heads] * 5 + [vp] + [heads] * 3 + [vp, sz, vp]
+    heads = vp  # (addresses of packed structures)
+    lib.hbp_rotary.argtypes = [vp, i32, i32, i64, i32, i32, i32, vp, i32, i64, i64, heads, heads, heads, heads, vp]
+    lib.hbp_attention_forward.argtypes = [vp, heads, heads, heads, heads, vp, vp]
+    lib.hbp_attention_scratch_bytes.argtypes = [vp, C.POINTER(sz)]
+    lib.hbp_attention_backward.argtypes = [vp] + [heads] * 5 + [vp] + [heads] * 3 + [vp, sz, vp]
     lib.hbp_checkpoint_store.argtypes = [i32, i64, i32, vp, i64, vp, vp, vp]
     lib.hbp_checkpoint_load.argtypes = [i32, i64, i32, vp, vp, vp, i64, vp]
     lib.hbp_checkpoint_gelu.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, vp, vp]
@@ -404,36 +406,71 @@ def compare(a, b, segments=1):
 
 
 # ---- a decoder's step on its own: rotary positions, attention over ragged batches, activations in 8 bits --------------------
-def _here(name, *tensors):
-    """Refuses tensors of another device than the current one: the library launches on the current device's stream."""
-    at = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != at):
-            raise HbpError(1, f"{name}: a tensor is on {t.device}, the current device is cuda:{at}")
+# These calls are short (a launch or two of some microseconds), so what Python does around them counts: structures are packed into a buffer
+# of the calling thread instead of being made anew (rotary positions of one token: 26 us a call with a ctypes structure
+# for each tensor, 14 so), and the stream's handle is asked for without an object around it.
+class _Packed(threading.local):
+    def __init__(self):
+        self.buf = C.create_string_buffer(512)
+        self.at = C.addressof(self.buf)
 
 
-def _shape(ok, name, what):
-    if not ok:
-        raise HbpError(2, f"{name}: {what}")
+_packed = _Packed()
+_ROTARY = struct.Struct("3i6f4x12q")        # hbp_rotary_spec, then four hbp_heads
+_ATTENTION = struct.Struct("8i2q2qf4xq")    # hbp_attention
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _refused(code, name, what):
+    raise HbpError(code, f"{name}: {what}")
+
+
+def _on(name, first, *others):
+    """The stream to launch on: the current one of the current device, which has to be every tensor's."""
+    at = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != at:
+            _refused(1, name, "the tensors are on different devices")
+    if at < 0 or at != torch.cuda.current_device():
+        _refused(1, name, f"a tensor is on {first.device}, which is not the current device")
+    return _raw_stream(at)
+
+
+def _code(t, name):
+    dt = t.dtype
+    if dt is torch.bfloat16:
+        return HBP_BF16
+    if dt is torch.float32:
+        return HBP_F32
+    _refused(3, name, f"dtype {dt}")
 
 
 def _heads(t, name):
-    """hbp_heads of a tensor [rows, heads, head_dim] whose channels are contiguous (any other strides)."""
-    _shape(t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] == 1), name, "wanted [rows, heads, head_dim] with contiguous channels")
-    # (torch gives dimensions of one element any stride)
-    return hbp_heads(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+    """Pointer and strides (elements) of a tensor [rows, heads, head_dim] whose channels are contiguous."""
+    st = t.stride()
+    if len(st) != 3 or (st[2] != 1 and t.shape[2] != 1):
+        _refused(2, name, "wanted [rows, heads, head_dim] with contiguous channels")
+    rows, heads, _ = t.shape  # (a dimension of one element has any stride)
+    return t.data_ptr(), st[0] if rows > 1 else 0, st[1] if heads > 1 else 0
 
 
 def _matrix(t, name):
-    _shape(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), name, "wanted [rows, channels] with contiguous channels")
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and t.shape[1] != 1):
+        _refused(2, name, "wanted [rows, channels] with contiguous channels")
     # (a single row has no stride of its own)
-    return _ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr(), st[0] if t.shape[0] > 1 else t.shape[1]
+
+
+def _alike(t, like, name, what):
+    if t.shape != like.shape or t.dtype != like.dtype:
+        _refused(2, name, what)
 
 
 def rotary_spec(rotary_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained_length=0.0, fast=32.0, slow=1.0,
                 amplitude=1.0) -> hbp_rotary_spec:
     if layout not in ROTARY_LAYOUTS or scaling not in ROTARY_SCALINGS:
-        raise HbpError(6, f"rotary layout {layout!r}, scaling {scaling!r}")
+        _refused(6, "rotary", f"layout {layout!r}, scaling {scaling!r}")
     return hbp_rotary_spec(ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], rotary_dim, base, factor, trained_length, fast, slow, amplitude)
 
 
@@ -442,47 +479,77 @@ def rotary(q, k=None, positions=None, first=0, period=0, rotary_dim=None, base=1
     """Rotary positions on q [rows, heads, head_dim] and, in the same launch, k [rows, kv_heads, head_dim]: see hbp_rotary.
     Returns (q_out, k_out), new tensors unless given (they may be q and k themselves); ``inverse`` is the gradient.
     ``positions``: int32 or int64 [rows] on the device, or None for first + row % period (period 0: first + row)."""
-    _here("rotary", q, k, positions, q_out, k_out)
+    if layout not in ROTARY_LAYOUTS or scaling not in ROTARY_SCALINGS:
+        _refused(6, "rotary", f"layout {layout!r}, scaling {scaling!r}")
+    q_out = torch.empty_like(q) if q_out is None else q_out
+    k_out = torch.empty_like(k) if k is not None and k_out is None else k_out
+    stream = _on("rotary", q, k, positions, q_out, k_out)
+    if q.dim() != 3:
+        _refused(2, "rotary", "wanted [rows, heads, head_dim]")
     rows, q_heads, head_dim = q.shape
-    spec = rotary_spec(head_dim if rotary_dim is None else rotary_dim, base, layout, scaling, factor, trained_length, fast, slow, amplitude)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    _shape(q_out.shape == q.shape and q_out.dtype == q.dtype, "rotary", "q_out is not like q")
-    kv_heads, kh, ko = 0, None, None
+    _alike(q_out, q, "rotary", "q_out is not like q")
+    kv_heads, kh, ko = 0, (0, 0, 0), (0, 0, 0)
     if k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
-        _shape(k.dim() == 3 and k.shape[0] == rows and k.shape[2] == head_dim and k.dtype == q.dtype, "rotary", "k is not like q")
-        _shape(k_out.shape == k.shape and k_out.dtype == k.dtype, "rotary", "k_out is not like k")
-        kv_heads, kh, ko = k.shape[1], C.byref(_heads(k, "rotary k")), C.byref(_heads(k_out, "rotary k_out"))
-    size = 0
+        if k.dim() != 3 or k.shape[0] != rows or k.shape[2] != head_dim or k.dtype != q.dtype:
+            _refused(2, "rotary", "k is not like q")
+        _alike(k_out, k, "rotary", "k_out is not like k")
+        kv_heads, kh, ko = k.shape[1], _heads(k, "rotary k"), _heads(k_out, "rotary k_out")
+    at, size = None, 0
     if positions is not None:
-        _shape(positions.shape == (rows,) and positions.is_contiguous() and positions.dtype in (torch.int32, torch.int64), "rotary",
-               "positions: wanted int32 or int64 [rows]")
-        size = positions.element_size()
-    _check(lib.hbp_rotary(C.byref(spec), int(inverse), _dtype_code(q.dtype), rows, q_heads, kv_heads, head_dim, _ptr(positions), size,
-                          first, period, C.byref(_heads(q, "rotary q")), C.byref(_heads(q_out, "rotary q_out")), kh, ko, _stream()), "hbp_rotary")
+        size = 4 if positions.dtype is torch.int32 else 8 if positions.dtype is torch.int64 else 0
+        if not size or positions.shape != (rows,) or not positions.is_contiguous():
+            _refused(2, "rotary", "positions: wanted int32 or int64 [rows]")
+        at = positions.data_ptr()
+    p = _packed
+    _ROTARY.pack_into(p.buf, 0, ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], head_dim if rotary_dim is None else rotary_dim, base, factor,
+                      trained_length, fast, slow, amplitude, *_heads(q, "rotary q"), *_heads(q_out, "rotary q_out"), *kh, *ko)
+    h = p.at + 40
+    _check(lib.hbp_rotary(p.at, inverse, _code(q, "rotary"), rows, q_heads, kv_heads, head_dim, at, size, first, period, h, h + 24, h + 48, h + 72,
+                          stream), "hbp_rotary")
     return q_out, k_out
 
 
 def _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status):
-    _shape(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.shape[2] == q.shape[2], name, "q, k and v do not belong together")
-    _shape(q.dtype == k.dtype == v.dtype, name, "q, k and v differ in type")
-    for off in (q_offsets, kv_offsets):
+    """Packs the hbp_attention."""
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:
+        _refused(2, name, "q, k and v do not belong together")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        _refused(2, name, "q, k and v differ in type")
+    at = [0, 0]
+    for i, off in enumerate((q_offsets, kv_offsets)):
         if off is None:
             continue
-        _shape(off.dim() == 1 and off.is_contiguous() and off.dtype == torch.int32 and off.numel() >= 1, name, "offsets: wanted int32 [sequences + 1]")
-        _shape(sequences is None or sequences == off.numel() - 1, name, "offsets of another number of sequences")
+        if off.dim() != 1 or not off.is_contiguous() or off.dtype is not torch.int32 or off.numel() < 1:
+            _refused(2, name, "offsets: wanted int32 [sequences + 1]")
+        if sequences is not None and sequences != off.numel() - 1:
+            _refused(2, name, "offsets of another number of sequences")
         sequences = off.numel() - 1
+        at[i] = off.data_ptr()
     if sequences is None:
         sequences = 1
+    q_rows, q_heads, head_dim = q.shape
+    kv_rows, kv_heads, _ = k.shape
     if q_len is None:
-        _shape(q_offsets is None, name, "q_len, the longest of the sequences, has to be given with q_offsets")
-        q_len = q.shape[0] // sequences if sequences else 0
+        if at[0]:
+            _refused(2, name, "q_len, the longest of the sequences, has to be given with q_offsets")
+        q_len = q_rows // sequences if sequences else 0
     if kv_len is None:
-        _shape(kv_offsets is None, name, "kv_len, the longest of the sequences, has to be given with kv_offsets")
-        kv_len = k.shape[0] // sequences if sequences else 0
-    _shape(status is None or (status.dtype == torch.int32 and status.numel() >= 1), name, "status: wanted an int32 tensor")
-    return hbp_attention(_dtype_code(q.dtype), int(causal), sequences, q.shape[1], k.shape[1], q.shape[2], q_len, kv_len, q.shape[0], k.shape[0],
-                         _ptr(q_offsets), _ptr(kv_offsets), q.shape[2] ** -0.5 if scale is None else scale, _ptr(status))
+        if at[1]:
+            _refused(2, name, "kv_len, the longest of the sequences, has to be given with kv_offsets")
+        kv_len = kv_rows // sequences if sequences else 0
+    if status is not None and (status.dtype is not torch.int32 or status.numel() < 1):
+        _refused(2, name, "status: wanted an int32 tensor")
+    _ATTENTION.pack_into(_packed.buf, 0, _code(q, name), causal, sequences, q_heads, kv_heads, head_dim, q_len, kv_len, q_rows, kv_rows, at[0], at[1],
+                         head_dim ** -0.5 if scale is None else scale, 0 if status is None else status.data_ptr())
+    return _packed.at
+
+
+_HEADS = [struct.Struct(f"{3 * n}q") for n in range(9)]
+
+
+def _lse_of(q, lse, name):
+    if lse.shape != (q.shape[1], q.shape[0]) or not lse.is_contiguous() or lse.dtype is not torch.float32:
+        _refused(2, name, "lse: wanted float [q_heads, q_rows]")
 
 
 def attention_forward(q, k, v, sequences=None, q_len=None, kv_len=None, q_offsets=None, kv_offsets=None, causal=True, scale=None,
@@ -490,35 +557,38 @@ def attention_forward(q, k, v, sequences=None, q_len=None, kv_len=None, q_offset
     """softmax(scale q k^T) v over pairs of sequences: see hbp_attention_forward.  q [q_rows, q_heads, head_dim], k and v
     [kv_rows, kv_heads, head_dim]; returns o like q and lse [q_heads, q_rows] (float).  Without offsets the rows are ``sequences``
     sequences of equal length; with them (int32 [sequences + 1], on the device) q_len / kv_len are the longest ones'."""
-    _here("attention_forward", q, k, v, q_offsets, kv_offsets, o, lse, status)
-    a = _attention("attention_forward", q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if o is None else o
+    name = "attention_forward"
+    a = _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
+    o = torch.empty_like(q) if o is None else o
     lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device) if lse is None else lse
-    _shape(o.shape == q.shape and o.dtype == q.dtype, "attention_forward", "o is not like q")
-    _shape(lse.shape == (q.shape[1], q.shape[0]) and lse.is_contiguous() and lse.dtype == torch.float32, "attention_forward", "lse: wanted float [q_heads, q_rows]")
-    _check(lib.hbp_attention_forward(C.byref(a), C.byref(_heads(q, "q")), C.byref(_heads(k, "k")), C.byref(_heads(v, "v")),
-                                     C.byref(_heads(o, "o")), _ptr(lse), _stream()), "hbp_attention_forward")
+    stream = _on(name, q, k, v, q_offsets, kv_offsets, o, lse, status)
+    _alike(o, q, name, "o is not like q")
+    _lse_of(q, lse, name)
+    _HEADS[4].pack_into(_packed.buf, 80, *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), *_heads(o, "o"))
+    _check(lib.hbp_attention_forward(a, a + 80, a + 104, a + 128, a + 152, lse.data_ptr(), stream), "hbp_attention_forward")
     return o, lse
 
 
 def attention_backward(d_o, q, k, v, o, lse, sequences=None, q_len=None, kv_len=None, q_offsets=None, kv_offsets=None, causal=True,
                        scale=None, dq=None, dk=None, dv=None, scratch=None, status=None):
     """The gradients (dq, dk, dv) of attention_forward's q, k and v from that of its output: see hbp_attention_backward."""
-    _here("attention_backward", d_o, q, k, v, o, lse, q_offsets, kv_offsets, dq, dk, dv, scratch, status)
-    a = _attention("attention_backward", q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
-    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
-    for t, like in ((d_o, q), (o, q), (dq, q), (dk, k), (dv, v)):
-        _shape(t.shape == like.shape and t.dtype == like.dtype, "attention_backward", "a gradient is not like its tensor")
-    _shape(lse.shape == (q.shape[1], q.shape[0]) and lse.is_contiguous() and lse.dtype == torch.float32, "attention_backward", "lse: wanted float [q_heads, q_rows]")
-    need = 4 * lse.numel()
-    if scratch is None:
-        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _check(lib.hbp_attention_backward(C.byref(a), C.byref(_heads(d_o, "d_o")), C.byref(_heads(q, "q")), C.byref(_heads(k, "k")),
-                                      C.byref(_heads(v, "v")), C.byref(_heads(o, "o")), _ptr(lse), C.byref(_heads(dq, "dq")),
-                                      C.byref(_heads(dk, "dk")), C.byref(_heads(dv, "dv")), _ptr(scratch),
-                                      scratch.numel() * scratch.element_size(), _stream()), "hbp_attention_backward")
+    name = "attention_backward"
+    a = _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
+    dq = torch.empty_like(q) if dq is None else dq
+    dk = torch.empty_like(k) if dk is None else dk
+    dv = torch.empty_like(v) if dv is None else dv
+    scratch = torch.empty_like(lse) if scratch is None else scratch
+    stream = _on(name, q, k, v, d_o, o, lse, q_offsets, kv_offsets, dq, dk, dv, scratch, status)
+    _alike(d_o, q, name, "d_o is not like q")
+    _alike(o, q, name, "o is not like q")
+    _alike(dq, q, name, "dq is not like q")
+    _alike(dk, k, name, "dk is not like k")
+    _alike(dv, v, name, "dv is not like v")
+    _lse_of(q, lse, name)
+    _HEADS[8].pack_into(_packed.buf, 80, *_heads(d_o, "d_o"), *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), *_heads(o, "o"), *_heads(dq, "dq"),
+                        *_heads(dk, "dk"), *_heads(dv, "dv"))
+    _check(lib.hbp_attention_backward(a, a + 80, a + 104, a + 128, a + 152, a + 176, lse.data_ptr(), a + 200, a + 224, a + 248, scratch.data_ptr(),
+                                      scratch.numel() * scratch.element_size(), stream), "hbp_attention_backward")
     return dq, dk, dv
 
 
@@ -526,69 +596,81 @@ def attention_scratch_bytes(q_heads, q_rows) -> int:
     """Bytes of the scratch of attention_backward."""
     a = hbp_attention(HBP_F32, 0, 0, q_heads, q_heads, 4, 0, 0, q_rows, 0, None, None, 1.0, None)
     n = C.c_size_t(0)
-    _check(lib.hbp_attention_scratch_bytes(C.byref(a), C.byref(n)), "hbp_attention_scratch_bytes")
+    _check(lib.hbp_attention_scratch_bytes(C.addressof(a), C.byref(n)), "hbp_attention_scratch_bytes")
     return n.value
 
 
 def _kept(rows, d, codes, scales, device, name):
+    """Codes and scales of an activation [rows, d], made where not given."""
     groups = (d + CHECKPOINT_GROUP - 1) // CHECKPOINT_GROUP
-    codes = torch.empty((rows, d), dtype=torch.int8, device=device) if codes is None else codes
-    scales = torch.empty((rows, groups), dtype=torch.uint8, device=device) if scales is None else scales
-    _shape(codes.shape == (rows, d) and codes.is_contiguous() and codes.dtype == torch.int8, name, "codes: wanted int8 [rows, channels]")
-    _shape(scales.shape == (rows, groups) and scales.is_contiguous() and scales.dtype == torch.uint8, name, "scales: wanted uint8 [rows, channels / 32 rounded up]")
+    if codes is None:
+        codes = torch.empty((rows, d), dtype=torch.int8, device=device)
+    elif codes.shape != (rows, d) or not codes.is_contiguous() or codes.dtype is not torch.int8:
+        _refused(2, name, "codes: wanted int8 [rows, channels]")
+    if scales is None:
+        scales = torch.empty((rows, groups), dtype=torch.uint8, device=device)
+    elif scales.shape != (rows, groups) or not scales.is_contiguous() or scales.dtype is not torch.uint8:
+        _refused(2, name, "scales: wanted uint8 [rows, channels / 32 rounded up]")
     return codes, scales
 
 
 def checkpoint_store(x, codes=None, scales=None):
     """x [rows, channels] in 8 bits: (codes int8 like x, scales uint8 [rows, channels / 32 rounded up]); see hbp_checkpoint_store."""
-    _here("checkpoint_store", x, codes, scales)
-    px, ld = _matrix(x, "checkpoint_store")
+    name = "checkpoint_store"
+    px, ld = _matrix(x, name)
     rows, d = x.shape
-    codes, scales = _kept(rows, d, codes, scales, x.device, "checkpoint_store")
-    _check(lib.hbp_checkpoint_store(_dtype_code(x.dtype), rows, d, px, ld, _ptr(codes), _ptr(scales), _stream()), "hbp_checkpoint_store")
+    codes, scales = _kept(rows, d, codes, scales, x.device, name)
+    _check(lib.hbp_checkpoint_store(_code(x, name), rows, d, px, ld, codes.data_ptr(), scales.data_ptr(), _on(name, x, codes, scales)), "hbp_checkpoint_store")
     return codes, scales
 
 
 def checkpoint_load(codes, scales, dtype=torch.bfloat16, out=None):
     """The values that checkpoint_store kept, exactly, in dtype."""
-    _here("checkpoint_load", codes, scales, out)
-    _shape(codes.dim() == 2, "checkpoint_load", "codes: wanted int8 [rows, channels]")
+    name = "checkpoint_load"
+    if codes.dim() != 2:
+        _refused(2, name, "codes: wanted int8 [rows, channels]")
     rows, d = codes.shape
-    codes, scales = _kept(rows, d, codes, scales, codes.device, "checkpoint_load")
-    out = torch.empty((rows, d), dtype=dtype, device=codes.device) if out is None else out
-    _shape(out.shape == codes.shape, "checkpoint_load", "out is not like codes")
-    px, ld = _matrix(out, "checkpoint_load")
-    _check(lib.hbp_checkpoint_load(_dtype_code(out.dtype), rows, d, _ptr(codes), _ptr(scales), px, ld, _stream()), "hbp_checkpoint_load")
+    codes, scales = _kept(rows, d, codes, scales, codes.device, name)
+    out = torch.empty_like(codes, dtype=dtype) if out is None else out
+    if out.shape != codes.shape:
+        _refused(2, name, "out is not like codes")
+    px, ld = _matrix(out, name)
+    _check(lib.hbp_checkpoint_load(_code(out, name), rows, d, codes.data_ptr(), scales.data_ptr(), px, ld, _on(name, codes, scales, out)), "hbp_checkpoint_load")
     return out
 
 
 def checkpoint_gelu(z, act=None, codes=None, scales=None):
     """(gelu(z), codes, scales): GELU of z [rows, channels] (``act`` may be z itself), and z in 8 bits for the backward pass."""
-    _here("checkpoint_gelu", z, act, codes, scales)
-    pz, ldz = _matrix(z, "checkpoint_gelu")
+    name = "checkpoint_gelu"
+    pz, ldz = _matrix(z, name)
     rows, d = z.shape
-    codes, scales = _kept(rows, d, codes, scales, z.device, "checkpoint_gelu")
+    codes, scales = _kept(rows, d, codes, scales, z.device, name)
     act = torch.empty((rows, d), dtype=z.dtype, device=z.device) if act is None else act
-    _shape(act.shape == z.shape and act.dtype == z.dtype, "checkpoint_gelu", "act is not like z")
-    pa, lda = _matrix(act, "checkpoint_gelu")
-    _check(lib.hbp_checkpoint_gelu(_dtype_code(z.dtype), rows, d, pz, ldz, pa, lda, _ptr(codes), _ptr(scales), _stream()), "hbp_checkpoint_gelu")
+    _alike(act, z, name, "act is not like z")
+    pa, lda = _matrix(act, name)
+    _check(lib.hbp_checkpoint_gelu(_code(z, name), rows, d, pz, ldz, pa, lda, codes.data_ptr(), scales.data_ptr(), _on(name, z, codes, scales, act)),
+           "hbp_checkpoint_gelu")
     return act, codes, scales
 
 
 def checkpoint_gelu_backward(d_act, codes, scales, with_act=False, dz=None, act=None):
     """dz = d_act * gelu'(z8) (``dz`` may be d_act itself) from the z that checkpoint_gelu kept, and with ``with_act`` (or
     ``act`` given) gelu(z8) too, the operand of the following product's weight gradient: dz, or (dz, act)."""
-    _here("checkpoint_gelu_backward", d_act, codes, scales, dz, act)
-    pd, ldd = _matrix(d_act, "checkpoint_gelu_backward")
+    name = "checkpoint_gelu_backward"
+    pd, ldd = _matrix(d_act, name)
     rows, d = d_act.shape
-    codes, scales = _kept(rows, d, codes, scales, d_act.device, "checkpoint_gelu_backward")
+    if codes is None or scales is None:
+        _refused(1, name, "codes and scales have to be given")
+    codes, scales = _kept(rows, d, codes, scales, d_act.device, name)
     dz = torch.empty((rows, d), dtype=d_act.dtype, device=d_act.device) if dz is None else dz
+    _alike(dz, d_act, name, "dz is not like d_act")
+    pz, ldz = _matrix(dz, name)
     if with_act and act is None:
         act = torch.empty((rows, d), dtype=d_act.dtype, device=d_act.device)
-    for t in (dz, act):
-        _shape(t is None or (t.shape == d_act.shape and t.dtype == d_act.dtype), "checkpoint_gelu_backward", "an output is not like d_act")
-    pz, ldz = _matrix(dz, "checkpoint_gelu_backward")
-    pa, lda = (None, 0) if act is None else _matrix(act, "checkpoint_gelu_backward")
-    _check(lib.hbp_checkpoint_gelu_backward(_dtype_code(d_act.dtype), rows, d, _ptr(codes), _ptr(scales), pd, ldd, pz, ldz, pa, lda, _stream()),
-           "hbp_checkpoint_gelu_backward")
+    pa, lda = None, 0
+    if act is not None:
+        _alike(act, d_act, name, "act is not like d_act")
+        pa, lda = _matrix(act, name)
+    _check(lib.hbp_checkpoint_gelu_backward(_code(d_act, name), rows, d, codes.data_ptr(), scales.data_ptr(), pd, ldd, pz, ldz, pa, lda,
+                                            _on(name, d_act, codes, scales, dz, act)), "hbp_checkpoint_gelu_backward")
     return dz if act is None else (dz, act)
