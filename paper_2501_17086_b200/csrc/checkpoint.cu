@@ -4,18 +4,23 @@
 // largest magnitude (the maximum is taken over bit patterns, so that infinities and NaN come out on top of it).  Powers of two
 // make both directions exact but for the one rounding to a whole number, and every stored value a bf16 number.
 //
-// HBM-bound: a thread moves kBatch vectors of 16 bytes, all loads before the first use.  A group is 4 (bf16) or 8 (float)
-// neighbouring lanes, its maximum 2 or 3 shuffles.  bf16 values leave 27 instruction slots a value before GELU costs more than
-// its bytes, and erff alone takes that many: there erfc is formed by formula 7.1.26 of Abramowitz and Stegun, "Handbook of
-// Mathematical Functions" (absolute error 1.5e-7; half a step of bf16 is 2^-9 of the value), whose exponential is GELU's
-// density as well: one ex2, one reciprocal and some 14 other instructions for gelu and gelu' together.
-#include "hbp_internal.h"
+// HBM-bound, if the arithmetic stays out of the way: at 6.5 TB/s an SM has 27 instruction slots for each bf16 value of GELU's forward
+// pass.  So whole numbers are rounded and widened by adding 1.5 * 2^23 (conversions run at an eighth of the rate),
+// magnitudes of bf16 pairs are compared two at a time, float arithmetic is done on pairs (one instruction for two values), and
+// erfc of bf16 values is formed by formula 7.1.26 of Abramowitz and Stegun, "Handbook of Mathematical Functions" (absolute error
+// 1.5e-7; half a step of bf16 is 2^-9 of the value; erff alone takes some 25 instructions), whose exponential is GELU's
+// density as well: one ex2 and one reciprocal serve gelu and gelu' together.
+// 8192 x 4096 bf16, us (of what a copy of the same bytes takes): store 18.5 (0.84), load 18.5 (0.84), GELU 28.9 (0.89), its backward
+// pass with gelu 39.0 (0.92).  With erff, conversions and one value at a time: 24.6, 24.8, 40.6, 57.4.
+// A thread moves kBatch vectors of 16 bytes, all loads before the first use.  A group is 4 (bf16) or 8 (float) neighbouring lanes, its
+// maximum 2 or 3 shuffles.  (kBatch 1, 2, 4: store 22.6, 18.5, 18.7; GELU 32.7, 28.9, 30.0; float 8192 x 1024 stored 12.6, 10.3, 10.3.)
+#include "float_pairs.cuh"
 
 namespace hbp {
 
 namespace {
 
-constexpr int kThreads = 256, kBatch = 4;
+constexpr int kThreads = 256, kBatch = 2;
 constexpr int kGroup = 32;
 
 enum Work { kStore = 0, kLoad = 1, kGelu = 2, kGeluBackward = 3 };
@@ -33,31 +38,65 @@ struct CheckpointParams {
   uint8_t* scales;
 };
 
-template <typename T, int N>
-struct alignas(sizeof(T) * N) Vec {
-  T v[N];
-};
-
-// gelu(z) and gelu'(z); every rounding is written out, so that no call's other outputs change them
-__device__ __forceinline__ void gelu_both(float z, float& act, float& slope, float) {
+// gelu(z) and gelu'(z) of two values; every rounding is written out, so that no call's other outputs change them
+__device__ __forceinline__ void gelu_one(float z, float& act, float& slope) {
   const float phi = fmaf(0.5f, erff(__fmul_rn(z, 0.70710678118654752440f)), 0.5f);
   act = __fmul_rn(z, phi);
   slope = fmaf(__fmul_rn(z, expf(__fmul_rn(__fmul_rn(-0.5f, z), z))), 0.39894228040143267794f, phi);
 }
-__device__ __forceinline__ void gelu_both(float z, float& act, float& slope, bf16) {
-  const float a = fabsf(z);
-  float e, t;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__fmul_rn(__fmul_rn(z, z), -0.72134752044448170368f)));      // e^(-z^2 / 2)
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(a, 0.23164188f, 1.0f)));            // 1 / (1 + p |z| / sqrt 2)
-  // the formula's coefficients over two: half of erfc(|z| / sqrt 2)
-  float q = fmaf(t, 0.5307027145f, -0.7265760135f);
-  q = fmaf(q, t, 0.7107068705f);
-  q = fmaf(q, t, -0.142248368f);
-  q = fmaf(q, t, 0.127414796f);
-  const float tail = __fmul_rn(__fmul_rn(q, t), e);
-  const float phi = z < 0.0f ? tail : __fsub_rn(1.0f, tail);
-  act = __fmul_rn(z, phi);
-  slope = fmaf(__fmul_rn(z, e), 0.39894228040143267794f, phi);
+__device__ __forceinline__ void gelu_pair(float2 z, float2& act, float2& slope, float) {
+  gelu_one(z.x, act.x, slope.x);
+  gelu_one(z.y, act.y, slope.y);
+}
+__device__ __forceinline__ void gelu_pair(float2 zf, float2& act, float2& slope, bf16) {
+  const f32x2 z = pair_of(zf.x, zf.y);
+  const float2 arg = floats_of(mul2(mul2(z, z), both(-0.72134752044448170368f)));
+  const float2 den = floats_of(fma2(pair_of(fabsf(zf.x), fabsf(zf.y)), both(0.23164188f), both(1.0f)));
+  float2 ef, tf;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ef.x) : "f"(arg.x));  // e^(-z^2 / 2)
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ef.y) : "f"(arg.y));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(tf.x) : "f"(den.x));  // 1 / (1 + p |z| / sqrt 2)
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(tf.y) : "f"(den.y));
+  const f32x2 e = pair_of(ef.x, ef.y), t = pair_of(tf.x, tf.y);
+  // minus the formula's coefficients over two: half of erfc(|z| / sqrt 2), negated
+  f32x2 q = fma2(t, both(-0.5307027145f), both(0.7265760135f));
+  q = fma2(q, t, both(-0.7107068705f));
+  q = fma2(q, t, both(0.142248368f));
+  q = fma2(q, t, both(-0.127414796f));
+  // the normal distribution's cumulative function: 1/2 +- (1/2 - that half)
+  const float2 m = floats_of(fma2(mul2(q, t), e, both(0.5f)));
+  const f32x2 phi = add2(pair_of(copysignf(m.x, zf.x), copysignf(m.y, zf.y)), both(0.5f));
+  act = floats_of(mul2(z, phi));
+  slope = floats_of(fma2(mul2(z, e), both(0.39894228040143267794f), phi));
+}
+
+// Bits of the largest magnitude of a vector, as a float's
+__device__ __forceinline__ uint32_t largest(const float* v) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(v[e]) & 0x7fffffffu);
+  return m;
+}
+__device__ __forceinline__ uint32_t largest(const bf16* v) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m = __vmaxu2(m, w[e] & 0x7fff7fffu);
+  return max(m << 16, m & 0xffff0000u);
+}
+constexpr float kMagic = 12582912.0f;  // 1.5 * 2^23: what is added to it is rounded to a whole number, in its low bits
+// four codes of four values
+__device__ __forceinline__ uint32_t codes_of(const float* f, float inv) {
+  uint32_t b[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) b[e] = __float_as_uint(fmaf(f[e], inv, kMagic));
+  return __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+}
+// and back
+__device__ __forceinline__ void values_of(uint32_t c, float step, float* f) {
+  c ^= 0x80808080u;  // codes + 128
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = __fmul_rn(__fsub_rn(__uint_as_float(__byte_perm(c, 0x4b000000u, 0x7440 + e)), 8388736.0f), step);
 }
 
 // e + 127 of a group whose largest magnitude has these bits; 255 where it is not finite
@@ -71,14 +110,14 @@ constexpr uint32_t kLargestScale = 249;  // steps of 2^122, of which 64 are 2^12
 // 2^e; a code times this is the stored value (a group that was not finite: NaN)
 __device__ __forceinline__ float step_of(uint32_t s) { return s == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(s << 23); }
 // 2^-e
-__device__ __forceinline__ float inverse_of(uint32_t s) { return __uint_as_float((254u - s) << 23); }
+__device__ __forceinline__ float inverse_of(uint32_t s) { return __uint_as_float((254u - min(s, 253u)) << 23); }
 
 // kFlat: rows are whole groups without gaps: one run of chunks
 template <typename T, int W, bool kFlat>
 __global__ void __launch_bounds__(kThreads) checkpoint_kernel(const CheckpointParams p) {
   constexpr int V = 16 / (int)sizeof(T), kLanes = kGroup / V;
   using VT = Vec<T, V>;
-  using VC = Vec<int8_t, V>;
+  using VC = Vec<uint32_t, V / 4>;  // four codes a word
   VT x[kBatch];
   VC code[kBatch];
   uint32_t scale[kBatch];
@@ -109,52 +148,60 @@ __global__ void __launch_bounds__(kThreads) checkpoint_kernel(const CheckpointPa
   for (int u = 0; u < kBatch; ++u) {
     const int64_t i = base + u * kThreads;
     const int64_t at_y = kFlat ? i * V : row[u] * p.ldy + col[u];
+    float f[V];
     if (W == kStore || W == kGelu) {
-      uint32_t amax = 0;
-      if (in[u]) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) amax = max(amax, __float_as_uint(to_f(x[u].v[e])) & 0x7fffffffu);
-      }
+      uint32_t amax = in[u] ? largest(x[u].v) : 0u;
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o >>= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, o));
       if (!in[u]) continue;
       const uint32_t s = scale_of(amax);
-      const float inv = s == 255u ? 0.0f : inverse_of(s);
+      const float inv = inverse_of(s);
+      widen<V>(x[u].v, f);
 #pragma unroll
-      for (int e = 0; e < V; ++e) code[u].v[e] = (int8_t)(s == 255u ? 0 : __float2int_rn(to_f(x[u].v[e]) * inv));
-      if (s == kLargestScale) {
+      for (int e = 0; e < V; e += 4) code[u].v[e / 4] = codes_of(f + e, inv);
+      if (s >= kLargestScale) {
+        int8_t* c = reinterpret_cast<int8_t*>(code[u].v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) code[u].v[e] = max(-63, min(63, (int)code[u].v[e]));
+        for (int e = 0; e < V; ++e) c[e] = (int8_t)(s == 255u ? 0 : fabsf(f[e]) >= 63.5f * 0x1p122f ? (f[e] < 0.0f ? -63 : 63) : c[e]);
       }
       *reinterpret_cast<VC*>(p.codes + (kFlat ? i * V : row[u] * p.d + col[u])) = code[u];
       if (i % kLanes == 0) p.scales[kFlat ? i / kLanes : row[u] * p.groups + col[u] / kGroup] = (uint8_t)s;
       if (W == kGelu) {
-        VT y;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          float act, slope;
-          gelu_both(to_f(x[u].v[e]), act, slope, T());
-          y.v[e] = from_f<T>(act);
+        for (int e = 0; e < V; e += 2) {
+          float2 act, slope;
+          gelu_pair(make_float2(f[e], f[e + 1]), act, slope, T());
+          f[e] = act.x;
+          f[e + 1] = act.y;
         }
+        VT y;
+        narrow<V>(f, y.v);
         *reinterpret_cast<VT*>((T*)p.y + at_y) = y;
       }
     } else if (in[u]) {
       const float step = step_of(scale[u]);
       VT y, a;
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float z = (float)code[u].v[e] * step;
-        if (W == kLoad) {
-          y.v[e] = from_f<T>(z);
-        } else {
-          float act, slope;
-          gelu_both(z, act, slope, T());
-          y.v[e] = from_f<T>(to_f(x[u].v[e]) * slope);
-          a.v[e] = from_f<T>(act);
+      for (int e = 0; e < V; e += 4) values_of(code[u].v[e / 4], step, f + e);
+      if (W == kGeluBackward) {
+        float g[V], af[V];
+        widen<V>(x[u].v, g);
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          float2 act, slope;
+          gelu_pair(make_float2(f[e], f[e + 1]), act, slope, T());
+          f[e] = __fmul_rn(g[e], slope.x);
+          f[e + 1] = __fmul_rn(g[e + 1], slope.y);
+          af[e] = act.x;
+          af[e + 1] = act.y;
+        }
+        if (p.act) {
+          narrow<V>(af, a.v);
+          *reinterpret_cast<VT*>((T*)p.act + (kFlat ? i * V : row[u] * p.lda + col[u])) = a;
         }
       }
+      narrow<V>(f, y.v);
       *reinterpret_cast<VT*>((T*)p.y + at_y) = y;
-      if (W == kGeluBackward && p.act) *reinterpret_cast<VT*>((T*)p.act + (kFlat ? i * V : row[u] * p.lda + col[u])) = a;
     }
   }
 }

@@ -1,132 +1,148 @@
 // Rotary positions on the queries and keys of an attention step (hbp_rotary).
 //
-// HBM-bound: every element is read and written once, and a pair costs 6 flops.  What could cost more are the angles: formed in double,
-// since a float product pos * f loses all of its fraction at positions of 2^17, and shared by all heads of a row.  So a thread
-// owns CV pairs of a row for a run of heads: it forms their cosines and sines once, as fractions of a turn (one product and one
-// rounding in double, then sincospif, which needs no reduction), keeps them in registers and streams the heads through,
-// kHeads at a time so that 2 * kHeads 16-byte loads are in flight.  Heads are split over threads only as far as
-// the rows do not fill the chip.
-// bf16, 16384 rows, 12 + 12 heads of 64 (101 MB): FILL
+// HBM-bound: every element is read and written once, and a pair costs 6 flops.  What costs more is everything around them, so
+//  - angles are whole-number fractions of a turn: position times f_i / 2 pi * 2^64, modulo 2^64.  That needs no reduction, is as exact far out as
+//    near (a float product pos * f loses all of its fraction at 2^17), and takes a few integer instructions where doubles took a
+//    conversion, a product, a rounding and a difference;
+//  - they are shared by all heads of a row: a block forms cosines and sines of its rows once, in shared memory, rows fastest, since the lanes of a
+//    warp that read different frequencies from the constant bank would be served one after the other;
+//  - a thread keeps CV pairs of a row (two vectors of up to 16 bytes) and walks over heads: its cosines and sines stay in registers
+//    and a head costs two loads, the rotation and two stores.
+// bf16, 16384 rows, 12 + 12 heads of 64 (101 MB): 22.5 us (4.5 TB/s; 15.4 at the rate of a copy), 8192 rows, 32 + 8 heads of 128 (168 MB): 34.3.
+// With the angles in double and every thread forming its own: 34.8 and 49.6; the pairs of a block dealt out one by one
+// (280 instructions a unit): 26.6 and 36.9.  Blocks of 256 threads and 16 rows, which all start at once and wait at once: 24.6 and 48.0.
+// What is left are the instructions of a unit and the first wait of a block, for its positions.
 #include <cmath>
 
-#include "hbp_internal.h"
+#include "float_pairs.cuh"
 
 namespace hbp {
 
 namespace {
 
-constexpr int kMaxPairs = 128, kHeads = 4, kThreads = 128;
+constexpr int kMaxPairs = 128, kUnroll = 2, kThreads = 128, kMaxRows = 8;
 
 struct RotaryParams {
-  double turns[kMaxPairs];  // f_i / 2 pi
+  uint64_t turns[kMaxPairs];  // f_i / 2 pi * 2^64
   float amplitude, sign;
   int64_t rows, first, period;
   const void* positions;
   int position_bytes;
-  int q_heads, heads;      // heads of q; of q and k
-  int heads_each;          // heads of one thread
-  int turn_chunks, chunks; // chunks of CV pairs that turn; with those that are copied
+  int q_heads, heads;       // heads of q; of q and k
+  int turn_chunks, chunks;  // units of a head that turn; with those that are copied
   int rotary_dim, head_dim;
   hbp_heads q, qo, k, ko;
 };
 
-template <typename T, int N>
-struct alignas(sizeof(T) * N) Vec {
-  T v[N];
-};
-
-// kHalf: the two members of a pair lie rotary_dim / 2 apart.  CV: pairs of a thread; a Vec<T, CV> is at most 16 bytes.
+// A unit is, of every head, in the half layout CV pairs: two vectors of CV channels rotary_dim / 2 apart; in the interleaved one
+// CV / 2 pairs: one vector.  (Two neighbouring vectors there: 49.3 us where this takes 36.9, 8192 rows, 32 + 8 heads of 128.)
+// A unit that is copied has as many vectors, side by side.
 template <typename T, int CV, bool kHalf>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryParams p) {
   using V = Vec<T, CV>;
-  const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = idx / p.chunks;
-  if (row >= p.rows) return;
-  const int c = (int)(idx - row * p.chunks);
+  constexpr int kPairs = kHalf ? CV : CV / 2, kVectors = kHalf ? 2 : 1;
+  // {cosine, sine} of pair i of unit c in row r at [r][i][c]: neighbouring threads, which have neighbouring units, read neighbouring words
+  extern __shared__ float2 table[];
+  const int c = threadIdx.x, slot = threadIdx.y, r = threadIdx.z, slots = blockDim.y, half = p.rotary_dim / 2;
+  const int64_t row = (int64_t)blockIdx.x * blockDim.z + r;
   const bool turning = c < p.turn_chunks;
-  // first channels of the two vectors of this chunk; a copied chunk is two vectors, the second of which may lie past the head
-  const int c0 = !turning ? p.rotary_dim + (c - p.turn_chunks) * 2 * CV : kHalf ? c * CV : 2 * c * CV;
-  const int c1 = turning && kHalf ? c0 + p.rotary_dim / 2 : c0 + CV;
-  const bool both = c1 < p.head_dim;
-  float cs[CV], sn[CV];
-  if (turning) {
+  if (row < p.rows && turning) {
     int64_t pos;
-    if (!p.positions) pos = p.first + (p.period ? row % p.period : row);
+    if (p.position_bytes == 4) pos = ((const int32_t*)p.positions)[row];
     else if (p.position_bytes == 8) pos = ((const int64_t*)p.positions)[row];
-    else pos = ((const int32_t*)p.positions)[row];
-#pragma unroll
-    for (int i = 0; i < CV; ++i) {
-      double t = (double)pos * p.turns[c * CV + i];
-      t -= rint(t);
-      float s, co;
-      sincospif(2.0f * (float)t, &s, &co);
-      cs[i] = p.amplitude * co;
-      sn[i] = p.amplitude * p.sign * s;
+    else pos = p.first + (p.period ? row % p.period : row);
+    for (int i = slot; i < kPairs; i += slots) {
+      const int32_t t = (int32_t)(((uint64_t)pos * p.turns[c * kPairs + i]) >> 32);  // of a turn, from -1/2 on
+      float sn, cs;
+      sincospif((float)t * 0x1p-31f, &sn, &cs);
+      table[(r * kPairs + i) * p.turn_chunks + c] = make_float2(p.amplitude * cs, p.amplitude * p.sign * sn);
     }
   }
-  const int h_end = min(p.heads, (int)(blockIdx.y + 1) * p.heads_each);
-  for (int h0 = blockIdx.y * p.heads_each; h0 < h_end; h0 += kHeads) {
-    V a[kHeads], b[kHeads];
+  __syncthreads();
+  if (row >= p.rows) return;
+  const int c0 = turning ? c * CV : p.rotary_dim + (c - p.turn_chunks) * kVectors * CV;  // first channels of the vectors
+  const int c1 = turning ? c0 + half : c0 + CV;
+  const bool two = kHalf && c1 < p.head_dim;
+  // half layout: cosines, and sines, of two neighbouring pairs at a time; interleaved: (cos, cos) and (-sin, sin) of a pair
+  constexpr int kTwos = kHalf ? (CV + 1) / 2 : kPairs;
+  f32x2 cs[kTwos], sn[kTwos];
+  if (turning) {
 #pragma unroll
-    for (int u = 0; u < kHeads; ++u) {
-      const int h = h0 + u;
-      if (h < h_end) {
-        const bool key = h >= p.q_heads;
-        const T* x = key ? (const T*)p.k.x + row * p.k.row_stride + (h - p.q_heads) * p.k.head_stride
-                         : (const T*)p.q.x + row * p.q.row_stride + h * p.q.head_stride;
-        a[u] = *reinterpret_cast<const V*>(x + c0);
-        if (both) b[u] = *reinterpret_cast<const V*>(x + c1);
+    for (int i = 0; i < kTwos; ++i) {
+      if (kHalf) {
+        const float2 e = table[(r * kPairs + 2 * i) * p.turn_chunks + c], f = table[(r * kPairs + (2 * i + 1) % CV) * p.turn_chunks + c];
+        cs[i] = pair_of(e.x, f.x);
+        sn[i] = pair_of(e.y, f.y);
+      } else {
+        const float2 e = table[(r * kPairs + i) * p.turn_chunks + c];
+        cs[i] = pair_of(e.x, e.x);
+        sn[i] = pair_of(-e.y, e.y);
       }
     }
+  }
+  auto heads = [&](const hbp_heads& in, const hbp_heads& out, int h, int count) {
+    const T* x = (const T*)in.x + row * in.row_stride + h * in.head_stride + c0;
+    T* y = (T*)out.x + row * out.row_stride + h * out.head_stride + c0;
+    const int64_t dx = slots * in.head_stride, dy = slots * out.head_stride;
+    for (; h < count; h += kUnroll * slots) {
+      V a[kUnroll], b[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kHeads; ++u) {
-      const int h = h0 + u;
-      if (h < h_end) {
-        if (turning) {
-          if (kHalf) {
+      for (int u = 0; u < kUnroll; ++u)
+        if (h + u * slots < count) {
+          a[u] = *reinterpret_cast<const V*>(x + u * dx);
+          if (two) b[u] = *reinterpret_cast<const V*>(x + u * dx + (c1 - c0));
+        }
 #pragma unroll
-            for (int i = 0; i < CV; ++i) {
-              const float x0 = to_f(a[u].v[i]), x1 = to_f(b[u].v[i]);
-              a[u].v[i] = from_f<T>(x0 * cs[i] - x1 * sn[i]);
-              b[u].v[i] = from_f<T>(x1 * cs[i] + x0 * sn[i]);
-            }
-          } else if (CV == 1) {
-            const float x0 = to_f(a[u].v[0]), x1 = to_f(b[u].v[0]);
-            a[u].v[0] = from_f<T>(x0 * cs[0] - x1 * sn[0]);
-            b[u].v[0] = from_f<T>(x1 * cs[0] + x0 * sn[0]);
-          } else {
+      for (int u = 0; u < kUnroll; ++u)
+        if (h + u * slots < count) {
+          if (turning) {
+            if (kHalf && CV == 1) {
+              const float2 k = floats_of(cs[0]), l = floats_of(sn[0]);
+              const float m = to_f(a[u].v[0]), n = to_f(b[u].v[0]);
+              a[u].v[0] = from_f<T>(fmaf(m, k.x, -__fmul_rn(n, l.x)));
+              b[u].v[0] = from_f<T>(fmaf(n, k.x, __fmul_rn(m, l.x)));
+            } else {
 #pragma unroll
-            for (int i = 0; i < CV; i += 2) {
-              const float x0 = to_f(a[u].v[i]), x1 = to_f(a[u].v[i + 1]), y0 = to_f(b[u].v[i]), y1 = to_f(b[u].v[i + 1]);
-              a[u].v[i] = from_f<T>(x0 * cs[i / 2] - x1 * sn[i / 2]);
-              a[u].v[i + 1] = from_f<T>(x1 * cs[i / 2] + x0 * sn[i / 2]);
-              b[u].v[i] = from_f<T>(y0 * cs[(CV + i) / 2] - y1 * sn[(CV + i) / 2]);
-              b[u].v[i + 1] = from_f<T>(y1 * cs[(CV + i) / 2] + y0 * sn[(CV + i) / 2]);
+              for (int i = 0; i + 1 < CV; i += 2) {
+                const f32x2 m = widen2(a[u].v + i);
+                if (kHalf) {
+                  const f32x2 n = widen2(b[u].v + i);
+                  const float2 t = floats_of(mul2(n, sn[i / 2]));
+                  narrow2(fma2(m, cs[i / 2], pair_of(-t.x, -t.y)), a[u].v + i);
+                  narrow2(fma2(n, cs[i / 2], mul2(m, sn[i / 2])), b[u].v + i);
+                } else {
+                  const float2 t = floats_of(m);
+                  narrow2(fma2(m, cs[i / 2], mul2(pair_of(t.y, t.x), sn[i / 2])), a[u].v + i);
+                }
+              }
             }
           }
+          *reinterpret_cast<V*>(y + u * dy) = a[u];
+          if (two) *reinterpret_cast<V*>(y + u * dy + (c1 - c0)) = b[u];
         }
-        const bool key = h >= p.q_heads;
-        T* y = key ? (T*)p.ko.x + row * p.ko.row_stride + (h - p.q_heads) * p.ko.head_stride
-                   : (T*)p.qo.x + row * p.qo.row_stride + h * p.qo.head_stride;
-        *reinterpret_cast<V*>(y + c0) = a[u];
-        if (both) *reinterpret_cast<V*>(y + c1) = b[u];
-      }
+      x += kUnroll * dx;
+      y += kUnroll * dy;
     }
-  }
+  };
+  heads(p.q, p.qo, slot, p.q_heads);
+  // (the threads that had one head of q fewer begin)
+  heads(p.k, p.ko, (slot + slots - p.q_heads % slots) % slots, p.heads - p.q_heads);
 }
 
-template <typename T, int CV>
-void launch(Launcher& lc, RotaryParams& p, bool half, bool copies) {
-  p.turn_chunks = p.rotary_dim / (2 * CV);
-  p.chunks = p.turn_chunks + (copies ? (p.head_dim - p.rotary_dim + 2 * CV - 1) / (2 * CV) : 0);
-  const int64_t blocks = (p.rows * p.chunks + kThreads - 1) / kThreads;
-  // heads over threads until there are eight blocks an SM, in whole batches of loads
-  const int most = (p.heads + kHeads - 1) / kHeads;
-  int64_t parts = (8 * 148 + blocks - 1) / blocks;
-  if (parts > most) parts = most;
-  p.heads_each = (int)((most + parts - 1) / parts) * kHeads;
-  const dim3 grid((unsigned)blocks, (unsigned)((p.heads + p.heads_each - 1) / p.heads_each));
-  if (half) rotary_kernel<T, CV, true><<<grid, kThreads, 0, lc.stream>>>(p);
-  else rotary_kernel<T, CV, false><<<grid, kThreads, 0, lc.stream>>>(p);
+template <typename T, int CV, bool kHalf>
+void launch(Launcher& lc, RotaryParams& p, bool copies) {
+  constexpr int kUnit = kHalf ? 2 * CV : CV;  // channels
+  p.turn_chunks = p.rotary_dim / kUnit;
+  p.chunks = p.turn_chunks + (copies ? (p.head_dim - p.rotary_dim + kUnit - 1) / kUnit : 0);
+  // as many rows to a block as leave four blocks an SM, up to kMaxRows; then as many threads to a unit as it still has
+  const int64_t want = p.rows / (4 * 148);
+  int rows = want < 1 ? 1 : want > kMaxRows ? kMaxRows : (int)want;
+  if (rows > kThreads / p.chunks) rows = kThreads / p.chunks;
+  int slots = kThreads / (p.chunks * rows);
+  if (slots > p.heads) slots = p.heads;
+  const int64_t blocks = (p.rows + rows - 1) / rows;
+  const size_t smem = (size_t)rows * (p.rotary_dim / 2) * sizeof(float2);
+  rotary_kernel<T, CV, kHalf><<<(unsigned)blocks, dim3(p.chunks, slots, rows), smem, lc.stream>>>(p);
   lc.count();
   lc.check();
 }
@@ -159,28 +175,31 @@ void rotary(Launcher& lc, const hbp_rotary_spec& s, bool inverse, int dtype, int
       w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
       f *= w + (1.0 - w) / s.factor;
     }
-    p.turns[i] = f / pi2;
+    p.turns[i] = (uint64_t)std::llrint(std::ldexp(f / pi2, 62)) << 2;  // (below 1/6 of a turn; a double has no more digits)
   }
   p.amplitude = s.amplitude;
   p.sign = inverse ? -1.0f : 1.0f;
   p.rows = rows; p.first = first; p.period = period;
-  p.positions = positions; p.position_bytes = position_bytes;
+  p.positions = positions; p.position_bytes = positions ? position_bytes : 0;
   p.q_heads = q_heads; p.heads = q_heads + kv_heads;
   p.rotary_dim = s.rotary_dim; p.head_dim = head_dim;
   p.q = q; p.qo = qo; p.k = k; p.ko = ko;
   const bool half = s.layout == HBP_ROTARY_HALF;
   auto in_place = [](const hbp_heads& a, const hbp_heads& b) { return a.x == b.x; };
   const bool copies = head_dim > s.rotary_dim && !(in_place(q, qo) && (kv_heads == 0 || in_place(k, ko)));
-  // The widest vectors that pairs and copied channels come in whole numbers of (rows and heads start on 16 bytes): half layout,
-  // vectors of rotary_dim / 2 channels; interleaved, two vectors side by side.
-  auto fits = [&](int cv) { return pairs % cv == 0 && (head_dim - s.rotary_dim) % cv == 0; };
+  // The widest vectors that the turning channels (half layout: each half of them) and the others come in whole numbers of; rows and heads start
+  // on 16 bytes.
+  const int run = half ? pairs : s.rotary_dim, rest = head_dim - s.rotary_dim;
+  auto fits = [&](int cv) { return run % cv == 0 && rest % cv == 0; };
   if (dtype == HBP_F32) {
-    if (fits(4)) launch<float, 4>(lc, p, half, copies);
-    else launch<float, 1>(lc, p, half, copies);
+    if (fits(4)) half ? launch<float, 4, true>(lc, p, copies) : launch<float, 4, false>(lc, p, copies);
+    else half ? launch<float, 1, true>(lc, p, copies) : launch<float, 2, false>(lc, p, copies);
+  } else if (fits(8)) {
+    half ? launch<bf16, 8, true>(lc, p, copies) : launch<bf16, 8, false>(lc, p, copies);
+  } else if (fits(4)) {
+    half ? launch<bf16, 4, true>(lc, p, copies) : launch<bf16, 4, false>(lc, p, copies);
   } else {
-    if (fits(8)) launch<bf16, 8>(lc, p, half, copies);
-    else if (fits(4)) launch<bf16, 4>(lc, p, half, copies);
-    else launch<bf16, 1>(lc, p, half, copies);
+    half ? launch<bf16, 1, true>(lc, p, copies) : launch<bf16, 2, false>(lc, p, copies);
   }
 }
 
@@ -196,7 +215,7 @@ extern "C" hbp_status hbp_rotary(const hbp_rotary_spec* spec, int32_t inverse, i
   if (rows < 0 || q_heads <= 0 || kv_heads < 0 || (int64_t)q_heads + kv_heads > 65535 || head_dim <= 0 || head_dim % v) return HBP_ERR_SHAPE;
   const hbp_status st = check_rotary_spec(spec, head_dim);
   if (st != HBP_OK) return st;
-  if (rows > (int64_t)INT32_MAX * kThreads / kMaxPairs) return HBP_ERR_SHAPE;
+  if (rows > INT32_MAX) return HBP_ERR_SHAPE;
   if (period < 0 || (positions && position_bytes != 4 && position_bytes != 8)) return HBP_ERR_INVALID_ARG;
   if (positions && ((uintptr_t)positions % position_bytes)) return HBP_ERR_SHAPE;
   if (!q || !q_out || (kv_heads && (!k || !k_out))) return HBP_ERR_INVALID_ARG;
