@@ -23,6 +23,7 @@
 // two buffers of scores, whose products run one tile ahead of the softmax warps; HD = 64 runs two blocks an SM instead.
 // All waits are bounded.
 #include "attention_ragged.cuh"
+#include "float_pairs.cuh"
 #include "ring_drain.cuh"
 
 namespace hbp {
@@ -238,7 +239,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
   } else {
     const int quarter = warp & 3, row = quarter * 32 + lane, qrow = q0 + row;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const float sign = p.a.scale < 0.0f ? -1.0f : 1.0f, scale2 = fabsf(p.a.scale) * LOG2E;
+    const float scale2 = fabsf(p.a.scale) * LOG2E;
     float top = -INFINITY, total = 0.0f;  // the reference of the sums, in units of log2; the sum
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
@@ -247,23 +248,25 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
       const int c0 = it * BIG;
       const int last = p.a.causal ? min(sq.nk - 1, qrow + shift) : sq.nk - 1;         // the last key this row sees
       const bool full = c0 + BIG <= sq.nk && (!p.a.causal || c0 + BIG - 1 <= q0 + shift);  // ... and every row of the block sees the whole tile
-      float most = -INFINITY;
+      float sc[BIG];  // this row's scores
 #pragma unroll
-      for (int c = 0; c < BIG; c += 32) {
-        float sc[32];
-        tc_ld32(tS + lanes + c, sc);
-        if (sign < 0.0f) {
+      for (int c = 0; c < BIG; c += 32) tc_ld32_async(tS + lanes + c, sc + c);
+      tc_ld_wait();
+      if (p.a.scale < 0.0f) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) sc[i] = -sc[i];
-        }
-        if (full) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) most = fmaxf(most, sc[i]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) most = c0 + c + i <= last ? fmaxf(most, sc[i]) : most;
-        }
+        for (int i = 0; i < BIG; ++i) sc[i] = -sc[i];
       }
+      if (!full) {
+#pragma unroll
+        for (int i = 0; i < BIG; ++i) sc[i] = c0 + i <= last ? sc[i] : -INFINITY;
+      }
+      float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int i = 0; i < BIG; i += 8) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) tops[e] = fmaxf(tops[e], fmaxf(sc[i + e], sc[i + 4 + e]));
+      }
+      float most = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
       most = most == -INFINITY ? most : most * scale2;  // (a scale of 0 times nothing is not a maximum)
       if (it == 0) {
         top = most;
@@ -286,28 +289,26 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
           tc_st_wait();
         }
       }
-      const float ref = top == -INFINITY ? 0.0f : top, mul = sign * scale2;
+      // (nothing seen so far: -infinity less 0; a scale of 0 times -infinity would not be -infinity)
+      const float ref = top == -INFINITY ? 0.0f : top, mul = scale2 > 0.0f ? scale2 : 1e-30f;
+      const f32x2 mul2v = both(mul), ref2 = both(-ref);
+      f32x2 sum0 = both(0.0f), sum1 = sum0;
 #pragma unroll
       for (int c = 0; c < BIG; c += 32) {
-        float sc[32];
-        tc_ld32(tS + lanes + c, sc);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) sc[i] = fast_exp2(fmaf(sc[i], mul, -ref));
-        if (!full) {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) sc[i] = c0 + c + i <= last ? sc[i] : 0.0f;
-        }
-        float s0 = 0.0f, s1 = 0.0f;
         uint32_t packed[16];
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          s0 += sc[i];
-          s1 += sc[i + 1];
-          packed[i / 2] = pack2(sc[i], sc[i + 1]);
+        for (int i = 0; i < 32; i += 4) {
+          const float2 x = floats_of(fma2(pair_of(sc[c + i], sc[c + i + 1]), mul2v, ref2)), y = floats_of(fma2(pair_of(sc[c + i + 2], sc[c + i + 3]), mul2v, ref2));
+          const float e0 = fast_exp2(x.x), e1 = fast_exp2(x.y), e2 = fast_exp2(y.x), e3 = fast_exp2(y.y);
+          sum0 = add2(sum0, pair_of(e0, e1));
+          sum1 = add2(sum1, pair_of(e2, e3));
+          packed[i / 2] = pack2(e0, e1);
+          packed[i / 2 + 1] = pack2(e2, e3);
         }
-        total += s0 + s1;
         tc_st16(tS + lanes + c / 2, packed);  // (columns whose scores this thread has read)
       }
+      const float2 sums = floats_of(add2(sum0, sum1));
+      total += sums.x + sums.y;
       tc_st_wait();
       tc_fence_before();
       __syncwarp();
