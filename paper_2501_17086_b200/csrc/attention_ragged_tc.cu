@@ -133,15 +133,15 @@ __device__ __forceinline__ void store_staged(uint32_t tile, int row0, int unit0,
 constexpr int FWD_THREADS = 192;  // warp 0 copies, warp 1 issues the products, warps 2..5 softmax (TMEM lane quarter = warp & 3)
 template <int HD>
 struct Fwd {
-  static constexpr int kStages = HD == 64 ? 2 : 1;  // (a key tile comes while the softmax of the one before runs)
-  static constexpr int kTile = BIG * HD * 2;
-  static constexpr int kSmem = kTile * (1 + 2 * kStages) + 256 + 1024;
+  static constexpr int kStages = HD == 64 ? 3 : 2;  // of keys, and of values
+  static constexpr int kBig = BIG * HD * 2, kSmall = SMALL * HD * 2;
+  static constexpr int kSmem = kBig + 2 * kStages * kSmall + 256 + 1024;
 };
 
 template <int HD>
 __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p) {
   using C = Fwd<HD>;
-  constexpr int NS = C::kStages;
+  constexpr int NS = C::kStages, NB = 2;
   const BlockOf w = block_of(p.a.q_len, BIG, p.a.q_heads, true);
   const SeqPair sq = sequence_pair(p.a, w.b);
   const int q0 = w.blk * BIG;
@@ -149,25 +149,28 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
   const int kh = w.h / (p.a.q_heads / p.a.kv_heads);
   const int shift = sq.nk - sq.nq;  // causal: query i sees keys 0 .. i + shift
   const int seen = p.a.causal ? min(sq.nk, min(q0 + BIG, sq.nq) + shift) : sq.nk;
-  const int n_it = seen > 0 ? (seen + BIG - 1) / BIG : 0;
+  const int n_it = seen > 0 ? (seen + SMALL - 1) / SMALL : 0;
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* aligned = smem_raw + (base - smem_u32(smem_raw));
-  const uint32_t sQ = base, sK = base + C::kTile, sV = sK + NS * C::kTile;
-  uint64_t* bar_mem = reinterpret_cast<uint64_t*>(aligned + C::kTile * (1 + 2 * NS));
+  const uint32_t sQ = base, sK = base + C::kBig, sV = sK + NS * C::kSmall;
+  uint64_t* bar_mem = reinterpret_cast<uint64_t*>(aligned + C::kBig + 2 * NS * C::kSmall);
   const uint32_t bars = smem_u32(bar_mem);
-  const uint32_t bQ = bars, bScores = bars + 8, bProbs = bars + 16, bDone = bars + 24, bTail = bars + 32;
-  auto bKFull = [&](int s) { return bars + 40 + 8 * s; };
-  auto bKFree = [&](int s) { return bars + 40 + 8 * (NS + s); };
-  auto bVFull = [&](int s) { return bars + 40 + 8 * (2 * NS + s); };
-  auto bVFree = [&](int s) { return bars + 40 + 8 * (3 * NS + s); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_mem + 5 + 4 * NS);
+  const uint32_t bQ = bars, bDone = bars + 8, bTail = bars + 16;
+  auto bProbs = [&](int b) { return bars + 24 + 8 * b; };
+  auto bScores = [&](int b) { return bars + 24 + 8 * (NB + b); };
+  auto bKFull = [&](int s) { return bars + 24 + 8 * (2 * NB + s); };
+  auto bKFree = [&](int s) { return bars + 24 + 8 * (2 * NB + NS + s); };
+  auto bVFull = [&](int s) { return bars + 24 + 8 * (2 * NB + 2 * NS + s); };
+  auto bVFree = [&](int s) { return bars + 24 + 8 * (2 * NB + 3 * NS + s); };
+  constexpr int kBars = 3 + 2 * NB + 4 * NS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_mem + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 5 + 4 * NS; ++i) mbar_init(bars + 8 * i, i == 2 ? 4 : 1);
+    for (int i = 0; i < kBars; ++i) mbar_init(bars + 8 * i, i >= 3 && i < 3 + NB ? 4 : 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -179,33 +182,33 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot, tS = tmem, tO = tmem + BIG;
+  const uint32_t tmem = *tmem_slot, tO = tmem + 64 * NB;  // scores, and then probabilities, of buffer b: columns 64 b ..
 
   if (warp == 0) {
     bool ok = n_it > 0;
     if (ok && lane == 0) {
-      mbar_expect_tx(bQ, C::kTile);
+      mbar_expect_tx(bQ, C::kBig);
       for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sQ + r * 128, BIG, &m.q, bQ, w.h, (int)sq.q0 + q0 + r);
     }
     for (int it = 0; it < n_it && ok; ++it) {
       const int s = it % NS;
       const uint32_t free_parity = ((uint32_t)(it / NS) & 1u) ^ 1u;
-      const int row = (int)sq.k0 + it * BIG;
+      const int row = (int)sq.k0 + it * SMALL;
       if (!wait_all(bKFree(s), free_parity, abort_flag, p.a.status)) { ok = false; break; }
       if (lane == 0) {
-        mbar_expect_tx(bKFull(s), C::kTile);
-        for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sK + s * C::kTile + r * 128, BIG, &m.k, bKFull(s), kh, row + r);
+        mbar_expect_tx(bKFull(s), C::kSmall);
+        copy_rows<HD>(sK + s * C::kSmall, SMALL, &m.k, bKFull(s), kh, row);
       }
       if (!wait_all(bVFree(s), free_parity, abort_flag, p.a.status)) { ok = false; break; }
-      const int there = sq.nk - it * BIG;  // rows of the sequence in this tile
-      const uint32_t bar = there < BIG ? bTail : bVFull(s);
+      const int there = sq.nk - it * SMALL;  // rows of the sequence in this tile
+      const uint32_t bar = there < SMALL ? bTail : bVFull(s);
       if (lane == 0) {
-        mbar_expect_tx(bar, C::kTile);
-        for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sV + s * C::kTile + r * 128, BIG, &m.v, bar, kh, row + r);
+        mbar_expect_tx(bar, C::kSmall);
+        copy_rows<HD>(sV + s * C::kSmall, SMALL, &m.v, bar, kh, row);
       }
-      if (there < BIG) {  // the last tile: what is behind the sequence becomes zeros
+      if (there < SMALL) {  // the last tile: what is behind the sequence becomes zeros
         if (!wait_all(bTail, 0, abort_flag, p.a.status)) { ok = false; break; }
-        clear_rows<HD>(sV + s * C::kTile, BIG, there, lane);
+        clear_rows<HD>(sV + s * C::kSmall, SMALL, there, lane);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bVFull(s));
@@ -213,26 +216,38 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
     }
   } else if (warp == 1) {
     const bool leader = elect_one();
-    const uint64_t dQ = make_desc(sQ, 16, 1024), dK = make_desc(sK, 16, 1024), dV = make_desc(sV, BIG * 128, 1024);
-    bool ok = n_it == 0 || wait_all(bQ, 0, abort_flag, p.a.status);
-    for (int it = 0; it < n_it && ok; ++it) {
-      const int s = it % NS;
-      const uint32_t full_parity = (uint32_t)(it / NS) & 1u, off = (uint32_t)s * C::kTile;
-      if (!wait_all(bKFull(s), full_parity, abort_flag, p.a.status)) { ok = false; break; }
-      tc_fence_after();
-      if (leader) {  // (in order behind the product that read the probabilities in these columns)
+    const uint64_t dQ = make_desc(sQ, 16, 1024), dK = make_desc(sK, 16, 1024), dV = make_desc(sV, SMALL * 128, 1024);
+    auto scores = [&](int it) {
+      const uint32_t off = (uint32_t)(it % NS) * C::kSmall, t = tmem + 64 * (it % NB);
+      if (leader) {
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k)
-          tc_mma(tS, desc_add(dQ, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dK, off + (k / 4) * BIG * 128 + 32 * (k % 4)), kIdesc<BIG, 0>, k != 0);
-        tc_commit(bScores);
-        tc_commit(bKFree(s));
+          tc_mma(t, desc_add(dQ, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dK, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+        tc_commit(bScores(it % NB));
+        tc_commit(bKFree(it % NS));
       }
-      if (!wait_all(bVFull(s), full_parity, abort_flag, p.a.status) || !wait_all(bProbs, (uint32_t)it & 1u, abort_flag, p.a.status)) { ok = false; break; }
+    };
+    bool ok = n_it == 0 || wait_all(bQ, 0, abort_flag, p.a.status);
+    for (int it = 0; it < NB && it < n_it && ok; ++it) {
+      ok = wait_all(bKFull(it % NS), 0, abort_flag, p.a.status);
+      tc_fence_after();
+      if (ok) scores(it);
+    }
+    for (int it = 0; it < n_it && ok; ++it) {
+      const int s = it % NS;
+      if (!wait_all(bVFull(s), (uint32_t)(it / NS) & 1u, abort_flag, p.a.status) ||
+          !wait_all(bProbs(it % NB), (uint32_t)(it / NB) & 1u, abort_flag, p.a.status)) { ok = false; break; }
       tc_fence_after();
       if (leader) {
 #pragma unroll
-        for (int k = 0; k < BIG / 16; ++k) tc_mma_ts(tO, tS + 8 * k, desc_add(dV, off + 2048 * k), kIdesc<HD, 1>, (it | k) != 0);
+        for (int k = 0; k < SMALL / 16; ++k)
+          tc_mma_ts(tO, tmem + 64 * (it % NB) + 8 * k, desc_add(dV, (uint32_t)s * C::kSmall + 2048 * k), kIdesc<HD, 1>, (it | k) != 0);
         tc_commit(bVFree(s));
+      }
+      if (it + NB < n_it) {  // into the buffer that these have read (products run in order)
+        if (!wait_all(bKFull((it + NB) % NS), (uint32_t)((it + NB) / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+        tc_fence_after();
+        scores(it + NB);
       }
     }
     if (leader) tc_commit(bDone);
@@ -240,29 +255,31 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
     const int quarter = warp & 3, row = quarter * 32 + lane, qrow = q0 + row;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const float scale2 = fabsf(p.a.scale) * LOG2E;
-    float top = -INFINITY, total = 0.0f;  // the reference of the sums, in units of log2; the sum
+    float top = -INFINITY;  // the reference of the sums, in units of log2
+    f32x2 sum0 = both(0.0f), sum1 = sum0;
+    const int last = p.a.causal ? min(sq.nk - 1, qrow + shift) : sq.nk - 1;  // the last key this row sees
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
-      if (!wait_all(bScores, (uint32_t)it & 1u, abort_flag, p.a.status)) { ok = false; break; }
+      if (!wait_all(bScores(it % NB), (uint32_t)(it / NB) & 1u, abort_flag, p.a.status)) { ok = false; break; }
       tc_fence_after();
-      const int c0 = it * BIG;
-      const int last = p.a.causal ? min(sq.nk - 1, qrow + shift) : sq.nk - 1;         // the last key this row sees
-      const bool full = c0 + BIG <= sq.nk && (!p.a.causal || c0 + BIG - 1 <= q0 + shift);  // ... and every row of the block sees the whole tile
-      float sc[BIG];  // this row's scores
-#pragma unroll
-      for (int c = 0; c < BIG; c += 32) tc_ld32_async(tS + lanes + c, sc + c);
+      const int c0 = it * SMALL;
+      const uint32_t t = tmem + lanes + 64 * (it % NB);
+      const bool full = c0 + SMALL <= sq.nk && (!p.a.causal || c0 + SMALL - 1 <= q0 + shift);  // every row of the block sees the whole tile
+      float sc[SMALL];  // this row's scores
+      tc_ld32_async(t, sc);
+      tc_ld32_async(t + 32, sc + 32);
       tc_ld_wait();
       if (p.a.scale < 0.0f) {
 #pragma unroll
-        for (int i = 0; i < BIG; ++i) sc[i] = -sc[i];
+        for (int i = 0; i < SMALL; ++i) sc[i] = -sc[i];
       }
       if (!full) {
 #pragma unroll
-        for (int i = 0; i < BIG; ++i) sc[i] = c0 + i <= last ? sc[i] : -INFINITY;
+        for (int i = 0; i < SMALL; ++i) sc[i] = c0 + i <= last ? sc[i] : -INFINITY;
       }
       float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int i = 0; i < BIG; i += 8) {
+      for (int i = 0; i < SMALL; i += 8) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) tops[e] = fmaxf(tops[e], fmaxf(sc[i + e], sc[i + 4 + e]));
       }
@@ -275,10 +292,11 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
         if (__any_sync(0xffffffffu, grown)) {  // scale what was summed down to the new reference
           const float keep = grown ? fast_exp2(top - most) : 1.0f;
           if (grown) top = most;
-          total *= keep;
+          sum0 = mul2(sum0, both(keep));
+          sum1 = mul2(sum1, both(keep));
           if (!wait_all(bVFree((it - 1) % NS), (uint32_t)((it - 1) / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
           tc_fence_after();
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < HD; c += 32) {
             float o[32];
             tc_ld32(tO + lanes + c, o);
@@ -286,37 +304,34 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
             for (int i = 0; i < 32; ++i) o[i] *= keep;
             tc_st32(tO + lanes + c, o);
           }
-          tc_st_wait();
         }
       }
       // (nothing seen so far: -infinity less 0; a scale of 0 times -infinity would not be -infinity)
-      const float ref = top == -INFINITY ? 0.0f : top, mul = scale2 > 0.0f ? scale2 : 1e-30f;
-      const f32x2 mul2v = both(mul), ref2 = both(-ref);
-      f32x2 sum0 = both(0.0f), sum1 = sum0;
+      const f32x2 mul = both(scale2 > 0.0f ? scale2 : 1e-30f), ref = both(top == -INFINITY ? 0.0f : -top);
 #pragma unroll
-      for (int c = 0; c < BIG; c += 32) {
+      for (int c = 0; c < SMALL; c += 32) {
         uint32_t packed[16];
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-          const float2 x = floats_of(fma2(pair_of(sc[c + i], sc[c + i + 1]), mul2v, ref2)), y = floats_of(fma2(pair_of(sc[c + i + 2], sc[c + i + 3]), mul2v, ref2));
+          const float2 x = floats_of(fma2(pair_of(sc[c + i], sc[c + i + 1]), mul, ref)), y = floats_of(fma2(pair_of(sc[c + i + 2], sc[c + i + 3]), mul, ref));
           const float e0 = fast_exp2(x.x), e1 = fast_exp2(x.y), e2 = fast_exp2(y.x), e3 = fast_exp2(y.y);
           sum0 = add2(sum0, pair_of(e0, e1));
           sum1 = add2(sum1, pair_of(e2, e3));
           packed[i / 2] = pack2(e0, e1);
           packed[i / 2 + 1] = pack2(e2, e3);
         }
-        tc_st16(tS + lanes + c / 2, packed);  // (columns whose scores this thread has read)
+        tc_st16(t + c / 2, packed);  // (columns whose scores this thread has read)
       }
-      const float2 sums = floats_of(add2(sum0, sum1));
-      total += sums.x + sums.y;
       tc_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bProbs);
+      if (lane == 0) mbar_arrive(bProbs(it % NB));
     }
     ok = ok && wait_all(bDone, 0, abort_flag, p.a.status);
     if (ok) {
       tc_fence_after();
+      const float2 sums = floats_of(add2(sum0, sum1));
+      const float total = sums.x + sums.y;
       const float inv = total > 0.0f ? 1.0f / total : total;  // nothing seen: 0 (a sum that is NaN stays NaN)
 #pragma unroll 1
       for (int c = 0; c < HD; c += 32) {
