@@ -351,13 +351,15 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
 }
 
 // ------------------------------------------------------------------------------------------- backward
-constexpr int BWD_THREADS = 320;  // warp 0 copies, warp 1 issues the products, warps 2..9 softmax, two to a TMEM lane quarter
 template <int HD>
 struct Bwd {
   static constexpr int kBuffers = HD == 64 ? 1 : 2;  // of scores
-  static constexpr int kStages = 3;
+  // Groups of eight softmax warps, two to a lane quarter of tensor memory; they take the tiles in turn.
+  static constexpr int kGroups = HD == 64 ? 1 : 2;
+  static constexpr int kThreads = 64 + 256 * kGroups;  // warp 0 copies, warp 1 issues the products
+  static constexpr int kStages = HD == 64 ? 3 : 4;
   static constexpr int kBig = BIG * HD * 2, kSmall = SMALL * HD * 2;
-  static constexpr int kStats = 2 * SMALL * 4;  // log-sum-exp and D of a tile's queries (dK, dV)
+  static constexpr int kStats = 2 * SMALL * 4;  // minus log-sum-exp and minus D of a tile's queries (dK, dV)
   static constexpr int kStage = 2 * kSmall;
   static constexpr int kSmem = 2 * kBig + kStages * (kStage + kStats) + 256 + 1024;
   static constexpr uint32_t kColumns = HD == 64 ? 256 : 512;
@@ -388,18 +390,21 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
   uint64_t* bar_mem = reinterpret_cast<uint64_t*>(aligned + 2 * C::kBig + NS * (C::kStage + C::kStats));
   const uint32_t bars = smem_u32(bar_mem);
   const uint32_t bBig = bars, bDone = bars + 8, bTail = bars + 16;
+  // of buffer b: the scores' columns may be taken over by the next ones (dK, dV: and hold probabilities); dS is there; scores; dP
   auto bProbs = [&](int b) { return bars + 24 + 8 * b; };
-  auto bScores = [&](int b) { return bars + 24 + 8 * (NB + b); };
-  auto bFull = [&](int s) { return bars + 24 + 8 * (2 * NB + s); };
-  auto bFree = [&](int s) { return bars + 24 + 8 * (2 * NB + NS + s); };
-  constexpr int kBars = 3 + 2 * NB + 2 * NS;
+  auto bDS = [&](int b) { return bars + 24 + 8 * (NB + b); };
+  auto bScores = [&](int b) { return bars + 24 + 8 * (2 * NB + b); };
+  auto bDP = [&](int b) { return bars + 24 + 8 * (3 * NB + b); };
+  auto bFull = [&](int s) { return bars + 24 + 8 * (4 * NB + s); };
+  auto bFree = [&](int s) { return bars + 24 + 8 * (4 * NB + NS + s); };
+  constexpr int kBars = 3 + 4 * NB + 2 * NS;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar_mem + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    // (probabilities: eight warps; full: the copies, and what the copying warp adds itself)
-    for (int i = 0; i < kBars; ++i) mbar_init(bars + 8 * i, i >= 3 && i < 3 + NB ? 8 : i >= 3 + 2 * NB && i < 3 + 2 * NB + NS ? 2 : 1);
+    // (probabilities, dS: eight warps; full: the copies, and what the copying warp adds itself)
+    for (int i = 0; i < kBars; ++i) mbar_init(bars + 8 * i, i >= 3 && i < 3 + 2 * NB ? 8 : i >= 3 + 4 * NB && i < 3 + 4 * NB + NS ? 2 : 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -452,8 +457,8 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {  // a query that sees nothing, or is none, has probabilities of 0: exp2(s - infinity)
-          st[i * 32 + lane] = v[i] == -INFINITY ? INFINITY : v[i] * LOG2E;
-          st[SMALL + i * 32 + lane] = v[2 + i];
+          st[i * 32 + lane] = v[i] == -INFINITY ? v[i] : v[i] * -LOG2E;
+          st[SMALL + i * 32 + lane] = -v[2 + i];
         }
       }
       if (tail) {
@@ -473,104 +478,142 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
     const uint64_t dB0 = make_desc(sBig0, 16, 1024), dB1 = make_desc(sBig1, 16, 1024);
     const uint64_t dS0 = make_desc(sSmall, 16, 1024), dS1 = make_desc(sSmall + C::kSmall, 16, 1024);
     const uint64_t dS0mn = make_desc(sSmall, SMALL * 128, 1024), dS1mn = make_desc(sSmall + C::kSmall, SMALL * 128, 1024);
-    auto scores = [&](int it) {  // both contract over channels
+    // Both contract over channels.
+    auto scores = [&](int it) {
       const uint32_t off = (uint32_t)(it % NS) * C::kStage, t = tmem + 128 * (it % NB);
       if (leader) {
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k)
           tc_mma(t, desc_add(dB0, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS0, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+        tc_commit(bScores(it % NB));
+      }
+    };
+    auto dp_scores = [&](int it) {
+      const uint32_t off = (uint32_t)(it % NS) * C::kStage, t = tmem + 128 * (it % NB) + 64;
+      if (leader) {
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k)
-          tc_mma(t + 64, desc_add(dB1, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS1, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
-        tc_commit(bScores(it % NB));
+          tc_mma(t, desc_add(dB1, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS1, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+        tc_commit(bDP(it % NB));
       }
     };
     bool ok = n_it == 0 || wait_all(bBig, 0, abort_flag, p.a.status);
     for (int it = 0; it < NB && it < n_it && ok; ++it) {
       ok = wait_all(bFull(it % NS), 0, abort_flag, p.a.status);
       tc_fence_after();
-      if (ok) scores(it);
+      if (ok) {
+        scores(it);
+        dp_scores(it);
+      }
     }
+    // A tile's two halves follow one another: the product with the probabilities, and the scores that take over their columns, run while the
+    // softmax warps form dS.  (Products run in order.)
     for (int it = 0; it < n_it && ok; ++it) {
-      if (!wait_all(bProbs(it % NB), (uint32_t)(it / NB) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+      const uint32_t off = (uint32_t)(it % NS) * C::kStage, t = tmem + 128 * (it % NB), parity = (uint32_t)(it / NB) & 1u;
+      if (!wait_all(bProbs(it % NB), parity, abort_flag, p.a.status)) { ok = false; break; }
       tc_fence_after();
-      const uint32_t off = (uint32_t)(it % NS) * C::kStage, t = tmem + 128 * (it % NB);
-      if (leader) {  // contraction over the tile's rows
-        if (kDKV) {
+      if (kDKV && leader) {
 #pragma unroll
-          for (int k = 0; k < SMALL / 16; ++k)  // dV += P^T dO
-            tc_mma_ts(tAcc1, t + (k / 2) * 32 + (k % 2) * 8, desc_add(dS1mn, off + 2048 * k), kIdesc<HD, 1>, (it | k) != 0);
-        }
+        for (int k = 0; k < SMALL / 16; ++k)  // dV += P^T dO: contraction over the tile's rows
+          tc_mma_ts(tAcc1, t + (k / 2) * 32 + (k % 2) * 8, desc_add(dS1mn, off + 2048 * k), kIdesc<HD, 1>, (it | k) != 0);
+      }
+      if (NB == 1 && it + NB < n_it) {
+        if (!wait_all(bFull((it + NB) % NS), (uint32_t)((it + NB) / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+        tc_fence_after();
+        scores(it + NB);
+      }
+      if (!wait_all(bDS(it % NB), parity, abort_flag, p.a.status)) { ok = false; break; }
+      tc_fence_after();
+      if (leader) {
 #pragma unroll
         for (int k = 0; k < SMALL / 16; ++k)  // dK += dS^T Q, dQ += dS K
           tc_mma_ts(tAcc0, t + 64 + (k / 2) * 32 + (k % 2) * 8, desc_add(dS0mn, off + 2048 * k), kIdesc<HD, 1>, (it | k) != 0);
         tc_commit(bFree(it % NS));
       }
-      if (it + NB < n_it) {  // into the buffer that these have read (products run in order)
-        if (!wait_all(bFull((it + NB) % NS), (uint32_t)((it + NB) / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
-        tc_fence_after();
-        scores(it + NB);
+      if (it + NB < n_it) {
+        if (NB > 1) {
+          if (!wait_all(bFull((it + NB) % NS), (uint32_t)((it + NB) / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+          tc_fence_after();
+          scores(it + NB);
+        }
+        dp_scores(it + NB);
       }
     }
     if (leader) tc_commit(bDone);
   } else {
-    const int ch = (warp - 2) >> 2;  // which 32 rows of a tile (columns of the scores) this warp has
+    const int group_id = (warp - 2) >> 3, ch = ((warp - 2) >> 2) & 1;  // which tiles, and which 32 of their rows (columns of the scores) this warp has
     const int quarter = warp & 3, row = quarter * 32 + lane, brow = big0 + row;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const float scale2 = p.a.scale * LOG2E;
-    float my_lse = INFINITY, my_d = 0.0f;
+    float my_lse = -INFINITY, my_d = 0.0f;  // dQ: minus log-sum-exp and minus D of this row
     if (!kDKV && brow < n_big) {
       const int64_t at = (int64_t)w.h * p.a.q_rows + sq.q0 + brow;
-      my_lse = p.lse[at] == -INFINITY ? INFINITY : p.lse[at] * LOG2E;
-      my_d = p.drow[at];
+      my_lse = p.lse[at] == -INFINITY ? -INFINITY : p.lse[at] * -LOG2E;
+      my_d = -p.drow[at];
     }
     bool ok = true;
-    for (int it = 0; it < n_it; ++it) {
-      if (!wait_all(bScores(it % NB), (uint32_t)(it / NB) & 1u, abort_flag, p.a.status)) { ok = false; break; }
+    for (int it = group_id; it < n_it; it += C::kGroups) {
+      const uint32_t parity = (uint32_t)(it / NB) & 1u;
+      if (!wait_all(bScores(it % NB), parity, abort_flag, p.a.status)) { ok = false; break; }
       // (over since before the scores were formed: makes the statistics that the copying warp wrote visible here)
       if (kDKV && !wait_all(bFull(it % NS), (uint32_t)(it / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
       tc_fence_after();
       const int c0 = (t_beg + it % tiles) * SMALL;
       const uint32_t t = tmem + lanes + 128 * (it % NB) + ch * 32;
-      float sc[32], dp[32];
-      tc_ld32_async(t, sc);
-      tc_ld32_async(t + 64, dp);
-      tc_ld_wait();
+      const ulonglong2* st = reinterpret_cast<const ulonglong2*>(stats + (it % NS) * 2 * SMALL + ch * 32);  // (dK, dV: of four columns each)
       // does every row of the block see (is every row of the block seen by) the whole tile?
       const bool full = kDKV ? (!p.a.causal || big0 + BIG - 1 <= c0 + shift) : (c0 + SMALL <= sq.nk && (!p.a.causal || c0 + SMALL - 1 <= big0 + shift));
-      if (kDKV) {
-        const float4* st = reinterpret_cast<const float4*>(stats + (it % NS) * 2 * SMALL + ch * 32);
-#pragma unroll
-        for (int c = 0; c < 32; c += 4) {
-          const float4 l4 = st[c / 4], d4 = st[SMALL / 4 + c / 4];
-          const float l[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            sc[c + e] = fast_exp2(fmaf(sc[c + e], scale2, -l[e]));
-            dp[c + e] = sc[c + e] * (dp[c + e] - dd[e]);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          sc[c] = fast_exp2(fmaf(sc[c], scale2, -my_lse));
-          dp[c] = sc[c] * (dp[c] - my_d);
-        }
+      float sc[32];
+      tc_ld32(t, sc);
+      if (!kDKV) {  // the scores' columns are free
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bProbs(it % NB));
       }
-      if (!full) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          const int col = c0 + ch * 32 + c;  // dK, dV: a query, the row a key; dQ: a key, the row a query
-          const bool vis = kDKV ? brow <= col + shift : (col <= brow + shift && col < sq.nk);
-          sc[c] = vis ? sc[c] : 0.0f;
-          dp[c] = vis ? dp[c] : 0.0f;
-        }
+      for (int c = 0; c < 32; c += 4) {
+        const ulonglong2 l = kDKV ? st[c / 4] : make_ulonglong2(both(my_lse), both(my_lse));
+        const float2 x = floats_of(fma2(pair_of(sc[c], sc[c + 1]), both(scale2), l.x)), y = floats_of(fma2(pair_of(sc[c + 2], sc[c + 3]), both(scale2), l.y));
+        sc[c] = fast_exp2(x.x);
+        sc[c + 1] = fast_exp2(x.y);
+        sc[c + 2] = fast_exp2(y.x);
+        sc[c + 3] = fast_exp2(y.y);
+      }
+      uint32_t seen = 0xffffffffu;  // of this row's 32 columns
+      if (!full) {
+        // dK, dV: a column is a query, the row a key, seen from query brow - shift on; dQ: a column is a key
+        const int first = c0 + ch * 32, from = kDKV ? brow - shift - first : 0, to = kDKV ? 32 : min(brow + shift, sq.nk - 1) + 1 - first;
+        seen = from >= 32 || to <= 0 ? 0u : (0xffffffffu << max(from, 0)) & (to >= 32 ? 0xffffffffu : (1u << to) - 1u);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) sc[c] = (seen >> c) & 1u ? sc[c] : 0.0f;
       }
       uint32_t packed[16];
       if (kDKV) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) packed[i] = pack2(sc[2 * i], sc[2 * i + 1]);
         tc_st16(t, packed);
+        tc_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bProbs(it % NB));
+      }
+      if (!wait_all(bDP(it % NB), parity, abort_flag, p.a.status)) { ok = false; break; }
+      tc_fence_after();
+      float dp[32];
+      tc_ld32(t + 64, dp);
+#pragma unroll
+      for (int c = 0; c < 32; c += 4) {
+        const ulonglong2 d = kDKV ? st[SMALL / 4 + c / 4] : make_ulonglong2(both(my_d), both(my_d));
+        const float2 x = floats_of(mul2(add2(pair_of(dp[c], dp[c + 1]), d.x), pair_of(sc[c], sc[c + 1])));
+        const float2 y = floats_of(mul2(add2(pair_of(dp[c + 2], dp[c + 3]), d.y), pair_of(sc[c + 2], sc[c + 3])));
+        dp[c] = x.x;
+        dp[c + 1] = x.y;
+        dp[c + 2] = y.x;
+        dp[c + 3] = y.y;
+      }
+      if (!full) {  // (a dP that is not finite times a probability of 0)
+#pragma unroll
+        for (int c = 0; c < 32; ++c) dp[c] = (seen >> c) & 1u ? dp[c] : 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) packed[i] = pack2(dp[2 * i], dp[2 * i + 1]);
@@ -578,29 +621,25 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
       tc_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bProbs(it % NB));
+      if (lane == 0) mbar_arrive(bDS(it % NB));
     }
     ok = ok && wait_all(bDone, 0, abort_flag, p.a.status);
     if (ok) {  // accumulators -> bf16 -> shared memory (the block's own tiles are free) -> rows
       tc_fence_after();
-      constexpr int kHalf = HD / 2;  // channels of this warp
+      const int at = (2 * group_id + ch) * 32;  // the first of this warp's 32 channels
 #pragma unroll 1
-      for (int o = 0; o < (kDKV ? 2 : 1); ++o) {
+      for (int o = 0; o < (kDKV ? 2 : 1) && at < HD; ++o) {
         const uint32_t tile = o == 0 ? sBig0 : sBig1;
         const float mul = o == 0 ? p.a.scale : 1.0f;  // dK and dQ carry the scores' scale
+        float v[32];
+        if (n_it > 0) tc_ld32((o == 0 ? tAcc0 : tAcc1) + lanes + at, v);
 #pragma unroll
-        for (int c = 0; c < kHalf; c += 32) {
-          float v[32];
-          const int at = ch * kHalf + c;
-          if (n_it > 0) tc_ld32((o == 0 ? tAcc0 : tAcc1) + lanes + at, v);
+        for (int i = 0; i < 32; ++i) v[i] = n_it > 0 ? v[i] * mul : 0.0f;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = n_it > 0 ? v[i] * mul : 0.0f;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) st_shared16(swz(tile + (at / SUB) * BIG * 128, row, (at % SUB) / 8 + u), pack8(v + 8 * u));
-        }
+        for (int u = 0; u < 4; ++u) st_shared16(swz(tile + (at / SUB) * BIG * 128, row, (at % SUB) / 8 + u), pack8(v + 8 * u));
         __syncwarp();
         const hbp_heads& out = kDKV ? (o == 0 ? p.dk : p.dv) : p.dq;
-        store_staged<kHalf / 8>(tile, quarter * 32, ch * kHalf / 8, (bf16*)out.x + ((kDKV ? sq.k0 : sq.q0) + big0) * out.row_stride + w.h * out.head_stride,
+        store_staged<4>(tile, quarter * 32, at / 8, (bf16*)out.x + ((kDKV ? sq.k0 : sq.q0) + big0) * out.row_stride + w.h * out.head_stride,
                                 out.row_stride, n_big - big0, p.a.head_dim, lane);
       }
     }
@@ -609,7 +648,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
 }
 
 template <int HD>
-__global__ void __launch_bounds__(BWD_THREADS, Bwd<HD>::kBlocksAnSm)
+__global__ void __launch_bounds__(Bwd<HD>::kThreads, Bwd<HD>::kBlocksAnSm)
 ragged_bwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p, const unsigned kv_blocks) {
   if (blockIdx.x < kv_blocks) ragged_bwd_body<HD, true>(m, p, block_at(blockIdx.x, p.a.kv_len, BIG, p.a.kv_heads, false));
   else ragged_bwd_body<HD, false>(m, p, block_at(blockIdx.x - kv_blocks, p.a.q_len, BIG, p.a.q_heads, true));
@@ -656,7 +695,7 @@ bool backward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
   static PerDevice<bool> set;
   if (!allow_smem(ragged_bwd_tc_kernel<HD>, Bwd<HD>::kSmem, set.here())) return false;
   const int64_t kv = blocks_of(r.a.kv_len, BIG, r.a.kv_heads, r.a.sequences), q = blocks_of(r.a.q_len, BIG, r.a.q_heads, r.a.sequences);
-  ragged_bwd_tc_kernel<HD><<<(unsigned)(kv + q), BWD_THREADS, Bwd<HD>::kSmem, lc.stream>>>(m, r, (unsigned)kv);
+  ragged_bwd_tc_kernel<HD><<<(unsigned)(kv + q), Bwd<HD>::kThreads, Bwd<HD>::kSmem, lc.stream>>>(m, r, (unsigned)kv);
   lc.count();
   lc.check();
   return true;
