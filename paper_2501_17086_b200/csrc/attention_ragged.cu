@@ -11,9 +11,12 @@
 // keeps the 16-byte reads of neighbouring rows in different banks; a thread forms 4 x 4 products of a score tile, or 4 rows times
 // every 16th vector of an output.  Bound by the FFMA pipe and the shared-memory reads that feed it (one 16-byte read per 8
 // FFMA in the scores).
+#include <cooperative_groups.h>
+
 #include <cmath>
 
 #include "attention_ragged.cuh"
+#include "float_pairs.cuh"
 
 namespace hbp {
 
@@ -38,26 +41,34 @@ __device__ __forceinline__ void load_tile(float* __restrict__ dst, const float* 
   }
 }
 
-// s[r][c] = sum over channels of A[ty * 4 + r] * B[tx + 16 * c]
+// s[r][c] = sum over channels of A[ty * 4 + r] * B[tx + 16 * c], those of even and of odd channels side by side (two in an instruction)
 template <int HD>
 __device__ __forceinline__ void score_tile(const float* __restrict__ A, const float* __restrict__ B, int ty, int tx, float (&s)[4][4]) {
   constexpr int LD = kStride<HD>;
+  f32x2 t[4][4];
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) s[r][c] = 0.0f;
+    for (int c = 0; c < 4; ++c) t[r][c] = both(0.0f);
 #pragma unroll 4
   for (int k = 0; k < HD; k += 4) {
-    float4 a[4], b[4];
+    ulonglong2 a[4], b[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) a[r] = *reinterpret_cast<const float4*>(A + (ty * 4 + r) * LD + k);
+    for (int r = 0; r < 4; ++r) a[r] = *reinterpret_cast<const ulonglong2*>(A + (ty * 4 + r) * LD + k);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) b[c] = *reinterpret_cast<const float4*>(B + (tx + 16 * c) * LD + k);
+    for (int c = 0; c < 4; ++c) b[c] = *reinterpret_cast<const ulonglong2*>(B + (tx + 16 * c) * LD + k);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[r][c] = fmaf(a[r].x, b[c].x, fmaf(a[r].y, b[c].y, fmaf(a[r].z, b[c].z, fmaf(a[r].w, b[c].w, s[r][c]))));
+      for (int c = 0; c < 4; ++c) t[r][c] = fma2(a[r].x, b[c].x, fma2(a[r].y, b[c].y, t[r][c]));
   }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float2 f = floats_of(t[r][c]);
+      s[r][c] = f.x + f.y;
+    }
 }
 
 // acc[r][4 v + e] += sum over rows j of W[j][ty * 4 + r] * X[j][(tx + 16 v) * 4 + e]; W has PS floats a row
@@ -207,7 +218,7 @@ __device__ __forceinline__ void row_statistics(const RaggedAttn& p, const SeqPai
 }
 
 template <int HD>
-__global__ void __launch_bounds__(THREADS) ragged_dq_kernel(const __grid_constant__ RaggedAttn p) {
+__device__ __forceinline__ void ragged_dq(const RaggedAttn& p, const BlockOf w) {
   extern __shared__ float4 smem4[];
   constexpr int LD = kStride<HD>;
   float* sQ = reinterpret_cast<float*>(smem4);
@@ -216,7 +227,6 @@ __global__ void __launch_bounds__(THREADS) ragged_dq_kernel(const __grid_constan
   float* sV = sK + TILE * LD;
   float* sSt = sV + TILE * LD;  // [key][query]
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const BlockOf w = block_of(p.a.q_len, TILE, p.a.q_heads, true);
   const SeqPair sq = sequence_pair(p.a, w.b);
   const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
   if (q0 >= sq.nq) return;
@@ -244,8 +254,11 @@ __global__ void __launch_bounds__(THREADS) ragged_dq_kernel(const __grid_constan
   store_rows<HD>((float*)p.dq.x + sq.q0 * p.dq.row_stride + w.h * p.dq.head_stride, p.dq.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, p.a.scale, acc);
 }
 
+// The query heads of a group are shared out over the blocks of a cluster: of one head's rows alone the chain of tiles is as long as dq's, and
+// a key head's blocks are few.  Each block leaves its sums in its shared memory, and each adds up those of all for its share of
+// the rows, in the blocks' order.
 template <int HD>
-__global__ void __launch_bounds__(THREADS) ragged_dkv_kernel(const __grid_constant__ RaggedAttn p) {
+__device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w, int rank, int ranks) {
   extern __shared__ float4 smem4[];
   constexpr int LD = kStride<HD>;
   float* sK = reinterpret_cast<float*>(smem4);
@@ -255,16 +268,15 @@ __global__ void __launch_bounds__(THREADS) ragged_dkv_kernel(const __grid_consta
   float* sP = sG + TILE * LD;  // [query][key]
   float* sS = sP + TILE * PS;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const BlockOf w = block_of(p.a.kv_len, TILE, p.a.kv_heads, false);
   const SeqPair sq = sequence_pair(p.a, w.b);
   const int k0 = w.blk * TILE, group = p.a.q_heads / p.a.kv_heads;
-  if (k0 >= sq.nk) return;
+  if (k0 >= sq.nk) return;  // (all blocks of the cluster)
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
   const int first = p.a.causal ? max(0, k0 - shift) / TILE * TILE : 0;  // the first block of queries that sees key k0
   load_tile<HD>(sK, (const float*)p.k.x + sq.k0 * p.k.row_stride + w.h * p.k.head_stride, p.k.row_stride, k0, sq.nk, p.a.head_dim);
   load_tile<HD>(sV, (const float*)p.v.x + sq.k0 * p.v.row_stride + w.h * p.v.head_stride, p.v.row_stride, k0, sq.nk, p.a.head_dim);
   float dk[4][HD / 16] = {}, dv[4][HD / 16] = {};
-  for (int h = w.h * group; h < (w.h + 1) * group; ++h) {
+  for (int h = w.h * group + rank; h < (w.h + 1) * group; h += ranks) {
     const float* q = (const float*)p.q.x + sq.q0 * p.q.row_stride + h * p.q.head_stride;
     const float* g = (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + h * p.d_o.head_stride;
     for (int q0 = first; q0 < sq.nq; q0 += TILE) {
@@ -288,8 +300,46 @@ __global__ void __launch_bounds__(THREADS) ragged_dkv_kernel(const __grid_consta
       add_product<HD>(sS, sQ, ty, tx, dk);
     }
   }
-  store_rows<HD>((float*)p.dk.x + sq.k0 * p.dk.row_stride + w.h * p.dk.head_stride, p.dk.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, p.a.scale, dk);
-  store_rows<HD>((float*)p.dv.x + sq.k0 * p.dv.row_stride + w.h * p.dv.head_stride, p.dv.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, 1.0f, dv);
+  float* dk_base = (float*)p.dk.x + sq.k0 * p.dk.row_stride + w.h * p.dk.head_stride;
+  float* dv_base = (float*)p.dv.x + sq.k0 * p.dv.row_stride + w.h * p.dv.head_stride;
+  if (ranks == 1) {
+    store_rows<HD>(dk_base, p.dk.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, p.a.scale, dk);
+    store_rows<HD>(dv_base, p.dv.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, 1.0f, dv);
+    return;
+  }
+  __syncthreads();  // (this block's tiles have been read)
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int v = 0; v < HD / 64; ++v) {
+      const int at = (ty * 4 + r) * LD + (tx + 16 * v) * 4;
+      *reinterpret_cast<float4*>(sK + at) = make_float4(dk[r][4 * v], dk[r][4 * v + 1], dk[r][4 * v + 2], dk[r][4 * v + 3]);
+      *reinterpret_cast<float4*>(sV + at) = make_float4(dv[r][4 * v], dv[r][4 * v + 1], dv[r][4 * v + 2], dv[r][4 * v + 3]);
+    }
+  cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  cluster.sync();
+  constexpr int VECS = HD / 4;
+  for (int i = rank * THREADS + threadIdx.x; i < 2 * TILE * VECS; i += ranks * THREADS) {
+    const int which = i / (TILE * VECS), r = i / VECS % TILE, c = i % VECS * 4;
+    if (k0 + r >= sq.nk || c >= p.a.head_dim) continue;
+    float* mine = (which ? sV : sK) + r * LD + c;
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int b = 0; b < ranks; ++b) {
+      const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(mine, b));
+      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+    const float mul = which ? 1.0f : p.a.scale;
+    *reinterpret_cast<float4*>((which ? dv_base + (int64_t)(k0 + r) * p.dv.row_stride : dk_base + (int64_t)(k0 + r) * p.dk.row_stride) + c) =
+        make_float4(mul * s.x, mul * s.y, mul * s.z, mul * s.w);
+  }
+  cluster.sync();  // (no block ends while another reads its shared memory)
+}
+
+// dk, dv and dq in one launch, in clusters of `ranks` blocks: a key block's, or one query block of as many heads.
+template <int HD>
+__global__ void __launch_bounds__(THREADS) ragged_bwd_kernel(const __grid_constant__ RaggedAttn p, const unsigned kv_blocks, const int ranks) {
+  if (blockIdx.x < kv_blocks) ragged_dkv<HD>(p, block_at(blockIdx.x / ranks, p.a.kv_len, TILE, p.a.kv_heads, false), (int)(blockIdx.x % ranks), ranks);
+  else ragged_dq<HD>(p, block_at(blockIdx.x - kv_blocks, p.a.q_len, TILE, p.a.q_heads, true));
 }
 
 // drow[h][row] = sum over channels of d_o * o, `lanes` (a power of two, 16 bytes each) to a row of a head; neighbouring lanes take neighbouring
@@ -318,27 +368,37 @@ constexpr int smem_of(int tiles, int scores) {
   return (tiles * TILE * kStride<HD> + scores * TILE * PS) * 4;
 }
 
-template <typename K>
-bool launch(Launcher& lc, K kernel, int64_t blocks, int smem, const RaggedAttn& r) {
-  if (blocks == 0) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
-    lc.check();
-    return false;
-  }
-  kernel<<<(unsigned)blocks, THREADS, smem, lc.stream>>>(r);
+template <typename K, typename... A>
+void launch(Launcher& lc, K kernel, int64_t blocks, int smem, int cluster, A... args) {
+  if (blocks == 0) return;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = lc.stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = cluster > 1 ? 1 : 0;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  if (e != cudaSuccess && lc.err == cudaSuccess) lc.err = e;
   lc.count();
   lc.check();
-  return true;
 }
 
 template <int HD>
 void forward_f32(Launcher& lc, const RaggedAttn& r) {
-  launch(lc, ragged_fwd_kernel<HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(3, 1), r);
+  launch(lc, ragged_fwd_kernel<HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(3, 1), 1, r);
 }
 template <int HD>
 void backward_f32(Launcher& lc, const RaggedAttn& r) {
-  launch(lc, ragged_dkv_kernel<HD>, blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences), smem_of<HD>(4, 2), r);
-  launch(lc, ragged_dq_kernel<HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(4, 1), r);
+  int ranks = 8;
+  while ((r.a.q_heads / r.a.kv_heads) % ranks) --ranks;
+  const int64_t kv = blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences) * ranks, q = blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences);
+  launch(lc, ragged_bwd_kernel<HD>, kv + q, smem_of<HD>(4, 2), ranks, r, (unsigned)kv, ranks);
 }
 
 void row_dots(Launcher& lc, const RaggedAttn& r) {
@@ -365,7 +425,7 @@ hbp_status check_attention(const hbp_attention* a) {
   if (!std::isfinite(a->scale)) return HBP_ERR_INVALID_ARG;
   if (((uintptr_t)a->q_offsets | (uintptr_t)a->kv_offsets | (uintptr_t)a->status) & 3u) return HBP_ERR_SHAPE;
   // (as many blocks of 64 rows as one grid holds)
-  if (blocks_of(a->q_len, TILE, a->q_heads, a->sequences) > INT32_MAX / 2 || blocks_of(a->kv_len, TILE, a->kv_heads, a->sequences) > INT32_MAX / 2 ||
+  if (blocks_of(a->q_len, TILE, a->q_heads, a->sequences) > INT32_MAX / 2 || blocks_of(a->kv_len, TILE, a->q_heads, a->sequences) > INT32_MAX / 2 ||
       a->q_rows * a->q_heads > (int64_t)INT32_MAX * 8)
     return HBP_ERR_SHAPE;
   return HBP_OK;
