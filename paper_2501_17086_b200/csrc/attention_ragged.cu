@@ -28,18 +28,24 @@ constexpr int PS = TILE + 4;  // floats between rows of a score tile
 template <int HD>
 constexpr int kStride = HD + 4;
 
-// `TILE` rows of a tensor from row r0 of a sequence of n rows on into shared memory as float, zeros behind the sequence's end and
+// Asks for `TILE` rows of a tensor from row r0 of a sequence of n rows on, into shared memory; zeros behind the sequence's end and
 // behind channel `width`.  base: the sequence's first row of one head.
 template <int HD>
-__device__ __forceinline__ void load_tile(float* __restrict__ dst, const float* __restrict__ base, int64_t row_stride, int r0, int n, int width) {
+__device__ __forceinline__ void ask_tile(float* __restrict__ dst, const float* __restrict__ base, int64_t row_stride, int r0, int n, int width) {
   constexpr int VECS = HD / 4;
+  const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
+#pragma unroll
   for (int i = threadIdx.x; i < TILE * VECS; i += THREADS) {
     const int r = i / VECS, c = (i % VECS) * 4;
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (r0 + r < n && c < width) v = *reinterpret_cast<const float4*>(base + (int64_t)(r0 + r) * row_stride + c);
-    *reinterpret_cast<float4*>(dst + r * kStride<HD> + c) = v;
+    const bool there = r0 + r < n && c < width;
+    const float* from = there ? base + (int64_t)(r0 + r) * row_stride + c : base;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (r * kStride<HD> + c) * 4), "l"(from), "r"(there ? 16 : 0) : "memory");
   }
 }
+__device__ __forceinline__ void asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// until all that was asked for before the last `kLater` groups is there (and then, for all threads, a barrier)
+template <int kLater>
+__device__ __forceinline__ void wait_asked() { asm volatile("cp.async.wait_group %0;" ::"n"(kLater) : "memory"); }
 
 // s[r][c] = sum over channels of A[ty * 4 + r] * B[tx + 16 * c], those of even and of odd channels side by side (two in an instruction)
 template <int HD>
@@ -116,9 +122,8 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
   extern __shared__ float4 smem4[];
   constexpr int LD = kStride<HD>;
   float* sQ = reinterpret_cast<float*>(smem4);
-  float* sK = sQ + TILE * LD;
-  float* sV = sK + TILE * LD;
-  float* sPt = sV + TILE * LD;  // [key][query]
+  float* sKV = sQ + TILE * LD;  // two stages of a key and a value tile: the next ones come while these are used
+  float* sPt = sKV + 4 * TILE * LD;  // [key][query]
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const BlockOf w = block_of(p.a.q_len, TILE, p.a.q_heads, true);
   const SeqPair sq = sequence_pair(p.a, w.b);
@@ -129,7 +134,16 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
   const float* v = (const float*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;  // query i sees keys 0 .. i + shift (capped by nk)
   const int seen = min(sq.nk, p.a.causal ? min(q0 + TILE, sq.nq) + shift : sq.nk);
-  load_tile<HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+  auto ask = [&](int k0) {
+    float* t = sKV + (k0 / TILE & 1) * 2 * TILE * LD;
+    ask_tile<HD>(t, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    ask_tile<HD>(t + TILE * LD, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+  };
+  if (seen > 0) {
+    ask_tile<HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+    ask(0);
+  }
+  asked();
   float acc[4][HD / 16], m[4], l[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -139,10 +153,11 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
     for (int e = 0; e < HD / 16; ++e) acc[r][e] = 0.0f;
   }
   for (int k0 = 0; k0 < seen; k0 += TILE) {
+    if (k0 + TILE < seen) ask(k0 + TILE);
+    asked();
+    wait_asked<1>();
     __syncthreads();
-    load_tile<HD>(sK, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
-    load_tile<HD>(sV, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
-    __syncthreads();
+    const float *sK = sKV + (k0 / TILE & 1) * 2 * TILE * LD, *sV = sK + TILE * LD;
     float s[4][4];
     score_tile<HD>(sQ, sK, ty, tx, s);
 #pragma unroll
@@ -174,6 +189,7 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
       *reinterpret_cast<float4*>(sPt + (tx + 16 * c) * PS + ty * 4) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
     __syncthreads();
     add_product<HD>(sPt, sV, ty, tx, acc);
+    __syncthreads();
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -223,9 +239,8 @@ __device__ __forceinline__ void ragged_dq(const RaggedAttn& p, const BlockOf w) 
   constexpr int LD = kStride<HD>;
   float* sQ = reinterpret_cast<float*>(smem4);
   float* sG = sQ + TILE * LD;
-  float* sK = sG + TILE * LD;
-  float* sV = sK + TILE * LD;
-  float* sSt = sV + TILE * LD;  // [key][query]
+  float* sKV = sG + TILE * LD;
+  float* sSt = sKV + 4 * TILE * LD;  // [key][query]
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const SeqPair sq = sequence_pair(p.a, w.b);
   const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
@@ -234,15 +249,25 @@ __device__ __forceinline__ void ragged_dq(const RaggedAttn& p, const BlockOf w) 
   const float* v = (const float*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
   const int seen = min(sq.nk, p.a.causal ? min(q0 + TILE, sq.nq) + shift : sq.nk);
-  load_tile<HD>(sQ, (const float*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride, p.q.row_stride, q0, sq.nq, p.a.head_dim);
-  load_tile<HD>(sG, (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + w.h * p.d_o.head_stride, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
+  auto ask = [&](int k0) {
+    float* t = sKV + (k0 / TILE & 1) * 2 * TILE * LD;
+    ask_tile<HD>(t, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    ask_tile<HD>(t + TILE * LD, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+  };
+  if (seen > 0) {
+    ask_tile<HD>(sQ, (const float*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+    ask_tile<HD>(sG, (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + w.h * p.d_o.head_stride, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
+    ask(0);
+  }
+  asked();
   float lse[4], dd[4], acc[4][HD / 16] = {};
   row_statistics(p, sq, w.h, q0, ty, lse, dd);
   for (int k0 = 0; k0 < seen; k0 += TILE) {
+    if (k0 + TILE < seen) ask(k0 + TILE);
+    asked();
+    wait_asked<1>();
     __syncthreads();
-    load_tile<HD>(sK, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
-    load_tile<HD>(sV, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
-    __syncthreads();
+    const float *sK = sKV + (k0 / TILE & 1) * 2 * TILE * LD, *sV = sK + TILE * LD;
     float pr[4][4], ds[4][4];
     probabilities<HD>(sQ, sK, sG, sV, ty, tx, q0, k0, sq, p, shift, lse, dd, pr, ds);
 #pragma unroll
@@ -250,6 +275,7 @@ __device__ __forceinline__ void ragged_dq(const RaggedAttn& p, const BlockOf w) 
       *reinterpret_cast<float4*>(sSt + (tx + 16 * c) * PS + ty * 4) = make_float4(ds[0][c], ds[1][c], ds[2][c], ds[3][c]);
     __syncthreads();
     add_product<HD>(sSt, sK, ty, tx, acc);
+    __syncthreads();
   }
   store_rows<HD>((float*)p.dq.x + sq.q0 * p.dq.row_stride + w.h * p.dq.head_stride, p.dq.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, p.a.scale, acc);
 }
@@ -263,42 +289,63 @@ __device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w,
   constexpr int LD = kStride<HD>;
   float* sK = reinterpret_cast<float*>(smem4);
   float* sV = sK + TILE * LD;
-  float* sQ = sV + TILE * LD;
-  float* sG = sQ + TILE * LD;
-  float* sP = sG + TILE * LD;  // [query][key]
-  float* sS = sP + TILE * PS;
+  float* sQG = sV + TILE * LD;
+  constexpr bool kOneTile = HD > 64;  // shared memory has room for the probabilities or for ds
+  float* sP = sQG + 4 * TILE * LD;  // [query][key]
+  float* sS = sP + (kOneTile ? 0 : TILE * PS);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const SeqPair sq = sequence_pair(p.a, w.b);
   const int k0 = w.blk * TILE, group = p.a.q_heads / p.a.kv_heads;
   if (k0 >= sq.nk) return;  // (all blocks of the cluster)
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
   const int first = p.a.causal ? max(0, k0 - shift) / TILE * TILE : 0;  // the first block of queries that sees key k0
-  load_tile<HD>(sK, (const float*)p.k.x + sq.k0 * p.k.row_stride + w.h * p.k.head_stride, p.k.row_stride, k0, sq.nk, p.a.head_dim);
-  load_tile<HD>(sV, (const float*)p.v.x + sq.k0 * p.v.row_stride + w.h * p.v.head_stride, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+  // the tiles of queries of this block's heads, one after the other
+  const int tiles = max(0, (sq.nq + TILE - 1) / TILE - first / TILE), heads = (group - rank + ranks - 1) / ranks;
+  int ask_h = w.h * group + rank, ask_q = first;
+  auto ask = [&](int it) {
+    float* t = sQG + (it & 1) * 2 * TILE * LD;
+    ask_tile<HD>(t, (const float*)p.q.x + sq.q0 * p.q.row_stride + ask_h * p.q.head_stride, p.q.row_stride, ask_q, sq.nq, p.a.head_dim);
+    ask_tile<HD>(t + TILE * LD, (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + ask_h * p.d_o.head_stride, p.d_o.row_stride, ask_q, sq.nq, p.a.head_dim);
+    ask_q += TILE;
+    if (ask_q >= sq.nq) { ask_q = first; ask_h += ranks; }
+  };
+  if (tiles > 0) {
+    ask_tile<HD>(sK, (const float*)p.k.x + sq.k0 * p.k.row_stride + w.h * p.k.head_stride, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    ask_tile<HD>(sV, (const float*)p.v.x + sq.k0 * p.v.row_stride + w.h * p.v.head_stride, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+    ask(0);
+  }
+  asked();
   float dk[4][HD / 16] = {}, dv[4][HD / 16] = {};
-  for (int h = w.h * group + rank; h < (w.h + 1) * group; h += ranks) {
-    const float* q = (const float*)p.q.x + sq.q0 * p.q.row_stride + h * p.q.head_stride;
-    const float* g = (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + h * p.d_o.head_stride;
-    for (int q0 = first; q0 < sq.nq; q0 += TILE) {
-      __syncthreads();
-      load_tile<HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
-      load_tile<HD>(sG, g, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
-      float lse[4], dd[4];
-      row_statistics(p, sq, h, q0, ty, lse, dd);
-      __syncthreads();
-      float pr[4][4], ds[4][4];
-      probabilities<HD>(sQ, sK, sG, sV, ty, tx, q0, k0, sq, p, shift, lse, dd, pr, ds);
+  int h = w.h * group + rank, q0 = first;
+  for (int it = 0; it < tiles * heads; ++it) {
+    if (it + 1 < tiles * heads) ask(it + 1);
+    asked();
+    float lse[4], dd[4];
+    row_statistics(p, sq, h, q0, ty, lse, dd);
+    wait_asked<1>();
+    __syncthreads();
+    const float *sQ = sQG + (it & 1) * 2 * TILE * LD, *sG = sQ + TILE * LD;
+    float pr[4][4], ds[4][4];
+    probabilities<HD>(sQ, sK, sG, sV, ty, tx, q0, k0, sq, p, shift, lse, dd, pr, ds);
+    auto put = [&](float* dst, const float (&x)[4][4]) {
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          sP[(ty * 4 + r) * PS + tx + 16 * c] = pr[r][c];
-          sS[(ty * 4 + r) * PS + tx + 16 * c] = ds[r][c];
-        }
+        for (int c = 0; c < 4; ++c) dst[(ty * 4 + r) * PS + tx + 16 * c] = x[r][c];
+    };
+    put(sP, pr);
+    if (!kOneTile) put(sS, ds);
+    __syncthreads();
+    add_product<HD>(sP, sG, ty, tx, dv);
+    if (kOneTile) {
       __syncthreads();
-      add_product<HD>(sP, sG, ty, tx, dv);
-      add_product<HD>(sS, sQ, ty, tx, dk);
+      put(sS, ds);
+      __syncthreads();
     }
+    add_product<HD>(sS, sQ, ty, tx, dk);
+    __syncthreads();
+    q0 += TILE;
+    if (q0 >= sq.nq) { q0 = first; h += ranks; }
   }
   float* dk_base = (float*)p.dk.x + sq.k0 * p.dk.row_stride + w.h * p.dk.head_stride;
   float* dv_base = (float*)p.dv.x + sq.k0 * p.dv.row_stride + w.h * p.dv.head_stride;
@@ -391,14 +438,14 @@ void launch(Launcher& lc, K kernel, int64_t blocks, int smem, int cluster, A... 
 
 template <int HD>
 void forward_f32(Launcher& lc, const RaggedAttn& r) {
-  launch(lc, ragged_fwd_kernel<HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(3, 1), 1, r);
+  launch(lc, ragged_fwd_kernel<HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(5, 1), 1, r);
 }
 template <int HD>
 void backward_f32(Launcher& lc, const RaggedAttn& r) {
   int ranks = 8;
   while ((r.a.q_heads / r.a.kv_heads) % ranks) --ranks;
   const int64_t kv = blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences) * ranks, q = blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences);
-  launch(lc, ragged_bwd_kernel<HD>, kv + q, smem_of<HD>(4, 2), ranks, r, (unsigned)kv, ranks);
+  launch(lc, ragged_bwd_kernel<HD>, kv + q, smem_of<HD>(6, HD > 64 ? 1 : 2), ranks, r, (unsigned)kv, ranks);
 }
 
 void row_dots(Launcher& lc, const RaggedAttn& r) {
