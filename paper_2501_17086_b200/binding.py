@@ -419,6 +419,7 @@ _packed = _Packed()
 _ROTARY = struct.Struct("3i6f4x12q")        # hbp_rotary_spec, then four hbp_heads
 _ATTENTION = struct.Struct("8i2q2qf4xq")    # hbp_attention
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch.cuda.current_device
 
 
 def _refused(code, name, what):
@@ -431,7 +432,7 @@ def _on(name, first, *others):
     for t in others:
         if t is not None and t.get_device() != at:
             _refused(1, name, "the tensors are on different devices")
-    if at < 0 or at != torch.cuda.current_device():
+    if at < 0 or at != _current_device():
         _refused(1, name, f"a tensor is on {first.device}, which is not the current device")
     return _raw_stream(at)
 
@@ -448,10 +449,13 @@ def _code(t, name):
 def _heads(t, name):
     """Pointer and strides (elements) of a tensor [rows, heads, head_dim] whose channels are contiguous."""
     st = t.stride()
-    if len(st) != 3 or (st[2] != 1 and t.shape[2] != 1):
-        _refused(2, name, "wanted [rows, heads, head_dim] with contiguous channels")
-    rows, heads, _ = t.shape  # (a dimension of one element has any stride)
-    return t.data_ptr(), st[0] if rows > 1 else 0, st[1] if heads > 1 else 0
+    if len(st) != 3:
+        _refused(2, name, "wanted [rows, heads, head_dim]")
+    rs, hs, cs = st
+    rows, heads, width = t.shape
+    if cs != 1 and width != 1:
+        _refused(2, name, "the channels are not contiguous")
+    return t.data_ptr(), rs if rows > 1 else 0, hs if heads > 1 else 0  # (a dimension of one element has any stride)
 
 
 def _matrix(t, name):
@@ -465,6 +469,9 @@ def _matrix(t, name):
 def _alike(t, like, name, what):
     if t.shape != like.shape or t.dtype != like.dtype:
         _refused(2, name, what)
+
+
+_NONE = (0, 0, 0)
 
 
 def rotary_spec(rotary_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained_length=0.0, fast=32.0, slow=1.0,
@@ -481,19 +488,24 @@ def rotary(q, k=None, positions=None, first=0, period=0, rotary_dim=None, base=1
     ``positions``: int32 or int64 [rows] on the device, or None for first + row % period (period 0: first + row)."""
     if layout not in ROTARY_LAYOUTS or scaling not in ROTARY_SCALINGS:
         _refused(6, "rotary", f"layout {layout!r}, scaling {scaling!r}")
-    q_out = torch.empty_like(q) if q_out is None else q_out
-    k_out = torch.empty_like(k) if k is not None and k_out is None else k_out
-    stream = _on("rotary", q, k, positions, q_out, k_out)
-    if q.dim() != 3:
-        _refused(2, "rotary", "wanted [rows, heads, head_dim]")
+    qh = _heads(q, "rotary q")
     rows, q_heads, head_dim = q.shape
-    _alike(q_out, q, "rotary", "q_out is not like q")
-    kv_heads, kh, ko = 0, (0, 0, 0), (0, 0, 0)
+    if q_out is None:
+        q_out = torch.empty_like(q)
+    else:
+        _alike(q_out, q, "rotary", "q_out is not like q")
+    kv_heads, kh, ko = 0, _NONE, _NONE
     if k is not None:
-        if k.dim() != 3 or k.shape[0] != rows or k.shape[2] != head_dim or k.dtype != q.dtype:
+        kh = _heads(k, "rotary k")
+        k_rows, kv_heads, k_dim = k.shape
+        if k_rows != rows or k_dim != head_dim or k.dtype is not q.dtype:
             _refused(2, "rotary", "k is not like q")
-        _alike(k_out, k, "rotary", "k_out is not like k")
-        kv_heads, kh, ko = k.shape[1], _heads(k, "rotary k"), _heads(k_out, "rotary k_out")
+        if k_out is None:
+            k_out = torch.empty_like(k)
+        else:
+            _alike(k_out, k, "rotary", "k_out is not like k")
+        ko = _heads(k_out, "rotary k_out")
+    stream = _on("rotary", q, k, positions, q_out, k_out)
     at, size = None, 0
     if positions is not None:
         size = 4 if positions.dtype is torch.int32 else 8 if positions.dtype is torch.int64 else 0
@@ -502,7 +514,7 @@ def rotary(q, k=None, positions=None, first=0, period=0, rotary_dim=None, base=1
         at = positions.data_ptr()
     p = _packed
     _ROTARY.pack_into(p.buf, 0, ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], head_dim if rotary_dim is None else rotary_dim, base, factor,
-                      trained_length, fast, slow, amplitude, *_heads(q, "rotary q"), *_heads(q_out, "rotary q_out"), *kh, *ko)
+                      trained_length, fast, slow, amplitude, *qh, *_heads(q_out, "rotary q_out"), *kh, *ko)
     h = p.at + 40
     _check(lib.hbp_rotary(p.at, inverse, _code(q, "rotary"), rows, q_heads, kv_heads, head_dim, at, size, first, period, h, h + 24, h + 48, h + 72,
                           stream), "hbp_rotary")
@@ -559,11 +571,15 @@ def attention_forward(q, k, v, sequences=None, q_len=None, kv_len=None, q_offset
     sequences of equal length; with them (int32 [sequences + 1], on the device) q_len / kv_len are the longest ones'."""
     name = "attention_forward"
     a = _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
-    o = torch.empty_like(q) if o is None else o
-    lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device) if lse is None else lse
+    if o is None:
+        o = torch.empty_like(q)
+    else:
+        _alike(o, q, name, "o is not like q")
+    if lse is None:
+        lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32)
+    else:
+        _lse_of(q, lse, name)
     stream = _on(name, q, k, v, q_offsets, kv_offsets, o, lse, status)
-    _alike(o, q, name, "o is not like q")
-    _lse_of(q, lse, name)
     _HEADS[4].pack_into(_packed.buf, 80, *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), *_heads(o, "o"))
     _check(lib.hbp_attention_forward(a, a + 80, a + 104, a + 128, a + 152, lse.data_ptr(), stream), "hbp_attention_forward")
     return o, lse
@@ -574,17 +590,24 @@ def attention_backward(d_o, q, k, v, o, lse, sequences=None, q_len=None, kv_len=
     """The gradients (dq, dk, dv) of attention_forward's q, k and v from that of its output: see hbp_attention_backward."""
     name = "attention_backward"
     a = _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
-    dq = torch.empty_like(q) if dq is None else dq
-    dk = torch.empty_like(k) if dk is None else dk
-    dv = torch.empty_like(v) if dv is None else dv
-    scratch = torch.empty_like(lse) if scratch is None else scratch
-    stream = _on(name, q, k, v, d_o, o, lse, q_offsets, kv_offsets, dq, dk, dv, scratch, status)
     _alike(d_o, q, name, "d_o is not like q")
     _alike(o, q, name, "o is not like q")
-    _alike(dq, q, name, "dq is not like q")
-    _alike(dk, k, name, "dk is not like k")
-    _alike(dv, v, name, "dv is not like v")
     _lse_of(q, lse, name)
+    if dq is None:
+        dq = torch.empty_like(q)
+    else:
+        _alike(dq, q, name, "dq is not like q")
+    if dk is None:
+        dk = torch.empty_like(k)
+    else:
+        _alike(dk, k, name, "dk is not like k")
+    if dv is None:
+        dv = torch.empty_like(v)
+    else:
+        _alike(dv, v, name, "dv is not like v")
+    if scratch is None:
+        scratch = torch.empty_like(lse)
+    stream = _on(name, q, k, v, d_o, o, lse, q_offsets, kv_offsets, dq, dk, dv, scratch, status)
     _HEADS[8].pack_into(_packed.buf, 80, *_heads(d_o, "d_o"), *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), *_heads(o, "o"), *_heads(dq, "dq"),
                         *_heads(dk, "dk"), *_heads(dv, "dv"))
     _check(lib.hbp_attention_backward(a, a + 80, a + 104, a + 128, a + 152, a + 176, lse.data_ptr(), a + 200, a + 224, a + 248, scratch.data_ptr(),
@@ -600,15 +623,16 @@ def attention_scratch_bytes(q_heads, q_rows) -> int:
     return n.value
 
 
-def _kept(rows, d, codes, scales, device, name):
-    """Codes and scales of an activation [rows, d], made where not given."""
+def _kept(like, codes, scales, name):
+    """Codes and scales of an activation like this one [rows, d], made where not given."""
+    rows, d = like.shape
     groups = (d + CHECKPOINT_GROUP - 1) // CHECKPOINT_GROUP
     if codes is None:
-        codes = torch.empty((rows, d), dtype=torch.int8, device=device)
+        codes = like.new_empty((rows, d), dtype=torch.int8)
     elif codes.shape != (rows, d) or not codes.is_contiguous() or codes.dtype is not torch.int8:
         _refused(2, name, "codes: wanted int8 [rows, channels]")
     if scales is None:
-        scales = torch.empty((rows, groups), dtype=torch.uint8, device=device)
+        scales = like.new_empty((rows, groups), dtype=torch.uint8)
     elif scales.shape != (rows, groups) or not scales.is_contiguous() or scales.dtype is not torch.uint8:
         _refused(2, name, "scales: wanted uint8 [rows, channels / 32 rounded up]")
     return codes, scales
@@ -619,7 +643,7 @@ def checkpoint_store(x, codes=None, scales=None):
     name = "checkpoint_store"
     px, ld = _matrix(x, name)
     rows, d = x.shape
-    codes, scales = _kept(rows, d, codes, scales, x.device, name)
+    codes, scales = _kept(x, codes, scales, name)
     _check(lib.hbp_checkpoint_store(_code(x, name), rows, d, px, ld, codes.data_ptr(), scales.data_ptr(), _on(name, x, codes, scales)), "hbp_checkpoint_store")
     return codes, scales
 
@@ -627,10 +651,10 @@ def checkpoint_store(x, codes=None, scales=None):
 def checkpoint_load(codes, scales, dtype=torch.bfloat16, out=None):
     """The values that checkpoint_store kept, exactly, in dtype."""
     name = "checkpoint_load"
-    if codes.dim() != 2:
-        _refused(2, name, "codes: wanted int8 [rows, channels]")
+    if codes.dim() != 2 or scales is None:
+        _refused(2, name, "codes: wanted int8 [rows, channels], and their scales")
     rows, d = codes.shape
-    codes, scales = _kept(rows, d, codes, scales, codes.device, name)
+    codes, scales = _kept(codes, codes, scales, name)
     out = torch.empty_like(codes, dtype=dtype) if out is None else out
     if out.shape != codes.shape:
         _refused(2, name, "out is not like codes")
@@ -644,9 +668,11 @@ def checkpoint_gelu(z, act=None, codes=None, scales=None):
     name = "checkpoint_gelu"
     pz, ldz = _matrix(z, name)
     rows, d = z.shape
-    codes, scales = _kept(rows, d, codes, scales, z.device, name)
-    act = torch.empty((rows, d), dtype=z.dtype, device=z.device) if act is None else act
-    _alike(act, z, name, "act is not like z")
+    codes, scales = _kept(z, codes, scales, name)
+    if act is None:
+        act = z.new_empty((rows, d))
+    else:
+        _alike(act, z, name, "act is not like z")
     pa, lda = _matrix(act, name)
     _check(lib.hbp_checkpoint_gelu(_code(z, name), rows, d, pz, ldz, pa, lda, codes.data_ptr(), scales.data_ptr(), _on(name, z, codes, scales, act)),
            "hbp_checkpoint_gelu")
@@ -661,12 +687,14 @@ def checkpoint_gelu_backward(d_act, codes, scales, with_act=False, dz=None, act=
     rows, d = d_act.shape
     if codes is None or scales is None:
         _refused(1, name, "codes and scales have to be given")
-    codes, scales = _kept(rows, d, codes, scales, d_act.device, name)
-    dz = torch.empty((rows, d), dtype=d_act.dtype, device=d_act.device) if dz is None else dz
-    _alike(dz, d_act, name, "dz is not like d_act")
+    codes, scales = _kept(d_act, codes, scales, name)
+    if dz is None:
+        dz = d_act.new_empty((rows, d))
+    else:
+        _alike(dz, d_act, name, "dz is not like d_act")
     pz, ldz = _matrix(dz, name)
     if with_act and act is None:
-        act = torch.empty((rows, d), dtype=d_act.dtype, device=d_act.device)
+        act = d_act.new_empty((rows, d))
     pa, lda = None, 0
     if act is not None:
         _alike(act, d_act, name, "act is not like d_act")
