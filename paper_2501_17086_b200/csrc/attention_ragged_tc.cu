@@ -403,8 +403,12 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   if (threadIdx.x == 0) {
-    // (probabilities, dS: eight warps; full: the copies, and what the copying warp adds itself)
-    for (int i = 0; i < kBars; ++i) mbar_init(bars + 8 * i, i >= 3 && i < 3 + 2 * NB ? 8 : i >= 3 + 4 * NB && i < 3 + 4 * NB + NS ? 2 : 1);
+    // probabilities, dS: eight warps; full: the copies, and what the copying warp adds itself; scores of dK, dV: the products, and the warp that
+    // issues them, which has seen the statistics there and passes them on
+    for (int i = 0; i < kBars; ++i) {
+      const bool warps = i >= 3 && i < 3 + 2 * NB, two = (kDKV && i >= 3 + 2 * NB && i < 3 + 3 * NB) || (i >= 3 + 4 * NB && i < 3 + 4 * NB + NS);
+      mbar_init(bars + 8 * i, warps ? 8 : two ? 2 : 1);
+    }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -485,6 +489,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k)
           tc_mma(t, desc_add(dB0, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS0, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+        if (kDKV) mbar_arrive(bScores(it % NB));
         tc_commit(bScores(it % NB));
       }
     };
@@ -555,8 +560,6 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
     for (int it = group_id; it < n_it; it += C::kGroups) {
       const uint32_t parity = (uint32_t)(it / NB) & 1u;
       if (!wait_all(bScores(it % NB), parity, abort_flag, p.a.status)) { ok = false; break; }
-      // (over since before the scores were formed: makes the statistics that the copying warp wrote visible here)
-      if (kDKV && !wait_all(bFull(it % NS), (uint32_t)(it / NS) & 1u, abort_flag, p.a.status)) { ok = false; break; }
       tc_fence_after();
       const int c0 = (t_beg + it % tiles) * SMALL;
       const uint32_t t = tmem + lanes + 128 * (it % NB) + ch * 32;
