@@ -385,6 +385,7 @@ __device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w,
 // dk, dv and dq in one launch, in clusters of `ranks` blocks: a key block's, or one query block of as many heads.
 template <int HD>
 __global__ void __launch_bounds__(THREADS) ragged_bwd_kernel(const __grid_constant__ RaggedAttn p, const unsigned kv_blocks, const int ranks) {
+  chain_wait();  // (D comes from the launch before)
   if (blockIdx.x < kv_blocks) ragged_dkv<HD>(p, block_at(blockIdx.x / ranks, p.a.kv_len, TILE, p.a.kv_heads, false), (int)(blockIdx.x % ranks), ranks);
   else ragged_dq<HD>(p, block_at(blockIdx.x - kv_blocks, p.a.q_len, TILE, p.a.q_heads, true));
 }
@@ -394,6 +395,7 @@ __global__ void __launch_bounds__(THREADS) ragged_bwd_kernel(const __grid_consta
 template <typename T>
 __global__ void __launch_bounds__(256) row_dot_kernel(const __grid_constant__ RaggedAttn p, int lanes) {
   constexpr int V = 16 / (int)sizeof(T);
+  chain_next();  // (the backward kernels read the sums behind a chain_wait)
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
   const int lane = threadIdx.x & (lanes - 1);
   const int64_t row = i / p.a.q_heads;
@@ -415,37 +417,31 @@ constexpr int smem_of(int tiles, int scores) {
   return (tiles * TILE * kStride<HD> + scores * TILE * PS) * 4;
 }
 
-template <typename K, typename... A>
-void launch(Launcher& lc, K kernel, int64_t blocks, int smem, int cluster, A... args) {
-  if (blocks == 0) return;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = lc.stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = cluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = cluster > 1 ? 1 : 0;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kernel, args...);
-  if (e != cudaSuccess && lc.err == cudaSuccess) lc.err = e;
-  lc.count();
-  lc.check();
+template <typename K>
+void allow_smem(Launcher& lc, K kernel, int smem, bool& done) {
+  if (done) return;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  done = e == cudaSuccess;
+  if (!done && lc.err == cudaSuccess) lc.err = e;
 }
 
 template <int HD>
 void forward_f32(Launcher& lc, const RaggedAttn& r) {
-  launch(lc, ragged_fwd_kernel<HD>, blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), smem_of<HD>(5, 1), 1, r);
+  static PerDevice<bool> set;
+  allow_smem(lc, ragged_fwd_kernel<HD>, smem_of<HD>(5, 1), set.here());
+  ragged_fwd_kernel<HD><<<(unsigned)blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), THREADS, smem_of<HD>(5, 1), lc.stream>>>(r);
+  lc.count();
+  lc.check();
 }
 template <int HD>
 void backward_f32(Launcher& lc, const RaggedAttn& r) {
   int ranks = 8;
   while ((r.a.q_heads / r.a.kv_heads) % ranks) --ranks;
   const int64_t kv = blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences) * ranks, q = blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences);
-  launch(lc, ragged_bwd_kernel<HD>, kv + q, smem_of<HD>(6, HD > 64 ? 1 : 2), ranks, r, (unsigned)kv, ranks);
+  constexpr int kSmem = smem_of<HD>(6, HD > 64 ? 1 : 2);
+  static PerDevice<bool> set;
+  allow_smem(lc, ragged_bwd_kernel<HD>, kSmem, set.here());
+  launch_chained(lc, ragged_bwd_kernel<HD>, dim3((unsigned)(kv + q)), THREADS, kSmem, ranks, r, (unsigned)kv, ranks);
 }
 
 void row_dots(Launcher& lc, const RaggedAttn& r) {

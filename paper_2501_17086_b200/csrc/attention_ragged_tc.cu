@@ -653,6 +653,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
 template <int HD>
 __global__ void __launch_bounds__(Bwd<HD>::kThreads, Bwd<HD>::kBlocksAnSm)
 ragged_bwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p, const unsigned kv_blocks) {
+  chain_wait();  // (D comes from the launch before)
   if (blockIdx.x < kv_blocks) ragged_bwd_body<HD, true>(m, p, block_at(blockIdx.x, p.a.kv_len, BIG, p.a.kv_heads, false));
   else ragged_bwd_body<HD, false>(m, p, block_at(blockIdx.x - kv_blocks, p.a.q_len, BIG, p.a.q_heads, true));
 }
@@ -698,9 +699,7 @@ bool backward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
   static PerDevice<bool> set;
   if (!allow_smem(ragged_bwd_tc_kernel<HD>, Bwd<HD>::kSmem, set.here())) return false;
   const int64_t kv = blocks_of(r.a.kv_len, BIG, r.a.kv_heads, r.a.sequences), q = blocks_of(r.a.q_len, BIG, r.a.q_heads, r.a.sequences);
-  ragged_bwd_tc_kernel<HD><<<(unsigned)(kv + q), Bwd<HD>::kThreads, Bwd<HD>::kSmem, lc.stream>>>(m, r, (unsigned)kv);
-  lc.count();
-  lc.check();
+  launch_chained(lc, ragged_bwd_tc_kernel<HD>, dim3((unsigned)(kv + q)), Bwd<HD>::kThreads, Bwd<HD>::kSmem, 1, m, r, (unsigned)kv);
   return true;
 }
 
