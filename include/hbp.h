@@ -342,6 +342,12 @@ hbp_status hbp_rotary(const hbp_rotary_spec* spec, int32_t inverse, int32_t dtyp
                       int32_t head_dim, const void* positions, int32_t position_bytes, int64_t first, int64_t period,
                       const hbp_heads* q, const hbp_heads* q_out, const hbp_heads* k, const hbp_heads* k_out, void* cuda_stream);
 
+/* Rotary positions in a decoder context (HBP_BLOCK_PRELN_TRANSFORMER; HBP_ERR_UNSUPPORTED for the other kinds): from the next hbp_forward
+ * on, queries and keys of every block are turned after their projection, row t of each sequence at position first + t, and the
+ * gradients are turned back in every VJP.  spec is copied; NULL takes the positions out again.  Backward calls are refused
+ * (HBP_ERR_STATE) until the next hbp_forward.  Host only. */
+hbp_status hbp_context_rotary(hbp_ctx* ctx, const hbp_rotary_spec* spec, int64_t first);
+
 /* Attention over `sequences` pairs of sequences: the queries of sequence b attend to its keys, o = softmax(scale * q k^T) v.
  *  heads     query head h reads key / value head h / (q_heads / kv_heads); q_heads is a multiple of kv_heads.
  *  offsets   device int32 [sequences + 1]: sequence b is rows offsets[b] .. offsets[b + 1] - 1 of the tensors; q_len (kv_len) is then

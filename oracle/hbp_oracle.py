@@ -107,11 +107,15 @@ class MLPStep:
 
 class AttnStep:
     """f(x) = MHA(LN(x)) Wo^T, causal softmax attention, x of shape [B, S, d]
-    (Table 1, row "Transformer (Pre-LN)"; attention sub-layer of Section 5.1.1)."""
+    (Table 1, row "Transformer (Pre-LN)"; attention sub-layer of Section 5.1.1).
 
-    def __init__(self, Wq, Wk, Wv, Wo, n_heads, eps=1e-5):
+    ``turn(t, back)``, if given, is a linear map of queries and keys [B, H, S, dh] after their projection (rotary
+    positions), with back=True its transpose."""
+
+    def __init__(self, Wq, Wk, Wv, Wo, n_heads, eps=1e-5, turn=None):
         self.Wq, self.Wk, self.Wv, self.Wo = Wq, Wk, Wv, Wo
         self.H, self.eps = int(n_heads), eps
+        self.turn = turn
 
     def _split(self, t):
         B, S, d = t.shape
@@ -127,6 +131,8 @@ class AttnStep:
         q = self._split(y @ _f64(self.Wq).T)
         k = self._split(y @ _f64(self.Wk).T)
         v = self._split(y @ _f64(self.Wv).T)
+        if self.turn is not None:
+            q, k = self.turn(q, False), self.turn(k, False)
         S = x.shape[1]
         scale = 1.0 / math.sqrt(q.shape[-1])
         s = (q @ k.transpose(0, 1, 3, 2)) * scale
@@ -147,6 +153,8 @@ class AttnStep:
         ds = p * (dp - (dp * p).sum(axis=-1, keepdims=True))
         dq = (ds @ k) * c["scale"]
         dk = (ds.transpose(0, 1, 3, 2) @ q) * c["scale"]
+        if self.turn is not None:
+            dq, dk = self.turn(dq, True), self.turn(dk, True)
         return self._merge(dq), self._merge(dk), self._merge(dv)
 
     def vjp(self, c, g):

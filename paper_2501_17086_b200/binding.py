@@ -27,7 +27,7 @@ EXPORTS = ["hbp_workspace_bytes", "hbp_create", "hbp_forward", "hbp_backward", "
            "hbp_context_modes", "hbp_selftest_wait_timeout", "hbp_selftest_gate_math", "hbp_recurrence_plan",
            "hbp_profile_enable", "hbp_profile_read", "hbp_cumsumprod_static", "hbp_cumsumprod_static_max_bytes",
            "hbp_compare_scratch_bytes", "hbp_compare", "hbp_iterate", "hbp_add_carry", "hbp_param_grads",
-           "hbp_rotary", "hbp_attention_forward", "hbp_attention_scratch_bytes", "hbp_attention_backward",
+           "hbp_rotary", "hbp_context_rotary", "hbp_attention_forward", "hbp_attention_scratch_bytes", "hbp_attention_backward",
            "hbp_checkpoint_store", "hbp_checkpoint_load", "hbp_checkpoint_gelu", "hbp_checkpoint_gelu_backward",
            "hbp_status_string", "hbp_destroy"]
 
@@ -101,6 +101,7 @@ def _load():
     lib.hbp_compare.argtypes = [i32, i32, i64, vp, vp, vp, vp, sz, vp]
     heads = vp  # (addresses of packed structures)
     lib.hbp_rotary.argtypes = [vp, i32, i32, i64, i32, i32, i32, vp, i32, i64, i64, heads, heads, heads, heads, vp]
+    lib.hbp_context_rotary.argtypes = [vp, C.POINTER(hbp_rotary_spec), i64]
     lib.hbp_attention_forward.argtypes = [vp, heads, heads, heads, heads, vp, vp]
     lib.hbp_attention_scratch_bytes.argtypes = [vp, C.POINTER(sz)]
     lib.hbp_attention_backward.argtypes = [vp] + [heads] * 5 + [vp] + [heads] * 3 + [vp, sz, vp]
@@ -319,6 +320,11 @@ class Context:
         _check(lib.hbp_param_grads(self._h, C.byref(p), _ptr(x_all), _ptr(inputs), _ptr(g_all), self._grads(grads),
                                    _stream()), "hbp_param_grads")
         return grads
+
+    def set_rotary(self, spec: hbp_rotary_spec | None, first=0):
+        """Decoder contexts: rotary positions (``rotary_spec``) from the next forward pass on, or none; row t of a sequence is at
+        position first + t."""
+        _check(lib.hbp_context_rotary(self._h, None if spec is None else C.byref(spec), first), "hbp_context_rotary")
 
     def sync_status(self):
         _check(lib.hbp_sync_status(self._h, _stream()), "hbp_sync_status")

@@ -101,9 +101,22 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int rows, int from, in
     st_shared16(tile + c * rows * 128 + (from + (r >> 3)) * 128 + (r & 7) * 16, make_uint4(0, 0, 0, 0));
   }
 }
-// A wait of the whole warp: all lanes go on or none does.
+// A bounded wait (mbar_wait) of the whole warp, where the status word may be missing: all lanes go on or none does.
 __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status));
+  bool ok = true;
+  uint64_t t0 = 0;
+  for (uint32_t spin = 0; !mbar_try_wait(bar, parity); ++spin) {
+    if ((spin & 255u) != 255u) continue;
+    const uint64_t now = global_ns();
+    if (t0 == 0) t0 = now;
+    if (*abort_flag || now - t0 > WAIT_LIMIT_NS) {
+      if (!*abort_flag && status) atomicExch(status, (int)HBP_ERR_TIMEOUT);
+      *abort_flag = 1;
+      ok = false;
+      break;
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
 }
 // The end of a block: after a wait that gave up, every copy and product is outlasted first.
 __device__ __forceinline__ void leave(int warp, uint32_t tmem, uint32_t columns, volatile int* abort_flag) {

@@ -102,6 +102,10 @@ struct hbp_ctx {
   float* drow = nullptr;   // [Lb][B][H][S]
   float2* dopart = nullptr;  // [Lb][N][do_slots] row sums of dO and dO * O per 64 columns (= per head)
   int do_slots = 0;
+  // decoder: rotary positions of queries and keys (hbp_context_rotary)
+  bool has_rotary = false;
+  hbp_rotary_spec rotary;
+  int64_t rotary_first = 0;
 };
 
 namespace {
@@ -548,6 +552,13 @@ struct Run {
     run_gemm(b);
   }
 
+  // Turns the queries and keys (back: their gradients, by the opposite angles) of nb layers' [N][3d] buffer in place.
+  void turn(char* qkv, int nb, bool back) {
+    if (!c->has_rotary) return;
+    const hbp_config& f = c->cfg;
+    const hbp_heads q = {qkv, 3 * d, f.head_dim}, k = {at(qkv, d), 3 * d, f.head_dim};
+    rotary(lc, c->rotary, back, f.dtype, nb * N, f.n_heads, f.n_heads, f.head_dim, nullptr, 0, c->rotary_first, f.seq, q, q, k, k);
+  }
   // ---- attention block of decoder layers [b0, b1) ------------------------------------------------
   void attn_vjp(int b0, int b1, bool want_dy) {
     const hbp_config& f = c->cfg;
@@ -575,6 +586,7 @@ struct Run {
     t.status = c->status;
     if (c->dopart && do_tc) { t.d_stats = c->dopart + (int64_t)b0 * N * c->do_slots; t.d_slots = c->do_slots; }
     attention_bwd(lc, t);
+    turn(at(c->dQKV, (int64_t)b0 * 3 * state), nb, true);
     if (!want_dy) return;
     GemmArgs b = base_args();  // dY = [dQ dK dV] [Wq; Wk; Wv]
     b.M = (int)N; b.N = (int)d; b.K = (int)(3 * d); b.batch = nb;
@@ -1176,6 +1188,20 @@ hbp_status hbp_selftest_wait_timeout(hbp_ctx* ctx, void* scratch, size_t scratch
   return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
 }
 
+hbp_status hbp_context_rotary(hbp_ctx* ctx, const hbp_rotary_spec* spec, int64_t first) {
+  if (!ctx) return HBP_ERR_INVALID_ARG;
+  if (ctx->cfg.block != HBP_BLOCK_PRELN_TRANSFORMER) return HBP_ERR_UNSUPPORTED;
+  if (spec) {
+    const hbp_status st = check_rotary_spec(spec, ctx->cfg.head_dim);
+    if (st != HBP_OK) return st;
+    ctx->rotary = *spec;
+    ctx->rotary_first = first;
+  }
+  ctx->has_rotary = spec != nullptr;
+  ctx->forward_done = false;  // the caches are those of other positions
+  return HBP_OK;
+}
+
 hbp_status hbp_forward(hbp_ctx* ctx, const hbp_params* params, const void* x0, const void* inputs, void* x_all,
                        void* cuda_stream) {
   hbp_status st = check_call(ctx, params, false);
@@ -1340,6 +1366,7 @@ hbp_status hbp_forward(hbp_ctx* ctx, const hbp_params* params, const void* x0, c
         q.B = r.at(ctx->Wqkv, (int64_t)b * 3 * d * d); q.b_sn = d; q.b_sk = 1;
         q.epi = EPI_STORE; q.D = r.at(ctx->QKV, (int64_t)b * 3 * state); q.ldd = 3 * d;
         r.run_gemm(q);
+        r.turn(r.at(ctx->QKV, (int64_t)b * 3 * state), 1, false);
         AttnArgs t;
         t.dtype = f.dtype; t.batch = f.batch; t.seq = f.seq; t.heads = f.n_heads; t.head_dim = f.head_dim;
         t.qkv = r.at(ctx->QKV, (int64_t)b * 3 * state);

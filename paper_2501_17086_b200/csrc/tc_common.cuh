@@ -55,7 +55,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
       if (t0 == 0) t0 = now;
       else if (now - t0 > limit_ns) {
         *abort_flag = 1;
-        if (status) atomicExch(status, (int)HBP_ERR_TIMEOUT);
+        atomicExch(status, (int)HBP_ERR_TIMEOUT);
         return false;
       }
     }
