@@ -149,6 +149,13 @@ hbp_status hbp_workspace_bytes(const hbp_config* cfg, size_t* bytes);
  * is smaller than any form of the products needs (float MLP stacks: see hbp_workspace_bytes) or misaligned. */
 hbp_status hbp_create(const hbp_config* cfg, void* workspace, size_t workspace_bytes, hbp_ctx** out);
 
+/* The same for contexts that keep their activations in 8 bits (the stacks and the decoder; HBP_ERR_UNSUPPORTED for the recurrent kinds):
+ * instead of gelu(Z) and gelu'(Z) of every layer, 2 to 4 bytes each, the workspace holds Z as hbp_checkpoint_store keeps it, 1.03 bytes.  The
+ * forward pass is that of Z itself (rounded to dtype); the VJPs and the weight gradients use gelu' and gelu of the kept values.
+ * Float stacks use none of the forms of few rows or of operands in parts. */
+hbp_status hbp_workspace_bytes_checkpointed(const hbp_config* cfg, size_t* bytes);
+hbp_status hbp_create_checkpointed(const hbp_config* cfg, void* workspace, size_t workspace_bytes, hbp_ctx** out);
+
 /* Section 3, h_i = f_i(h_{i-1}): runs the steps from x0 [N][d] and stores every state in
  * x_all [steps+1][N][d] (x_all[0] = x0) plus, in the workspace, what the block VJPs need.
  * `inputs` is the recurrent kinds' x [L][batch][in_dim] (NULL otherwise). */
@@ -280,6 +287,7 @@ int64_t hbp_form_count(const hbp_ctx* ctx, int32_t form);
  * CTAs), the reverse scan between two all-step VJPs (Eq. 9 followed by Eq. 8) also writes
  * the next VJP's left operand g_{t+1} * tanh'(z_t), split for the tensor cores, instead of the intermediate
  * iterate: the default; HBP_SCAN_OPERAND=0 keeps the separate pass (same bits in every result, a cross-check).
+ * bit 3 = the context keeps its activations in 8 bits (hbp_create_checkpointed).
  * HBP_LAYER_GROUP=n (no bit) caps the layers whose hidden-size scratch is held at once at n, where the stack's size asks for no
  * smaller group already: a small stack then takes the group by group path of the largest ones.
  * The modes belong to the context: contexts created
@@ -390,7 +398,8 @@ hbp_status hbp_attention_backward(const hbp_attention* a, const hbp_heads* d_o, 
  *  store          codes, scales of x
  *  load           x of codes, scales
  *  gelu           act = gelu(z) from z itself (act may be z), and z's codes and scales
- *  gelu_backward  dz = d_act * gelu'(z8) (dz may be d_act) and, where act is given, gelu(z8), z8 being the stored values */
+ *  gelu_backward  dz = d_act * gelu'(z8) (dz may be d_act) and, where act is given, gelu(z8), z8 being the stored values; gelu(z8) alone where
+ *                 d_act and dz are NULL */
 hbp_status hbp_checkpoint_store(int32_t dtype, int64_t rows, int32_t d, const void* x, int64_t ldx, int8_t* codes, uint8_t* scales,
                                 void* cuda_stream);
 hbp_status hbp_checkpoint_load(int32_t dtype, int64_t rows, int32_t d, const int8_t* codes, const uint8_t* scales, void* x, int64_t ldx,

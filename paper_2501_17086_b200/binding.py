@@ -22,7 +22,7 @@ GATE_ONE, GATE_CHANNEL_SHARED, GATE_CHANNEL_PER_STEP = 0, 1, 2
 LOSS_FINAL, LOSS_EVERY_STEP = 0, 1
 FORMS = ("cell_cluster", "rnn_cluster", "rnn_four_rows", "step", "gemm_f32", "gemm_simt", "gemm_parts", "gemm_cell", "few_rows")
 
-EXPORTS = ["hbp_workspace_bytes", "hbp_create", "hbp_forward", "hbp_backward", "hbp_exact",
+EXPORTS = ["hbp_workspace_bytes", "hbp_create", "hbp_workspace_bytes_checkpointed", "hbp_create_checkpointed", "hbp_forward", "hbp_backward", "hbp_exact",
            "hbp_cumsumprod_scratch_bytes", "hbp_cumsumprod", "hbp_cumsumprod_status", "hbp_sync_status", "hbp_launch_count", "hbp_form_count",
            "hbp_context_modes", "hbp_selftest_wait_timeout", "hbp_selftest_gate_math", "hbp_recurrence_plan",
            "hbp_profile_enable", "hbp_profile_read", "hbp_cumsumprod_static", "hbp_cumsumprod_static_max_bytes",
@@ -81,6 +81,8 @@ def _load():
     vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
     lib.hbp_workspace_bytes.argtypes = [C.POINTER(hbp_config), C.POINTER(sz)]
     lib.hbp_create.argtypes = [C.POINTER(hbp_config), vp, sz, C.POINTER(vp)]
+    lib.hbp_workspace_bytes_checkpointed.argtypes = lib.hbp_workspace_bytes.argtypes
+    lib.hbp_create_checkpointed.argtypes = lib.hbp_create.argtypes
     lib.hbp_forward.argtypes = [vp, C.POINTER(hbp_params), vp, vp, vp, vp]
     lib.hbp_backward.argtypes = [vp, C.POINTER(hbp_params), i32, vp, vp, vp, vp, C.POINTER(hbp_grads), vp]
     lib.hbp_exact.argtypes = [vp, C.POINTER(hbp_params), vp, vp, vp, vp, C.POINTER(hbp_grads), vp]
@@ -170,9 +172,10 @@ def config_from_workload(w) -> hbp_config:
                        w.batch, gate, loss, w.ln_eps, getattr(w, "gamma", 0.0))
 
 
-def workspace_bytes(cfg: hbp_config) -> int:
+def workspace_bytes(cfg: hbp_config, checkpointed=False) -> int:
     n = C.c_size_t(0)
-    _check(lib.hbp_workspace_bytes(C.byref(cfg), C.byref(n)), "hbp_workspace_bytes")
+    ask = lib.hbp_workspace_bytes_checkpointed if checkpointed else lib.hbp_workspace_bytes
+    _check(ask(C.byref(cfg), C.byref(n)), "hbp_workspace_bytes")
     return n.value
 
 
@@ -210,19 +213,21 @@ _BLOCK_NAMES = {v: k for k, v in BLOCKS.items()}
 
 
 class Context:
-    """One hbp_ctx over a torch-allocated workspace on the current CUDA device."""
+    """One hbp_ctx over a torch-allocated workspace on the current CUDA device.  ``checkpointed``: the activations of the stacks and of
+    the decoder are kept in 8 bits."""
 
-    def __init__(self, cfg: hbp_config, device="cuda"):
+    def __init__(self, cfg: hbp_config, device="cuda", checkpointed=False):
         self.cfg = cfg
         self.device = torch.device(device)
         self.dtype = torch.float32 if cfg.dtype == HBP_F32 else torch.bfloat16
         self.block = _BLOCK_NAMES[cfg.block]
         self.steps = 2 * cfg.L if self.block == "preln_transformer" else cfg.L
-        nbytes = workspace_bytes(cfg)
+        nbytes = workspace_bytes(cfg, checkpointed)
         self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         base = (self.workspace.data_ptr() + 255) // 256 * 256
         handle = C.c_void_p()
-        _check(lib.hbp_create(C.byref(cfg), C.c_void_p(base), nbytes, C.byref(handle)), "hbp_create")
+        create = lib.hbp_create_checkpointed if checkpointed else lib.hbp_create
+        _check(create(C.byref(cfg), C.c_void_p(base), nbytes, C.byref(handle)), "hbp_create")
         self._h = handle
         self._keep = None
 
@@ -238,7 +243,7 @@ class Context:
     @property
     def modes(self) -> int:
         """Bit 0: CUDA-core kernels forced; bit 1: paired-CTA GEMM; bit 2: the scan writes the next VJP's operand
-        (float tanh RNN).  Fixed at creation, per context."""
+        (float tanh RNN); bit 3: activations in 8 bits.  Fixed at creation, per context."""
         return int(lib.hbp_context_modes(self._h))
 
     def close(self):

@@ -23,7 +23,7 @@ namespace {
 constexpr int kThreads = 256, kBatch = 2;
 constexpr int kGroup = 32;
 
-enum Work { kStore = 0, kLoad = 1, kGelu = 2, kGeluBackward = 3 };
+enum Work { kStore = 0, kLoad = 1, kGelu = 2, kGeluBackward = 3, kGeluAgain = 4 };  // the last: gelu(z8) alone
 
 struct CheckpointParams {
   int64_t rows;
@@ -137,8 +137,8 @@ __global__ void __launch_bounds__(kThreads) checkpoint_kernel(const CheckpointPa
       in[u] = i < p.chunks && col[u] < p.d;
     }
     if (in[u]) {
-      if (W != kLoad) x[u] = *reinterpret_cast<const VT*>((const T*)p.x + (kFlat ? i * V : row[u] * p.ldx + col[u]));
-      if (W == kLoad || W == kGeluBackward) {
+      if (W != kLoad && W != kGeluAgain) x[u] = *reinterpret_cast<const VT*>((const T*)p.x + (kFlat ? i * V : row[u] * p.ldx + col[u]));
+      if (W == kLoad || W == kGeluBackward || W == kGeluAgain) {
         code[u] = *reinterpret_cast<const VC*>(p.codes + (kFlat ? i * V : row[u] * p.d + col[u]));
         scale[u] = p.scales[kFlat ? i / kLanes : row[u] * p.groups + col[u] / kGroup];
       }
@@ -200,6 +200,15 @@ __global__ void __launch_bounds__(kThreads) checkpoint_kernel(const CheckpointPa
           *reinterpret_cast<VT*>((T*)p.act + (kFlat ? i * V : row[u] * p.lda + col[u])) = a;
         }
       }
+      if (W == kGeluAgain) {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          float2 act, slope;
+          gelu_pair(make_float2(f[e], f[e + 1]), act, slope, T());
+          f[e] = act.x;
+          f[e + 1] = act.y;
+        }
+      }
       narrow<V>(f, y.v);
       *reinterpret_cast<VT*>((T*)p.y + at_y) = y;
     }
@@ -212,12 +221,24 @@ void launch(Launcher& lc, CheckpointParams& p) {
   p.groups = (p.d + kGroup - 1) / kGroup;
   p.per_row = p.groups * (kGroup / V);
   p.chunks = p.rows * p.per_row;
-  const bool flat = p.d % kGroup == 0 && (W == kLoad || p.ldx == p.d) && (W == kStore || p.ldy == p.d) && (!p.act || p.lda == p.d);
+  const bool flat = p.d % kGroup == 0 && (W == kLoad || W == kGeluAgain || p.ldx == p.d) && (W == kStore || p.ldy == p.d) && (!p.act || p.lda == p.d);
   const int64_t blocks = (p.chunks + kThreads * kBatch - 1) / (kThreads * kBatch);
   if (flat) checkpoint_kernel<T, W, true><<<(unsigned)blocks, kThreads, 0, lc.stream>>>(p);
   else checkpoint_kernel<T, W, false><<<(unsigned)blocks, kThreads, 0, lc.stream>>>(p);
   lc.count();
   lc.check();
+}
+
+template <int W>
+void run(Launcher& lc, int dtype, int64_t rows, int d, const void* x, int64_t ldx, void* y, int64_t ldy, void* act, int64_t lda, int8_t* codes,
+         uint8_t* scales) {
+  CheckpointParams p = {};
+  p.rows = rows; p.d = d;
+  p.x = x; p.y = y; p.act = act;
+  p.ldx = ldx; p.ldy = ldy; p.lda = lda;
+  p.codes = codes; p.scales = scales;
+  if (dtype == HBP_F32) launch<float, W>(lc, p);
+  else launch<bf16, W>(lc, p);
 }
 
 template <int W>
@@ -229,23 +250,28 @@ hbp_status call(int dtype, int64_t rows, int d, const void* x, int64_t ldx, void
   const int64_t per_row = (d + kGroup - 1) / kGroup * (kGroup / v);
   if (rows > (int64_t)INT32_MAX * kThreads / per_row) return HBP_ERR_SHAPE;
   if (rows == 0) return HBP_OK;
-  if (!codes || !scales || (W != kLoad && !x) || (W != kStore && !y)) return HBP_ERR_INVALID_ARG;
+  constexpr bool kIn = W != kLoad && W != kGeluAgain;
+  if (!codes || !scales || (kIn && !x) || (W != kStore && !y)) return HBP_ERR_INVALID_ARG;
   auto bad = [&](const void* t, int64_t ld) { return ((uintptr_t)t & 15u) || ld < d || ld % v; };
-  if (((uintptr_t)codes & 15u) || (W != kLoad && bad(x, ldx)) || (W != kStore && bad(y, ldy)) || (act && bad(act, lda))) return HBP_ERR_SHAPE;
+  if (((uintptr_t)codes & 15u) || (kIn && bad(x, ldx)) || (W != kStore && bad(y, ldy)) || (act && bad(act, lda))) return HBP_ERR_SHAPE;
   if (x && x == y && ldx != ldy) return HBP_ERR_INVALID_ARG;  // in place, but rows elsewhere
   Launcher lc;
   lc.stream = (cudaStream_t)stream;
-  CheckpointParams p = {};
-  p.rows = rows; p.d = d;
-  p.x = x; p.y = y; p.act = act;
-  p.ldx = ldx; p.ldy = ldy; p.lda = lda;
-  p.codes = codes; p.scales = scales;
-  if (dtype == HBP_F32) launch<float, W>(lc, p);
-  else launch<bf16, W>(lc, p);
+  run<W>(lc, dtype, rows, d, x, ldx, y, ldy, act, lda, codes, scales);
   return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
 }
 
 }  // namespace
+
+void checkpoint_gelu(Launcher& lc, int dtype, int64_t rows, int d, void* z, int8_t* codes, uint8_t* scales) {
+  run<kGelu>(lc, dtype, rows, d, z, d, z, d, nullptr, 0, codes, scales);
+}
+void checkpoint_gelu_backward(Launcher& lc, int dtype, int64_t rows, int d, const int8_t* codes, const uint8_t* scales, void* dz) {
+  run<kGeluBackward>(lc, dtype, rows, d, dz, d, dz, d, nullptr, 0, const_cast<int8_t*>(codes), const_cast<uint8_t*>(scales));
+}
+void checkpoint_gelu_again(Launcher& lc, int dtype, int64_t rows, int d, const int8_t* codes, const uint8_t* scales, void* act) {
+  run<kGeluAgain>(lc, dtype, rows, d, nullptr, 0, act, d, nullptr, 0, const_cast<int8_t*>(codes), const_cast<uint8_t*>(scales));
+}
 
 }  // namespace hbp
 
@@ -267,6 +293,8 @@ hbp_status hbp_checkpoint_gelu(int32_t dtype, int64_t rows, int32_t d, const voi
 }
 hbp_status hbp_checkpoint_gelu_backward(int32_t dtype, int64_t rows, int32_t d, const int8_t* codes, const uint8_t* scales, const void* d_act,
                                         int64_t ldd, void* dz, int64_t ldz, void* act, int64_t lda, void* cuda_stream) {
+  if (!d_act && !dz && act)
+    return call<kGeluAgain>(dtype, rows, d, nullptr, 0, act, lda, nullptr, 0, const_cast<int8_t*>(codes), const_cast<uint8_t*>(scales), cuda_stream);
   return call<kGeluBackward>(dtype, rows, d, d_act, ldd, dz, ldz, act, lda, const_cast<int8_t*>(codes), const_cast<uint8_t*>(scales), cuda_stream);
 }
 

@@ -53,6 +53,12 @@ struct hbp_ctx {
   float* rstd = nullptr;   // [steps][N]
   char* ACT = nullptr;     // [layers][N][h] gelu(Z)
   char* DACT = nullptr;    // [layers][N][h] gelu'(Z)
+  // Instead of both, contexts made by hbp_create_checkpointed: Z in 8 bits [layers][N][h] with its scales [layers][N][h / 32 rounded up], and
+  // gelu of what they stand for, of the layers of one group [group][N][h]
+  bool checkpointed = false;
+  int8_t* Z8 = nullptr;
+  uint8_t* Z8s = nullptr;
+  char* ACTg = nullptr;
   float* xres = nullptr;   // [N][d] float master of the residual stream (bf16 only)
   double* hres = nullptr;  // RNN: 2 x [B][d] double master of the recurrent state (ping-pong)
   double* Pd = nullptr;    // tanh RNN: [T][B][d] input projections U x_t in double for the one-launch recurrence
@@ -118,7 +124,7 @@ constexpr int kMaxSplit = 256;
 
 inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 
-hbp_status check_config(const hbp_config* c) {
+hbp_status check_config(const hbp_config* c, bool checkpointed = false) {
   if (!c) return HBP_ERR_INVALID_ARG;
   if (c->dtype != HBP_F32 && c->dtype != HBP_BF16) return HBP_ERR_DTYPE;
   if (c->block < 0 || c->block > HBP_BLOCK_POSTLN_MLP) return HBP_ERR_UNSUPPORTED;
@@ -137,6 +143,7 @@ hbp_status check_config(const hbp_config* c) {
   // that land near zero, and each such element changes its whole gradient path; float only
   if (c->block == HBP_BLOCK_RELU_MLP && c->dtype != HBP_F32) return HBP_ERR_UNSUPPORTED;
   if (c->block == HBP_BLOCK_LSTM && (c->hidden <= 0 || c->hidden % v || 2 * c->hidden != c->d)) return HBP_ERR_SHAPE;
+  if (checkpointed && (c->block == HBP_BLOCK_RNN_TANH || gated_cell)) return HBP_ERR_UNSUPPORTED;  // no GELU, nothing to keep
   if (c->block == HBP_BLOCK_RNN_TANH || gated_cell) {
     if (c->in_dim <= 0 || c->in_dim % v) return HBP_ERR_SHAPE;
     if (c->batch != c->tokens) return HBP_ERR_SHAPE;
@@ -157,8 +164,9 @@ hbp_status check_config(const hbp_config* c) {
 // 1.48; 16 layers 68 (136) x 4096 rows 1.72 and 1.68; 8 layers 132 (260) x 1000 1.50 and 1.53; 16 layers 1024 (4096) x 40 rows 1.60
 // and 2.85, x 2000 1.89 and 2.06.  Below 64 wide the tiles are mostly padding (36 (64) x 40 rows 0.91 and 0.94), and up to 32 rows
 // the CUDA cores are faster (gemm_f32.cu).
-bool keeps_parts(const hbp_config& f) {
-  return f.dtype == HBP_F32 && (f.block == HBP_BLOCK_MLP || f.block == HBP_BLOCK_PRELN_MLP || f.block == HBP_BLOCK_RELU_MLP || f.block == HBP_BLOCK_POSTLN_MLP) &&
+bool keeps_parts(const hbp_ctx* c) {
+  const hbp_config& f = c->cfg;
+  return !c->checkpointed && f.dtype == HBP_F32 && (f.block == HBP_BLOCK_MLP || f.block == HBP_BLOCK_PRELN_MLP || f.block == HBP_BLOCK_RELU_MLP || f.block == HBP_BLOCK_POSTLN_MLP) &&
          f.tokens > 32 && f.d >= 64 && f.hidden >= 64;
 }
 
@@ -296,9 +304,15 @@ size_t carve(hbp_ctx* c, char* base, int weight_layers) {
       take_planes(c->W2p, weight_layers, d, h);
       take_planes(c->ACTp, layers, N, h);
     }
-    c->ACT = parts ? (char*)c->ACTp.p : take(layers * N * h * es);
-    c->DACT = take(layers * N * h * es);
-    const size_t per_layer = parts ? 3 * 2 * N * (plane_cols(d) + plane_cols(h)) : N * h * es;  // Gp and DZp, or H1
+    if (c->checkpointed) {
+      c->Z8 = (int8_t*)take(layers * N * h);
+      c->Z8s = (uint8_t*)take(layers * N * ((h + 31) / 32));
+    } else {
+      c->ACT = parts ? (char*)c->ACTp.p : take(layers * N * h * es);
+      c->DACT = take(layers * N * h * es);
+    }
+    // Gp and DZp, or H1 (and ACTg)
+    const size_t per_layer = parts ? 3 * 2 * N * (plane_cols(d) + plane_cols(h)) : N * h * es * (c->checkpointed ? 2 : 1);
     size_t grp = ((size_t)6 << 30) / per_layer;
     if (grp < 1) grp = 1;
     if (grp > (size_t)c->layers) grp = (size_t)c->layers;
@@ -307,7 +321,8 @@ size_t carve(hbp_ctx* c, char* base, int weight_layers) {
       take_planes(c->Gp, grp, N, d);
       take_planes(c->DZp, grp, N, h);
     }
-    c->H1 = parts ? (char*)c->DZp.p : take(grp * per_layer);
+    c->H1 = parts ? (char*)c->DZp.p : take(grp * N * h * es);
+    if (c->checkpointed) c->ACTg = take(grp * N * h * es);
   }
   if (f.block == HBP_BLOCK_PRELN_TRANSFORMER) {
     const size_t Lb = (size_t)f.L;
@@ -346,7 +361,7 @@ void read_modes(hbp_ctx* c) {
 // in us, split inside / runs / all planes: 400 rows 3010, 7900, 5100 / 1400, 4560, 2180 / 1380, 3890, 2560; 128 rows
 // 3070, 2550, 4400 / 1280, 2190, 1620 / 1290, 1830, 1720.
 int weight_layers_in(hbp_ctx* c, size_t limit) {
-  if (!keeps_parts(c->cfg) || c->force_simt || !c->gemm_pair) return 0;
+  if (!keeps_parts(c) || c->force_simt || !c->gemm_pair) return 0;
   const size_t without = carve(c, nullptr, 0), small = (size_t)64 << 20, half = (size_t)90 << 30;
   size_t most = without + (2 * without > small ? 2 * without : small);
   if (most > half) most = half;
@@ -502,6 +517,10 @@ struct Run {
                     at(g, (int64_t)(b0 + 1) * state), (int64_t)(b1 - b0) * state);
   }
 
+  // The kept Z of layer b on (contexts made by hbp_create_checkpointed).
+  int8_t* z8(int b) const { return c->Z8 + (int64_t)b * N * h; }
+  uint8_t* z8s(int b) const { return c->Z8s + (int64_t)b * N * ((h + 31) / 32); }
+
   // ---- MLP block: u = J^T g for layers [b0, b1) (b1 - b0 <= group), from states g[step+1] -------
   // dA = G W2, dZ = dA * gelu'(Z) -> H1 from layer `slot` on (cached derivative);  dY = dZ W1 -> U[step].
   void mlp_vjp(int b0, int b1, bool want_dy, int slot = 0) {
@@ -516,11 +535,12 @@ struct Run {
     a.M = (int)N; a.N = (int)h; a.K = (int)d; a.batch = nb;
     a.A = upstream(b0); a.a_sm = d; a.a_sk = 1; a.a_sb = ss * state;
     a.B = at(p->W2, (int64_t)b0 * d * h); a.b_sn = 1; a.b_sk = h; a.b_sb = d * h;
-    a.epi = EPI_MUL;
-    a.E = at(c->DACT, (int64_t)b0 * N * h); a.lde = h; a.e_sb = N * h;
+    a.epi = c->checkpointed ? EPI_STORE : EPI_MUL;
+    if (!c->checkpointed) { a.E = at(c->DACT, (int64_t)b0 * N * h); a.lde = h; a.e_sb = N * h; }
     const char* dz = at(c->H1, (int64_t)slot * N * h);
     a.D = const_cast<char*>(dz); a.ldd = h; a.d_sb = N * h;
     run_gemm(a);
+    if (c->checkpointed) checkpoint_gelu_backward(lc, c->cfg.dtype, nb * N, (int)h, z8(b0), z8s(b0), const_cast<char*>(dz));
     if (!want_dy) return;
     GemmArgs b = base_args();
     b.M = (int)N; b.N = (int)d; b.K = (int)h; b.batch = nb;
@@ -536,10 +556,11 @@ struct Run {
   void mlp_wgrad(int b0, int b1, const hbp_grads* gr) {
     if (c->use_parts) return mlp_wgrad_parts(b0, b1, gr);
     const int nb = b1 - b0, ss = step_stride();
+    if (c->checkpointed) checkpoint_gelu_again(lc, c->cfg.dtype, nb * N, (int)h, z8(b0), z8s(b0), c->ACTg);
     GemmArgs a = base_args();
     a.M = (int)d; a.N = (int)h; a.K = (int)N; a.batch = nb;
     a.A = upstream(b0); a.a_sm = 1; a.a_sk = d; a.a_sb = ss * state;
-    a.B = at(c->ACT, (int64_t)b0 * N * h); a.b_sn = 1; a.b_sk = h; a.b_sb = N * h;
+    a.B = c->checkpointed ? c->ACTg : at(c->ACT, (int64_t)b0 * N * h); a.b_sn = 1; a.b_sk = h; a.b_sb = N * h;
     a.epi = EPI_STORE; a.d_f32 = true;
     a.D = gr->dW2 + (int64_t)b0 * d * h; a.ldd = h; a.d_sb = d * h;
     run_gemm(a);
@@ -622,7 +643,7 @@ struct Run {
   // ---- float MLP stacks of few rows (few_rows.cu) -------------------------------------------------
   bool few_rows() const {
     const hbp_config& f = c->cfg;
-    return f.dtype == HBP_F32 && (f.block == HBP_BLOCK_MLP || f.block == HBP_BLOCK_PRELN_MLP) && !lc.force_simt && lc.gemm_pair && !c->use_parts &&
+    return f.dtype == HBP_F32 && (f.block == HBP_BLOCK_MLP || f.block == HBP_BLOCK_PRELN_MLP) && !lc.force_simt && lc.gemm_pair && !c->use_parts && !c->checkpointed &&
            !c->few_refused && few_rows_take(N, f.d, f.hidden);
   }
   FewRows few_rows_args() const {
@@ -1047,26 +1068,31 @@ const char* hbp_status_string(hbp_status s) {
   return "unknown status";
 }
 
-hbp_status hbp_workspace_bytes(const hbp_config* cfg, size_t* bytes) {
+static hbp_status workspace_bytes_of(const hbp_config* cfg, bool checkpointed, size_t* bytes) {
   if (!bytes) return HBP_ERR_INVALID_ARG;
-  hbp_status st = check_config(cfg);
+  hbp_status st = check_config(cfg, checkpointed);
   if (st != HBP_OK) return st;
   hbp_ctx tmp;
   tmp.cfg = *cfg;
+  tmp.checkpointed = checkpointed;
   read_modes(&tmp);
   *bytes = carve(&tmp, nullptr, weight_layers_in(&tmp, SIZE_MAX));
   return HBP_OK;
 }
 
-hbp_status hbp_create(const hbp_config* cfg, void* workspace, size_t workspace_bytes, hbp_ctx** out) {
+hbp_status hbp_workspace_bytes(const hbp_config* cfg, size_t* bytes) { return workspace_bytes_of(cfg, false, bytes); }
+hbp_status hbp_workspace_bytes_checkpointed(const hbp_config* cfg, size_t* bytes) { return workspace_bytes_of(cfg, true, bytes); }
+
+static hbp_status create(const hbp_config* cfg, bool checkpointed, void* workspace, size_t workspace_bytes, hbp_ctx** out) {
   if (!out) return HBP_ERR_INVALID_ARG;
   *out = nullptr;
-  hbp_status st = check_config(cfg);
+  hbp_status st = check_config(cfg, checkpointed);
   if (st != HBP_OK) return st;
   if (!workspace || ((uintptr_t)workspace % kAlign)) return HBP_ERR_WORKSPACE;
   hbp_ctx* c = new (std::nothrow) hbp_ctx;
   if (!c) return HBP_ERR_INVALID_ARG;
   c->cfg = *cfg;
+  c->checkpointed = checkpointed;
   read_modes(c);
   const size_t need = carve(c, (char*)workspace, weight_layers_in(c, workspace_bytes));
   if (workspace_bytes < need) {
@@ -1086,6 +1112,13 @@ hbp_status hbp_create(const hbp_config* cfg, void* workspace, size_t workspace_b
   }
   *out = c;
   return HBP_OK;
+}
+
+hbp_status hbp_create(const hbp_config* cfg, void* workspace, size_t workspace_bytes, hbp_ctx** out) {
+  return create(cfg, false, workspace, workspace_bytes, out);
+}
+hbp_status hbp_create_checkpointed(const hbp_config* cfg, void* workspace, size_t workspace_bytes, hbp_ctx** out) {
+  return create(cfg, true, workspace, workspace_bytes, out);
 }
 
 void hbp_destroy(hbp_ctx* ctx) {
@@ -1130,7 +1163,7 @@ int64_t hbp_launch_count(const hbp_ctx* ctx) { return ctx ? ctx->launches : 0; }
 
 int64_t hbp_form_count(const hbp_ctx* ctx, int32_t form) { return ctx && form >= 0 && form < HBP_FORM_COUNT ? ctx->forms[form] : 0; }
 
-int32_t hbp_context_modes(const hbp_ctx* ctx) { return ctx ? (ctx->force_simt ? 1 : 0) | (ctx->gemm_pair ? 2 : 0) | (ctx->scan_operand ? 4 : 0) : 0; }
+int32_t hbp_context_modes(const hbp_ctx* ctx) { return ctx ? (ctx->force_simt ? 1 : 0) | (ctx->gemm_pair ? 2 : 0) | (ctx->scan_operand ? 4 : 0) | (ctx->checkpointed ? 8 : 0) : 0; }
 
 hbp_status hbp_selftest_gate_math(const double* v, double* out, int64_t n, void* cuda_stream) {
   if (!v || !out) return HBP_ERR_INVALID_ARG;
@@ -1393,13 +1426,15 @@ hbp_status hbp_forward(hbp_ctx* ctx, const hbp_params* params, const void* x0, c
         a.M = (int)N; a.N = (int)h; a.K = (int)d;
         a.A = r.mlp_operand(b); a.a_sm = d; a.a_sk = 1;
         a.B = r.at(params->W1, (int64_t)b * h * d); a.b_sn = d; a.b_sk = 1;
-        a.epi = EPI_GELU_FWD;
-        a.D = r.at(ctx->ACT, (int64_t)b * N * h); a.ldd = h;
-        a.D2 = r.at(ctx->DACT, (int64_t)b * N * h); a.ldd2 = h;
+        char* act = ctx->checkpointed ? ctx->H1 : r.at(ctx->ACT, (int64_t)b * N * h);  // (H1: nothing else is in it yet)
+        a.epi = ctx->checkpointed ? EPI_STORE : EPI_GELU_FWD;
+        a.D = act; a.ldd = h;
+        if (!ctx->checkpointed) { a.D2 = r.at(ctx->DACT, (int64_t)b * N * h); a.ldd2 = h; }
         r.run_gemm(a);
+        if (ctx->checkpointed) checkpoint_gelu(r.lc, f.dtype, N, (int)h, act, r.z8(b), r.z8s(b));
         GemmArgs c2 = r.base_args();
         c2.M = (int)N; c2.N = (int)d; c2.K = (int)h;
-        c2.A = r.at(ctx->ACT, (int64_t)b * N * h); c2.a_sm = h; c2.a_sk = 1;
+        c2.A = act; c2.a_sm = h; c2.a_sk = 1;
         c2.B = r.at(params->W2, (int64_t)b * d * h); c2.b_sn = h; c2.b_sk = 1;
         resid_gemm(c2, step);
       }

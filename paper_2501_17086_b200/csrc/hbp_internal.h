@@ -351,6 +351,11 @@ hbp_status check_rotary_spec(const hbp_rotary_spec* spec, int head_dim);
 void rotary(Launcher& lc, const hbp_rotary_spec& spec, bool inverse, int dtype, int64_t rows, int q_heads, int kv_heads, int head_dim,
             const void* positions, int position_bytes, int64_t first, int64_t period, const hbp_heads& q, const hbp_heads& q_out,
             const hbp_heads& k, const hbp_heads& k_out);
+// GELU from 8-bit checkpoints (checkpoint.cu), rows without gaps, codes of row r and channel c at codes[r * d + c], 8-byte (bf16) or 4-byte aligned:
+// z becomes gelu(z) and is kept; dz, d_act before, becomes d_act * gelu'(z8); act receives gelu(z8).
+void checkpoint_gelu(Launcher& lc, int dtype, int64_t rows, int d, void* z, int8_t* codes, uint8_t* scales);
+void checkpoint_gelu_backward(Launcher& lc, int dtype, int64_t rows, int d, const int8_t* codes, const uint8_t* scales, void* dz);
+void checkpoint_gelu_again(Launcher& lc, int dtype, int64_t rows, int d, const int8_t* codes, const uint8_t* scales, void* act);
 // hbp_attention_forward / _backward (attention_ragged.cu); the arguments have been checked.
 struct RaggedAttn {
   hbp_attention a;
