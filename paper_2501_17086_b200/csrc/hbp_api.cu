@@ -53,12 +53,10 @@ struct hbp_ctx {
   float* rstd = nullptr;   // [steps][N]
   char* ACT = nullptr;     // [layers][N][h] gelu(Z)
   char* DACT = nullptr;    // [layers][N][h] gelu'(Z)
-  // Instead of both, contexts made by hbp_create_checkpointed: Z in 8 bits [layers][N][h] with its scales [layers][N][h / 32 rounded up], and
-  // gelu of what they stand for, of the layers of one group [group][N][h]
+  // Instead of both, contexts made by hbp_create_checkpointed: Z in 8 bits [layers][N][h] with its scales [layers][N][h / 32 rounded up]
   bool checkpointed = false;
   int8_t* Z8 = nullptr;
   uint8_t* Z8s = nullptr;
-  char* ACTg = nullptr;
   float* xres = nullptr;   // [N][d] float master of the residual stream (bf16 only)
   double* hres = nullptr;  // RNN: 2 x [B][d] double master of the recurrent state (ping-pong)
   double* Pd = nullptr;    // tanh RNN: [T][B][d] input projections U x_t in double for the one-launch recurrence
@@ -311,8 +309,7 @@ size_t carve(hbp_ctx* c, char* base, int weight_layers) {
       c->ACT = parts ? (char*)c->ACTp.p : take(layers * N * h * es);
       c->DACT = take(layers * N * h * es);
     }
-    // Gp and DZp, or H1 (and ACTg)
-    const size_t per_layer = parts ? 3 * 2 * N * (plane_cols(d) + plane_cols(h)) : N * h * es * (c->checkpointed ? 2 : 1);
+    const size_t per_layer = parts ? 3 * 2 * N * (plane_cols(d) + plane_cols(h)) : N * h * es;  // Gp and DZp, or H1
     size_t grp = ((size_t)6 << 30) / per_layer;
     if (grp < 1) grp = 1;
     if (grp > (size_t)c->layers) grp = (size_t)c->layers;
@@ -321,8 +318,7 @@ size_t carve(hbp_ctx* c, char* base, int weight_layers) {
       take_planes(c->Gp, grp, N, d);
       take_planes(c->DZp, grp, N, h);
     }
-    c->H1 = parts ? (char*)c->DZp.p : take(grp * N * h * es);
-    if (c->checkpointed) c->ACTg = take(grp * N * h * es);
+    c->H1 = parts ? (char*)c->DZp.p : take(grp * per_layer);
   }
   if (f.block == HBP_BLOCK_PRELN_TRANSFORMER) {
     const size_t Lb = (size_t)f.L;
@@ -556,21 +552,24 @@ struct Run {
   void mlp_wgrad(int b0, int b1, const hbp_grads* gr) {
     if (c->use_parts) return mlp_wgrad_parts(b0, b1, gr);
     const int nb = b1 - b0, ss = step_stride();
-    if (c->checkpointed) checkpoint_gelu_again(lc, c->cfg.dtype, nb * N, (int)h, z8(b0), z8s(b0), c->ACTg);
-    GemmArgs a = base_args();
-    a.M = (int)d; a.N = (int)h; a.K = (int)N; a.batch = nb;
-    a.A = upstream(b0); a.a_sm = 1; a.a_sk = d; a.a_sb = ss * state;
-    a.B = c->checkpointed ? c->ACTg : at(c->ACT, (int64_t)b0 * N * h); a.b_sn = 1; a.b_sk = h; a.b_sb = N * h;
-    a.epi = EPI_STORE; a.d_f32 = true;
-    a.D = gr->dW2 + (int64_t)b0 * d * h; a.ldd = h; a.d_sb = d * h;
-    run_gemm(a);
     GemmArgs b = base_args();
     b.M = (int)h; b.N = (int)d; b.K = (int)N; b.batch = nb;
     b.A = c->H1; b.a_sm = 1; b.a_sk = h; b.a_sb = N * h;
     b.B = mlp_operand(b0); b.b_sn = 1; b.b_sk = d; b.b_sb = ss * state;
     b.epi = EPI_STORE; b.d_f32 = true;
     b.D = gr->dW1 + (int64_t)b0 * h * d; b.ldd = d; b.d_sb = h * d;
+    GemmArgs a = base_args();
+    a.M = (int)d; a.N = (int)h; a.K = (int)N; a.batch = nb;
+    a.A = upstream(b0); a.a_sm = 1; a.a_sk = d; a.a_sb = ss * state;
+    a.B = c->checkpointed ? c->H1 : at(c->ACT, (int64_t)b0 * N * h); a.b_sn = 1; a.b_sk = h; a.b_sb = N * h;
+    a.epi = EPI_STORE; a.d_f32 = true;
+    a.D = gr->dW2 + (int64_t)b0 * d * h; a.ldd = h; a.d_sb = d * h;
+    if (!c->checkpointed) run_gemm(a);
     run_gemm(b);
+    if (c->checkpointed) {  // dZ has been used: its place takes gelu of what was kept of Z
+      checkpoint_gelu_again(lc, c->cfg.dtype, nb * N, (int)h, z8(b0), z8s(b0), c->H1);
+      run_gemm(a);
+    }
   }
 
   // Turns the queries and keys (back: their gradients, by the opposite angles) of nb layers' [N][3d] buffer in place.
