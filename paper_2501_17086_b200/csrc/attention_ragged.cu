@@ -20,6 +20,8 @@
 
 namespace hbp {
 
+namespace cg = cooperative_groups;
+
 namespace {
 
 constexpr int TILE = 64, THREADS = 256;
@@ -116,32 +118,61 @@ __device__ __forceinline__ void store_rows(float* __restrict__ base, int64_t row
   }
 }
 
+// Leaves a block's sums in its shared memory, rows LD floats apart.
+template <int HD>
+__device__ __forceinline__ void leave_rows(float* __restrict__ dst, int ty, int tx, const float (&acc)[4][HD / 16]) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int v = 0; v < HD / 64; ++v)
+      *reinterpret_cast<float4*>(dst + (ty * 4 + r) * kStride<HD> + (tx + 16 * v) * 4) =
+          make_float4(acc[r][4 * v], acc[r][4 * v + 1], acc[r][4 * v + 2], acc[r][4 * v + 3]);
+}
+// What all blocks of a cluster have left at `mine` (an address in this block's shared memory), added up in the blocks' order, each times
+// weight(block).
+template <typename W>
+__device__ __forceinline__ float4 gather(cg::cluster_group& cluster, float* mine, int ranks, W weight) {
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int b = 0; b < ranks; ++b) {
+    const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(mine, b));
+    const float w = weight(b);
+    s.x = fmaf(w, x.x, s.x); s.y = fmaf(w, x.y, s.y); s.z = fmaf(w, x.z, s.z); s.w = fmaf(w, x.w, s.w);
+  }
+  return s;
+}
+
+// Few blocks with long walks leave most of the chip idle.  Then the tiles of a walk are dealt out to the `ranks` blocks of a cluster; each leaves its
+// sums in its shared memory, and each puts together those of all for its share of the rows, in the blocks' order (kRanks below).
+
 // ------------------------------------------------------------------------------------------- forward
 template <int HD>
-__global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_constant__ RaggedAttn p) {
+__global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_constant__ RaggedAttn p, const int ranks) {
   extern __shared__ float4 smem4[];
   constexpr int LD = kStride<HD>;
   float* sQ = reinterpret_cast<float*>(smem4);
   float* sKV = sQ + TILE * LD;  // two stages of a key and a value tile: the next ones come while these are used
   float* sPt = sKV + 4 * TILE * LD;  // [key][query]
+  chain_wait();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const BlockOf w = block_of(p.a.q_len, TILE, p.a.q_heads, true);
+  const int rank = (int)(blockIdx.x % ranks);
+  const BlockOf w = block_at(blockIdx.x / ranks, p.a.q_len, TILE, p.a.q_heads, true);
   const SeqPair sq = sequence_pair(p.a, w.b);
   const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
-  if (q0 >= sq.nq) return;
+  if (q0 >= sq.nq) return;  // (all blocks of the cluster)
   const float* q = (const float*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride;
   const float* k = (const float*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
   const float* v = (const float*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;  // query i sees keys 0 .. i + shift (capped by nk)
   const int seen = min(sq.nk, p.a.causal ? min(q0 + TILE, sq.nq) + shift : sq.nk);
+  const int step = ranks * TILE;
+  auto stage = [&](int k0) { return sKV + (k0 / step & 1) * 2 * TILE * LD; };
   auto ask = [&](int k0) {
-    float* t = sKV + (k0 / TILE & 1) * 2 * TILE * LD;
-    ask_tile<HD>(t, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
-    ask_tile<HD>(t + TILE * LD, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+    ask_tile<HD>(stage(k0), k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    ask_tile<HD>(stage(k0) + TILE * LD, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
   };
-  if (seen > 0) {
+  if (rank * TILE < seen) {
     ask_tile<HD>(sQ, q, p.q.row_stride, q0, sq.nq, p.a.head_dim);
-    ask(0);
+    ask(rank * TILE);
   }
   asked();
   float acc[4][HD / 16], m[4], l[4];
@@ -152,12 +183,12 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
 #pragma unroll
     for (int e = 0; e < HD / 16; ++e) acc[r][e] = 0.0f;
   }
-  for (int k0 = 0; k0 < seen; k0 += TILE) {
-    if (k0 + TILE < seen) ask(k0 + TILE);
+  for (int k0 = rank * TILE; k0 < seen; k0 += step) {
+    if (k0 + step < seen) ask(k0 + step);
     asked();
     wait_asked<1>();
     __syncthreads();
-    const float *sK = sKV + (k0 / TILE & 1) * 2 * TILE * LD, *sV = sK + TILE * LD;
+    const float *sK = stage(k0), *sV = sK + TILE * LD;
     float s[4][4];
     score_tile<HD>(sQ, sK, ty, tx, s);
 #pragma unroll
@@ -192,16 +223,46 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
     __syncthreads();
   }
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
+  for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
-    const float inv = l[r] > 0.0f ? 1.0f / l[r] : l[r];  // nothing seen: zeros (a sum that is NaN stays NaN)
+  float* lse = p.lse + w.h * p.a.q_rows + sq.q0 + q0;
+  float* out = (float*)p.o.x + sq.q0 * p.o.row_stride + w.h * p.o.head_stride;
+  // nothing seen: zeros and -infinity (a sum that is NaN stays NaN)
+  auto inverse = [](float sum) { return sum > 0.0f ? 1.0f / sum : sum; };
+  if (ranks == 1) {
 #pragma unroll
-    for (int e = 0; e < HD / 16; ++e) acc[r][e] *= inv;
-    const int row = q0 + ty * 4 + r;
-    if (tx == 0 && row < sq.nq) p.lse[w.h * p.a.q_rows + sq.q0 + row] = l[r] == 0.0f ? -INFINITY : m[r] + logf(l[r]);
+    for (int r = 0; r < 4; ++r) {
+      const float inv = inverse(l[r]);
+#pragma unroll
+      for (int e = 0; e < HD / 16; ++e) acc[r][e] *= inv;
+      if (tx == 0 && q0 + ty * 4 + r < sq.nq) lse[ty * 4 + r] = l[r] == 0.0f ? -INFINITY : m[r] + logf(l[r]);
+    }
+    store_rows<HD>(out, p.o.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, 1.0f, acc);
+    return;
   }
-  store_rows<HD>((float*)p.o.x + sq.q0 * p.o.row_stride + w.h * p.o.head_stride, p.o.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, 1.0f, acc);
+  leave_rows<HD>(sKV, ty, tx, acc);  // (the last tile has been used by all)
+  float2* sML = reinterpret_cast<float2*>(sPt);
+  if (tx == 0) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) sML[ty * 4 + r] = make_float2(m[r], l[r]);
+  }
+  cg::cluster_group cluster = cg::this_cluster();
+  cluster.sync();
+  constexpr int VECS = HD / 4;
+  for (int i = rank * THREADS + threadIdx.x; i < TILE * VECS; i += ranks * THREADS) {
+    const int r = i / VECS, c = i % VECS * 4;
+    if (q0 + r >= sq.nq || c >= p.a.head_dim) continue;
+    float top = -INFINITY, sum = 0.0f;
+    for (int b = 0; b < ranks; ++b) top = fmaxf(top, cluster.map_shared_rank(sML + r, b)->x);
+    auto weight = [&](int b) { return top == -INFINITY ? 1.0f : expf(cluster.map_shared_rank(sML + r, b)->x - top); };
+    for (int b = 0; b < ranks; ++b) sum = fmaf(weight(b), cluster.map_shared_rank(sML + r, b)->y, sum);
+    const float4 o = gather(cluster, sKV + r * LD + c, ranks, weight);
+    const float inv = inverse(sum);
+    *reinterpret_cast<float4*>(out + (int64_t)(q0 + r) * p.o.row_stride + c) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (c == 0) lse[r] = sum == 0.0f ? -INFINITY : top + logf(sum);
+  }
+  cluster.sync();  // (no block ends while another reads its shared memory)
 }
 
 // ------------------------------------------------------------------------------------------- backward
@@ -249,10 +310,10 @@ __device__ __forceinline__ void ragged_dq(const RaggedAttn& p, const BlockOf w) 
   const float* v = (const float*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
   const int seen = min(sq.nk, p.a.causal ? min(q0 + TILE, sq.nq) + shift : sq.nk);
+  auto stage = [&](int k0) { return sKV + (k0 / TILE & 1) * 2 * TILE * LD; };
   auto ask = [&](int k0) {
-    float* t = sKV + (k0 / TILE & 1) * 2 * TILE * LD;
-    ask_tile<HD>(t, k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
-    ask_tile<HD>(t + TILE * LD, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
+    ask_tile<HD>(stage(k0), k, p.k.row_stride, k0, sq.nk, p.a.head_dim);
+    ask_tile<HD>(stage(k0) + TILE * LD, v, p.v.row_stride, k0, sq.nk, p.a.head_dim);
   };
   if (seen > 0) {
     ask_tile<HD>(sQ, (const float*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride, p.q.row_stride, q0, sq.nq, p.a.head_dim);
@@ -267,7 +328,7 @@ __device__ __forceinline__ void ragged_dq(const RaggedAttn& p, const BlockOf w) 
     asked();
     wait_asked<1>();
     __syncthreads();
-    const float *sK = sKV + (k0 / TILE & 1) * 2 * TILE * LD, *sV = sK + TILE * LD;
+    const float *sK = stage(k0), *sV = sK + TILE * LD;
     float pr[4][4], ds[4][4];
     probabilities<HD>(sQ, sK, sG, sV, ty, tx, q0, k0, sq, p, shift, lse, dd, pr, ds);
 #pragma unroll
@@ -280,11 +341,8 @@ __device__ __forceinline__ void ragged_dq(const RaggedAttn& p, const BlockOf w) 
   store_rows<HD>((float*)p.dq.x + sq.q0 * p.dq.row_stride + w.h * p.dq.head_stride, p.dq.row_stride, q0, sq.nq, p.a.head_dim, ty, tx, p.a.scale, acc);
 }
 
-// The query heads of a group are shared out over the blocks of a cluster: of one head's rows alone the chain of tiles is as long as dq's, and
-// a key head's blocks are few.  Each block leaves its sums in its shared memory, and each adds up those of all for its share of
-// the rows, in the blocks' order.
 template <int HD>
-__device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w, int rank, int ranks) {
+__device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w, const int rank, const int ranks) {
   extern __shared__ float4 smem4[];
   constexpr int LD = kStride<HD>;
   float* sK = reinterpret_cast<float*>(smem4);
@@ -299,32 +357,30 @@ __device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w,
   if (k0 >= sq.nk) return;  // (all blocks of the cluster)
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
   const int first = p.a.causal ? max(0, k0 - shift) / TILE * TILE : 0;  // the first block of queries that sees key k0
-  // the tiles of queries of this block's heads, one after the other
-  const int tiles = max(0, (sq.nq + TILE - 1) / TILE - first / TILE), heads = (group - rank + ranks - 1) / ranks;
-  int ask_h = w.h * group + rank, ask_q = first;
+  // the tiles of queries of all heads of the group, one head after the other
+  const int tiles = max(0, (sq.nq + TILE - 1) / TILE - first / TILE), total = tiles * group;
   auto ask = [&](int it) {
-    float* t = sQG + (it & 1) * 2 * TILE * LD;
-    ask_tile<HD>(t, (const float*)p.q.x + sq.q0 * p.q.row_stride + ask_h * p.q.head_stride, p.q.row_stride, ask_q, sq.nq, p.a.head_dim);
-    ask_tile<HD>(t + TILE * LD, (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + ask_h * p.d_o.head_stride, p.d_o.row_stride, ask_q, sq.nq, p.a.head_dim);
-    ask_q += TILE;
-    if (ask_q >= sq.nq) { ask_q = first; ask_h += ranks; }
+    float* t = sQG + (it / ranks & 1) * 2 * TILE * LD;
+    const int h = w.h * group + it / tiles, q0 = first + it % tiles * TILE;
+    ask_tile<HD>(t, (const float*)p.q.x + sq.q0 * p.q.row_stride + h * p.q.head_stride, p.q.row_stride, q0, sq.nq, p.a.head_dim);
+    ask_tile<HD>(t + TILE * LD, (const float*)p.d_o.x + sq.q0 * p.d_o.row_stride + h * p.d_o.head_stride, p.d_o.row_stride, q0, sq.nq, p.a.head_dim);
   };
-  if (tiles > 0) {
+  if (rank < total) {
     ask_tile<HD>(sK, (const float*)p.k.x + sq.k0 * p.k.row_stride + w.h * p.k.head_stride, p.k.row_stride, k0, sq.nk, p.a.head_dim);
     ask_tile<HD>(sV, (const float*)p.v.x + sq.k0 * p.v.row_stride + w.h * p.v.head_stride, p.v.row_stride, k0, sq.nk, p.a.head_dim);
-    ask(0);
+    ask(rank);
   }
   asked();
   float dk[4][HD / 16] = {}, dv[4][HD / 16] = {};
-  int h = w.h * group + rank, q0 = first;
-  for (int it = 0; it < tiles * heads; ++it) {
-    if (it + 1 < tiles * heads) ask(it + 1);
+  for (int it = rank; it < total; it += ranks) {
+    if (it + ranks < total) ask(it + ranks);
     asked();
+    const int h = w.h * group + it / tiles, q0 = first + it % tiles * TILE;
     float lse[4], dd[4];
     row_statistics(p, sq, h, q0, ty, lse, dd);
     wait_asked<1>();
     __syncthreads();
-    const float *sQ = sQG + (it & 1) * 2 * TILE * LD, *sG = sQ + TILE * LD;
+    const float *sQ = sQG + (it / ranks & 1) * 2 * TILE * LD, *sG = sQ + TILE * LD;
     float pr[4][4], ds[4][4];
     probabilities<HD>(sQ, sK, sG, sV, ty, tx, q0, k0, sq, p, shift, lse, dd, pr, ds);
     auto put = [&](float* dst, const float (&x)[4][4]) {
@@ -344,8 +400,6 @@ __device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w,
     }
     add_product<HD>(sS, sQ, ty, tx, dk);
     __syncthreads();
-    q0 += TILE;
-    if (q0 >= sq.nq) { q0 = first; h += ranks; }
   }
   float* dk_base = (float*)p.dk.x + sq.k0 * p.dk.row_stride + w.h * p.dk.head_stride;
   float* dv_base = (float*)p.dv.x + sq.k0 * p.dv.row_stride + w.h * p.dv.head_stride;
@@ -354,40 +408,29 @@ __device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w,
     store_rows<HD>(dv_base, p.dv.row_stride, k0, sq.nk, p.a.head_dim, ty, tx, 1.0f, dv);
     return;
   }
-  __syncthreads();  // (this block's tiles have been read)
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-#pragma unroll
-    for (int v = 0; v < HD / 64; ++v) {
-      const int at = (ty * 4 + r) * LD + (tx + 16 * v) * 4;
-      *reinterpret_cast<float4*>(sK + at) = make_float4(dk[r][4 * v], dk[r][4 * v + 1], dk[r][4 * v + 2], dk[r][4 * v + 3]);
-      *reinterpret_cast<float4*>(sV + at) = make_float4(dv[r][4 * v], dv[r][4 * v + 1], dv[r][4 * v + 2], dv[r][4 * v + 3]);
-    }
-  cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  __syncthreads();  // (a block without tiles of its own asked for nothing; the others' keys have been used by all)
+  leave_rows<HD>(sK, ty, tx, dk);
+  leave_rows<HD>(sV, ty, tx, dv);
+  cg::cluster_group cluster = cg::this_cluster();
   cluster.sync();
   constexpr int VECS = HD / 4;
   for (int i = rank * THREADS + threadIdx.x; i < 2 * TILE * VECS; i += ranks * THREADS) {
     const int which = i / (TILE * VECS), r = i / VECS % TILE, c = i % VECS * 4;
     if (k0 + r >= sq.nk || c >= p.a.head_dim) continue;
-    float* mine = (which ? sV : sK) + r * LD + c;
-    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int b = 0; b < ranks; ++b) {
-      const float4 x = *reinterpret_cast<const float4*>(cluster.map_shared_rank(mine, b));
-      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
-    }
     const float mul = which ? 1.0f : p.a.scale;
-    *reinterpret_cast<float4*>((which ? dv_base + (int64_t)(k0 + r) * p.dv.row_stride : dk_base + (int64_t)(k0 + r) * p.dk.row_stride) + c) =
-        make_float4(mul * s.x, mul * s.y, mul * s.z, mul * s.w);
+    const float4 x = gather(cluster, (which ? sV : sK) + r * LD + c, ranks, [&](int) { return mul; });
+    *reinterpret_cast<float4*>((which ? dv_base + (int64_t)(k0 + r) * p.dv.row_stride : dk_base + (int64_t)(k0 + r) * p.dk.row_stride) + c) = x;
   }
   cluster.sync();  // (no block ends while another reads its shared memory)
 }
 
-// dk, dv and dq in one launch, in clusters of `ranks` blocks: a key block's, or one query block of as many heads.
+// dk, dv and dq in one launch: clusters of `ranks` blocks for the former; a block of dq's clusters works by itself.
 template <int HD>
-__global__ void __launch_bounds__(THREADS) ragged_bwd_kernel(const __grid_constant__ RaggedAttn p, const unsigned kv_blocks, const int ranks) {
+__global__ void __launch_bounds__(THREADS) ragged_bwd_kernel(const __grid_constant__ RaggedAttn p, const unsigned kv_walks, const unsigned q_walks, const int ranks) {
   chain_wait();  // (D comes from the launch before)
+  const unsigned kv_blocks = kv_walks * ranks;
   if (blockIdx.x < kv_blocks) ragged_dkv<HD>(p, block_at(blockIdx.x / ranks, p.a.kv_len, TILE, p.a.kv_heads, false), (int)(blockIdx.x % ranks), ranks);
-  else ragged_dq<HD>(p, block_at(blockIdx.x - kv_blocks, p.a.q_len, TILE, p.a.q_heads, true));
+  else if (blockIdx.x - kv_blocks < q_walks) ragged_dq<HD>(p, block_at(blockIdx.x - kv_blocks, p.a.q_len, TILE, p.a.q_heads, true));
 }
 
 // drow[h][row] = sum over channels of d_o * o, `lanes` (a power of two, 16 bytes each) to a row of a head; neighbouring lanes take neighbouring
@@ -425,23 +468,32 @@ void allow_smem(Launcher& lc, K kernel, int smem, bool& done) {
   if (!done && lc.err == cudaSuccess) lc.err = e;
 }
 
+// Blocks that share each of `walks` walks of `tiles` tiles: twice as many for as long as blocks are fewer than the chip takes at a time and every
+// block has a tile.  RANKS
+int ranks_of(int64_t walks, int64_t at_a_time, int64_t tiles) {
+  int r = 1;
+  while (r < 8 && walks * r < at_a_time && 2 * r <= tiles) r *= 2;
+  return r;
+}
+
 template <int HD>
 void forward_f32(Launcher& lc, const RaggedAttn& r) {
+  constexpr int kSmem = smem_of<HD>(5, 1);
   static PerDevice<bool> set;
-  allow_smem(lc, ragged_fwd_kernel<HD>, smem_of<HD>(5, 1), set.here());
-  ragged_fwd_kernel<HD><<<(unsigned)blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences), THREADS, smem_of<HD>(5, 1), lc.stream>>>(r);
-  lc.count();
-  lc.check();
+  allow_smem(lc, ragged_fwd_kernel<HD>, kSmem, set.here());
+  const int64_t blocks = blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences);
+  const int ranks = ranks_of(blocks, HD == 64 ? 2 * 148 : 148, (r.a.kv_len + TILE - 1) / TILE);
+  launch_chained(lc, ragged_fwd_kernel<HD>, dim3((unsigned)(blocks * ranks)), THREADS, kSmem, ranks, r, ranks);
 }
 template <int HD>
 void backward_f32(Launcher& lc, const RaggedAttn& r) {
-  int ranks = 8;
-  while ((r.a.q_heads / r.a.kv_heads) % ranks) --ranks;
-  const int64_t kv = blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences) * ranks, q = blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences);
   constexpr int kSmem = smem_of<HD>(6, HD > 64 ? 1 : 2);
   static PerDevice<bool> set;
   allow_smem(lc, ragged_bwd_kernel<HD>, kSmem, set.here());
-  launch_chained(lc, ragged_bwd_kernel<HD>, dim3((unsigned)(kv + q)), THREADS, kSmem, ranks, r, (unsigned)kv, ranks);
+  const int64_t kv = blocks_of(r.a.kv_len, TILE, r.a.kv_heads, r.a.sequences), q = blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences);
+  const int ranks = ranks_of(kv, 148, (int64_t)(r.a.q_heads / r.a.kv_heads) * ((r.a.q_len + TILE - 1) / TILE));
+  const int64_t blocks = (kv + (q + ranks - 1) / ranks) * ranks;
+  if (blocks) launch_chained(lc, ragged_bwd_kernel<HD>, dim3((unsigned)blocks), THREADS, kSmem, ranks, r, (unsigned)kv, (unsigned)q, ranks);
 }
 
 void row_dots(Launcher& lc, const RaggedAttn& r) {
@@ -468,7 +520,7 @@ hbp_status check_attention(const hbp_attention* a) {
   if (!std::isfinite(a->scale)) return HBP_ERR_INVALID_ARG;
   if (((uintptr_t)a->q_offsets | (uintptr_t)a->kv_offsets | (uintptr_t)a->status) & 3u) return HBP_ERR_SHAPE;
   // (as many blocks of 64 rows as one grid holds)
-  if (blocks_of(a->q_len, TILE, a->q_heads, a->sequences) > INT32_MAX / 2 || blocks_of(a->kv_len, TILE, a->q_heads, a->sequences) > INT32_MAX / 2 ||
+  if (blocks_of(a->q_len, TILE, a->q_heads, a->sequences) > INT32_MAX / 2 || blocks_of(a->kv_len, TILE, a->kv_heads, a->sequences) > INT32_MAX / 2 ||
       a->q_rows * a->q_heads > (int64_t)INT32_MAX * 8)
     return HBP_ERR_SHAPE;
   return HBP_OK;
