@@ -10,17 +10,26 @@
 // the scores came from and are the A operand of the next product there: they never pass through shared memory, whose bandwidth
 // the products need (M = 128, N = 64, K = 16 reads 6 KB in the 32 clocks that it takes at the tensor cores' rate).
 //
-// Forward: a block owns 128 queries and walks over tiles of 128 keys with a running maximum and sum, one row per thread of four
-// warps.  The output stays in tensor memory; it is scaled down only when a row's maximum has grown by more than 2^8
-// since the last time, which is rare (sums are float: 2^8 costs no precision).  Two blocks share an SM, so that the exponentials of
-// one run under the products of the other.
+// Forward: a block owns 128 queries and walks over tiles of 64 keys with a running maximum and sum, one row per thread of four
+// warps.  Two buffers of scores, so that the next ones are formed under these exponentials.  The output stays in tensor memory; it is scaled
+// down only when a row's maximum has grown by more than 2^8 since the last time, which is rare (sums are float: 2^8 costs no
+// precision).  Two blocks share an SM.  2 x 4096 rows, causal: 16 heads of 128 134 us (1.03 PFLOP/s of the products that are needed), 16 of 64 113 us
+// (0.61).  Bound, at 64 channels, by the exponentials (512 clocks a tile and SM for 128 x 64 at 16 a clock; measured 670 in the loop), at 128
+// by what the products read from shared memory.  Tiles of 128 keys in one buffer: 150 and 132 us, the scores read twice from tensor memory 176
+// and 161.
 //
 // Backward: two kinds of block in one launch, so that every output has one owner and one order of its sums:
 //   dK, dV   128 keys of a key head; walks over tiles of 64 queries of all query heads of its group
 //            S^T = K Q^T, dP^T = V dO^T;  P^T = exp(S^T - lse), dS^T = P^T (dP^T - D);  dV += P^T dO, dK += dS^T Q
 //   dQ       128 queries; walks over tiles of 64 keys:  S = Q K^T, dP = dO V^T;  dQ += dS K
-// That is seven products where five would do with sums in memory that blocks add to in no fixed order.  HD = 128 takes all of tensor memory:
-// two buffers of scores, whose products run one tile ahead of the softmax warps; HD = 64 runs two blocks an SM instead.
+// That is seven products where five would do with sums in memory that blocks add to in no fixed order.  Probabilities and dS are rounded to
+// bf16 as operands, and so is o, which D comes from: gradients are off by 2.4e-3 to 2.6e-3 in the norm, 1.7e-3 of it the output's own
+// rounding.  HD = 128 takes all of tensor memory: two buffers of scores, two groups of softmax warps that take the tiles in turn; HD = 64 runs
+// two blocks an SM, a buffer each, and overlaps the two halves of a tile (scores and probabilities, dP and dS) instead.  2 x 4096 rows, causal, of the
+// five products that are needed: 16 heads of 128 443 us (0.78 PFLOP/s), 16 of 64 295 us (0.59).  At 128 channels the products and the
+// copies read and write 1400 (dK, dV) and 1150 (dQ) clocks' worth of shared memory a tile, of 1670 and 1420 measured; at 64 a tile's chain of
+// product, exponentials and product bounds it (2100 and 1630 clocks, two at a time).  HD = 64 with three buffers and one block an SM: 366 us; sixteen
+// columns a warp instead of 32: 308.
 // All waits are bounded.
 #include "attention_ragged.cuh"
 #include "float_pairs.cuh"
@@ -146,7 +155,7 @@ __device__ __forceinline__ void store_staged(uint32_t tile, int row0, int unit0,
 constexpr int FWD_THREADS = 192;  // warp 0 copies, warp 1 issues the products, warps 2..5 softmax (TMEM lane quarter = warp & 3)
 template <int HD>
 struct Fwd {
-  static constexpr int kStages = HD == 64 ? 3 : 2;  // of keys, and of values
+  static constexpr int kStages = HD == 64 ? 3 : 2;  // of keys, and of values (as many as two blocks an SM have room for)
   static constexpr int kBig = BIG * HD * 2, kSmall = SMALL * HD * 2;
   static constexpr int kSmem = kBig + 2 * kStages * kSmall + 256 + 1024;
 };
