@@ -1,4 +1,4 @@
-"""ctypes binding over libhbp.so: argument marshalling only.
+"""Binding over libhbp.so (ctypes; the short calls through an extension module): argument marshalling only.
 
 torch is used for device memory and streams; every step of the path runs in
 the library's CUDA kernels.  Importing this module without a built
@@ -8,8 +8,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
-import threading
 
 import torch
 
@@ -70,12 +68,11 @@ class hbp_attention(C.Structure):
 
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "by_parts": 2}
-CHECKPOINT_GROUP = 32
 
 
 def _load():
-    if not os.path.exists(LIB_PATH):
-        raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2501_17086_b200.build` "
+    if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_calls.so")):
+        raise ImportError(f"{LIB_PATH} or _calls.so beside it is missing: build it with `python -m paper_2501_17086_b200.build` "
                           "(the library has no fallback path)")
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
@@ -101,7 +98,7 @@ def _load():
     lib.hbp_param_grads.argtypes = [vp, C.POINTER(hbp_params), vp, vp, vp, C.POINTER(hbp_grads), vp]
     lib.hbp_compare_scratch_bytes.argtypes = [i32]
     lib.hbp_compare.argtypes = [i32, i32, i64, vp, vp, vp, vp, sz, vp]
-    heads = vp  # (addresses of packed structures)
+    heads = vp
     lib.hbp_rotary.argtypes = [vp, i32, i32, i64, i32, i32, i32, vp, i32, i64, i64, heads, heads, heads, heads, vp]
     lib.hbp_context_rotary.argtypes = [vp, C.POINTER(hbp_rotary_spec), i64]
     lib.hbp_attention_forward.argtypes = [vp, heads, heads, heads, heads, vp, vp]
@@ -131,6 +128,10 @@ def _load():
 
 
 lib = _load()
+
+from . import _calls  # noqa: E402 (needs the library above; no fallback here either)
+
+_calls.set_error(HbpError)
 
 
 def status_string(code: int) -> str:
@@ -417,79 +418,20 @@ def compare(a, b, segments=1):
 
 
 # ---- a decoder's step on its own: rotary positions, attention over ragged batches, activations in 8 bits --------------------
-# These calls are short (a launch or two of some microseconds), so what Python does around them counts: structures are packed into a buffer
-# of the calling thread instead of being made anew (rotary positions of one token: 26 us a call with a ctypes structure
-# for each tensor, 14 so), and the stream's handle is asked for without an object around it.
-class _Packed(threading.local):
-    def __init__(self):
-        self.buf = C.create_string_buffer(512)
-        self.at = C.addressof(self.buf)
-
-
-_packed = _Packed()
-_ROTARY = struct.Struct("3i6f4x12q")        # hbp_rotary_spec, then four hbp_heads
-_ATTENTION = struct.Struct("8i2q2qf4xq")    # hbp_attention
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch.cuda.current_device
-
-
-def _refused(code, name, what):
-    raise HbpError(code, f"{name}: {what}")
-
-
-def _on(name, first, *others):
-    """The stream to launch on: the current one of the current device, which has to be every tensor's."""
-    at = first.get_device()
-    for t in others:
-        if t is not None and t.get_device() != at:
-            _refused(1, name, "the tensors are on different devices")
-    if at < 0 or at != _current_device():
-        _refused(1, name, f"a tensor is on {first.device}, which is not the current device")
-    return _raw_stream(at)
-
-
-def _code(t, name):
-    dt = t.dtype
-    if dt is torch.bfloat16:
-        return HBP_BF16
-    if dt is torch.float32:
-        return HBP_F32
-    _refused(3, name, f"dtype {dt}")
-
-
-def _heads(t, name):
-    """Pointer and strides (elements) of a tensor [rows, heads, head_dim] whose channels are contiguous."""
-    st = t.stride()
-    if len(st) != 3:
-        _refused(2, name, "wanted [rows, heads, head_dim]")
-    rs, hs, cs = st
-    rows, heads, width = t.shape
-    if cs != 1 and width != 1:
-        _refused(2, name, "the channels are not contiguous")
-    return t.data_ptr(), rs if rows > 1 else 0, hs if heads > 1 else 0  # (a dimension of one element has any stride)
-
-
-def _matrix(t, name):
-    st = t.stride()
-    if len(st) != 2 or (st[1] != 1 and t.shape[1] != 1):
-        _refused(2, name, "wanted [rows, channels] with contiguous channels")
-    # (a single row has no stride of its own)
-    return t.data_ptr(), st[0] if t.shape[0] > 1 else t.shape[1]
-
-
-def _alike(t, like, name, what):
-    if t.shape != like.shape or t.dtype != like.dtype:
-        _refused(2, name, what)
-
-
-_NONE = (0, 0, 0)
-
-
+# These calls are a launch or two of some microseconds; what is around them - checks, new outputs, pointers, the stream - is done by the
+# extension module built beside the library (csrc/calls.cpp).  Tensors are those of the current device; work goes to its current
+# stream.
 def rotary_spec(rotary_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained_length=0.0, fast=32.0, slow=1.0,
                 amplitude=1.0) -> hbp_rotary_spec:
-    if layout not in ROTARY_LAYOUTS or scaling not in ROTARY_SCALINGS:
-        _refused(6, "rotary", f"layout {layout!r}, scaling {scaling!r}")
-    return hbp_rotary_spec(ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], rotary_dim, base, factor, trained_length, fast, slow, amplitude)
+    return hbp_rotary_spec(_choice(ROTARY_LAYOUTS, layout), _choice(ROTARY_SCALINGS, scaling), rotary_dim, base, factor, trained_length, fast,
+                           slow, amplitude)
+
+
+def _choice(table, name):
+    try:
+        return table[name]
+    except (KeyError, TypeError):
+        raise HbpError(6, f"rotary: {name!r} is none of {', '.join(table)}") from None
 
 
 def rotary(q, k=None, positions=None, first=0, period=0, rotary_dim=None, base=10000.0, layout="half", scaling="none", factor=1.0,
@@ -497,133 +439,24 @@ def rotary(q, k=None, positions=None, first=0, period=0, rotary_dim=None, base=1
     """Rotary positions on q [rows, heads, head_dim] and, in the same launch, k [rows, kv_heads, head_dim]: see hbp_rotary.
     Returns (q_out, k_out), new tensors unless given (they may be q and k themselves); ``inverse`` is the gradient.
     ``positions``: int32 or int64 [rows] on the device, or None for first + row % period (period 0: first + row)."""
-    if layout not in ROTARY_LAYOUTS or scaling not in ROTARY_SCALINGS:
-        _refused(6, "rotary", f"layout {layout!r}, scaling {scaling!r}")
-    qh = _heads(q, "rotary q")
-    rows, q_heads, head_dim = q.shape
-    if q_out is None:
-        q_out = torch.empty_like(q)
-    else:
-        _alike(q_out, q, "rotary", "q_out is not like q")
-    kv_heads, kh, ko = 0, _NONE, _NONE
-    if k is not None:
-        kh = _heads(k, "rotary k")
-        k_rows, kv_heads, k_dim = k.shape
-        if k_rows != rows or k_dim != head_dim or k.dtype is not q.dtype:
-            _refused(2, "rotary", "k is not like q")
-        if k_out is None:
-            k_out = torch.empty_like(k)
-        else:
-            _alike(k_out, k, "rotary", "k_out is not like k")
-        ko = _heads(k_out, "rotary k_out")
-    stream = _on("rotary", q, k, positions, q_out, k_out)
-    at, size = None, 0
-    if positions is not None:
-        size = 4 if positions.dtype is torch.int32 else 8 if positions.dtype is torch.int64 else 0
-        if not size or positions.shape != (rows,) or not positions.is_contiguous():
-            _refused(2, "rotary", "positions: wanted int32 or int64 [rows]")
-        at = positions.data_ptr()
-    p = _packed
-    _ROTARY.pack_into(p.buf, 0, ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling], head_dim if rotary_dim is None else rotary_dim, base, factor,
-                      trained_length, fast, slow, amplitude, *qh, *_heads(q_out, "rotary q_out"), *kh, *ko)
-    h = p.at + 40
-    _check(lib.hbp_rotary(p.at, inverse, _code(q, "rotary"), rows, q_heads, kv_heads, head_dim, at, size, first, period, h, h + 24, h + 48, h + 72,
-                          stream), "hbp_rotary")
-    return q_out, k_out
-
-
-def _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status):
-    """Packs the hbp_attention."""
-    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:
-        _refused(2, name, "q, k and v do not belong together")
-    if k.dtype != q.dtype or v.dtype != q.dtype:
-        _refused(2, name, "q, k and v differ in type")
-    at = [0, 0]
-    for i, off in enumerate((q_offsets, kv_offsets)):
-        if off is None:
-            continue
-        if off.dim() != 1 or not off.is_contiguous() or off.dtype is not torch.int32 or off.numel() < 1:
-            _refused(2, name, "offsets: wanted int32 [sequences + 1]")
-        if sequences is not None and sequences != off.numel() - 1:
-            _refused(2, name, "offsets of another number of sequences")
-        sequences = off.numel() - 1
-        at[i] = off.data_ptr()
-    if sequences is None:
-        sequences = 1
-    q_rows, q_heads, head_dim = q.shape
-    kv_rows, kv_heads, _ = k.shape
-    if q_len is None:
-        if at[0]:
-            _refused(2, name, "q_len, the longest of the sequences, has to be given with q_offsets")
-        q_len = q_rows // sequences if sequences else 0
-    if kv_len is None:
-        if at[1]:
-            _refused(2, name, "kv_len, the longest of the sequences, has to be given with kv_offsets")
-        kv_len = kv_rows // sequences if sequences else 0
-    if status is not None and (status.dtype is not torch.int32 or status.numel() < 1):
-        _refused(2, name, "status: wanted an int32 tensor")
-    _ATTENTION.pack_into(_packed.buf, 0, _code(q, name), causal, sequences, q_heads, kv_heads, head_dim, q_len, kv_len, q_rows, kv_rows, at[0], at[1],
-                         head_dim ** -0.5 if scale is None else scale, 0 if status is None else status.data_ptr())
-    return _packed.at
-
-
-_HEADS = [struct.Struct(f"{3 * n}q") for n in range(9)]
-
-
-def _lse_of(q, lse, name):
-    if lse.shape != (q.shape[1], q.shape[0]) or not lse.is_contiguous() or lse.dtype is not torch.float32:
-        _refused(2, name, "lse: wanted float [q_heads, q_rows]")
+    return _calls.rotary(q, k, positions, first, period, rotary_dim, base, _choice(ROTARY_LAYOUTS, layout), _choice(ROTARY_SCALINGS, scaling),
+                         factor, trained_length, fast, slow, amplitude, inverse, q_out, k_out)
 
 
 def attention_forward(q, k, v, sequences=None, q_len=None, kv_len=None, q_offsets=None, kv_offsets=None, causal=True, scale=None,
                       o=None, lse=None, status=None):
     """softmax(scale q k^T) v over pairs of sequences: see hbp_attention_forward.  q [q_rows, q_heads, head_dim], k and v
     [kv_rows, kv_heads, head_dim]; returns o like q and lse [q_heads, q_rows] (float).  Without offsets the rows are ``sequences``
-    sequences of equal length; with them (int32 [sequences + 1], on the device) q_len / kv_len are the longest ones'."""
-    name = "attention_forward"
-    a = _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
-    if o is None:
-        o = torch.empty_like(q)
-    else:
-        _alike(o, q, name, "o is not like q")
-    if lse is None:
-        lse = q.new_empty((q.shape[1], q.shape[0]), dtype=torch.float32)
-    else:
-        _lse_of(q, lse, name)
-    stream = _on(name, q, k, v, q_offsets, kv_offsets, o, lse, status)
-    _HEADS[4].pack_into(_packed.buf, 80, *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), *_heads(o, "o"))
-    _check(lib.hbp_attention_forward(a, a + 80, a + 104, a + 128, a + 152, lse.data_ptr(), stream), "hbp_attention_forward")
-    return o, lse
+    sequences of equal length; with them (int32 [sequences + 1], on the device) q_len / kv_len are the longest ones'.  scale:
+    head_dim ** -0.5 if not given."""
+    return _calls.attention_forward(q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status, o, lse)
 
 
 def attention_backward(d_o, q, k, v, o, lse, sequences=None, q_len=None, kv_len=None, q_offsets=None, kv_offsets=None, causal=True,
                        scale=None, dq=None, dk=None, dv=None, scratch=None, status=None):
     """The gradients (dq, dk, dv) of attention_forward's q, k and v from that of its output: see hbp_attention_backward."""
-    name = "attention_backward"
-    a = _attention(name, q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status)
-    _alike(d_o, q, name, "d_o is not like q")
-    _alike(o, q, name, "o is not like q")
-    _lse_of(q, lse, name)
-    if dq is None:
-        dq = torch.empty_like(q)
-    else:
-        _alike(dq, q, name, "dq is not like q")
-    if dk is None:
-        dk = torch.empty_like(k)
-    else:
-        _alike(dk, k, name, "dk is not like k")
-    if dv is None:
-        dv = torch.empty_like(v)
-    else:
-        _alike(dv, v, name, "dv is not like v")
-    if scratch is None:
-        scratch = torch.empty_like(lse)
-    stream = _on(name, q, k, v, d_o, o, lse, q_offsets, kv_offsets, dq, dk, dv, scratch, status)
-    _HEADS[8].pack_into(_packed.buf, 80, *_heads(d_o, "d_o"), *_heads(q, "q"), *_heads(k, "k"), *_heads(v, "v"), *_heads(o, "o"), *_heads(dq, "dq"),
-                        *_heads(dk, "dk"), *_heads(dv, "dv"))
-    _check(lib.hbp_attention_backward(a, a + 80, a + 104, a + 128, a + 152, a + 176, lse.data_ptr(), a + 200, a + 224, a + 248, scratch.data_ptr(),
-                                      scratch.numel() * scratch.element_size(), stream), "hbp_attention_backward")
-    return dq, dk, dv
+    return _calls.attention_backward(d_o, q, k, v, o, lse, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status, dq, dk, dv,
+                                     scratch)
 
 
 def attention_scratch_bytes(q_heads, q_rows) -> int:
@@ -634,82 +467,22 @@ def attention_scratch_bytes(q_heads, q_rows) -> int:
     return n.value
 
 
-def _kept(like, codes, scales, name):
-    """Codes and scales of an activation like this one [rows, d], made where not given."""
-    rows, d = like.shape
-    groups = (d + CHECKPOINT_GROUP - 1) // CHECKPOINT_GROUP
-    if codes is None:
-        codes = like.new_empty((rows, d), dtype=torch.int8)
-    elif codes.shape != (rows, d) or not codes.is_contiguous() or codes.dtype is not torch.int8:
-        _refused(2, name, "codes: wanted int8 [rows, channels]")
-    if scales is None:
-        scales = like.new_empty((rows, groups), dtype=torch.uint8)
-    elif scales.shape != (rows, groups) or not scales.is_contiguous() or scales.dtype is not torch.uint8:
-        _refused(2, name, "scales: wanted uint8 [rows, channels / 32 rounded up]")
-    return codes, scales
-
-
 def checkpoint_store(x, codes=None, scales=None):
     """x [rows, channels] in 8 bits: (codes int8 like x, scales uint8 [rows, channels / 32 rounded up]); see hbp_checkpoint_store."""
-    name = "checkpoint_store"
-    px, ld = _matrix(x, name)
-    rows, d = x.shape
-    codes, scales = _kept(x, codes, scales, name)
-    _check(lib.hbp_checkpoint_store(_code(x, name), rows, d, px, ld, codes.data_ptr(), scales.data_ptr(), _on(name, x, codes, scales)), "hbp_checkpoint_store")
-    return codes, scales
+    return _calls.checkpoint_store(x, codes, scales)
 
 
 def checkpoint_load(codes, scales, dtype=torch.bfloat16, out=None):
-    """The values that checkpoint_store kept, exactly, in dtype."""
-    name = "checkpoint_load"
-    if codes.dim() != 2 or scales is None:
-        _refused(2, name, "codes: wanted int8 [rows, channels], and their scales")
-    rows, d = codes.shape
-    codes, scales = _kept(codes, codes, scales, name)
-    out = torch.empty_like(codes, dtype=dtype) if out is None else out
-    if out.shape != codes.shape:
-        _refused(2, name, "out is not like codes")
-    px, ld = _matrix(out, name)
-    _check(lib.hbp_checkpoint_load(_code(out, name), rows, d, codes.data_ptr(), scales.data_ptr(), px, ld, _on(name, codes, scales, out)), "hbp_checkpoint_load")
-    return out
+    """The values that checkpoint_store kept, exactly, in dtype (or out's)."""
+    return _calls.checkpoint_load(codes, scales, _dtype_code(dtype) == HBP_F32, out)
 
 
 def checkpoint_gelu(z, act=None, codes=None, scales=None):
     """(gelu(z), codes, scales): GELU of z [rows, channels] (``act`` may be z itself), and z in 8 bits for the backward pass."""
-    name = "checkpoint_gelu"
-    pz, ldz = _matrix(z, name)
-    rows, d = z.shape
-    codes, scales = _kept(z, codes, scales, name)
-    if act is None:
-        act = z.new_empty((rows, d))
-    else:
-        _alike(act, z, name, "act is not like z")
-    pa, lda = _matrix(act, name)
-    _check(lib.hbp_checkpoint_gelu(_code(z, name), rows, d, pz, ldz, pa, lda, codes.data_ptr(), scales.data_ptr(), _on(name, z, codes, scales, act)),
-           "hbp_checkpoint_gelu")
-    return act, codes, scales
+    return _calls.checkpoint_gelu(z, act, codes, scales)
 
 
 def checkpoint_gelu_backward(d_act, codes, scales, with_act=False, dz=None, act=None):
     """dz = d_act * gelu'(z8) (``dz`` may be d_act itself) from the z that checkpoint_gelu kept, and with ``with_act`` (or
     ``act`` given) gelu(z8) too, the operand of the following product's weight gradient: dz, or (dz, act)."""
-    name = "checkpoint_gelu_backward"
-    pd, ldd = _matrix(d_act, name)
-    rows, d = d_act.shape
-    if codes is None or scales is None:
-        _refused(1, name, "codes and scales have to be given")
-    codes, scales = _kept(d_act, codes, scales, name)
-    if dz is None:
-        dz = d_act.new_empty((rows, d))
-    else:
-        _alike(dz, d_act, name, "dz is not like d_act")
-    pz, ldz = _matrix(dz, name)
-    if with_act and act is None:
-        act = d_act.new_empty((rows, d))
-    pa, lda = None, 0
-    if act is not None:
-        _alike(act, d_act, name, "act is not like d_act")
-        pa, lda = _matrix(act, name)
-    _check(lib.hbp_checkpoint_gelu_backward(_code(d_act, name), rows, d, codes.data_ptr(), scales.data_ptr(), pd, ldd, pz, ldz, pa, lda,
-                                            _on(name, d_act, codes, scales, dz, act)), "hbp_checkpoint_gelu_backward")
-    return dz if act is None else (dz, act)
+    return _calls.checkpoint_gelu_backward(d_act, codes, scales, with_act, dz, act)

@@ -1,22 +1,25 @@
-"""Builds libhbp.so (sm_100a only) next to this file with nvcc; no GPU needed."""
+"""Builds libhbp.so (sm_100a only, nvcc) and the extension module _calls.so (marshalling of the short calls, g++ with torch's
+headers) next to this file; no GPU needed."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhbp.so")
+CALLS = os.path.join(HERE, "_calls.so")
 SOURCES = ["hbp_api.cu", "gemm_simt.cu", "gemm_tc.cu", "gemm_f32.cu", "gemm_parts.cu", "gemm_cell.cu", "few_rows.cu", "scan.cu", "scan_static.cu", "scan_ring.cu", "attention.cu", "attention_tc.cu", "rnn.cu", "rnn_persistent.cu", "rnn_cluster.cu", "cell_cluster.cu", "gru.cu", "lstm.cu", "diag.cu", "rotary.cu",
            "checkpoint.cu", "attention_ragged.cu", "attention_ragged_tc.cu"]
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "hbp.h")]
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -31,7 +34,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
               "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
     if verbose:
         common += ["-Xptxas", "-v"]
-    procs = []
+    procs = [("calls.cpp", _compile_calls(obj_dir))]
     objs = []
     for src in SOURCES:
         obj = os.path.join(obj_dir, src.replace(".cu", ".o"))
@@ -48,7 +51,26 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     if failed:
         raise RuntimeError("nvcc failed")
     subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", LIB] + objs + ["-lcudart"])
+    _link_calls(obj_dir)
     return LIB
+
+
+def _compile_calls(obj_dir: str) -> subprocess.Popen:
+    import torch
+    base = os.path.join(os.path.dirname(torch.__file__), "include")
+    cuda = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
+    return subprocess.Popen(["g++", "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                             "-isystem", base, "-isystem", os.path.join(base, "torch", "csrc", "api", "include"), "-isystem", cuda,
+                             "-isystem", sysconfig.get_paths()["include"], "-I" + os.path.join(ROOT, "include"), "-c",
+                             os.path.join(CSRC, "calls.cpp"), "-o", os.path.join(obj_dir, "calls.o")],
+                            stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _link_calls(obj_dir: str) -> None:
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    subprocess.check_call(["g++", "-shared", "-o", CALLS, os.path.join(obj_dir, "calls.o"), "-L" + HERE, "-lhbp", "-L" + libs, "-ltorch_python", "-ltorch_cpu",
+                           "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"])
 
 
 if __name__ == "__main__":
