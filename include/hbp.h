@@ -342,7 +342,7 @@ typedef struct {
 
 /* Turns q_heads heads of q into q_out and kv_heads heads of k into k_out (kv_heads may be 0; k and k_out are then ignored),
  * `rows` rows each, in one launch.  inverse != 0: by the opposite angles, which is the gradient (same amplitude).  An output
- * may be its input (same pointer and strides); otherwise they must not overlap.
+ * may be its input (same pointer and strides); otherwise they must not overlap, nor may an output's own rows and heads.
  * The position of a row: positions[row] (device, int32 if position_bytes is 4, int64 if 8), or, where positions is NULL,
  * first + row % period (period 0: first + row).  Angles are whole-number fractions of a turn (off by |position| * 2^-62
  * turns), the rotation is in float, and rounded once to dtype.  head_dim up to 256. */
@@ -365,7 +365,8 @@ hbp_status hbp_context_rotary(hbp_ctx* ctx, const hbp_rotary_spec* spec, int64_t
  * A query that sees no key has output 0, log-sum-exp -infinity and gradient 0.  A sequence whose offsets decrease, leave the tensor or
  * span more than q_len (kv_len) rows is skipped, and *status (device int32, may be NULL; zeroed by the caller) becomes
  * HBP_ERR_INVALID_ARG; a bounded wait that runs out makes it HBP_ERR_TIMEOUT and leaves outputs incomplete.
- * head_dim up to 128, a multiple of 16 bytes. */
+ * head_dim up to 128, a multiple of 16 bytes.  Inputs may be broadcast (strides of 0) and share memory; outputs overlap neither themselves nor anything
+ * else. */
 typedef struct {
   int32_t dtype, causal;
   int32_t sequences, q_heads, kv_heads, head_dim;

@@ -535,6 +535,13 @@ hbp_status check_heads(const hbp_attention& a, const hbp_heads* const* t, int n)
   }
   return HBP_OK;
 }
+// An output: no two of its elements in one place, rows of heads or heads of rows.
+hbp_status check_output(const hbp_attention& a, const hbp_heads& t, int64_t rows, int heads) {
+  const int64_t rs = t.row_stride, hs = t.head_stride, w = a.head_dim;
+  const bool apart = (rows <= 1 || rs >= (heads - 1) * hs + w) && (heads <= 1 || hs >= w);
+  const bool across = (heads <= 1 || hs >= (rows - 1) * rs + w) && (rows <= 1 || rs >= w);
+  return apart || across ? HBP_OK : HBP_ERR_SHAPE;
+}
 
 }  // namespace
 
@@ -551,7 +558,7 @@ hbp_status hbp_attention_forward(const hbp_attention* a, const hbp_heads* q, con
   if (a->sequences == 0 || a->q_len == 0) return HBP_OK;
   const hbp_heads* const qt[4] = {q, o, k, v};
   st = check_heads(*a, qt, a->kv_len ? 4 : 2);  // (no keys at all: their tensors may be empty)
-  if (st != HBP_OK) return st;
+  if (st != HBP_OK || (st = check_output(*a, *o, a->q_rows, a->q_heads)) != HBP_OK) return st;
   if (!lse) return HBP_ERR_INVALID_ARG;
   if ((uintptr_t)lse & 3u) return HBP_ERR_SHAPE;
   Launcher lc;
@@ -586,8 +593,10 @@ hbp_status hbp_attention_backward(const hbp_attention* a, const hbp_heads* d_o, 
   if (a->sequences == 0 || (a->q_len == 0 && a->kv_len == 0)) return HBP_OK;
   const hbp_heads* const qt[4] = {d_o, q, o, dq};
   const hbp_heads* const kt[4] = {k, v, dk, dv};
-  if (a->q_len && (st = check_heads(*a, qt, 4)) != HBP_OK) return st;
-  if (a->kv_len && (st = check_heads(*a, kt, 4)) != HBP_OK) return st;
+  if (a->q_len && ((st = check_heads(*a, qt, 4)) != HBP_OK || (st = check_output(*a, *dq, a->q_rows, a->q_heads)) != HBP_OK)) return st;
+  if (a->kv_len && ((st = check_heads(*a, kt, 4)) != HBP_OK || (st = check_output(*a, *dk, a->kv_rows, a->kv_heads)) != HBP_OK ||
+                    (st = check_output(*a, *dv, a->kv_rows, a->kv_heads)) != HBP_OK))
+    return st;
   RaggedAttn r = {};
   r.a = *a;
   if (a->q_len) {

@@ -224,11 +224,17 @@ extern "C" hbp_status hbp_rotary(const hbp_rotary_spec* spec, int32_t inverse, i
   const hbp_heads t[4] = {*q, *q_out, kv_heads ? *k : none, kv_heads ? *k_out : none};
   for (int i = 0; i < (kv_heads ? 4 : 2); ++i) {
     if (!t[i].x) return HBP_ERR_INVALID_ARG;
-    if (((uintptr_t)t[i].x & 15u) || t[i].row_stride % v || t[i].head_stride % v) return HBP_ERR_SHAPE;
+    if (((uintptr_t)t[i].x & 15u) || t[i].row_stride % v || t[i].head_stride % v || t[i].row_stride < 0 || t[i].head_stride < 0) return HBP_ERR_SHAPE;
   }
   for (int i = 0; i < 4; i += 2)
     if (t[i].x && t[i].x == t[i + 1].x && (t[i].row_stride != t[i + 1].row_stride || t[i].head_stride != t[i + 1].head_stride))
       return HBP_ERR_INVALID_ARG;  // in place, but rows or heads elsewhere
+  for (int i = 1; i < (kv_heads ? 4 : 2); i += 2) {  // outputs: no two elements in one place, rows of heads or heads of rows
+    const int64_t rs = t[i].row_stride, hs = t[i].head_stride, heads = i == 1 ? q_heads : kv_heads;
+    const bool apart = (rows <= 1 || rs >= (heads - 1) * hs + head_dim) && (heads <= 1 || hs >= head_dim);
+    const bool across = (heads <= 1 || hs >= (rows - 1) * rs + head_dim) && (rows <= 1 || rs >= head_dim);
+    if (!apart && !across) return HBP_ERR_SHAPE;
+  }
   Launcher lc;
   lc.stream = (cudaStream_t)cuda_stream;
   rotary(lc, *spec, inverse != 0, dtype, rows, q_heads, kv_heads, head_dim, positions, position_bytes, first, period, t[0], t[1], t[2], t[3]);

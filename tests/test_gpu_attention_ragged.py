@@ -227,6 +227,26 @@ def test_parts_of_one_buffer(B, dtype, hd):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+def test_broadcast_inputs(B, dtype):
+    """One key head seen as four (stride 0), one row of d_o seen as all: the gradients are those of the copies, every head's own."""
+    n, hd = 140, 64
+    q, k, v, d_o = make(n, 4, hd, dtype, 0), make(n, 1, hd, dtype, 1).expand(n, 4, hd), make(n, 1, hd, dtype, 2).expand(n, 4, hd), make(1, 4, hd, dtype, 3).expand(n, 4, hd)
+    o, lse = B.attention_forward(q, k, v)
+    grads = B.attention_backward(d_o, q, k, v, o, lse)
+    want = reference(q, k, v, d_o, [n], [n], True, hd ** -0.5)
+    for name, got in zip(("o", "lse", "dq", "dk", "dv"), (o, lse, *grads)):
+        check(got, want[name], name)
+    with pytest.raises(B.HbpError) as e:
+        B.attention_backward(d_o, q, k, v, o, lse, dk=make(n, 1, hd, dtype, 4).expand(n, 4, hd))
+    assert e.value.code == 2
+
+
+def test_narrowest_heads(B):
+    case(B, F32, [70], [70], 3, 3, 4, True)
+    case(B, F32, [70], [130], 2, 1, 12, False)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_beyond_32_bits(B, dtype):
     """Rows 2^23 elements apart, 300 of them: elements beyond 2^31 from the first."""
     n, hd = 300, 64

@@ -56,6 +56,8 @@ def test_rotary_refusals(B):
     assert _rotary(B, q=B.hbp_heads(P + 4, 128, 64)) == SHAPE
     assert _rotary(B, ko=B.hbp_heads(P, 66, 64)) == SHAPE
     assert _rotary(B, qo=B.hbp_heads(P, 192, 64)) == INVALID           # in place, other rows
+    for rs, hs in ((0, 64), (64, 64), (128, 0), (-128, 64)):             # outputs on one another
+        assert _rotary(B, qo=B.hbp_heads(P + 4096, rs, hs)) == SHAPE, (rs, hs)
     with pytest.raises(B.HbpError) as e:
         S(64, layout="other")
     assert e.value.code == UNSUPPORTED
@@ -91,6 +93,9 @@ def test_attention_refusals(B, backward):
         for bad, code in ((B.hbp_heads(0, 256, 64), INVALID), (B.hbp_heads(P + 8, 256, 64), SHAPE), (B.hbp_heads(P, 260, 64), SHAPE),
                           (B.hbp_heads(P, 256, 4), SHAPE), (B.hbp_heads(P, -256, 64), SHAPE)):
             assert call(tensors=[bad if j == i else good for j in range(n)]) == code, (i, bad.row_stride)
+    for i in ((5, 6, 7) if backward else (3,)):  # outputs whose rows or heads lie on one another; heads before rows is another matter
+        for rs, hs in ((0, 64), (256, 0), (192, 64), (256, 56), (48, 2048)):
+            assert call(tensors=[B.hbp_heads(P, rs, hs) if j == i else good for j in range(n)], kv_heads=4) == SHAPE, (i, rs, hs)
     if backward:
         assert call(scratch=None) == WORKSPACE
         assert call(scratch_bytes=4 * 4 * 32 - 1) == WORKSPACE
