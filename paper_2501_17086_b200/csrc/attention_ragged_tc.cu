@@ -105,10 +105,9 @@ __device__ __forceinline__ void copy_rows(uint32_t dst, int tile_rows, const CUt
 // rows [from, rows) of a tile become zeros; the whole warp
 template <int HD>
 __device__ __forceinline__ void clear_rows(uint32_t tile, int rows, int from, int lane) {
-  for (int i = lane; i < (rows - from) * 8 * (HD / SUB); i += 32) {
-    const int c = i / ((rows - from) * 8), r = i - c * (rows - from) * 8;
-    st_shared16(tile + c * rows * 128 + (from + (r >> 3)) * 128 + (r & 7) * 16, make_uint4(0, 0, 0, 0));
-  }
+#pragma unroll
+  for (int c = 0; c < HD / SUB; ++c)
+    for (int i = from * 8 + lane; i < rows * 8; i += 32) st_shared16(tile + c * rows * 128 + i * 16, make_uint4(0, 0, 0, 0));
 }
 // A bounded wait (mbar_wait) of the whole warp, where the status word may be missing: all lanes go on or none does.
 __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
