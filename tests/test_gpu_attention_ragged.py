@@ -409,3 +409,45 @@ def test_an_attention_step_with_rotary_positions(B, dtype):
     tol = 15 * U[dtype] if dtype == BF16 else 15 * 64 * U[dtype]
     for got, want in ((o, y), (dq, a.grad), (dk, b.grad), (dv, c.grad)):
         assert float((got.double() - want).norm() / want.norm()) <= tol
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hd", [40, 64, 72, 128])
+@pytest.mark.parametrize("ql,kl,qh,kh", [([1], [4096], 4, 1), ([3, 128, 0, 130], [4100, 70, 0, 1], 2, 1), ([4200], [130], 1, 1),
+                                         ([1100, 5], [1100, 64], 1, 1), ([512, 3], [100, 900], 8, 1), ([2, 1], [1030, 1], 3, 3)])
+def test_walks_that_several_blocks_share(B, dtype, causal, hd, ql, kl, qh, kh):
+    """Few blocks with long walks; sequences with fewer tiles than blocks leave some of them nothing.  Putting parts together multiplies them by an
+    exponential, which the 2^-19 of a probability hold as well (it is off by 2^-21 at most)."""
+    case(B, dtype, ql, kl, qh, kh, hd, causal)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_shared_walks_agree_bit_for_bit_and_keep_to_themselves(B, dtype, hd):
+    """Runs agree; what is in no sequence is NaN and stays as it was; a row of large scores and one of keys that are all the same among the rows."""
+    ql, kl = [70, 2], [2050, 4097]
+    q, d_o = make(80, 4, hd, dtype, 1), make(80, 4, hd, dtype, 2)
+    k, v = make(6200, 2, hd, dtype, 3), make(6200, 2, hd, dtype, 4)
+    q[3 + 5] *= 50
+    k[10 + 2050:10 + 2050 + 300] = k[10 + 2050].clone()
+    for x, at, n in ((q, 3, 72), (d_o, 3, 72), (k, 10, 6147), (v, 10, 6147)):
+        x[:at], x[at + n:] = math.nan, math.nan
+    kw = dict(q_offsets=offsets(ql, 3), kv_offsets=offsets(kl, 10), q_len=70, kv_len=4097, causal=True, status=torch.zeros(1, dtype=torch.int32, device="cuda"))
+    want = reference(q, k, v, d_o, ql, kl, True, hd ** -0.5, q_at=3, k_at=10)
+    first = None
+    for _ in range(3):
+        o, lse = torch.full_like(q, 7), torch.full((4, 80), 7.0, device="cuda")
+        dq, dk, dv = torch.full_like(q, 7), torch.full_like(k, 7), torch.full_like(v, 7)
+        B.attention_forward(q, k, v, o=o, lse=lse, **kw)
+        B.attention_backward(d_o, q, k, v, o, lse, dq=dq, dk=dk, dv=dv, **kw)
+        got = [o, lse, dq, dk, dv]
+        if first is None:
+            first = [x.clone() for x in got]
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
+    assert int(kw["status"]) == 0
+    for name, x, at, n in (("o", o, 3, 72), ("dq", dq, 3, 72), ("dk", dk, 10, 6147), ("dv", dv, 10, 6147)):
+        check(x[at:at + n], tuple(y[at:at + n] for y in want[name]), name)
+        assert bool((x[:at] == 7).all()) and bool((x[at + n:] == 7).all())
+    check(lse[:, 3:75], tuple(y[:, 3:75] for y in want["lse"]), "lse")
+    assert bool((lse[:, :3] == 7).all()) and bool((lse[:, 75:] == 7).all())
