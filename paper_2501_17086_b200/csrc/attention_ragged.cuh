@@ -54,6 +54,28 @@ __device__ __forceinline__ SeqPair sequence_pair(const hbp_attention& a, int b) 
   }
   return s;
 }
+// Ragged batches of up to a warp's lanes of sequences are taken longest walks first (over_keys: walks over the keys, else over the queries), so that
+// no long walk begins when the others are nearly done: w.b, a place in that order, becomes the sequence.  12 sequences of up to 509 queries and 1301
+// keys, 10 heads of 80, forward: 33 against 42 us in the batch's order.  More sequences even out by themselves.
+__device__ __forceinline__ SeqPair sequence_pair(const hbp_attention& a, BlockOf& w, bool over_keys) {
+  const int n = a.sequences;
+  if ((a.q_offsets || a.kv_offsets) && n > 1 && n <= 32) {
+    const int lane = threadIdx.x & 31;
+    int len = 0, before = 0;
+    if (lane < n) {
+      const int32_t* off = over_keys ? a.kv_offsets : a.q_offsets;
+      const int32_t* own = over_keys ? a.q_offsets : a.kv_offsets;
+      len = off ? (int)((unsigned)off[lane + 1] - (unsigned)off[lane]) : 0;
+      if (own && own[lane + 1] == own[lane]) len = -1;  // (none of its blocks does anything)
+    }
+    for (int i = 0; i < n; ++i) {
+      const int other = __shfl_sync(0xffffffffu, len, i);
+      before += other > len || (other == len && i < lane);
+    }
+    w.b = __ffs((int)__ballot_sync(0xffffffffu, lane < n && before == w.b)) - 1;
+  }
+  return sequence_pair(a, w.b);
+}
 
 // bf16 on the tensor cores (attention_ragged_tc.cu); false if a tensor's strides or address are not such as tile copies take, in which case
 // nothing was launched.

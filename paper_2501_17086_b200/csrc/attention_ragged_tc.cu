@@ -127,6 +127,18 @@ __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile
   }
   return __all_sync(0xffffffffu, ok);
 }
+// Tensor memory is taken by warp 1, which gives up the permit for more at once: an SM's next block does not begin before.
+__device__ __forceinline__ void take(uint32_t* slot, uint32_t columns) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(columns) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+// A block that has nothing to do.
+__device__ __forceinline__ void give_back(int warp, const uint32_t* slot, uint32_t columns) {
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*reinterpret_cast<const volatile uint32_t*>(slot)), "r"(columns) : "memory");
+}
 // The end of a block: after a wait that gave up, every copy and product is outlasted first.
 __device__ __forceinline__ void leave(int warp, uint32_t tmem, uint32_t columns, volatile int* abort_flag) {
   tc_fence_before();
@@ -153,6 +165,7 @@ __device__ __forceinline__ void store_staged(uint32_t tile, int row0, int unit0,
 
 // ---- walks shared by a cluster: few blocks with long walks leave most of the chip idle.  The blocks of a cluster take the tiles of a walk in
 // turn; each leaves its sums in its shared memory, and each puts together those of all for its share of the rows, in the blocks' order.
+constexpr int MOST_RANKS = 8;
 __device__ __forceinline__ int tiles_of(int tiles, int rank, int ranks) { return ranks == 1 ? tiles : (tiles - rank + ranks - 1) / ranks; }
 // Rows of HD floats, their 16-byte units permuted among eight by the row: one row per lane is written without bank conflicts.
 template <int HD>
@@ -179,18 +192,58 @@ __device__ __forceinline__ float2 ld_cluster2(uint32_t addr) {
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
   return v;
 }
-// v += f * channels 8 u .. 8 u + 7 of row r of the sums at `base` in a block of the cluster
-template <int HD>
-__device__ __forceinline__ void add_sums(uint32_t base, int r, int u, float f, float (&v)[8]) {
+__device__ __forceinline__ float4 ld_cluster4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+// The rows' sums of all blocks of the cluster times factor(row of this block's share, block), added up: put(row, unit, sums) for each eight channels of
+// the first `there` rows of this block's share.  Sixteen loads of a thread are under way at a time: one block's two at a time, two blocks' 128 rows of 80 channels took 5 us instead of 2.5.
+template <int HD, int R, typename Factor, typename Put>
+__device__ __forceinline__ void merge_sums(uint32_t base, int rank, int there, int t, int threads, Factor factor, Put put) {
+  constexpr int NI = MOST_RANKS / R, units = HD / 8;
+  const int n_units = min(BIG / R, there) * units;
+  for (int i = t; i < n_units; i += NI * threads) {
+    float4 x[NI][R][2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float4 x;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(sum_at<HD>(base, r, 2 * u + h)) : "memory");
-    v[4 * h] = fmaf(f, x.x, v[4 * h]);
-    v[4 * h + 1] = fmaf(f, x.y, v[4 * h + 1]);
-    v[4 * h + 2] = fmaf(f, x.z, v[4 * h + 2]);
-    v[4 * h + 3] = fmaf(f, x.w, v[4 * h + 3]);
+    for (int n = 0; n < NI; ++n) {
+      const int j = min(i + n * threads, n_units - 1);
+#pragma unroll
+      for (int b = 0; b < R; ++b) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[n][b][h] = ld_cluster4(sum_at<HD>(map_to_cta(base, b), rank * (BIG / R) + j / units, 2 * (j % units) + h));
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      const int j = i + n * threads;
+      if (j >= n_units) break;
+      float v[8] = {};
+#pragma unroll
+      for (int b = 0; b < R; ++b) {
+        const float f = factor(j / units, b);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          v[4 * h] = fmaf(f, x[n][b][h].x, v[4 * h]);
+          v[4 * h + 1] = fmaf(f, x[n][b][h].y, v[4 * h + 1]);
+          v[4 * h + 2] = fmaf(f, x[n][b][h].z, v[4 * h + 2]);
+          v[4 * h + 3] = fmaf(f, x[n][b][h].w, v[4 * h + 3]);
+        }
+      }
+      put(j / units, j % units, v);
+    }
   }
+}
+template <int HD, typename Factor, typename Put>
+__device__ __forceinline__ void merge_sums(int ranks, uint32_t base, int rank, int there, int t, int threads, Factor factor, Put put) {
+  if (ranks == 2) merge_sums<HD, 2>(base, rank, there, t, threads, factor, put);
+  else if (ranks == 4) merge_sums<HD, 4>(base, rank, there, t, threads, factor, put);
+  else merge_sums<HD, 8>(base, rank, there, t, threads, factor, put);
+}
+// No block ends while another reads its shared memory (what was read has arrived; nothing that was written is handed over).
+__device__ __forceinline__ void cluster_end() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 // Nothing seen: sums of 0, outputs of 0 and a log-sum-exp of -infinity (a sum that is NaN stays NaN)
 __device__ __forceinline__ float inverse(float total) { return total > 0.0f ? 1.0f / total : total; }
@@ -206,23 +259,15 @@ struct Fwd {
 };
 
 // kShared: walks are shared by a cluster (a kernel of its own: in one, the others' took 119 us instead of 113, 2 x 4096 rows, 16 heads of 64).
+// 128 registers (256 threads are told): at 132 a quarter of an SM holds three warps but not four, and when the second of two blocks ends first, a new one
+// has to wait for the other too (ragged batch of cross attention 31 against 36 us, 16 heads of 128 126 against 131).
 template <int HD, bool kShared>
-__global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p,
+__global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p,
                                                                        const int ranks_given) {
   const int ranks = kShared ? ranks_given : 1;
   using C = Fwd<HD>;
   constexpr int NS = C::kStages, NB = 2;
   const int rank = kShared ? (int)(blockIdx.x % ranks) : 0;
-  const BlockOf w = block_at(kShared ? blockIdx.x / ranks : blockIdx.x, p.a.q_len, BIG, p.a.q_heads, true);
-  const SeqPair sq = sequence_pair(p.a, w.b);
-  const int q0 = w.blk * BIG;
-  if (q0 >= sq.nq) return;  // (all blocks of the cluster)
-  const int kh = w.h / (p.a.q_heads / p.a.kv_heads);
-  const int shift = sq.nk - sq.nq;  // causal: query i sees keys 0 .. i + shift
-  const int seen = p.a.causal ? min(sq.nk, min(q0 + BIG, sq.nq) + shift) : sq.nk;
-  // this block's tiles: rank, rank + ranks, ...
-  const int tiles = seen > 0 ? (seen + SMALL - 1) / SMALL : 0, n_it = kShared ? tiles_of(tiles, rank, ranks) : tiles;
-
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* aligned = smem_raw + (base - smem_u32(smem_raw));
@@ -241,15 +286,33 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+  if (warp == 1) take(tmem_slot, 256);  // (first of all, so that the SM's second block begins 0.8 us earlier: 16 heads of 128, 126 against 127 us)
+
+  BlockOf w = block_at(kShared ? blockIdx.x / ranks : blockIdx.x, p.a.q_len, BIG, p.a.q_heads, true);
+  const SeqPair sq = sequence_pair(p.a, w, true);
+  const int q0 = w.blk * BIG;
+  if (q0 >= sq.nq) {  // (all blocks of the cluster)
+    give_back(warp, tmem_slot, 256);
+    return;
+  }
+  const int kh = w.h / (p.a.q_heads / p.a.kv_heads);
+  const int shift = sq.nk - sq.nq;  // causal: query i sees keys 0 .. i + shift
+  const int seen = p.a.causal ? min(sq.nk, min(q0 + BIG, sq.nq) + shift) : sq.nk;
+  // this block's tiles: rank, rank + ranks, ...
+  const int tiles = seen > 0 ? (seen + SMALL - 1) / SMALL : 0, n_it = kShared ? tiles_of(tiles, rank, ranks) : tiles;
+
+
   if (threadIdx.x == 0) {
     for (int i = 0; i < kBars; ++i) mbar_init(bars + 8 * i, i >= 3 && i < 3 + NB ? 4 : 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(256) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (n_it > 0) {  // the first copies are under way while the others get ready
+      mbar_expect_tx(bQ, C::kBig);
+      for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sQ + r * 128, BIG, &m.q, bQ, w.h, (int)sq.q0 + q0 + r);
+      mbar_expect_tx(bKFull(0), C::kSmall);
+      copy_rows<HD>(sK, SMALL, &m.k, bKFull(0), kh, (int)sq.k0 + rank * SMALL);
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -258,16 +321,12 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
 
   if (warp == 0) {
     bool ok = n_it > 0;
-    if (ok && lane == 0) {
-      mbar_expect_tx(bQ, C::kBig);
-      for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sQ + r * 128, BIG, &m.q, bQ, w.h, (int)sq.q0 + q0 + r);
-    }
     for (int it = 0; it < n_it && ok; ++it) {
       const int s = it % NS;
       const uint32_t free_parity = ((uint32_t)(it / NS) & 1u) ^ 1u;
       const int tile = kShared ? rank + it * ranks : it, row = (int)sq.k0 + tile * SMALL;
       if (!wait_all(bKFree(s), free_parity, abort_flag, p.a.status)) { ok = false; break; }
-      if (lane == 0) {
+      if (lane == 0 && it > 0) {
         mbar_expect_tx(bKFull(s), C::kSmall);
         copy_rows<HD>(sK + s * C::kSmall, SMALL, &m.k, bKFull(s), kh, row);
       }
@@ -288,13 +347,14 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
     }
   } else if (warp == 1) {
     const bool leader = elect_one();
+    const int steps = (p.a.head_dim + 15) / 16;  // of the contraction over channels (the channels behind are zeros)
     const uint64_t dQ = make_desc(sQ, 16, 1024), dK = make_desc(sK, 16, 1024), dV = make_desc(sV, SMALL * 128, 1024);
     auto scores = [&](int it) {
       const uint32_t off = (uint32_t)(it % NS) * C::kSmall, t = tmem + 64 * (it % NB);
       if (leader) {
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k)
-          tc_mma(t, desc_add(dQ, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dK, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+          if (HD == 64 || k < steps) tc_mma(t, desc_add(dQ, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dK, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
         tc_commit(bScores(it % NB));
         tc_commit(bKFree(it % NS));
       }
@@ -425,30 +485,40 @@ __global__ void __launch_bounds__(FWD_THREADS, 2) ragged_fwd_tc_kernel(const __g
       asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(sQ + row * 8), "f"(top), "f"(total) : "memory");
     }
   }
+  // (before the blocks of a cluster wait for one another: two clusters of two calls that each held tensor memory the other needs would wait for good)
+  leave(warp, tmem, 256, abort_flag);
   if (kShared) {
     cluster_sync();
-    const int t = (int)threadIdx.x - 64, rows = BIG / ranks;
-    bf16* out = (bf16*)p.o.x + (sq.q0 + q0) * p.o.row_stride + w.h * p.o.head_stride;
-    for (int i = t; t >= 0 && i < rows * (HD / 8); i += FWD_THREADS - 64) {
-      const int r = rank * rows + i / (HD / 8), u = i % (HD / 8);
-      if (q0 + r >= sq.nq || u * 8 >= p.a.head_dim) continue;
-      float most = -INFINITY, total = 0.0f, v[8] = {};
-      for (int b = 0; b < ranks; ++b) most = fmaxf(most, ld_cluster2(map_to_cta(sQ + r * 8, b)).x);
-      for (int b = 0; b < ranks; ++b) {
-        const float2 st = ld_cluster2(map_to_cta(sQ + r * 8, b));
-        const float f = most == -INFINITY ? 1.0f : fast_exp2(st.x - most);
-        total = fmaf(f, st.y, total);
-        add_sums<HD>(map_to_cta(sK, b), r, u, f, v);
-      }
-      const float inv = inverse(total);
+    const int rows = BIG / ranks, first = rank * rows, t = threadIdx.x;  // this block's share
+    float* factors = reinterpret_cast<float*>(aligned + BIG * 8);             // [row][16]: the blocks' factors; 1 / total (-1: nothing seen)
+    if (t < rows) {
+      float most = -INFINITY, total = 0.0f;
+      float2 st[MOST_RANKS];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = total == 0.0f ? 0.0f : v[e] * inv;
-      *reinterpret_cast<uint4*>(out + (int64_t)r * p.o.row_stride + u * 8) = pack8(v);
-      if (u == 0) p.lse[w.h * p.a.q_rows + sq.q0 + q0 + r] = log_sum(most, total);
+      for (int b = 0; b < MOST_RANKS; ++b) st[b] = b < ranks ? ld_cluster2(map_to_cta(sQ + (first + t) * 8, b)) : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+      for (int b = 0; b < MOST_RANKS; ++b) most = fmaxf(most, st[b].x);
+#pragma unroll
+      for (int b = 0; b < MOST_RANKS; ++b) {
+        const float f = most == -INFINITY ? 1.0f : fast_exp2(st[b].x - most);
+        total = fmaf(f, st[b].y, total);
+        factors[t * 16 + b] = f;
+      }
+      factors[t * 16 + MOST_RANKS] = total == 0.0f ? -1.0f : inverse(total);
+      if (q0 + first + t < sq.nq) p.lse[w.h * p.a.q_rows + sq.q0 + q0 + first + t] = log_sum(most, total);
     }
-    cluster_sync();  // (no block ends while another reads its shared memory)
+    __syncthreads();
+    bf16* out = (bf16*)p.o.x + (sq.q0 + q0 + first) * p.o.row_stride + w.h * p.o.head_stride;
+    merge_sums<HD>(ranks, sK, rank, sq.nq - q0 - first, t, FWD_THREADS, [&](int r, int b) { return factors[r * 16 + b]; },
+                   [&](int r, int u, float (&v)[8]) {
+                     if (u * 8 >= p.a.head_dim) return;
+                     const float inv = factors[r * 16 + MOST_RANKS];
+#pragma unroll
+                     for (int e = 0; e < 8; ++e) v[e] = inv < 0.0f ? 0.0f : v[e] * inv;
+                     *reinterpret_cast<uint4*>(out + (int64_t)r * p.o.row_stride + u * 8) = pack8(v);
+                   });
+    cluster_end();
   }
-  leave(warp, tmem, 256, abort_flag);
 }
 
 // ------------------------------------------------------------------------------------------- backward
@@ -468,22 +538,9 @@ struct Bwd {
 };
 
 template <int HD, bool kDKV, bool kShared>
-__device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const RaggedAttn& p, const BlockOf w, const int rank, const int ranks) {
+__device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const RaggedAttn& p, BlockOf w, const int rank, const int ranks) {
   using C = Bwd<HD>;
   constexpr int NB = C::kBuffers, NS = C::kStages;
-  const SeqPair sq = sequence_pair(p.a, w.b);
-  const int big0 = w.blk * BIG, n_big = kDKV ? sq.nk : sq.nq, n_small = kDKV ? sq.nq : sq.nk;
-  if (big0 >= n_big) return;  // (all blocks of a cluster)
-  const int group = p.a.q_heads / p.a.kv_heads;
-  const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;  // query i sees keys 0 .. i + shift (capped by nk)
-  // tiles of the other side: queries from the first that sees key big0 on; keys up to the last that the block's last query sees
-  const int t_beg = kDKV && p.a.causal ? max(0, big0 - shift) / SMALL : 0;
-  const int t_rows = kDKV ? n_small : p.a.causal ? min(n_small, min(big0 + BIG, n_big) + shift) : n_small;
-  const int tiles = max(0, (max(t_rows, 0) + SMALL - 1) / SMALL - t_beg);
-  // this block's tiles among those of all heads, one head after the other: rank, rank + ranks, ...
-  const int n_all = kDKV ? tiles * group : tiles, n_it = kShared ? tiles_of(n_all, rank, ranks) : n_all;
-  const int q_head0 = kDKV ? w.h * group : w.h, k_head = kDKV ? w.h : w.h / group;
-
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* aligned = smem_raw + (base - smem_u32(smem_raw));
@@ -504,6 +561,24 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+
+  const SeqPair sq = sequence_pair(p.a, w, !kDKV);
+  const int big0 = w.blk * BIG, n_big = kDKV ? sq.nk : sq.nq, n_small = kDKV ? sq.nq : sq.nk;
+  if (big0 >= n_big) {  // (all blocks of a cluster)
+    chain_wait();
+    return;
+  }
+  const int group = p.a.q_heads / p.a.kv_heads;
+  const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;  // query i sees keys 0 .. i + shift (capped by nk)
+  // tiles of the other side: queries from the first that sees key big0 on; keys up to the last that the block's last query sees
+  const int t_beg = kDKV && p.a.causal ? max(0, big0 - shift) / SMALL : 0;
+  const int t_rows = kDKV ? n_small : p.a.causal ? min(n_small, min(big0 + BIG, n_big) + shift) : n_small;
+  const int tiles = max(0, (max(t_rows, 0) + SMALL - 1) / SMALL - t_beg);
+  // this block's tiles among those of all heads, one head after the other: rank, rank + ranks, ...
+  const int n_all = kDKV ? tiles * group : tiles, n_it = kShared ? tiles_of(n_all, rank, ranks) : n_all;
+  const int q_head0 = kDKV ? w.h * group : w.h, k_head = kDKV ? w.h : w.h / group;
+
+
   if (threadIdx.x == 0) {
     // probabilities, dS: eight warps; full: the copies, and what the copying warp adds itself; scores of dK, dV: the products, and the warp that
     // issues them, which has seen the statistics there and passes them on
@@ -514,11 +589,16 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    if (n_it > 0) {
+      mbar_expect_tx(bBig, 2 * C::kBig);
+      for (int r = 0; r < BIG; r += SMALL) {
+        const int row = (int)(kDKV ? sq.k0 : sq.q0) + big0 + r;
+        copy_rows<HD>(sBig0 + r * 128, BIG, kDKV ? &m.k : &m.q, bBig, w.h, row);
+        copy_rows<HD>(sBig1 + r * 128, BIG, kDKV ? &m.v : &m.d_o, bBig, w.h, row);
+      }
+    }
   }
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::kColumns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == 1) take(tmem_slot, C::kColumns);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -530,14 +610,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
   if (warp == 0) {
     bool ok = n_it > 0;
     int tails = 0;
-    if (ok && lane == 0) {
-      mbar_expect_tx(bBig, 2 * C::kBig);
-      for (int r = 0; r < BIG; r += SMALL) {
-        const int row = (int)(kDKV ? sq.k0 : sq.q0) + big0 + r;
-        copy_rows<HD>(sBig0 + r * 128, BIG, kDKV ? &m.k : &m.q, bBig, w.h, row);
-        copy_rows<HD>(sBig1 + r * 128, BIG, kDKV ? &m.v : &m.d_o, bBig, w.h, row);
-      }
-    }
+    chain_wait();
     for (int it = 0; it < n_it && ok; ++it) {
       const int s = it % NS, nth = kShared ? rank + it * ranks : it, r0 = (t_beg + nth % tiles) * SMALL, head = kDKV ? q_head0 + nth / tiles : k_head;
       const uint32_t tile = sSmall + s * C::kStage;
@@ -581,6 +654,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
     }
   } else if (warp == 1) {
     const bool leader = elect_one();
+    const int steps = (p.a.head_dim + 15) / 16;  // of the contractions over channels (the channels behind are zeros)
     const uint64_t dB0 = make_desc(sBig0, 16, 1024), dB1 = make_desc(sBig1, 16, 1024);
     const uint64_t dS0 = make_desc(sSmall, 16, 1024), dS1 = make_desc(sSmall + C::kSmall, 16, 1024);
     const uint64_t dS0mn = make_desc(sSmall, SMALL * 128, 1024), dS1mn = make_desc(sSmall + C::kSmall, SMALL * 128, 1024);
@@ -590,7 +664,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
       if (leader) {
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k)
-          tc_mma(t, desc_add(dB0, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS0, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+          if (HD == 64 || k < steps) tc_mma(t, desc_add(dB0, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS0, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
         if (kDKV) mbar_arrive(bScores(it % NB));
         tc_commit(bScores(it % NB));
       }
@@ -600,7 +674,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
       if (leader) {
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k)
-          tc_mma(t, desc_add(dB1, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS1, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
+          if (HD == 64 || k < steps) tc_mma(t, desc_add(dB1, (k / 4) * BIG * 128 + 32 * (k % 4)), desc_add(dS1, off + (k / 4) * SMALL * 128 + 32 * (k % 4)), kIdesc<SMALL, 0>, k != 0);
         tc_commit(bDP(it % NB));
       }
     };
@@ -653,6 +727,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const float scale2 = p.a.scale * LOG2E;
     float my_lse = -INFINITY, my_d = 0.0f;  // dQ: minus log-sum-exp and minus D of this row
+    chain_wait();
     if (!kDKV && brow < n_big) {
       const int64_t at = (int64_t)w.h * p.a.q_rows + sq.q0 + brow;
       my_lse = p.lse[at] == -INFINITY ? -INFINITY : p.lse[at] * -LOG2E;
@@ -756,25 +831,25 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
       }
     }
   }
+  // (before the blocks of a cluster wait for one another, as above)
+  leave(warp, tmem, C::kColumns, abort_flag);
   if (kShared) {
     // the sums of dK and dQ in the place of the block's own tiles, those of dV in the place of the others
     cluster_sync();
-    const int t = (int)threadIdx.x - 64, rows = BIG / ranks, units = rows * (HD / 8);
-    for (int i = t; t >= 0 && i < units * (kDKV ? 2 : 1); i += C::kThreads - 64) {
-      const bool second = i >= units;
-      const int j = second ? i - units : i, r = rank * rows + j / (HD / 8), u = j % (HD / 8);
-      if (big0 + r >= n_big || u * 8 >= p.a.head_dim) continue;
-      float v[8] = {};
-      for (int b = 0; b < ranks; ++b) add_sums<HD>(map_to_cta(second ? sSmall : sBig0, b), r, u, 1.0f, v);
-      const float mul = second ? 1.0f : p.a.scale;
+    const int first = big0 + rank * (BIG / ranks);
+    auto put = [&](const hbp_heads& out, float mul) {
+      return [&, mul](int r, int u, float (&v)[8]) {
+        if (u * 8 >= p.a.head_dim) return;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= mul;
-      const hbp_heads& out = kDKV ? (second ? p.dv : p.dk) : p.dq;
-      *reinterpret_cast<uint4*>((bf16*)out.x + ((kDKV ? sq.k0 : sq.q0) + big0 + r) * out.row_stride + w.h * out.head_stride + u * 8) = pack8(v);
-    }
-    cluster_sync();  // (no block ends while another reads its shared memory)
+        for (int e = 0; e < 8; ++e) v[e] *= mul;
+        *reinterpret_cast<uint4*>((bf16*)out.x + ((kDKV ? sq.k0 : sq.q0) + first + r) * out.row_stride + w.h * out.head_stride + u * 8) = pack8(v);
+      };
+    };
+    auto all = [](int, int) { return 1.0f; };
+    merge_sums<HD>(ranks, sBig0, rank, n_big - first, (int)threadIdx.x, C::kThreads, all, put(kDKV ? p.dk : p.dq, p.a.scale));
+    if (kDKV) merge_sums<HD>(ranks, sSmall, rank, n_big - first, (int)threadIdx.x, C::kThreads, all, put(p.dv, 1.0f));
+    cluster_end();
   }
-  leave(warp, tmem, C::kColumns, abort_flag);
 }
 
 // kShared: walks are shared by clusters of `ranks` blocks.  The first `first` walks are those of one kind, the longer ones: 4 x 1 query, 4096 keys, 16 query
@@ -783,7 +858,9 @@ template <int HD, bool kShared>
 __global__ void __launch_bounds__(Bwd<HD>::kThreads, Bwd<HD>::kBlocksAnSm)
 ragged_bwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p, const unsigned first, const bool kv_first,
                      const int ranks) {
-  chain_wait();  // (D comes from the launch before)
+  // What the launch before leaves is D, waited for where it is read; that launch began when everything before it was over.  Without queries there is
+  // no such launch.
+  if (p.a.q_rows == 0) chain_wait();
   const unsigned i = kShared ? blockIdx.x / ranks : blockIdx.x;
   const int rank = kShared ? (int)(blockIdx.x % ranks) : 0;
   const unsigned nth = i < first ? i : i - first;
@@ -812,7 +889,7 @@ bool map_heads(CUtensorMap* tm, const hbp_heads& t, int64_t rows, int heads, int
 constexpr int kLeast = 8;
 int ranks_of(int64_t walks, int64_t at_a_time, int64_t tiles) {
   int r = 1;
-  while (r < 8 && 2 * walks * r <= at_a_time && 2 * r * kLeast <= tiles) r *= 2;
+  while (r < MOST_RANKS && 2 * walks * r <= at_a_time && 2 * r * kLeast <= tiles) r *= 2;
   return r;
 }
 template <typename... P, typename... A>
