@@ -13,8 +13,8 @@
 // Forward: a block owns 128 queries and walks over tiles of 64 keys with a running maximum and sum, one row per thread of four
 // warps.  Two buffers of scores, so that the next ones are formed under these exponentials.  The output stays in tensor memory; it is scaled
 // down only when a row's maximum has grown by more than 2^8 since the last time, which is rare (sums are float: 2^8 costs no
-// precision).  Two blocks share an SM.  2 x 4096 rows, causal: 16 heads of 128 134 us (1.03 PFLOP/s of the products that are needed), 16 of 64 113 us
-// (0.61).  Bound, at 64 channels, by the exponentials (512 clocks a tile and SM for 128 x 64 at 16 a clock; measured 670 in the loop), at 128
+// precision).  Two blocks share an SM.  2 x 4096 rows, causal: 16 heads of 128 127 us (1.08 PFLOP/s of the products that are needed), 16 of 64 111 us
+// (0.62).  Bound, at 64 channels, by the exponentials (512 clocks a tile and SM for 128 x 64 at 16 a clock; measured 670 in the loop), at 128
 // by what the products read from shared memory.  Tiles of 128 keys in one buffer: 150 and 132 us, the scores read twice from tensor memory 176
 // and 161.
 //
@@ -30,7 +30,8 @@
 // copies read and write 1400 (dK, dV) and 1150 (dQ) clocks' worth of shared memory a tile, of 1670 and 1420 measured; at 64 a tile's chain of
 // product, exponentials and product bounds it (2100 and 1630 clocks, two at a time).  HD = 64 with three buffers and one block an SM: 366 us; sixteen
 // columns a warp instead of 32: 308.
-// Few blocks with long walks are shared by clusters, in both passes (ranks_of below).
+// Few blocks with long walks are shared by clusters, in both passes (ranks_of below); the query heads of a key head share a block where queries are
+// few (packed_heads): single queries are bound by the keys' and values' bytes (16 x 1 query, 4096 keys, 4 key heads of 128: 4.9 TB/s).
 // All waits are bounded.
 #include "attention_ragged.cuh"
 #include "float_pairs.cuh"
@@ -236,7 +237,8 @@ __device__ __forceinline__ void merge_sums(uint32_t base, int rank, int there, i
 }
 template <int HD, typename Factor, typename Put>
 __device__ __forceinline__ void merge_sums(int ranks, uint32_t base, int rank, int there, int t, int threads, Factor factor, Put put) {
-  if (ranks == 2) merge_sums<HD, 2>(base, rank, there, t, threads, factor, put);
+  if (ranks == 1) merge_sums<HD, 1>(base, rank, there, t, threads, factor, put);
+  else if (ranks == 2) merge_sums<HD, 2>(base, rank, there, t, threads, factor, put);
   else if (ranks == 4) merge_sums<HD, 4>(base, rank, there, t, threads, factor, put);
   else merge_sums<HD, 8>(base, rank, there, t, threads, factor, put);
 }
@@ -258,13 +260,13 @@ struct Fwd {
   static constexpr int kSmem = kBig + 2 * kStages * kSmall + 256 + 1024;
 };
 
-// kShared: walks are shared by a cluster (a kernel of its own: in one, the others' took 119 us instead of 113, 2 x 4096 rows, 16 heads of 64).
+// kShared: walks are shared by a cluster; kPacked, of those: `pack` query heads are a block's rows, query by query (a kernel of its own: in one, the others' took 119 us instead of 113, 2 x 4096 rows, 16 heads of 64).
 // 128 registers (256 threads are told): at 132 a quarter of an SM holds three warps but not four, and when the second of two blocks ends first, a new one
 // has to wait for the other too (ragged batch of cross attention 31 against 36 us, 16 heads of 128 126 against 131).
-template <int HD, bool kShared>
+template <int HD, bool kShared, bool kPacked>
 __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p,
-                                                                       const int ranks_given) {
-  const int ranks = kShared ? ranks_given : 1;
+                                                                       const int ranks_given, const int pack_given) {
+  const int ranks = kShared ? ranks_given : 1, pack = kPacked ? pack_given : 1;
   using C = Fwd<HD>;
   constexpr int NS = C::kStages, NB = 2;
   const int rank = kShared ? (int)(blockIdx.x % ranks) : 0;
@@ -288,14 +290,14 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
 
   if (warp == 1) take(tmem_slot, 256);  // (first of all, so that the SM's second block begins 0.8 us earlier: 16 heads of 128, 126 against 127 us)
 
-  BlockOf w = block_at(kShared ? blockIdx.x / ranks : blockIdx.x, p.a.q_len, BIG, p.a.q_heads, true);
+  BlockOf w = block_at(kShared ? blockIdx.x / ranks : blockIdx.x, p.a.q_len, BIG, kPacked ? p.a.q_heads / pack : p.a.q_heads, true);
   const SeqPair sq = sequence_pair(p.a, w, true);
   const int q0 = w.blk * BIG;
   if (q0 >= sq.nq) {  // (all blocks of the cluster)
     give_back(warp, tmem_slot, 256);
     return;
   }
-  const int kh = w.h / (p.a.q_heads / p.a.kv_heads);
+  const int kh = kPacked ? w.h : w.h / (p.a.q_heads / p.a.kv_heads);
   const int shift = sq.nk - sq.nq;  // causal: query i sees keys 0 .. i + shift
   const int seen = p.a.causal ? min(sq.nk, min(q0 + BIG, sq.nq) + shift) : sq.nk;
   // this block's tiles: rank, rank + ranks, ...
@@ -308,8 +310,13 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     if (n_it > 0) {  // the first copies are under way while the others get ready
-      mbar_expect_tx(bQ, C::kBig);
-      for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sQ + r * 128, BIG, &m.q, bQ, w.h, (int)sq.q0 + q0 + r);
+      if (kPacked) {  // (one box of heads and queries; the rows behind hold anything)
+        mbar_expect_tx(bQ, HD * 2 * pack * p.a.q_len);
+        copy_rows<HD>(sQ, BIG, &m.q, bQ, w.h * pack, (int)sq.q0);
+      } else {
+        mbar_expect_tx(bQ, C::kBig);
+        for (int r = 0; r < BIG; r += SMALL) copy_rows<HD>(sQ + r * 128, BIG, &m.q, bQ, w.h, (int)sq.q0 + q0 + r);
+      }
       mbar_expect_tx(bKFull(0), C::kSmall);
       copy_rows<HD>(sK, SMALL, &m.k, bKFull(0), kh, (int)sq.k0 + rank * SMALL);
     }
@@ -384,7 +391,7 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
     }
     if (leader) tc_commit(bDone);
   } else {
-    const int quarter = warp & 3, row = quarter * 32 + lane, qrow = q0 + row;
+    const int quarter = warp & 3, row = quarter * 32 + lane, qrow = q0 + (kPacked ? row / pack : row);
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const float scale2 = fabsf(p.a.scale) * LOG2E;
     float top = -INFINITY;  // the reference of the sums, in units of log2
@@ -481,7 +488,7 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
       tc_fence_after();
       const float2 sums = floats_of(add2(sum0, sum1));
       const float total = sums.x + sums.y;
-      leave_sums<HD>(sK, n_it > 0, tO + lanes, row);
+      if (quarter * 32 < (sq.nq - q0) * pack) leave_sums<HD>(sK, n_it > 0, tO + lanes, row);
       asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(sQ + row * 8), "f"(top), "f"(total) : "memory");
     }
   }
@@ -490,8 +497,9 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
   if (kShared) {
     cluster_sync();
     const int rows = BIG / ranks, first = rank * rows, t = threadIdx.x;  // this block's share
-    float* factors = reinterpret_cast<float*>(aligned + BIG * 8);             // [row][16]: the blocks' factors; 1 / total (-1: nothing seen)
-    if (t < rows) {
+    const int there = min(rows, (sq.nq - q0) * pack - first);
+    float* factors = reinterpret_cast<float*>(aligned + BIG * 8);        // [row][16]: the blocks' factors; 1 / total (-1: nothing seen)
+    if (t < there) {
       float most = -INFINITY, total = 0.0f;
       float2 st[MOST_RANKS];
 #pragma unroll
@@ -505,17 +513,17 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
         factors[t * 16 + b] = f;
       }
       factors[t * 16 + MOST_RANKS] = total == 0.0f ? -1.0f : inverse(total);
-      if (q0 + first + t < sq.nq) p.lse[w.h * p.a.q_rows + sq.q0 + q0 + first + t] = log_sum(most, total);
+      p.lse[(w.h * pack + (first + t) % pack) * p.a.q_rows + sq.q0 + q0 + (first + t) / pack] = log_sum(most, total);
     }
     __syncthreads();
-    bf16* out = (bf16*)p.o.x + (sq.q0 + q0 + first) * p.o.row_stride + w.h * p.o.head_stride;
-    merge_sums<HD>(ranks, sK, rank, sq.nq - q0 - first, t, FWD_THREADS, [&](int r, int b) { return factors[r * 16 + b]; },
+    bf16* out = (bf16*)p.o.x + (sq.q0 + q0) * p.o.row_stride + (int64_t)(w.h * pack) * p.o.head_stride;
+    merge_sums<HD>(ranks, sK, rank, there, t, FWD_THREADS, [&](int r, int b) { return factors[r * 16 + b]; },
                    [&](int r, int u, float (&v)[8]) {
                      if (u * 8 >= p.a.head_dim) return;
                      const float inv = factors[r * 16 + MOST_RANKS];
 #pragma unroll
                      for (int e = 0; e < 8; ++e) v[e] = inv < 0.0f ? 0.0f : v[e] * inv;
-                     *reinterpret_cast<uint4*>(out + (int64_t)r * p.o.row_stride + u * 8) = pack8(v);
+                     *reinterpret_cast<uint4*>(out + (int64_t)((first + r) / pack) * p.o.row_stride + (int64_t)((first + r) % pack) * p.o.head_stride + u * 8) = pack8(v);
                    });
     cluster_end();
   }
@@ -868,15 +876,15 @@ ragged_bwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant
   else ragged_bwd_body<HD, false, kShared>(m, p, block_at(nth, p.a.q_len, BIG, p.a.q_heads, true), rank, ranks);
 }
 
-// Map {channel, head, row} of a [rows][heads][head_dim] tensor: boxes of 64 channels x 1 head x 64 rows.
-bool map_heads(CUtensorMap* tm, const hbp_heads& t, int64_t rows, int heads, int head_dim) {
+// Map {channel, head, row} of a [rows][heads][head_dim] tensor: boxes of 64 channels.
+bool map_heads(CUtensorMap* tm, const hbp_heads& t, int64_t rows, int heads, int head_dim, int box_heads = 1, int box_rows = SMALL) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   // (the stride of a dimension of one element is never used, but is checked all the same)
   const int64_t hs = heads > 1 ? t.head_stride : head_dim, rs = rows > 1 ? t.row_stride : head_dim;
   cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows};
   cuuint64_t strides[2] = {(cuuint64_t)hs * 2, (cuuint64_t)rs * 2};
-  cuuint32_t box[3] = {SUB, 1, SMALL}, estr[3] = {1, 1, 1};
+  cuuint32_t box[3] = {SUB, (cuuint32_t)box_heads, (cuuint32_t)box_rows}, estr[3] = {1, 1, 1};
   return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, t.x, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -891,6 +899,16 @@ int ranks_of(int64_t walks, int64_t at_a_time, int64_t tiles) {
   int r = 1;
   while (r < MOST_RANKS && 2 * walks * r <= at_a_time && 2 * r * kLeast <= tiles) r *= 2;
   return r;
+}
+// Forward: the query heads of a key head whose rows, of all its queries, are one tile's at most become the rows of one block, which reads the keys
+// and values once for all, where that makes the launch fit the chip at once or lets more blocks share a walk.  Packed against a block a head: 32 x 1 query, 1000 keys,
+// 32 heads on 4 of 128, 18.6 against 76 us; 16 x 1, 4096 keys, 16 on 4 of 128, 27 (4.9 TB/s) against 66; 8 x 4, 2048 keys, 12 on 4 of 64, 12 against 19.5; where neither
+// holds, 1 x 1, 300 keys, 4 on one of 64, 8.1 against 7.0.
+int packed_heads(const hbp_attention& a) {
+  const int group = a.q_heads / a.kv_heads;
+  if ((int64_t)a.q_len * group > SMALL) return 1;
+  const int64_t alone = blocks_of(a.q_len, BIG, a.q_heads, a.sequences), tiles = (a.kv_len + SMALL - 1) / SMALL;
+  return alone > 2 * 148 || ranks_of(alone / group, 2 * 148, tiles) > ranks_of(alone, 2 * 148, tiles) ? group : 1;
 }
 template <typename... P, typename... A>
 void launch_clusters(Launcher& lc, void (*kernel)(P...), int64_t blocks, int threads, size_t smem, int ranks, A&&... args) {
@@ -925,12 +943,16 @@ bool allow_smem(K kernel, int bytes, bool& done) {
 
 template <int HD>
 bool forward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
-  static PerDevice<bool> set, set_shared;
-  if (!allow_smem(ragged_fwd_tc_kernel<HD, false>, Fwd<HD>::kSmem, set.here()) || !allow_smem(ragged_fwd_tc_kernel<HD, true>, Fwd<HD>::kSmem, set_shared.here()))
+  static PerDevice<bool> set, set_shared, set_packed;
+  if (!allow_smem(ragged_fwd_tc_kernel<HD, false, false>, Fwd<HD>::kSmem, set.here()) ||
+      !allow_smem(ragged_fwd_tc_kernel<HD, true, false>, Fwd<HD>::kSmem, set_shared.here()) ||
+      !allow_smem(ragged_fwd_tc_kernel<HD, true, true>, Fwd<HD>::kSmem, set_packed.here()))
     return false;
-  const int64_t blocks = blocks_of(r.a.q_len, BIG, r.a.q_heads, r.a.sequences);
-  const int ranks = ranks_of(blocks, 2 * 148, (r.a.kv_len + SMALL - 1) / SMALL);
-  launch_clusters(lc, ranks > 1 ? ragged_fwd_tc_kernel<HD, true> : ragged_fwd_tc_kernel<HD, false>, blocks * ranks, FWD_THREADS, Fwd<HD>::kSmem, ranks, m, r, ranks);
+  const int pack = packed_heads(r.a);
+  const int64_t walks = blocks_of(r.a.q_len, BIG, r.a.q_heads / pack, r.a.sequences);
+  const int ranks = ranks_of(walks, 2 * 148, (r.a.kv_len + SMALL - 1) / SMALL);
+  const auto kernel = pack > 1 ? ragged_fwd_tc_kernel<HD, true, true> : ranks > 1 ? ragged_fwd_tc_kernel<HD, true, false> : ragged_fwd_tc_kernel<HD, false, false>;
+  launch_clusters(lc, kernel, walks * ranks, FWD_THREADS, Fwd<HD>::kSmem, ranks, m, r, ranks, pack);
   return true;
 }
 
@@ -951,7 +973,8 @@ bool backward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
 // A side without rows has no tensors: its maps are never used.
 bool maps(const RaggedAttn& r, bool back, RaggedMaps& m) {
   const hbp_attention& a = r.a;
-  if (a.q_len && !map_heads(&m.q, r.q, a.q_rows, a.q_heads, a.head_dim)) return false;
+  const int pack = back ? 1 : packed_heads(a);
+  if (a.q_len && !map_heads(&m.q, r.q, a.q_rows, a.q_heads, a.head_dim, pack, pack > 1 ? a.q_len : SMALL)) return false;
   if (a.q_len && back && !map_heads(&m.d_o, r.d_o, a.q_rows, a.q_heads, a.head_dim)) return false;
   return !a.kv_len || (map_heads(&m.k, r.k, a.kv_rows, a.kv_heads, a.head_dim) && map_heads(&m.v, r.v, a.kv_rows, a.kv_heads, a.head_dim));
 }

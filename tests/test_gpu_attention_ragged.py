@@ -451,3 +451,34 @@ def test_shared_walks_agree_bit_for_bit_and_keep_to_themselves(B, dtype, hd):
         assert bool((x[:at] == 7).all()) and bool((x[at + n:] == 7).all())
     check(lse[:, 3:75], tuple(y[:, 3:75] for y in want["lse"]), "lse")
     assert bool((lse[:, :3] == 7).all()) and bool((lse[:, 75:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hd", [64, 72, 128])
+@pytest.mark.parametrize("ql,kl,qh,kh", [([1], [70], 2, 1), ([1] * 5, [1, 64, 65, 300, 2000], 8, 2), ([4, 0, 1, 3], [200, 5, 0, 1300], 12, 4),
+                                         ([21, 20], [21, 700], 3, 1), ([16, 16], [90, 16], 4, 1), ([1, 1], [33, 1100], 64, 1), ([2, 1], [40, 3], 34, 1), ([7], [3], 5, 1),
+                                         ([1] * 40, [1 + 61 * i % 200 for i in range(40)], 8, 2), ([i % 4 for i in range(30)], [37 * i % 150 for i in range(30)], 12, 4),
+                                         ([1, 2, 1, 0], [4096, 100, 3000, 5], 16, 4), ([1] * 6, [300, 1, 64, 65, 0, 128], 64, 1),
+                                         ([21 - i % 3 for i in range(100)], [30 - i % 25 for i in range(100)], 3, 1), ([8] * 20, [1040 - 50 * i for i in range(20)], 16, 2)])
+def test_few_queries_of_many_heads_to_a_key_head(B, dtype, causal, hd, ql, kl, qh, kh):
+    """All query heads of a key head in one block, and the groups that are just too many for that."""
+    case(B, dtype, ql, kl, qh, kh, hd, causal)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("kv", [50, 1100])
+def test_single_queries_from_and_to_parts_of_larger_buffers(B, hd, kv):
+    n, qh, kh = 40, 8, 2
+    qkv = make(n, 2 * qh + 3, hd + 8, BF16, 1)
+    q = qkv[:, 1:2 * qh + 1:2, :hd]
+    k, v = make(n * kv, kh, hd, BF16, 2), make(n * kv, kh, hd, BF16, 3)
+    buf = torch.full((n, qh + 2, hd + 16), 7.0, dtype=BF16, device="cuda")
+    lse = torch.full((qh, n), 7.0, device="cuda")
+    o, _ = B.attention_forward(q, k, v, sequences=n, o=buf[:, 1:1 + qh, 8:8 + hd], lse=lse)
+    want = reference(q, k, v, torch.zeros_like(q), [1] * n, [kv] * n, True, hd ** -0.5)
+    check(o, want["o"], "o")
+    check(lse, want["lse"], "lse")
+    rest = buf.clone()
+    rest[:, 1:1 + qh, 8:8 + hd] = 7
+    assert bool((rest == 7).all())
