@@ -156,9 +156,9 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
   chain_wait();
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int rank = (int)(blockIdx.x % ranks);
-  BlockOf w = block_at(blockIdx.x / ranks, p.a.q_len, TILE, p.a.q_heads, true);
+  BlockOf w = block_at(blockIdx.x / ranks, p.q_walks, true);
   const SeqPair sq = sequence_pair(p.a, w, true);
-  const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
+  const int q0 = w.blk * TILE, kh = (int)p.by_group((uint32_t)w.h);
   if (q0 >= sq.nq) return;  // (all blocks of the cluster)
   const float* q = (const float*)p.q.x + sq.q0 * p.q.row_stride + w.h * p.q.head_stride;
   const float* k = (const float*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
@@ -305,7 +305,7 @@ __device__ __forceinline__ void ragged_dq(const RaggedAttn& p, BlockOf w) {
   float* sSt = sKV + 4 * TILE * LD;  // [key][query]
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const SeqPair sq = sequence_pair(p.a, w, true);
-  const int q0 = w.blk * TILE, kh = w.h / (p.a.q_heads / p.a.kv_heads);
+  const int q0 = w.blk * TILE, kh = (int)p.by_group((uint32_t)w.h);
   if (q0 >= sq.nq) return;
   const float* k = (const float*)p.k.x + sq.k0 * p.k.row_stride + kh * p.k.head_stride;
   const float* v = (const float*)p.v.x + sq.k0 * p.v.row_stride + kh * p.v.head_stride;
@@ -355,7 +355,7 @@ __device__ __forceinline__ void ragged_dkv(const RaggedAttn& p, const BlockOf w,
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   // (in the batch's order: with the longest first, the clusters of dK and dV and the blocks of dQ end less evenly, 128 against 122 us, 6 x 421 rows)
   const SeqPair sq = sequence_pair(p.a, w.b);
-  const int k0 = w.blk * TILE, group = p.a.q_heads / p.a.kv_heads;
+  const int k0 = w.blk * TILE, group = p.group;
   if (k0 >= sq.nk) return;  // (all blocks of the cluster)
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;
   const int first = p.a.causal ? max(0, k0 - shift) / TILE * TILE : 0;  // the first block of queries that sees key k0
@@ -431,8 +431,8 @@ template <int HD>
 __global__ void __launch_bounds__(THREADS) ragged_bwd_kernel(const __grid_constant__ RaggedAttn p, const unsigned kv_walks, const unsigned q_walks, const int ranks) {
   chain_wait();  // (D comes from the launch before)
   const unsigned kv_blocks = kv_walks * ranks;
-  if (blockIdx.x < kv_blocks) ragged_dkv<HD>(p, block_at(blockIdx.x / ranks, p.a.kv_len, TILE, p.a.kv_heads, false), (int)(blockIdx.x % ranks), ranks);
-  else if (blockIdx.x - kv_blocks < q_walks) ragged_dq<HD>(p, block_at(blockIdx.x - kv_blocks, p.a.q_len, TILE, p.a.q_heads, true));
+  if (blockIdx.x < kv_blocks) ragged_dkv<HD>(p, block_at(blockIdx.x / ranks, p.kv_walks, false), (int)(blockIdx.x % ranks), ranks);
+  else if (blockIdx.x - kv_blocks < q_walks) ragged_dq<HD>(p, block_at(blockIdx.x - kv_blocks, p.q_walks, true));
 }
 
 // drow[h][row] = sum over channels of d_o * o, `lanes` (a power of two, 16 bytes each) to a row of a head; neighbouring lanes take neighbouring
@@ -481,7 +481,8 @@ int ranks_of(int64_t walks, int64_t at_a_time, int64_t tiles) {
 }
 
 template <int HD>
-void forward_f32(Launcher& lc, const RaggedAttn& r) {
+void forward_f32(Launcher& lc, const RaggedAttn& given) {
+  const RaggedAttn r = with_walks(given, TILE);
   constexpr int kSmem = smem_of<HD>(5, 1);
   static PerDevice<bool> set;
   allow_smem(lc, ragged_fwd_kernel<HD>, kSmem, set.here());
@@ -490,7 +491,8 @@ void forward_f32(Launcher& lc, const RaggedAttn& r) {
   launch_chained(lc, ragged_fwd_kernel<HD>, dim3((unsigned)(blocks * ranks)), THREADS, kSmem, ranks, r, ranks);
 }
 template <int HD>
-void backward_f32(Launcher& lc, const RaggedAttn& r) {
+void backward_f32(Launcher& lc, const RaggedAttn& given) {
+  const RaggedAttn r = with_walks(given, TILE);
   constexpr int kSmem = smem_of<HD>(6, HD > 64 ? 1 : 2);
   static PerDevice<bool> set;
   allow_smem(lc, ragged_bwd_kernel<HD>, kSmem, set.here());

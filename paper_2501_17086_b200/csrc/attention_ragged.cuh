@@ -13,18 +13,25 @@ struct BlockOf {
 };
 // Heads are the fastest, so that blocks that run together read the same keys (the query heads of a group) and take equally long.
 // last_first: the blocks of the last rows, which see the most keys of a causal batch, come before the others.
-__device__ __forceinline__ BlockOf block_at(unsigned i, int longest, int tile, int heads, bool last_first) {
-  const unsigned n = (unsigned)(longest + tile - 1) / tile;
+__device__ __forceinline__ BlockOf block_at(unsigned i, const RaggedWalks& walks, bool last_first) {
   BlockOf w;
-  w.h = (int)(i % heads);
-  i /= heads;
-  const unsigned blk = i % n;
-  w.blk = (int)(last_first ? n - 1 - blk : blk);
-  w.b = (int)(i / n);
+  const unsigned rest = walks.by_heads(i), b = walks.by_blocks(rest), blk = rest - b * walks.blocks;
+  w.h = (int)(i - rest * walks.heads);
+  w.blk = (int)(last_first ? walks.blocks - 1 - blk : blk);
+  w.b = (int)b;
   return w;
 }
-__device__ __forceinline__ BlockOf block_of(int longest, int tile, int heads, bool last_first) {
-  return block_at(blockIdx.x, longest, tile, heads, last_first);
+// r with the walks of blocks of `tile` rows, `pack` query heads to a block.
+inline RaggedAttn with_walks(RaggedAttn r, int tile, int pack = 1) {
+  const auto walks = [&](int longest, int heads) {
+    const uint32_t n = (uint32_t)((longest + (int64_t)tile - 1) / tile);
+    return RaggedWalks{(uint32_t)heads, n, divider((uint32_t)heads), divider(n > 1 ? n : 1)};
+  };
+  r.q_walks = walks(r.a.q_len, r.a.q_heads / pack);
+  r.kv_walks = walks(r.a.kv_len, r.a.kv_heads);
+  r.group = r.a.q_heads / r.a.kv_heads;
+  r.by_group = divider((uint32_t)r.group);
+  return r;
 }
 
 struct SeqPair {

@@ -154,20 +154,26 @@ __device__ __forceinline__ void leave(int warp, uint32_t tmem, uint32_t columns,
 // along a row; rows behind the sequence and channels behind the head are left alone.
 template <int kUnits>
 __device__ __forceinline__ void store_staged(uint32_t tile, int row0, int unit0, bf16* base, int64_t row_stride, int rows_there, int head_dim, int lane) {
-  constexpr int kRows = 32 / kUnits;
-  const int u = unit0 + lane % kUnits;
+  constexpr int kRows = 32 / kUnits, kAtOnce = 4;
+  const int u = unit0 + lane % kUnits, first = row0 + lane / kUnits;
+  bf16* at = base + (int64_t)first * row_stride + u * 8;
 #pragma unroll
-  for (int r = lane / kUnits; r < 32; r += kRows) {
-    const int row = row0 + r;
-    if (row < rows_there && u * 8 < head_dim)
-      *reinterpret_cast<uint4*>(base + (int64_t)row * row_stride + u * 8) = ld_shared16(swz(tile + (u >> 3) * BIG * 128, row, u & 7));
+  for (int i = 0; i < kUnits; i += kAtOnce) {  // (32 rows are kUnits steps of kRows)
+    uint4 x[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) x[j] = ld_shared16(swz(tile + (u >> 3) * BIG * 128, first + (i + j) * kRows, u & 7));
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      if (first + (i + j) * kRows < rows_there && u * 8 < head_dim) *reinterpret_cast<uint4*>(at) = x[j];
+      at += kRows * row_stride;
+    }
   }
 }
 
 // ---- walks shared by a cluster: few blocks with long walks leave most of the chip idle.  The blocks of a cluster take the tiles of a walk in
 // turn; each leaves its sums in its shared memory, and each puts together those of all for its share of the rows, in the blocks' order.
 constexpr int MOST_RANKS = 8;
-__device__ __forceinline__ int tiles_of(int tiles, int rank, int ranks) { return ranks == 1 ? tiles : (tiles - rank + ranks - 1) / ranks; }
+__device__ __forceinline__ int tiles_of(int tiles, int rank, int ranks) { return (tiles - rank + ranks - 1) >> (__ffs(ranks) - 1); }
 // Rows of HD floats, their 16-byte units permuted among eight by the row: one row per lane is written without bank conflicts.
 template <int HD>
 __device__ __forceinline__ uint32_t sum_at(uint32_t base, int row, int unit) {
@@ -269,7 +275,7 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
   const int ranks = kShared ? ranks_given : 1, pack = kPacked ? pack_given : 1;
   using C = Fwd<HD>;
   constexpr int NS = C::kStages, NB = 2;
-  const int rank = kShared ? (int)(blockIdx.x % ranks) : 0;
+  const int rank = kShared ? (int)(blockIdx.x & (unsigned)(ranks - 1)) : 0;  // (a power of two of them)
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* aligned = smem_raw + (base - smem_u32(smem_raw));
@@ -290,14 +296,14 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
 
   if (warp == 1) take(tmem_slot, 256);  // (first of all, so that the SM's second block begins 0.8 us earlier: 16 heads of 128, 126 against 127 us)
 
-  BlockOf w = block_at(kShared ? blockIdx.x / ranks : blockIdx.x, p.a.q_len, BIG, kPacked ? p.a.q_heads / pack : p.a.q_heads, true);
+  BlockOf w = block_at(kShared ? blockIdx.x >> (__ffs(ranks) - 1) : blockIdx.x, p.q_walks, true);
   const SeqPair sq = sequence_pair(p.a, w, true);
   const int q0 = w.blk * BIG;
   if (q0 >= sq.nq) {  // (all blocks of the cluster)
     give_back(warp, tmem_slot, 256);
     return;
   }
-  const int kh = kPacked ? w.h : w.h / (p.a.q_heads / p.a.kv_heads);
+  const int kh = kPacked ? w.h : (int)p.by_group((uint32_t)w.h);
   const int shift = sq.nk - sq.nq;  // causal: query i sees keys 0 .. i + shift
   const int seen = p.a.causal ? min(sq.nk, min(q0 + BIG, sq.nq) + shift) : sq.nk;
   // this block's tiles: rank, rank + ranks, ...
@@ -473,13 +479,17 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
       const float total = sums.x + sums.y;
       const float inv = inverse(total);
 #pragma unroll 1
-      for (int c = 0; c < HD; c += 32) {
-        float o[32];
-        if (n_it > 0) tc_ld32(tO + lanes + c, o);
+      for (int c = 0; c < HD; c += 64) {
+        float o[64];
+        if (n_it > 0) {
+          tc_ld32_async(tO + lanes + c, o);
+          tc_ld32_async(tO + lanes + c + 32, o + 32);
+          tc_ld_wait();
+        }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = total == 0.0f ? 0.0f : o[i] * inv;
+        for (int i = 0; i < 64; ++i) o[i] = total == 0.0f ? 0.0f : o[i] * inv;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) st_shared16(swz(sQ + (c / SUB) * BIG * 128, row, (c % SUB) / 8 + u), pack8(o + 8 * u));
+        for (int u = 0; u < 8; ++u) st_shared16(swz(sQ + (c / SUB) * BIG * 128, row, u), pack8(o + 8 * u));
       }
       __syncwarp();
       store_staged<HD / 8>(sQ, quarter * 32, 0, (bf16*)p.o.x + (sq.q0 + q0) * p.o.row_stride + w.h * p.o.head_stride, p.o.row_stride, sq.nq - q0, p.a.head_dim, lane);
@@ -546,7 +556,8 @@ struct Bwd {
 };
 
 template <int HD, bool kDKV, bool kShared>
-__device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const RaggedAttn& p, BlockOf w, const int rank, const int ranks) {
+__device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const RaggedAttn& p, BlockOf w, const int rank, const int ranks_given) {
+  const int ranks = kShared ? ranks_given : 1;
   using C = Bwd<HD>;
   constexpr int NB = C::kBuffers, NS = C::kStages;
   extern __shared__ uint8_t smem_raw[];
@@ -576,16 +587,14 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
     chain_wait();
     return;
   }
-  const int group = p.a.q_heads / p.a.kv_heads;
   const int shift = p.a.causal ? sq.nk - sq.nq : sq.nk;  // query i sees keys 0 .. i + shift (capped by nk)
   // tiles of the other side: queries from the first that sees key big0 on; keys up to the last that the block's last query sees
   const int t_beg = kDKV && p.a.causal ? max(0, big0 - shift) / SMALL : 0;
   const int t_rows = kDKV ? n_small : p.a.causal ? min(n_small, min(big0 + BIG, n_big) + shift) : n_small;
   const int tiles = max(0, (max(t_rows, 0) + SMALL - 1) / SMALL - t_beg);
   // this block's tiles among those of all heads, one head after the other: rank, rank + ranks, ...
-  const int n_all = kDKV ? tiles * group : tiles, n_it = kShared ? tiles_of(n_all, rank, ranks) : n_all;
-  const int q_head0 = kDKV ? w.h * group : w.h, k_head = kDKV ? w.h : w.h / group;
-
+  const int n_all = kDKV ? tiles * p.group : tiles, n_it = kShared ? tiles_of(n_all, rank, ranks) : n_all;
+  const int q_head0 = kDKV ? w.h * p.group : w.h, k_head = kDKV ? w.h : (int)p.by_group((uint32_t)w.h);
 
   if (threadIdx.x == 0) {
     // probabilities, dS: eight warps; full: the copies, and what the copying warp adds itself; scores of dK, dV: the products, and the warp that
@@ -617,10 +626,12 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
 
   if (warp == 0) {
     bool ok = n_it > 0;
-    int tails = 0;
+    int tails = 0, at_tile = 0, head = kDKV ? q_head0 : k_head;
     chain_wait();
     for (int it = 0; it < n_it && ok; ++it) {
-      const int s = it % NS, nth = kShared ? rank + it * ranks : it, r0 = (t_beg + nth % tiles) * SMALL, head = kDKV ? q_head0 + nth / tiles : k_head;
+      at_tile += it == 0 ? rank : ranks;
+      for (; kDKV && at_tile >= tiles; at_tile -= tiles) ++head;
+      const int s = it % NS, r0 = (t_beg + at_tile) * SMALL;
       const uint32_t tile = sSmall + s * C::kStage;
       if (!wait_all(bFree(s), ((uint32_t)(it / NS) & 1u) ^ 1u, abort_flag, p.a.status)) { ok = false; break; }
       const int there = n_small - r0;
@@ -742,11 +753,14 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
       my_d = -p.drow[at];
     }
     bool ok = true;
+    int at_tile = 0;
     for (int it = group_id; it < n_it; it += C::kGroups) {
       const uint32_t parity = (uint32_t)(it / NB) & 1u;
       if (!wait_all(bScores(it % NB), parity, abort_flag, p.a.status)) { ok = false; break; }
       tc_fence_after();
-      const int c0 = (t_beg + (kShared ? rank + it * ranks : it) % tiles) * SMALL;
+      at_tile += it == group_id ? rank + group_id * ranks : C::kGroups * ranks;
+      while (kDKV && at_tile >= tiles) at_tile -= tiles;
+      const int c0 = (t_beg + at_tile) * SMALL;
       const uint32_t t = tmem + lanes + 128 * (it % NB) + ch * 32;
       const ulonglong2* st = reinterpret_cast<const ulonglong2*>(stats + (it % NS) * 2 * SMALL + ch * 32);  // (dK, dV: of four columns each)
       // does every row of the block see (is every row of the block seen by) the whole tile?
@@ -869,11 +883,11 @@ ragged_bwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant
   // What the launch before leaves is D, waited for where it is read; that launch began when everything before it was over.  Without queries there is
   // no such launch.
   if (p.a.q_rows == 0) chain_wait();
-  const unsigned i = kShared ? blockIdx.x / ranks : blockIdx.x;
-  const int rank = kShared ? (int)(blockIdx.x % ranks) : 0;
+  const unsigned i = kShared ? blockIdx.x >> (__ffs(ranks) - 1) : blockIdx.x;
+  const int rank = kShared ? (int)(blockIdx.x & (unsigned)(ranks - 1)) : 0;  // (a power of two of them)
   const unsigned nth = i < first ? i : i - first;
-  if ((i < first) == kv_first) ragged_bwd_body<HD, true, kShared>(m, p, block_at(nth, p.a.kv_len, BIG, p.a.kv_heads, false), rank, ranks);
-  else ragged_bwd_body<HD, false, kShared>(m, p, block_at(nth, p.a.q_len, BIG, p.a.q_heads, true), rank, ranks);
+  if ((i < first) == kv_first) ragged_bwd_body<HD, true, kShared>(m, p, block_at(nth, p.kv_walks, false), rank, ranks);
+  else ragged_bwd_body<HD, false, kShared>(m, p, block_at(nth, p.q_walks, true), rank, ranks);
 }
 
 // Map {channel, head, row} of a [rows][heads][head_dim] tensor: boxes of 64 channels.
@@ -942,13 +956,14 @@ bool allow_smem(K kernel, int bytes, bool& done) {
 }
 
 template <int HD>
-bool forward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
+bool forward(Launcher& lc, const RaggedAttn& given, const RaggedMaps& m) {
   static PerDevice<bool> set, set_shared, set_packed;
   if (!allow_smem(ragged_fwd_tc_kernel<HD, false, false>, Fwd<HD>::kSmem, set.here()) ||
       !allow_smem(ragged_fwd_tc_kernel<HD, true, false>, Fwd<HD>::kSmem, set_shared.here()) ||
       !allow_smem(ragged_fwd_tc_kernel<HD, true, true>, Fwd<HD>::kSmem, set_packed.here()))
     return false;
-  const int pack = packed_heads(r.a);
+  const int pack = packed_heads(given.a);
+  const RaggedAttn r = with_walks(given, BIG, pack);
   const int64_t walks = blocks_of(r.a.q_len, BIG, r.a.q_heads / pack, r.a.sequences);
   const int ranks = ranks_of(walks, 2 * 148, (r.a.kv_len + SMALL - 1) / SMALL);
   const auto kernel = pack > 1 ? ragged_fwd_tc_kernel<HD, true, true> : ranks > 1 ? ragged_fwd_tc_kernel<HD, true, false> : ragged_fwd_tc_kernel<HD, false, false>;
@@ -957,8 +972,9 @@ bool forward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
 }
 
 template <int HD>
-bool backward(Launcher& lc, const RaggedAttn& r, const RaggedMaps& m) {
+bool backward(Launcher& lc, const RaggedAttn& given, const RaggedMaps& m) {
   using C = Bwd<HD>;
+  const RaggedAttn r = with_walks(given, BIG);
   static PerDevice<bool> set, set_shared;
   if (!allow_smem(ragged_bwd_tc_kernel<HD, false>, C::kSmem, set.here()) || !allow_smem(ragged_bwd_tc_kernel<HD, true>, C::kSmem, set_shared.here())) return false;
   const int64_t kv = blocks_of(r.a.kv_len, BIG, r.a.kv_heads, r.a.sequences), q = blocks_of(r.a.q_len, BIG, r.a.q_heads, r.a.sequences);

@@ -357,11 +357,31 @@ void checkpoint_gelu(Launcher& lc, int dtype, int64_t rows, int d, void* z, int8
 void checkpoint_gelu_backward(Launcher& lc, int dtype, int64_t rows, int d, const int8_t* codes, const uint8_t* scales, void* dz);
 void checkpoint_gelu_again(Launcher& lc, int dtype, int64_t rows, int d, const int8_t* codes, const uint8_t* scales, void* act);
 // hbp_attention_forward / _backward (attention_ragged.cu); the arguments have been checked.
+// n / d for n < 2^31 without a division: the product with 2^(31 + s) / d, rounded up, s the least for which 2^s >= d (it is off by less than 2^s / 2^(31 + s)
+// of n, too little for the next whole number).
+struct Divider {
+  uint32_t m;
+  int shift;
+  __host__ __device__ uint32_t operator()(uint32_t n) const { return (uint32_t)(((uint64_t)n * m) >> shift); }
+};
+inline Divider divider(uint32_t d) {
+  int s = 0;
+  while (s < 31 && (1u << s) < d) ++s;
+  return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), 31 + s};
+}
+// The blocks of rows of one side: heads are the fastest, sequences the slowest.
+struct RaggedWalks {
+  uint32_t heads, blocks;
+  Divider by_heads, by_blocks;
+};
 struct RaggedAttn {
   hbp_attention a;
   hbp_heads q, k, v, o, d_o, dq, dk, dv;
   float* lse;   // [q_heads][q_rows]
   float* drow;  // [q_heads][q_rows]: sum of d_o * o
+  RaggedWalks q_walks, kv_walks;  // for the kernel's tiles
+  Divider by_group;               // by the query heads to a key head:
+  int group;
 };
 
 // ---------------------------------------------------------------- device math
