@@ -223,7 +223,7 @@ class Context:
         self.dtype = torch.float32 if cfg.dtype == HBP_F32 else torch.bfloat16
         self.block = _BLOCK_NAMES[cfg.block]
         self.steps = 2 * cfg.L if self.block == "preln_transformer" else cfg.L
-        nbytes = workspace_bytes(cfg, checkpointed)
+        nbytes = workspace_bytes(cfg, True) if checkpointed else workspace_bytes(cfg)
         self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         base = (self.workspace.data_ptr() + 255) // 256 * 256
         handle = C.c_void_p()
