@@ -23,10 +23,10 @@
 //            S^T = K Q^T, dP^T = V dO^T;  P^T = exp(S^T - lse), dS^T = P^T (dP^T - D);  dV += P^T dO, dK += dS^T Q
 //   dQ       128 queries; walks over tiles of 64 keys:  S = Q K^T, dP = dO V^T;  dQ += dS K
 // That is seven products where five would do with sums in memory that blocks add to in no fixed order.  Probabilities and dS are rounded to
-// bf16 as operands, and so is o, which D comes from: gradients are off by 2.4e-3 to 2.6e-3 in the norm, 1.7e-3 of it the output's own
+// bf16 as operands, and so is o, which D comes from: gradients are off by 2.4e-3 to 2.8e-3 in the norm, 1.7e-3 of it the output's own
 // rounding.  HD = 128 takes all of tensor memory: two buffers of scores, two groups of softmax warps that take the tiles in turn; HD = 64 runs
 // two blocks an SM, a buffer each, and overlaps the two halves of a tile (scores and probabilities, dP and dS) instead.  2 x 4096 rows, causal, of the
-// five products that are needed: 16 heads of 128 443 us (0.78 PFLOP/s), 16 of 64 295 us (0.59).  At 128 channels the products and the
+// five products that are needed: 16 heads of 128 440 us (0.78 PFLOP/s), 16 of 64 288 us (0.60).  At 128 channels the products and the
 // copies read and write 1400 (dK, dV) and 1150 (dQ) clocks' worth of shared memory a tile, of 1670 and 1420 measured; at 64 a tile's chain of
 // product, exponentials and product bounds it (2100 and 1630 clocks, two at a time).  HD = 64 with three buffers and one block an SM: 366 us; sixteen
 // columns a warp instead of 32: 308.
