@@ -482,3 +482,40 @@ def test_single_queries_from_and_to_parts_of_larger_buffers(B, hd, kv):
     rest = buf.clone()
     rest[:, 1:1 + qh, 8:8 + hd] = 7
     assert bool((rest == 7).all())
+
+
+def test_shared_walks_on_two_streams_and_replayed(B):
+    """Calls whose blocks wait for others of their cluster run beside each other, 64 and 128 channels wide, also from a graph with other offsets."""
+    calls = []
+    for hd, ql, kl, qh, kh in ((64, [40, 100], [1100, 1500], 8, 4), (128, [1, 2], [2000, 1030], 32, 8)):
+        q, d_o = make(sum(ql), qh, hd, BF16, hd), make(sum(ql), qh, hd, BF16, hd + 1)
+        k, v = make(sum(kl), kh, hd, BF16, hd + 2), make(sum(kl), kh, hd, BF16, hd + 3)
+        kw = dict(q_offsets=offsets(ql), kv_offsets=offsets(kl), q_len=max(ql), kv_len=max(kl))
+
+        def call(q=q, k=k, v=v, d_o=d_o, kw=kw):
+            o, lse = B.attention_forward(q, k, v, **kw)
+            return (o, lse, *B.attention_backward(d_o, q, k, v, o, lse, **kw))
+
+        calls.append((call, q, k, v, d_o, kw, ql, kl, hd))
+    first = [c[0]() for c in calls]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for i in range(20):
+        with torch.cuda.stream(side):
+            there = [calls[i % 2][0]() for _ in range(3)]
+        here = [calls[1 - i % 2][0]() for _ in range(3)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for x in there for a, b in zip(first[i % 2], x))
+        assert all(torch.equal(a, b) for x in here for a, b in zip(first[1 - i % 2], x))
+    for call, q, k, v, d_o, kw, ql, kl, hd in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = call()
+        for turned in (False, True):
+            ql, kl = (ql[::-1], kl[::-1]) if turned else (ql, kl)
+            kw["q_offsets"].copy_(offsets(ql))
+            kw["kv_offsets"].copy_(offsets(kl))
+            graph.replay()
+            want = reference(q, k, v, d_o, ql, kl, True, hd ** -0.5)
+            for name, x in zip(("o", "lse", "dq", "dk", "dv"), got):
+                check(x, want[name], name)
