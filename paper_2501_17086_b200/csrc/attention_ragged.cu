@@ -143,7 +143,7 @@ __device__ __forceinline__ float4 gather(cg::cluster_group& cluster, float* mine
 }
 
 // Few blocks with long walks leave most of the chip idle.  Then the tiles of a walk are dealt out to the `ranks` blocks of a cluster; each leaves its
-// sums in its shared memory, and each puts together those of all for its share of the rows, in the blocks' order (kRanks below).
+// sums in its shared memory, and each puts together those of all for its share of the rows, in the blocks' order (ranks_of below).
 
 // ------------------------------------------------------------------------------------------- forward
 template <int HD>
@@ -473,7 +473,7 @@ void allow_smem(Launcher& lc, K kernel, int smem, bool& done) {
 // Blocks that share each of `walks` walks of `tiles` tiles: twice as many for as long as blocks are fewer than the chip takes at a time and every
 // block has a tile.  Shared against one block a walk: 3 x 421 rows, 6 query heads on 2 key heads of 64, 39 against 45 us forward and 116 against 226
 // backward; 2 x 1024 rows, 8 on 2 of 128, backward 504 against 1044; 2048 rows, 8 heads of 64, forward 163 against 228; 5 x 77 rows, 4 heads of 64,
-// 12.6 against 16.4 and 21 against 27.
+// 12.6 against 16.4 and 21 against 27.  Backward up to 296 blocks instead of 148: 3 x 421 rows 131 against 112, 4 x 512 rows of 8 heads 198 against 175.
 int ranks_of(int64_t walks, int64_t at_a_time, int64_t tiles) {
   int r = 1;
   while (r < 8 && walks * r < at_a_time && 2 * r <= tiles) r *= 2;
