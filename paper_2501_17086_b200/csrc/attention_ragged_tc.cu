@@ -880,9 +880,9 @@ template <int HD, bool kShared>
 __global__ void __launch_bounds__(Bwd<HD>::kThreads, Bwd<HD>::kBlocksAnSm)
 ragged_bwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p, const unsigned first, const bool kv_first,
                      const int ranks) {
-  // What the launch before leaves is D, waited for where it is read; that launch began when everything before it was over.  Without queries there is
-  // no such launch.
-  if (p.a.q_rows == 0) chain_wait();
+  // What the launch before leaves is D, waited for where it is read; that launch began when everything before it was over.  Without queries (the
+  // longest sequence of them has none, whatever rows the tensors have) there is no such launch, and the offsets may still be on their way.
+  if (p.a.q_len == 0) chain_wait();
   const unsigned i = kShared ? blockIdx.x >> (__ffs(ranks) - 1) : blockIdx.x;
   const int rank = kShared ? (int)(blockIdx.x & (unsigned)(ranks - 1)) : 0;  // (a power of two of them)
   const unsigned nth = i < first ? i : i - first;

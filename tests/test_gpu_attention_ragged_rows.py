@@ -1,0 +1,43 @@
+"""Attention over ragged batches: rows that are in no sequence, and sequences without queries."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_attention_ragged import BF16, F32, check, make, offsets, reference
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2501_17086_b200 import binding
+    return binding
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_of_q_but_no_queries(B, dtype, hd, causal):
+    """A buffer for queries that holds none of them (q_len = 0): the gradients of the keys and values that are in a sequence are 0, the
+    others stay as they were.  The offsets come from the kernel just before."""
+    kl, at = [70, 0, 300, 1], 5
+    q, d_o, o = (make(40, 4, hd, dtype, s) for s in (0, 1, 2))
+    k, v = make(at + sum(kl) + 9, 2, hd, dtype, 3), make(at + sum(kl) + 9, 2, hd, dtype, 4)
+    lse = torch.zeros(4, 40, device="cuda")
+    there, none = offsets(kl, at), torch.zeros(len(kl) + 1, dtype=torch.int32, device="cuda")
+    big = torch.ones(1 << 26, device="cuda")
+    for _ in range(3):
+        q_off, k_off = torch.full_like(none, -7), torch.full_like(none, -7)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        dq, dk, dv = torch.full_like(q, 7.0), torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+        torch.cuda.synchronize()
+        big.mul_(1.0)
+        q_off.copy_(none)
+        torch.add(there, 0, out=k_off)
+        B.attention_backward(d_o, q, k, v, o, lse, q_offsets=q_off, kv_offsets=k_off, q_len=0, kv_len=300, causal=causal, dq=dq, dk=dk, dv=dv,
+                             status=status)
+        assert int(status) == 0 and bool((dq == 7).all())
+        for t in (dk, dv):
+            assert bool((t[at:at + sum(kl)] == 0).all())
+            assert bool((t[:at] == 7).all()) and bool((t[at + sum(kl):] == 7).all())
