@@ -214,7 +214,8 @@ __device__ __forceinline__ void merge_sums(uint32_t base, int rank, int there, i
     float4 x[NI][R][2];
 #pragma unroll
     for (int n = 0; n < NI; ++n) {
-      const int j = min(i + n * threads, n_units - 1);
+      const int j = i + n * threads;
+      if (j >= n_units) break;  // (every load's value is used: none is under way at the end)
 #pragma unroll
       for (int b = 0; b < R; ++b) {
 #pragma unroll
@@ -247,11 +248,6 @@ __device__ __forceinline__ void merge_sums(int ranks, uint32_t base, int rank, i
   else if (ranks == 2) merge_sums<HD, 2>(base, rank, there, t, threads, factor, put);
   else if (ranks == 4) merge_sums<HD, 4>(base, rank, there, t, threads, factor, put);
   else merge_sums<HD, 8>(base, rank, there, t, threads, factor, put);
-}
-// No block ends while another reads its shared memory (what was read has arrived; nothing that was written is handed over).
-__device__ __forceinline__ void cluster_end() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 // Nothing seen: sums of 0, outputs of 0 and a log-sum-exp of -infinity (a sum that is NaN stays NaN)
 __device__ __forceinline__ float inverse(float total) { return total > 0.0f ? 1.0f / total : total; }
@@ -535,7 +531,7 @@ __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_cons
                      for (int e = 0; e < 8; ++e) v[e] = inv < 0.0f ? 0.0f : v[e] * inv;
                      *reinterpret_cast<uint4*>(out + (int64_t)((first + r) / pack) * p.o.row_stride + (int64_t)((first + r) % pack) * p.o.head_stride + u * 8) = pack8(v);
                    });
-    cluster_end();
+    cluster_sync();  // (no block ends while another reads its shared memory)
   }
 }
 
@@ -870,7 +866,7 @@ __device__ __forceinline__ void ragged_bwd_body(const RaggedMaps& m, const Ragge
     auto all = [](int, int) { return 1.0f; };
     merge_sums<HD>(ranks, sBig0, rank, n_big - first, (int)threadIdx.x, C::kThreads, all, put(kDKV ? p.dk : p.dq, p.a.scale));
     if (kDKV) merge_sums<HD>(ranks, sSmall, rank, n_big - first, (int)threadIdx.x, C::kThreads, all, put(p.dv, 1.0f));
-    cluster_end();
+    cluster_sync();  // (no block ends while another reads its shared memory)
   }
 }
 

@@ -41,3 +41,22 @@ def test_rows_of_q_but_no_queries(B, dtype, hd, causal):
         for t in (dk, dv):
             assert bool((t[at:at + sum(kl)] == 0).all())
             assert bool((t[:at] == 7).all()) and bool((t[at + sum(kl):] == 7).all())
+
+
+@pytest.mark.parametrize("hd", [64, 80, 128])
+@pytest.mark.parametrize("ql,kl,qh,kh", [([100, 128], [2100, 2048], 8, 8), ([128], [4096], 16, 4), ([33, 1, 128], [1025, 3000, 64], 4, 4)])
+def test_merges_of_clusters_of_every_size(B, hd, ql, kl, qh, kh):
+    """Clusters of two, four and eight blocks whose shares of the rows come in no whole number of steps, calls on one another's heels."""
+    q, d_o = make(sum(ql), qh, hd, BF16, 1), make(sum(ql), qh, hd, BF16, 2)
+    k, v = make(sum(kl), kh, hd, BF16, 3), make(sum(kl), kh, hd, BF16, 4)
+    kw = dict(q_offsets=offsets(ql), kv_offsets=offsets(kl), q_len=max(ql), kv_len=max(kl), causal=True)
+    o, lse = B.attention_forward(q, k, v, **kw)
+    got = [(o, lse, *B.attention_backward(d_o, q, k, v, o, lse, **kw))]
+    for _ in range(20):
+        o, lse = B.attention_forward(q, k, v, **kw)
+        got.append((o, lse, *B.attention_backward(d_o, q, k, v, o, lse, **kw)))
+    want = reference(q, k, v, d_o, ql, kl, True, hd ** -0.5)
+    for name, x in zip(("o", "lse", "dq", "dk", "dv"), got[0]):
+        check(x, want[name], name)
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
