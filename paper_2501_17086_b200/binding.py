@@ -447,7 +447,7 @@ def attention_forward(q, k, v, sequences=None, q_len=None, kv_len=None, q_offset
                       o=None, lse=None, status=None):
     """softmax(scale q k^T) v over pairs of sequences: see hbp_attention_forward.  q [q_rows, q_heads, head_dim], k and v
     [kv_rows, kv_heads, head_dim]; returns o like q and lse [q_heads, q_rows] (float).  Without offsets the rows are ``sequences``
-    sequences of equal length; with them (int32 [sequences + 1], on the device) q_len / kv_len are the longest ones'.  scale:
+    sequences of equal length (q_len, kv_len; all rows, if not given: refused where they cannot be); with them (int32 [sequences + 1], on the device) q_len / kv_len are the longest ones'.  scale:
     head_dim ** -0.5 if not given."""
     return _calls.attention_forward(q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status, o, lse)
 

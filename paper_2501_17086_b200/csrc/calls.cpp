@@ -222,6 +222,7 @@ hbp_attention attention_of(Call& c, const at::Tensor& q, const at::Tensor& k, co
   auto length = [&](PyObject* o, const at::Tensor* t, int64_t rows, const char* what) {
     if (o != Py_None) return c.whole32(o);
     if (t) refuse(HBP_ERR_SHAPE, c.name, what);
+    if (sequences ? rows % sequences : rows) refuse(HBP_ERR_SHAPE, c.name, "the rows are no whole number of sequences of equal length");
     return c.narrow(sequences ? rows / sequences : 0);
   };
   s.q_len = length(a[1], off[0], s.q_rows, "q_len, the longest of the sequences, has to be given with q_offsets");

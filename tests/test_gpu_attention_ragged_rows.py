@@ -60,3 +60,18 @@ def test_merges_of_clusters_of_every_size(B, hd, ql, kl, qh, kh):
         check(x, want[name], name)
     for other in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+def test_rows_that_are_no_whole_number_of_sequences(B):
+    """Refused: the rows that are left over would be in no sequence.  With the length given they are meant to be."""
+    q, k = make(100, 4, 64, BF16, 0), make(99, 2, 64, BF16, 1)
+    o, lse = B.attention_forward(q, k, k, sequences=3, q_len=33)
+    for call in (lambda: B.attention_forward(q, k, k, sequences=3), lambda: B.attention_forward(k, k[:97], k[:97], sequences=3),
+                 lambda: B.attention_backward(q, q, k, k, o, lse, sequences=3), lambda: B.attention_forward(q, k, k, sequences=0),
+                 lambda: B.attention_forward(q, k, k, q_offsets=offsets([50, 50]), q_len=50)):
+        with pytest.raises(B.HbpError) as e:
+            call()
+        assert e.value.code == 2
+    B.attention_forward(k, k, k, sequences=3)
+    B.attention_forward(q[:0], k[:0], k[:0], sequences=0)
+    B.attention_forward(q, k, k, q_offsets=offsets([50, 40, 10]), q_len=50)
