@@ -374,8 +374,13 @@ typedef struct {
   int64_t q_rows, kv_rows;
   const int32_t *q_offsets, *kv_offsets;
   float scale;
+  int32_t fresh; /* of hbp_attention_fresh; 0 where callers know of no such thing */
   int32_t* status;
 } hbp_attention;
+
+/* Outputs that are new memory.  Of those, the rows that are in no sequence, or in none that is not skipped, become 0 (lse: -infinity) instead of being
+ * left alone. */
+typedef enum { HBP_FRESH_O = 1, HBP_FRESH_LSE = 2, HBP_FRESH_DQ = 4, HBP_FRESH_DK = 8, HBP_FRESH_DV = 16 } hbp_attention_fresh;
 
 /* o [q_rows][q_heads][head_dim] and lse [q_heads][q_rows] (float, natural logarithm), which the backward pass reads. */
 hbp_status hbp_attention_forward(const hbp_attention* a, const hbp_heads* q, const hbp_heads* k, const hbp_heads* v,

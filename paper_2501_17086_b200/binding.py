@@ -60,7 +60,7 @@ class hbp_rotary_spec(C.Structure):
                 ("trained_length", C.c_float), ("fast", C.c_float), ("slow", C.c_float), ("amplitude", C.c_float)]
 
 
-class hbp_attention(C.Structure):
+class hbp_attention(C.Structure):  # (``fresh``, the four bytes before ``status``, stays 0)
     _fields_ = [("dtype", C.c_int32), ("causal", C.c_int32), ("sequences", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("q_len", C.c_int32), ("kv_len", C.c_int32), ("q_rows", C.c_int64), ("kv_rows", C.c_int64),
                 ("q_offsets", C.c_void_p), ("kv_offsets", C.c_void_p), ("scale", C.c_float), ("status", C.c_void_p)]
@@ -448,13 +448,18 @@ def attention_forward(q, k, v, sequences=None, q_len=None, kv_len=None, q_offset
     """softmax(scale q k^T) v over pairs of sequences: see hbp_attention_forward.  q [q_rows, q_heads, head_dim], k and v
     [kv_rows, kv_heads, head_dim]; returns o like q and lse [q_heads, q_rows] (float).  Without offsets the rows are ``sequences``
     sequences of equal length (q_len, kv_len; all rows, if not given: refused where they cannot be); with them (int32 [sequences + 1], on the device) q_len / kv_len are the longest ones'.  scale:
-    head_dim ** -0.5 if not given."""
+    head_dim ** -0.5 if not given.
+
+    Rows in no sequence are left as they were in outputs that are given, and are 0 (lse: -infinity) in new ones, as are those of sequences that
+    are skipped for their offsets.  Those, and waits that ran out, are reported in ``status`` (int32 [1], zeroed by the caller) and nowhere else:
+    reading it is up to the caller, a call does not wait for the device."""
     return _calls.attention_forward(q, k, v, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status, o, lse)
 
 
 def attention_backward(d_o, q, k, v, o, lse, sequences=None, q_len=None, kv_len=None, q_offsets=None, kv_offsets=None, causal=True,
                        scale=None, dq=None, dk=None, dv=None, scratch=None, status=None):
-    """The gradients (dq, dk, dv) of attention_forward's q, k and v from that of its output: see hbp_attention_backward."""
+    """The gradients (dq, dk, dv) of attention_forward's q, k and v from that of its output: see hbp_attention_backward.  Rows in no
+    sequence and ``status`` as there."""
     return _calls.attention_backward(d_o, q, k, v, o, lse, sequences, q_len, kv_len, q_offsets, kv_offsets, causal, scale, status, dq, dk, dv,
                                      scratch)
 

@@ -154,6 +154,7 @@ __global__ void __launch_bounds__(THREADS) ragged_fwd_kernel(const __grid_consta
   float* sKV = sQ + TILE * LD;  // two stages of a key and a value tile: the next ones come while these are used
   float* sPt = sKV + 4 * TILE * LD;  // [key][query]
   chain_wait();
+  if (blockIdx.x >= p.pass_blocks) return clear_block(p, false, (int)(blockIdx.x - p.pass_blocks), THREADS);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int rank = (int)(blockIdx.x % ranks);
   BlockOf w = block_at(blockIdx.x / ranks, p.q_walks, true);
@@ -436,11 +437,12 @@ __global__ void __launch_bounds__(THREADS) ragged_bwd_kernel(const __grid_consta
 }
 
 // drow[h][row] = sum over channels of d_o * o, `lanes` (a power of two, 16 bytes each) to a row of a head; neighbouring lanes take neighbouring
-// heads of a row.
+// heads of a row.  (32 registers: at the 40 that clearing would take, 8 x 1024 rows of 12 heads cost a microsecond more.)
 template <typename T>
-__global__ void __launch_bounds__(256) row_dot_kernel(const __grid_constant__ RaggedAttn p, int lanes) {
+__global__ void __launch_bounds__(256, 8) row_dot_kernel(const __grid_constant__ RaggedAttn p, int lanes) {
   constexpr int V = 16 / (int)sizeof(T);
   chain_next();  // (the backward kernels read the sums behind a chain_wait)
+  if (blockIdx.x >= p.pass_blocks) return clear_block(p, true, (int)(blockIdx.x - p.pass_blocks), 256);
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
   const int lane = threadIdx.x & (lanes - 1);
   const int64_t row = i / p.a.q_heads;
@@ -455,6 +457,14 @@ __global__ void __launch_bounds__(256) row_dot_kernel(const __grid_constant__ Ra
   }
   for (int o = lanes / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (row < p.a.q_rows && lane == 0) p.drow[h * p.a.q_rows + row] = s;
+}
+
+// Where the pass itself has nothing to do
+__global__ void __launch_bounds__(256) clear_kernel(const __grid_constant__ RaggedAttn p, bool backward) { clear_block(p, backward, blockIdx.x, 256); }
+void clear_alone(Launcher& lc, const RaggedAttn& r, bool backward) {
+  clear_kernel<<<kClearers, 256, 0, lc.stream>>>(r, backward);
+  lc.count();
+  lc.check();
 }
 
 template <int HD>
@@ -482,13 +492,14 @@ int ranks_of(int64_t walks, int64_t at_a_time, int64_t tiles) {
 
 template <int HD>
 void forward_f32(Launcher& lc, const RaggedAttn& given) {
-  const RaggedAttn r = with_walks(given, TILE);
+  RaggedAttn r = with_walks(given, TILE);
   constexpr int kSmem = smem_of<HD>(5, 1);
   static PerDevice<bool> set;
   allow_smem(lc, ragged_fwd_kernel<HD>, kSmem, set.here());
   const int64_t blocks = blocks_of(r.a.q_len, TILE, r.a.q_heads, r.a.sequences);
   const int ranks = ranks_of(blocks, HD == 64 ? 2 * 148 : 148, (r.a.kv_len + TILE - 1) / TILE);
-  launch_chained(lc, ragged_fwd_kernel<HD>, dim3((unsigned)(blocks * ranks)), THREADS, kSmem, ranks, r, ranks);
+  r.pass_blocks = (uint32_t)(blocks * ranks);
+  launch_chained(lc, ragged_fwd_kernel<HD>, dim3((unsigned)(blocks * ranks) + (r.a.fresh ? kClearers : 0)), THREADS, kSmem, ranks, r, ranks);
 }
 template <int HD>
 void backward_f32(Launcher& lc, const RaggedAttn& given) {
@@ -502,14 +513,15 @@ void backward_f32(Launcher& lc, const RaggedAttn& given) {
   if (blocks) launch_chained(lc, ragged_bwd_kernel<HD>, dim3((unsigned)blocks), THREADS, kSmem, ranks, r, (unsigned)kv, (unsigned)q, ranks);
 }
 
-void row_dots(Launcher& lc, const RaggedAttn& r) {
-  if (r.a.q_rows == 0) return;
+void row_dots(Launcher& lc, RaggedAttn r) {
   const int v = r.a.dtype == HBP_F32 ? 4 : 8;
   int lanes = 1;
   while (lanes * v < r.a.head_dim) lanes *= 2;
   const int64_t blocks = (r.a.q_rows * r.a.q_heads * lanes + 255) / 256;
-  if (r.a.dtype == HBP_F32) row_dot_kernel<float><<<(unsigned)blocks, 256, 0, lc.stream>>>(r, lanes);
-  else row_dot_kernel<bf16><<<(unsigned)blocks, 256, 0, lc.stream>>>(r, lanes);
+  r.pass_blocks = (uint32_t)blocks;
+  const unsigned grid = (unsigned)blocks + (r.a.fresh ? kClearers : 0);
+  if (r.a.dtype == HBP_F32) row_dot_kernel<float><<<grid, 256, 0, lc.stream>>>(r, lanes);
+  else row_dot_kernel<bf16><<<grid, 256, 0, lc.stream>>>(r, lanes);
   lc.count();
   lc.check();
 }
@@ -523,7 +535,7 @@ hbp_status check_attention(const hbp_attention* a) {
   if (!a->q_offsets && (int64_t)a->sequences * a->q_len > a->q_rows) return HBP_ERR_SHAPE;
   if (!a->kv_offsets && (int64_t)a->sequences * a->kv_len > a->kv_rows) return HBP_ERR_SHAPE;
   if (a->q_len > a->q_rows || a->kv_len > a->kv_rows) return HBP_ERR_SHAPE;
-  if (!std::isfinite(a->scale)) return HBP_ERR_INVALID_ARG;
+  if (!std::isfinite(a->scale) || a->fresh & ~(HBP_FRESH_O | HBP_FRESH_LSE | HBP_FRESH_DQ | HBP_FRESH_DK | HBP_FRESH_DV)) return HBP_ERR_INVALID_ARG;
   if (((uintptr_t)a->q_offsets | (uintptr_t)a->kv_offsets | (uintptr_t)a->status) & 3u) return HBP_ERR_SHAPE;
   // (as many blocks of 64 rows as one grid holds)
   if (blocks_of(a->q_len, TILE, a->q_heads, a->sequences) > INT32_MAX / 2 || blocks_of(a->kv_len, TILE, a->kv_heads, a->sequences) > INT32_MAX / 2 ||
@@ -560,9 +572,11 @@ hbp_status hbp_attention_forward(const hbp_attention* a, const hbp_heads* q, con
                                  float* lse, void* cuda_stream) {
   hbp_status st = check_attention(a);
   if (st != HBP_OK) return st;
-  if (a->sequences == 0 || a->q_len == 0) return HBP_OK;
+  const bool nothing = a->sequences == 0 || a->q_len == 0;
+  const int fresh = rows_left_over(*a, a->q_rows, a->q_len) && a->q_rows ? a->fresh & (HBP_FRESH_O | HBP_FRESH_LSE) : 0;
+  if (nothing && !fresh) return HBP_OK;
   const hbp_heads* const qt[4] = {q, o, k, v};
-  st = check_heads(*a, qt, a->kv_len ? 4 : 2);  // (no keys at all: their tensors may be empty)
+  st = nothing ? check_heads(*a, qt + 1, 1) : check_heads(*a, qt, a->kv_len ? 4 : 2);  // (no keys at all: their tensors may be empty)
   if (st != HBP_OK || (st = check_output(*a, *o, a->q_rows, a->q_heads)) != HBP_OK) return st;
   if (!lse) return HBP_ERR_INVALID_ARG;
   if ((uintptr_t)lse & 3u) return HBP_ERR_SHAPE;
@@ -570,7 +584,13 @@ hbp_status hbp_attention_forward(const hbp_attention* a, const hbp_heads* q, con
   lc.stream = (cudaStream_t)cuda_stream;
   RaggedAttn r = {};
   r.a = *a;
-  r.q = *q; r.o = *o; r.lse = lse;
+  r.a.fresh = fresh;
+  r.o = *o; r.lse = lse;
+  if (nothing) {
+    clear_alone(lc, r, false);
+    return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
+  }
+  r.q = *q;
   if (a->kv_len) { r.k = *k; r.v = *v; }
   if (a->dtype == HBP_BF16) {
     if (!ragged_forward_tc(lc, r)) return lc.err == cudaSuccess ? HBP_ERR_UNSUPPORTED : HBP_ERR_CUDA;
@@ -595,27 +615,42 @@ hbp_status hbp_attention_backward(const hbp_attention* a, const hbp_heads* d_o, 
                                   void* scratch, size_t scratch_bytes, void* cuda_stream) {
   hbp_status st = check_attention(a);
   if (st != HBP_OK) return st;
-  if (a->sequences == 0 || (a->q_len == 0 && a->kv_len == 0)) return HBP_OK;
+  const bool nothing = a->sequences == 0 || (a->q_len == 0 && a->kv_len == 0);
+  const int fresh = (rows_left_over(*a, a->q_rows, a->q_len) && a->q_rows ? a->fresh & HBP_FRESH_DQ : 0) |
+                    (rows_left_over(*a, a->kv_rows, a->kv_len) && a->kv_rows ? a->fresh & (HBP_FRESH_DK | HBP_FRESH_DV) : 0);
+  if (nothing && !fresh) return HBP_OK;
   const hbp_heads* const qt[4] = {d_o, q, o, dq};
   const hbp_heads* const kt[4] = {k, v, dk, dv};
-  if (a->q_len && ((st = check_heads(*a, qt, 4)) != HBP_OK || (st = check_output(*a, *dq, a->q_rows, a->q_heads)) != HBP_OK)) return st;
-  if (a->kv_len && ((st = check_heads(*a, kt, 4)) != HBP_OK || (st = check_output(*a, *dk, a->kv_rows, a->kv_heads)) != HBP_OK ||
-                    (st = check_output(*a, *dv, a->kv_rows, a->kv_heads)) != HBP_OK))
-    return st;
+  const bool queries = !nothing && a->q_len, keys = !nothing && a->kv_len;
+  auto output = [&](const hbp_heads* t, int64_t rows, int heads) {
+    const hbp_status bad = check_heads(*a, &t, 1);
+    return bad != HBP_OK ? bad : check_output(*a, *t, rows, heads);
+  };
+  if (queries && (st = check_heads(*a, qt, 3)) != HBP_OK) return st;
+  if (keys && (st = check_heads(*a, kt, 2)) != HBP_OK) return st;
+  if ((queries || fresh & HBP_FRESH_DQ) && (st = output(dq, a->q_rows, a->q_heads)) != HBP_OK) return st;
+  if ((keys || fresh & HBP_FRESH_DK) && (st = output(dk, a->kv_rows, a->kv_heads)) != HBP_OK) return st;
+  if ((keys || fresh & HBP_FRESH_DV) && (st = output(dv, a->kv_rows, a->kv_heads)) != HBP_OK) return st;
   RaggedAttn r = {};
   r.a = *a;
-  if (a->q_len) {
+  r.a.fresh = fresh;
+  if (queries || fresh & HBP_FRESH_DQ) r.dq = *dq;
+  if (keys || fresh & HBP_FRESH_DK) r.dk = *dk;
+  if (keys || fresh & HBP_FRESH_DV) r.dv = *dv;
+  if (queries) {
     if (!lse) return HBP_ERR_INVALID_ARG;
     if (!scratch || ((uintptr_t)scratch & 15u) || scratch_bytes < (size_t)a->q_heads * a->q_rows * sizeof(float)) return HBP_ERR_WORKSPACE;
     if ((uintptr_t)lse & 3u) return HBP_ERR_SHAPE;
-    r.q = *q; r.o = *o; r.d_o = *d_o; r.dq = *dq;
+    r.q = *q; r.o = *o; r.d_o = *d_o;
     r.lse = const_cast<float*>(lse);
     r.drow = (float*)scratch;
   }
-  if (a->kv_len) { r.k = *k; r.v = *v; r.dk = *dk; r.dv = *dv; }
+  if (keys) { r.k = *k; r.v = *v; }
   Launcher lc;
   lc.stream = (cudaStream_t)cuda_stream;
-  if (a->q_len) row_dots(lc, r);
+  if (queries) row_dots(lc, r);
+  else if (fresh) clear_alone(lc, r, true);
+  if (nothing) return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
   if (a->dtype == HBP_BF16) {
     if (!ragged_backward_tc(lc, r)) return lc.err == cudaSuccess ? HBP_ERR_UNSUPPORTED : HBP_ERR_CUDA;
   } else if (a->head_dim <= 64) {

@@ -268,6 +268,7 @@ struct Fwd {
 template <int HD, bool kShared, bool kPacked>
 __global__ void __launch_bounds__(256, 2) ragged_fwd_tc_kernel(const __grid_constant__ RaggedMaps m, const __grid_constant__ RaggedAttn p,
                                                                        const int ranks_given, const int pack_given) {
+  if (blockIdx.x >= p.pass_blocks) return clear_block(p, false, (int)(blockIdx.x - p.pass_blocks), FWD_THREADS);
   const int ranks = kShared ? ranks_given : 1, pack = kPacked ? pack_given : 1;
   using C = Fwd<HD>;
   constexpr int NS = C::kStages, NB = 2;
@@ -959,11 +960,12 @@ bool forward(Launcher& lc, const RaggedAttn& given, const RaggedMaps& m) {
       !allow_smem(ragged_fwd_tc_kernel<HD, true, true>, Fwd<HD>::kSmem, set_packed.here()))
     return false;
   const int pack = packed_heads(given.a);
-  const RaggedAttn r = with_walks(given, BIG, pack);
+  RaggedAttn r = with_walks(given, BIG, pack);
   const int64_t walks = blocks_of(r.a.q_len, BIG, r.a.q_heads / pack, r.a.sequences);
   const int ranks = ranks_of(walks, 2 * 148, (r.a.kv_len + SMALL - 1) / SMALL);
   const auto kernel = pack > 1 ? ragged_fwd_tc_kernel<HD, true, true> : ranks > 1 ? ragged_fwd_tc_kernel<HD, true, false> : ragged_fwd_tc_kernel<HD, false, false>;
-  launch_clusters(lc, kernel, walks * ranks, FWD_THREADS, Fwd<HD>::kSmem, ranks, m, r, ranks, pack);
+  r.pass_blocks = (uint32_t)(walks * ranks);
+  launch_clusters(lc, kernel, walks * ranks + (r.a.fresh ? kClearers : 0), FWD_THREADS, Fwd<HD>::kSmem, ranks, m, r, ranks, pack);
   return true;
 }
 

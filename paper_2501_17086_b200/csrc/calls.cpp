@@ -246,12 +246,13 @@ PyObject* attention_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   wanted(n, 13, "attention_forward");
   Call c("attention_forward");
   const at::Tensor &q = c.tensor(a[0], "q is no tensor"), &k = c.tensor(a[1], "k is no tensor"), &v = c.tensor(a[2], "v is no tensor");
-  const hbp_attention s = attention_of(c, q, k, v, a + 3);
+  hbp_attention s = attention_of(c, q, k, v, a + 3);
   const at::Tensor o = c.output(a[11], q, "o is not like q");
   const at::Tensor* given = c.maybe(a[12], "lse is no tensor");
   if (given) lse_of(c, q, *given);
   const at::Tensor lse = given ? *given : at::empty({q.size(1), q.size(0)}, q.options().dtype(at::kFloat));
   const hbp_heads qh = c.heads(q), kh = c.heads(k), vh = c.heads(v), oh = c.heads(o);
+  s.fresh = (a[11] == Py_None ? HBP_FRESH_O : 0) | (given ? 0 : HBP_FRESH_LSE);
   check(hbp_attention_forward(&s, &qh, &kh, &vh, &oh, lse.data_ptr<float>(), c.stream()), "hbp_attention_forward");
   return two(o, lse);
   CALL_END
@@ -264,7 +265,7 @@ PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Call c("attention_backward");
   const at::Tensor &q = c.tensor(a[1], "q is no tensor"), &k = c.tensor(a[2], "k is no tensor"), &v = c.tensor(a[3], "v is no tensor");
   const at::Tensor &d_o = c.tensor(a[0], "d_o is no tensor"), &o = c.tensor(a[4], "o is no tensor"), &lse = c.tensor(a[5], "lse is no tensor");
-  const hbp_attention s = attention_of(c, q, k, v, a + 6);
+  hbp_attention s = attention_of(c, q, k, v, a + 6);
   c.alike(d_o, q, "d_o is not like q");
   c.alike(o, q, "o is not like q");
   lse_of(c, q, lse);
@@ -272,6 +273,7 @@ PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor* given = c.maybe(a[17], "scratch is no tensor");
   const at::Tensor scratch = given ? *given : at::empty_like(lse);
   const hbp_heads gh = c.heads(d_o), qh = c.heads(q), kh = c.heads(k), vh = c.heads(v), oh = c.heads(o), dqh = c.heads(dq), dkh = c.heads(dk), dvh = c.heads(dv);
+  s.fresh = (a[14] == Py_None ? HBP_FRESH_DQ : 0) | (a[15] == Py_None ? HBP_FRESH_DK : 0) | (a[16] == Py_None ? HBP_FRESH_DV : 0);
   check(hbp_attention_backward(&s, &gh, &qh, &kh, &vh, &oh, lse.data_ptr<float>(), &dqh, &dkh, &dvh, scratch.data_ptr(),
                                scratch.is_contiguous() ? scratch.nbytes() : 0, c.stream()),
         "hbp_attention_backward");

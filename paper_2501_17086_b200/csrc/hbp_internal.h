@@ -382,6 +382,7 @@ struct RaggedAttn {
   RaggedWalks q_walks, kv_walks;  // for the kernel's tiles
   Divider by_group;               // by the query heads to a key head:
   int group;
+  uint32_t pass_blocks;  // a launch's blocks behind these clear rows of fresh outputs
 };
 
 // ---------------------------------------------------------------- device math

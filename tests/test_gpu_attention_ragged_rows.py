@@ -75,3 +75,89 @@ def test_rows_that_are_no_whole_number_of_sequences(B):
     B.attention_forward(k, k, k, sequences=3)
     B.attention_forward(q[:0], k[:0], k[:0], sequences=0)
     B.attention_forward(q, k, k, q_offsets=offsets([50, 40, 10]), q_len=50)
+
+
+def spoil(*tensors):
+    """NaN in the memory that new tensors of these sizes will have."""
+    some = [torch.full(t.shape, math.nan, dtype=t.dtype, device="cuda") for t in tensors for _ in range(4)]
+    del some
+
+
+NEW = [([70, 0, 130], [70, 90, 131], 11, 19), ([3], [700], 0, 1), ([1] * 300, [2] * 300, 1, 0), ([0, 0], [0, 5], 40, 0)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("hd", [64, 40, 128])
+@pytest.mark.parametrize("ql,kl,at,more", NEW)
+def test_new_outputs_of_rows_in_no_sequence(B, dtype, hd, ql, kl, at, more):
+    """0, and a log-sum-exp of -infinity, before the first sequence and behind the last; the others as ever."""
+    rows = [at + sum(ql) + more, at + sum(kl) + more]
+    q, d_o = make(rows[0], 4, hd, dtype, 0), make(rows[0], 4, hd, dtype, 1)
+    k, v = make(rows[1], 2, hd, dtype, 2), make(rows[1], 2, hd, dtype, 3)
+    want = reference(q, k, v, d_o, ql, kl, True, hd ** -0.5, q_at=at, k_at=at)  # (0 outside)
+    kw = dict(q_offsets=offsets(ql, at), kv_offsets=offsets(kl, at), q_len=max(ql), kv_len=max(kl))
+    spoil(q, torch.empty(4, rows[0]))
+    o, lse = B.attention_forward(q, k, v, **kw)
+    spoil(q, k, v)
+    got = (o, lse, *B.attention_backward(d_o, q, k, v, o, lse, **kw))
+    for name, x in zip(("o", "lse", "dq", "dk", "dv"), got):
+        check(x, want[name], name)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_new_outputs_where_lengths_leave_rows_over(B, dtype):
+    q, k, v, d_o = (make(100, 2, 64, dtype, s) for s in range(4))
+    want = reference(q, k, v, d_o, [33, 33], [40, 40], True, 0.125)
+    kw = dict(sequences=2, q_len=33, kv_len=40)
+    spoil(q, torch.empty(2, 100))
+    o, lse = B.attention_forward(q, k, v, **kw)
+    spoil(q, k, v)
+    given = torch.full_like(k, 7.0)
+    got = (o, lse, *B.attention_backward(d_o, q, k, v, o, lse, dk=given, **kw))
+    assert bool((given[80:] == 7).all())  # what is given keeps its rows
+    given[80:] = 0
+    for name, x in zip(("o", "lse", "dq", "dk", "dv"), got):
+        check(x, want[name], name)
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    spoil(q, torch.empty(2, 100))
+    o, lse = B.attention_forward(q, k, v, q_offsets=none, kv_offsets=none, q_len=0, kv_len=0)  # no sequences at all
+    assert bool((o == 0).all()) and bool((lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("off", [[0, 40, 30, 90], [0, 40, 80, 101], [-3, 40, 80, 90], [0, 70, 80, 90], [90, 40, 60, 20]])
+@pytest.mark.parametrize("side", ["q", "kv"])
+def test_new_outputs_of_skipped_sequences(B, dtype, off, side):
+    """Bad offsets of either side: the sequence's rows of both are 0, those of the others what they are."""
+    q, k, v, d_o = (make(100, 2, 64, dtype, s) for s in range(4))
+    fine, bad = torch.tensor([0, 30, 60, 90], device="cuda", dtype=torch.int32), torch.tensor(off, device="cuda", dtype=torch.int32)
+    kw = dict(q_offsets=bad if side == "q" else fine, kv_offsets=fine if side == "q" else bad, q_len=50, kv_len=50)
+    full = lambda: torch.full_like(q, 0.0)  # noqa: E731
+    o, lse = full(), torch.full((2, 100), -math.inf, device="cuda")
+    want = [o, lse, full(), full(), full()]
+    B.attention_forward(q, k, v, o=o, lse=lse, **kw)
+    B.attention_backward(d_o, q, k, v, o, lse, dq=want[2], dk=want[3], dv=want[4], **kw)
+    spoil(q, lse)
+    o, lse = B.attention_forward(q, k, v, **kw)
+    spoil(q, k, v)
+    got = (o, lse, *B.attention_backward(d_o, q, k, v, o, lse, **kw))
+    for name, a, b in zip(("o", "lse", "dq", "dk", "dv"), got, want):
+        assert torch.equal(a, b), name
+
+
+def test_new_outputs_of_a_replayed_graph(B):
+    q, k, v, d_o = (make(200, 2, 64, BF16, s) for s in range(4))
+    off = offsets([100, 100])
+    kw = dict(q_offsets=off, kv_offsets=off, q_len=200, kv_len=200)
+    o, lse = B.attention_forward(q, k, v, **kw)
+    B.attention_backward(d_o, q, k, v, o, lse, **kw)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, lse = B.attention_forward(q, k, v, **kw)
+        got = (o, lse, *B.attention_backward(d_o, q, k, v, o, lse, **kw))
+    for at, lens in ((0, [100, 100]), (7, [90, 20]), (50, [0, 150])):
+        off.copy_(offsets(lens, at))
+        graph.replay()
+        want = reference(q, k, v, d_o, lens, lens, True, 0.125, q_at=at, k_at=at)
+        for name, x in zip(("o", "lse", "dq", "dk", "dv"), got):
+            check(x, want[name], name)

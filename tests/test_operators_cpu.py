@@ -130,3 +130,15 @@ def test_checkpoint_refusals(B):
     assert lib.hbp_checkpoint_load(1, 4, 64, P, P, None, 64, None) == INVALID
     assert lib.hbp_checkpoint_load(7, 4, 64, P, P, P, 64, None) == DTYPE
     assert lib.hbp_checkpoint_load(1, 0, 64, None, None, None, 64, None) == OK
+
+
+def test_fresh_outputs_are_named_by_known_bits(B):
+    """hbp_attention's `fresh` lies before `status` (its ctypes structure leaves the four bytes out)."""
+    for bits, code in ((1 << 5, INVALID), (-1, INVALID), (31, OK)):
+        for backward in (False, True):
+            a = B.hbp_attention(1, 1, 0, 4, 2, 64, 0, 0, 0, 0, None, None, 0.125, None)  # (no sequences, no rows: nothing to do)
+            C.c_int32.from_buffer(a, B.hbp_attention.status.offset - 4).value = bits
+            t = C.byref(B.hbp_heads(P, 256, 64))
+            got = (B.lib.hbp_attention_backward(C.byref(a), t, t, t, t, t, P, t, t, t, P, 1 << 20, None) if backward else
+                   B.lib.hbp_attention_forward(C.byref(a), t, t, t, t, P, None))
+            assert got == code, (bits, backward)
