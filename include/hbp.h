@@ -344,8 +344,9 @@ typedef struct {
  * `rows` rows each, in one launch.  inverse != 0: by the opposite angles, which is the gradient (same amplitude).  An output
  * may be its input (same pointer and strides); otherwise they must not overlap, nor may an output's own rows and heads.
  * The position of a row: positions[row] (device, int32 if position_bytes is 4, int64 if 8), or, where positions is NULL,
- * first + row % period (period 0: first + row).  Angles are whole-number fractions of a turn (off by |position| * 2^-62
- * turns), the rotation is in float, and rounded once to dtype.  head_dim up to 256. */
+ * first + row % period (period 0: first + row).  Angles are whole-number fractions of a turn, off by |position| * 2^-62
+ * turns (BY_PARTS: times fast / (fast - slow) on the ramp) and 2^-32 turns; sines, cosines and the rotation are in float, and rounded once to dtype.
+ * head_dim up to 256. */
 hbp_status hbp_rotary(const hbp_rotary_spec* spec, int32_t inverse, int32_t dtype, int64_t rows, int32_t q_heads, int32_t kv_heads,
                       int32_t head_dim, const void* positions, int32_t position_bytes, int64_t first, int64_t period,
                       const hbp_heads* q, const hbp_heads* q_out, const hbp_heads* k, const hbp_heads* k_out, void* cuda_stream);

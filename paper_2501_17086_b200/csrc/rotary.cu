@@ -1,9 +1,9 @@
 // Rotary positions on the queries and keys of an attention step (hbp_rotary).
 //
 // HBM-bound: every element is read and written once, and a pair costs 6 flops.  What costs more is everything around them, so
-//  - angles are whole-number fractions of a turn: position times f_i / 2 pi * 2^64, modulo 2^64.  That needs no reduction, is as exact far out as
-//    near (a float product pos * f loses all of its fraction at 2^17), and takes a few integer instructions where doubles took a
-//    conversion, a product, a rounding and a difference;
+//  - angles are whole-number fractions of a turn: position times f_i / 2 pi * 2^64, modulo 2^64.  That needs no reduction, is off by 2^-64 turns a
+//    position and 2^-33 turns (a float product pos * f loses all of its fraction at 2^17; a float fraction alone would be off by 2^-26), and takes a
+//    few integer instructions where doubles took a conversion, a product, a rounding and a difference;
 //  - they are shared by all heads of a row: a block forms cosines and sines of its rows once, in shared memory, rows fastest, since the lanes of a
 //    warp that read different frequencies from the constant bank would be served one after the other;
 //  - a thread keeps CV pairs of a row (two vectors of up to 16 bytes) and walks over heads: its cosines and sines stay in registers
@@ -52,9 +52,14 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
     else if (p.position_bytes == 8) pos = ((const int64_t*)p.positions)[row];
     else pos = p.first + (p.period ? row % p.period : row);
     for (int i = slot; i < kPairs; i += slots) {
-      const int32_t t = (int32_t)(((uint64_t)pos * p.turns[c * kPairs + i]) >> 32);  // of a turn, from -1/2 on
+      const int32_t t = (int32_t)(((uint64_t)pos * p.turns[c * kPairs + i] + 0x80000000u) >> 32);  // of a turn, from -1/2 on
+      const float f = (float)t;
       float sn, cs;
-      sincospif((float)t * 0x1p-31f, &sn, &cs);
+      sincospif(f * 0x1p-31f, &sn, &cs);
+      // what the float has lost of it, up to 2^-26 turns: an angle so small that it is its own sine
+      const float rest = (float)(t - (int32_t)f) * (3.14159265358979323846f * 0x1p-31f), s0 = sn;
+      sn = fmaf(rest, cs, sn);
+      cs = fmaf(-rest, s0, cs);
       table[(r * kPairs + i) * p.turn_chunks + c] = make_float2(p.amplitude * cs, p.amplitude * p.sign * sn);
     }
   }
@@ -166,16 +171,22 @@ void rotary(Launcher& lc, const hbp_rotary_spec& s, bool inverse, int dtype, int
             const hbp_heads& k, const hbp_heads& ko) {
   RotaryParams p;
   const int pairs = s.rotary_dim / 2;
-  const double pi2 = 6.283185307179586476925;
+  // In 64 binary digits (a double's 53 would be off by 2^-57 turns a position): base^(-2i/r) = 2^(i c), whose exponent is off by 2 |i c| 2^-64, which
+  // is less than 2^-64 of a turn whatever the base, since 2^-x x is below 0.54.  Eight at a time from one: a power takes as long as pow in double did.
+  typedef long double wide;
+  const wide pi2 = 6.283185307179586476925286766559L, c = -2.0L / s.rotary_dim * std::log2((wide)s.base);
+  wide low[8], high = 1.0L;
+  for (int i = 0; i < 8 && i < pairs; ++i) low[i] = std::exp2(c * i);
   for (int i = 0; i < pairs; ++i) {
-    double f = std::pow((double)s.base, -2.0 * i / s.rotary_dim);
+    if (i && i % 8 == 0) high = std::exp2(c * i);
+    wide f = high * low[i % 8];
     if (s.scaling == HBP_ROTARY_LINEAR) f /= s.factor;
     if (s.scaling == HBP_ROTARY_BY_PARTS) {
-      double w = ((double)s.trained_length * f / pi2 - s.slow) / ((double)s.fast - s.slow);
-      w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
-      f *= w + (1.0 - w) / s.factor;
+      wide w = ((wide)s.trained_length * f / pi2 - s.slow) / ((wide)s.fast - s.slow);
+      w = w < 0.0L ? 0.0L : w > 1.0L ? 1.0L : w;
+      f *= w + (1.0L - w) / s.factor;
     }
-    p.turns[i] = (uint64_t)std::llrint(std::ldexp(f / pi2, 62)) << 2;  // (below 1/6 of a turn; a double has no more digits)
+    p.turns[i] = (uint64_t)(int64_t)(f * (18446744073709551616.0L / pi2) + 0.5L);  // (below 1/6 of 2^64)
   }
   p.amplitude = s.amplitude;
   p.sign = inverse ? -1.0f : 1.0f;
