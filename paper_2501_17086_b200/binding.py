@@ -71,8 +71,8 @@ ROTARY_SCALINGS = {"none": 0, "linear": 1, "by_parts": 2}
 
 
 def _load():
-    if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_calls.so")):
-        raise ImportError(f"{LIB_PATH} or _calls.so beside it is missing: build it with `python -m paper_2501_17086_b200.build` "
+    if not os.path.exists(LIB_PATH):
+        raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2501_17086_b200.build` "
                           "(the library has no fallback path)")
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
@@ -129,9 +129,23 @@ def _load():
 
 lib = _load()
 
-from . import _calls  # noqa: E402 (needs the library above; no fallback here either)
 
-_calls.set_error(HbpError)
+class _NoCalls:
+    """In the place of the extension module where that cannot be loaded: contexts do without it, the short calls say why they cannot."""
+
+    def __init__(self, why):
+        self.why = why
+
+    def __getattr__(self, name):
+        raise ImportError(f"{name} needs _calls.so beside {LIB_PATH}: build it with `python -m paper_2501_17086_b200.build` "
+                          f"(there is no fallback path; {self.why})")
+
+
+try:
+    from . import _calls  # noqa: E402 (needs the library above)
+    _calls.set_error(HbpError)
+except ImportError as e:
+    _calls = _NoCalls(e)
 
 
 def status_string(code: int) -> str:

@@ -2,6 +2,7 @@
 headers) next to this file; no GPU needed."""
 from __future__ import annotations
 
+import importlib.metadata
 import os
 import subprocess
 import sys
@@ -12,13 +13,21 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhbp.so")
 CALLS = os.path.join(HERE, "_calls.so")
+CALLS_FOR = os.path.join(HERE, "_build", "calls.for")  # what the extension module was built against
 SOURCES = ["hbp_api.cu", "gemm_simt.cu", "gemm_tc.cu", "gemm_f32.cu", "gemm_parts.cu", "gemm_cell.cu", "few_rows.cu", "scan.cu", "scan_static.cu", "scan_ring.cu", "attention.cu", "attention_tc.cu", "rnn.cu", "rnn_persistent.cu", "rnn_cluster.cu", "cell_cluster.cu", "gru.cu", "lstm.cu", "diag.cu", "rotary.cu",
            "checkpoint.cu", "attention_ragged.cu", "attention_ragged_tc.cu"]
 
 
+def _built_for() -> str:
+    return f"torch {importlib.metadata.version('torch')}, python {sys.version}"
+
+
 def _stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(CALLS):
+    if not os.path.exists(LIB) or not os.path.exists(CALLS) or not os.path.exists(CALLS_FOR):
         return True
+    with open(CALLS_FOR) as f:
+        if f.read() != _built_for():
+            return True
     t = min(os.path.getmtime(LIB), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "hbp.h")]
     return any(os.path.getmtime(d) > t for d in deps)
@@ -34,8 +43,8 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
               "-Xcompiler", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
     if verbose:
         common += ["-Xptxas", "-v"]
-    procs = [("calls.cpp", _compile_calls(obj_dir))]
-    objs = []
+    calls = _compile_calls(obj_dir)
+    procs, objs = [], []
     for src in SOURCES:
         obj = os.path.join(obj_dir, src.replace(".cu", ".o"))
         objs.append(obj)
@@ -51,7 +60,14 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     if failed:
         raise RuntimeError("nvcc failed")
     subprocess.check_call([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", LIB] + objs + ["-lcudart"])
+    out, _ = calls.communicate()
+    if out.strip():
+        print(out, file=sys.stderr)
+    if calls.returncode != 0:  # (the library is there: contexts work without the extension module)
+        raise RuntimeError("g++ failed: no extension module for the short calls")
     _link_calls(obj_dir)
+    with open(CALLS_FOR, "w") as f:
+        f.write(_built_for())
     return LIB
 
 
