@@ -46,6 +46,17 @@ void check(hbp_status st, const char* where) {
   throw Refused();
 }
 
+// A call of the library without Python's lock: a launch waits where the device's queue is full.  (The entries throw nothing; their arguments have been
+// read from the tensors before, which the caller holds.)
+template <typename... P, typename... A>
+hbp_status unlocked(hbp_status (*call)(P...), A... args) {
+  hbp_status st;
+  Py_BEGIN_ALLOW_THREADS
+  st = call(args...);
+  Py_END_ALLOW_THREADS
+  return st;
+}
+
 // One call: its name, and the device that all of its tensors are on.
 struct Call {
   const char* name;
@@ -185,7 +196,7 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int32_t type = c.dtype(q);
   const at::Tensor qo = c.output(a[15], q, "q_out is not like q"), ko = k ? c.output(a[16], *k, "k_out is not like k") : at::Tensor();
   const hbp_heads qoh = c.heads(qo), koh = k ? c.heads(ko) : hbp_heads{};
-  check(hbp_rotary(&s, c.truth(a[14]), type, rows, c.narrow(q.size(1)), k ? c.narrow(k->size(1)) : 0, c.narrow(head_dim), pos ? pos->data_ptr() : nullptr,
+  check(unlocked(hbp_rotary, &s, c.truth(a[14]), type, rows, c.narrow(q.size(1)), k ? c.narrow(k->size(1)) : 0, c.narrow(head_dim), pos ? pos->data_ptr() : nullptr,
                    size, c.whole(a[3]), c.whole(a[4]), &qh, &qoh, &kh, &koh, c.stream()),
         "hbp_rotary");
   if (k) return two(qo, ko);
@@ -253,7 +264,7 @@ PyObject* attention_forward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor lse = given ? *given : at::empty({q.size(1), q.size(0)}, q.options().dtype(at::kFloat));
   const hbp_heads qh = c.heads(q), kh = c.heads(k), vh = c.heads(v), oh = c.heads(o);
   s.fresh = (a[11] == Py_None ? HBP_FRESH_O : 0) | (given ? 0 : HBP_FRESH_LSE);
-  check(hbp_attention_forward(&s, &qh, &kh, &vh, &oh, lse.data_ptr<float>(), c.stream()), "hbp_attention_forward");
+  check(unlocked(hbp_attention_forward, &s, &qh, &kh, &vh, &oh, lse.data_ptr<float>(), c.stream()), "hbp_attention_forward");
   return two(o, lse);
   CALL_END
 }
@@ -274,7 +285,7 @@ PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor scratch = given ? *given : at::empty_like(lse);
   const hbp_heads gh = c.heads(d_o), qh = c.heads(q), kh = c.heads(k), vh = c.heads(v), oh = c.heads(o), dqh = c.heads(dq), dkh = c.heads(dk), dvh = c.heads(dv);
   s.fresh = (a[14] == Py_None ? HBP_FRESH_DQ : 0) | (a[15] == Py_None ? HBP_FRESH_DK : 0) | (a[16] == Py_None ? HBP_FRESH_DV : 0);
-  check(hbp_attention_backward(&s, &gh, &qh, &kh, &vh, &oh, lse.data_ptr<float>(), &dqh, &dkh, &dvh, scratch.data_ptr(),
+  check(unlocked(hbp_attention_backward, &s, &gh, &qh, &kh, &vh, &oh, lse.data_ptr<float>(), &dqh, &dkh, &dvh, scratch.data_ptr(),
                                scratch.is_contiguous() ? scratch.nbytes() : 0, c.stream()),
         "hbp_attention_backward");
   return three(dq, dk, dv);
@@ -316,7 +327,7 @@ PyObject* checkpoint_store(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int64_t ld = c.apart(x);
   const int32_t type = c.dtype(x);
   const Kept k = kept(c, x, a[1], a[2]);
-  check(hbp_checkpoint_store(type, x.size(0), c.narrow(x.size(1)), x.data_ptr(), ld, codes_of(k), scales_of(k), c.stream()), "hbp_checkpoint_store");
+  check(unlocked(hbp_checkpoint_store, type, x.size(0), c.narrow(x.size(1)), x.data_ptr(), ld, codes_of(k), scales_of(k), c.stream()), "hbp_checkpoint_store");
   return two(k.codes, k.scales);
   CALL_END
 }
@@ -334,7 +345,7 @@ PyObject* checkpoint_load(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (given && given->sizes() != codes.sizes()) refuse(HBP_ERR_SHAPE, c.name, "out is not like codes");
   const at::Tensor out = given ? *given : at::empty(codes.sizes(), codes.options().dtype(c.truth(a[2]) ? at::kFloat : at::kBFloat16));
   const int64_t ld = c.apart(out);
-  check(hbp_checkpoint_load(c.dtype(out), out.size(0), c.narrow(out.size(1)), codes_of(k), scales_of(k), out.data_ptr(), ld, c.stream()), "hbp_checkpoint_load");
+  check(unlocked(hbp_checkpoint_load, c.dtype(out), out.size(0), c.narrow(out.size(1)), codes_of(k), scales_of(k), out.data_ptr(), ld, c.stream()), "hbp_checkpoint_load");
   return THPVariable_Wrap(out);
   CALL_END
 }
@@ -350,7 +361,7 @@ PyObject* checkpoint_gelu(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor act = a[1] == Py_None ? packed_like(z) : c.output(a[1], z, "act is not like z");
   const int64_t lda = c.apart(act);
   const Kept k = kept(c, z, a[2], a[3]);
-  check(hbp_checkpoint_gelu(type, z.size(0), c.narrow(z.size(1)), z.data_ptr(), ldz, act.data_ptr(), lda, codes_of(k), scales_of(k), c.stream()),
+  check(unlocked(hbp_checkpoint_gelu, type, z.size(0), c.narrow(z.size(1)), z.data_ptr(), ldz, act.data_ptr(), lda, codes_of(k), scales_of(k), c.stream()),
         "hbp_checkpoint_gelu");
   return three(act, k.codes, k.scales);
   CALL_END
@@ -370,7 +381,7 @@ PyObject* checkpoint_gelu_backward(PyObject*, PyObject* const* a, Py_ssize_t n) 
   const at::Tensor dz = a[4] == Py_None ? packed_like(g) : c.output(a[4], g, "dz is not like d_act");
   const bool with_act = a[5] != Py_None || c.truth(a[3]);
   const at::Tensor act = !with_act ? at::Tensor() : a[5] == Py_None ? packed_like(g) : c.output(a[5], g, "act is not like d_act");
-  check(hbp_checkpoint_gelu_backward(type, g.size(0), c.narrow(g.size(1)), codes_of(k), scales_of(k), g.data_ptr(), ldg, dz.data_ptr(), c.apart(dz),
+  check(unlocked(hbp_checkpoint_gelu_backward, type, g.size(0), c.narrow(g.size(1)), codes_of(k), scales_of(k), g.data_ptr(), ldg, dz.data_ptr(), c.apart(dz),
                                      with_act ? act.data_ptr() : nullptr, with_act ? c.apart(act) : 0, c.stream()),
         "hbp_checkpoint_gelu_backward");
   return with_act ? two(dz, act) : THPVariable_Wrap(dz);

@@ -1,0 +1,49 @@
+"""What the short calls owe the program around them: other threads, and automatic differentiation."""
+import threading
+import time
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2501_17086_b200 import binding
+    return binding
+
+
+def test_other_threads_run_while_a_launch_waits(B):
+    """A second and a half of work in front, and more launches than a queue holds: a call waits, the interpreter does not."""
+    x = torch.randn(32, 256, device="cuda")
+    codes, scales = B.checkpoint_store(x)
+    torch.cuda._sleep(1000)
+    torch.cuda.synchronize()
+    t = time.perf_counter()
+    torch.cuda._sleep(100_000_000)
+    torch.cuda.synchronize()
+    a_second = int(100_000_000 / (time.perf_counter() - t))
+    gaps, stop = [0.0], threading.Event()
+
+    def watch():
+        last = time.perf_counter()
+        while not stop.is_set():
+            time.sleep(0.001)
+            now = time.perf_counter()
+            gaps[0] = max(gaps[0], now - last)
+            last = now
+
+    watcher = threading.Thread(target=watch)
+    watcher.start()
+    time.sleep(0.05)
+    torch.cuda._sleep(3 * a_second // 2)
+    t = time.perf_counter()
+    for _ in range(4000):
+        B.checkpoint_store(x, codes=codes, scales=scales)
+    waited = time.perf_counter() - t
+    stop.set()
+    watcher.join()
+    torch.cuda.synchronize()
+    assert waited > 1.0  # (the queue was full)
+    assert gaps[0] < 0.5 * waited, (gaps[0], waited)
