@@ -434,7 +434,8 @@ def compare(a, b, segments=1):
 # ---- a decoder's step on its own: rotary positions, attention over ragged batches, activations in 8 bits --------------------
 # These calls are a launch or two of some microseconds; what is around them - checks, new outputs, pointers, the stream - is done by the
 # extension module built beside the library (csrc/calls.cpp).  Tensors are those of the current device; work goes to its current
-# stream.
+# stream.  Nothing is recorded for automatic differentiation: gradients are calls of their own, and a tensor that asks for gradients is
+# refused where they are being recorded (not under torch.no_grad(), nor inside an autograd.Function).
 def rotary_spec(rotary_dim, base=10000.0, layout="half", scaling="none", factor=1.0, trained_length=0.0, fast=32.0, slow=1.0,
                 amplitude=1.0) -> hbp_rotary_spec:
     return hbp_rotary_spec(_choice(ROTARY_LAYOUTS, layout), _choice(ROTARY_SCALINGS, scaling), rotary_dim, base, factor, trained_length, fast,

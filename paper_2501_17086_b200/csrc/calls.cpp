@@ -6,6 +6,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -70,6 +71,9 @@ struct Call {
   }
   const at::Tensor* maybe(PyObject* o, const char* what) { return o == Py_None ? nullptr : &tensor(o, what); }
   const at::Tensor& on(const at::Tensor& t) {
+    // (what comes back has no gradient: without a word the step's parameters would be short of it)
+    if (t.requires_grad() && at::GradMode::is_enabled())
+      refuse(HBP_ERR_UNSUPPORTED, name, "a tensor asks for gradients, which are calls of their own here: torch.no_grad(), or an autograd.Function around them");
     const int at = t.is_cuda() ? (int)t.get_device() : -1;
     if (!any) {
       device = at;

@@ -47,3 +47,35 @@ def test_other_threads_run_while_a_launch_waits(B):
     torch.cuda.synchronize()
     assert waited > 1.0  # (the queue was full)
     assert gaps[0] < 0.5 * waited, (gaps[0], waited)
+
+
+def test_tensors_that_ask_for_gradients(B):
+    """Refused where gradients are recorded, wherever they stand; taken under no_grad and inside an autograd.Function, which brings the backward call."""
+    q = torch.randn(40, 2, 64, device="cuda")
+    k, v = torch.randn_like(q), torch.randn_like(q).requires_grad_()
+    for call in (lambda: B.attention_forward(q, k, v), lambda: B.rotary(v), lambda: B.rotary(q, v), lambda: B.attention_forward(q, k, k, o=v)):
+        with pytest.raises(B.HbpError) as e:
+            call()
+        assert e.value.code == 6
+        with torch.no_grad():
+            call()
+
+    class Attend(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v):
+            o, lse = B.attention_forward(q, k, v)
+            ctx.save_for_backward(q, k, v, o, lse)
+            return o
+
+        @staticmethod
+        def backward(ctx, d_o):
+            q, k, v, o, lse = ctx.saved_tensors
+            return B.attention_backward(d_o.contiguous(), q, k, v, o, lse)
+
+    v = torch.randn(40, 2, 64, device="cuda").requires_grad_()
+    w = torch.randn_like(q)
+    o = Attend.apply(q, k, v)
+    o.backward(w)
+    with torch.no_grad():
+        o, lse = B.attention_forward(q, k, v)
+        assert torch.equal(v.grad, B.attention_backward(w, q, k, v, o, lse)[2])

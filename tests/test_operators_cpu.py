@@ -142,3 +142,22 @@ def test_fresh_outputs_are_named_by_known_bits(B):
             got = (B.lib.hbp_attention_backward(C.byref(a), t, t, t, t, t, P, t, t, t, P, 1 << 20, None) if backward else
                    B.lib.hbp_attention_forward(C.byref(a), t, t, t, t, P, None))
             assert got == code, (bits, backward)
+
+
+def test_tensors_that_ask_for_gradients_are_refused(B):
+    """Where gradients are recorded; elsewhere the next check speaks (here that of the device)."""
+    import torch
+    x, plain = torch.zeros(4, 2, 64, requires_grad=True), torch.zeros(4, 2, 64)
+    m, codes, scales = torch.zeros(4, 64, requires_grad=True), torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4, 2, dtype=torch.uint8)
+    calls = [lambda: B.rotary(x), lambda: B.attention_forward(x, plain, plain), lambda: B.attention_backward(x, x, x, x, x, x), lambda: B.checkpoint_store(m),
+             lambda: B.checkpoint_gelu(m), lambda: B.checkpoint_gelu_backward(m, codes, scales)]
+    for call in calls:
+        with pytest.raises(B.HbpError) as e:
+            call()
+        assert e.value.code == UNSUPPORTED
+        with torch.no_grad(), pytest.raises(B.HbpError) as e:
+            call()
+        assert e.value.code == INVALID
+    with torch.no_grad(), pytest.raises(B.HbpError) as e:
+        B.rotary(plain, plain)
+    assert e.value.code == INVALID
