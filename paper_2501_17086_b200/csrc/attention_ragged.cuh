@@ -117,19 +117,34 @@ __device__ __forceinline__ void clear_side(const hbp_attention& a, bool keys, co
     if (keys) end = beg + len;
     return q && k;
   };
-  int64_t beg, end;
-  bool fine = true;  // (then the offsets do not decrease, and all between the first and the last is in a sequence)
-  const int64_t first = off ? off[0] : 0, last = off ? off[n] : (int64_t)n * longest;
-  for (int b = lane; b < n; b += 32) fine = taken(b, beg, end) && fine;
-  if (n > 0 && __all_sync(0xffffffffu, fine)) {
-    for (int64_t row = part; row < first; row += parts) clear(row);
-    for (int64_t row = last + part; row < rows; row += parts) clear(row);
-    return;
-  }
-  for (int64_t row = part; row < rows; row += parts) {
-    bool in = false;
-    for (int b = lane; b < n; b += 32) in = in || (taken(b, beg, end) && row >= beg && row < end);
-    if (!__any_sync(0xffffffffu, in)) clear(row);
+  // is a row of from .. to - 1 in a sequence that is taken?
+  auto overlap = [&](int64_t from, int64_t to) {
+    bool any = false;
+#pragma unroll 4
+    for (int b = lane; b < n; b += 32) {
+      int64_t beg, end;
+      any = (taken(b, beg, end) && beg < to && end > from && beg < end) || any;
+    }
+    return __any_sync(0xffffffffu, any) != 0;
+  };
+  auto clear_range = [&](int64_t from, int64_t to, int at, int step) {
+    from = from < 0 ? 0 : from;
+    to = to > rows ? rows : to;
+    if (from >= to) return;
+    const bool some = overlap(from, to);  // (only where offsets decrease somewhere)
+    for (int64_t row = from + at; row < to; row += step)
+      if (!some || !overlap(row, row + 1)) clear(row);
+  };
+  // A row in no sequence that is taken lies before the first offset, behind the last, or between those of a sequence that is skipped.
+  clear_range(0, off ? off[0] : 0, part, parts);
+  clear_range(off ? off[n] : (int64_t)n * longest, rows, part, parts);
+  for (int64_t b0 = (int64_t)part * 32; b0 < n; b0 += (int64_t)parts * 32) {
+    int64_t beg, end;
+    unsigned skipped = __ballot_sync(0xffffffffu, b0 + lane < n && !taken((int)b0 + lane, beg, end));
+    for (; skipped; skipped &= skipped - 1) {
+      const int b = (int)b0 + __ffs((int)skipped) - 1;
+      clear_range(off ? off[b] : (int64_t)b * longest, off ? off[b + 1] : (int64_t)(b + 1) * longest, 0, 1);
+    }
   }
 }
 // This block's share of a launch's clearing, `block` of kClearers (a call, so that the registers are those of the passes)

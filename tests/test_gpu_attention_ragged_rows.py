@@ -161,3 +161,28 @@ def test_new_outputs_of_a_replayed_graph(B):
         want = reference(q, k, v, d_o, lens, lens, True, 0.125, q_at=at, k_at=at)
         for name, x in zip(("o", "lse", "dq", "dk", "dv"), got):
             check(x, want[name], name)
+
+
+@pytest.mark.parametrize("off", [[0, 500, 480, 700, 1500, 1490, 1600, 2400], [900, 1300, 1250, 100, 500, 500, 3000, 2999], [5, 20, 21, 22, 23, 24, 25, 30]])
+@pytest.mark.parametrize("many", [False, True])
+def test_new_outputs_of_many_sequences_some_of_them_skipped(B, off, many):
+    """Rows in no sequence that is taken are 0, wherever the offsets go; more sequences than a launch's warps have lanes."""
+    if many:
+        off = off + [off[-1] + i // 20 for i in range(1, 2000 * 20)]
+    rows = 2600
+    q, d_o = make(rows, 2, 8, F32, 1), make(rows, 2, 8, F32, 2)
+    o32 = torch.tensor(off, device="cuda", dtype=torch.int32)
+    kw = dict(q_offsets=o32, kv_offsets=o32, q_len=450, kv_len=450)
+    taken = torch.zeros(rows, dtype=torch.bool)
+    for a, b in zip(off, off[1:]):
+        if 0 <= a <= b <= rows and b - a <= 450:
+            taken[a:b] = True
+    spoil(q, torch.empty(2, rows))
+    o, lse = B.attention_forward(q, q, q, **kw)
+    spoil(q, q, q)
+    grads = B.attention_backward(d_o, q, q, q, o, lse, **kw)
+    taken = taken.cuda()
+    assert bool((lse[:, ~taken] == -math.inf).all()) and bool(torch.isfinite(lse[:, taken]).all())
+    for x in (o, *grads):
+        assert bool((x[~taken] == 0).all()) and bool(torch.isfinite(x).all())
+    assert bool((o[taken] != 0).any(-1).all()) if bool(taken.any()) else True

@@ -79,3 +79,41 @@ def test_tensors_that_ask_for_gradients(B):
     with torch.no_grad():
         o, lse = B.attention_forward(q, k, v)
         assert torch.equal(v.grad, B.attention_backward(w, q, k, v, o, lse)[2])
+
+
+def test_calls_of_several_threads(B):
+    """Four threads, each on its own stream, all operators at once: what one thread alone gets."""
+    x = torch.randn(200, 256, device="cuda").bfloat16()
+    q = torch.randn(300, 4, 64, device="cuda")
+
+    def calls():
+        act, codes, scales = B.checkpoint_gelu(x)
+        out = [act, codes, scales, B.checkpoint_gelu_backward(x, codes, scales)]
+        for t in (q, q.bfloat16()):
+            a, b = B.rotary(t, t.clone(), period=100)
+            o, lse = B.attention_forward(a, b, t, sequences=3)
+            out += [a, b, o, lse, *B.attention_backward(t, a, b, t, o, lse, sequences=3)]
+        return out
+
+    alone = calls()
+    torch.cuda.synchronize()
+    results, errors = [None] * 4, []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(20):
+                    results[i] = calls()
+            stream.synchronize()
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for r in results:
+        assert all(torch.equal(a, b) for a, b in zip(alone, r))
