@@ -7,13 +7,14 @@
 // HBM-bound, if the arithmetic stays out of the way: at 6.5 TB/s an SM has 27 instruction slots for each bf16 value of GELU's forward
 // pass.  So whole numbers are rounded and widened by adding 1.5 * 2^23 (conversions run at an eighth of the rate),
 // magnitudes of bf16 pairs are compared two at a time, float arithmetic is done on pairs (one instruction for two values), and
-// erfc(x) of bf16 values is e^(-x^2) times a polynomial in t = 1 / (1 + p x) without a constant term, the form of 7.1.26 in Abramowitz and
-// Stegun, "Handbook of Mathematical Functions" (erff alone takes some 25 instructions); its exponential is GELU's density as well: one ex2 and one
-// reciprocal serve gelu and gelu' together.  7.1.26 itself is off by up to 1.5e-7, which is 0.2 % of erfc at z = -5 and 1 % at -8; half a step of bf16 is
-// 0.4 %.  So p and the coefficients, one more than there, are those for which the larger of (error of erfc / 2) / 6e-8 and (error relative to erfc) / 1e-4 is
-// least over 0 <= x <= 9.4 (a linear programme for each p): 0.88.
-// 8192 x 4096 bf16, us (of what a copy of the same bytes takes): store 18.5 (0.84), load 18.5 (0.84), GELU 28.9 (0.89), its backward
-// pass with gelu 39.0 (0.92).  With erff, conversions and one value at a time: 24.6, 24.8, 40.6, 57.4.
+// erfc(x) is e^(-x^2) times a polynomial in t = 1 / (1 + p x) without a constant term, the form of 7.1.26 in Abramowitz and Stegun, "Handbook of
+// Mathematical Functions" (erff alone takes some 25 instructions); its exponential is GELU's density as well: one ex2 and one reciprocal serve gelu and
+// gelu' together.  7.1.26 itself is off by up to 1.5e-7, which is 0.2 % of erfc at z = -5 and 1 % at -8; half a step of bf16 is 0.4 %.  So for bf16 p and
+// the coefficients, one more than there, are those for which the larger of (error of erfc / 2) / 6e-8 and (error relative to erfc) / 1e-4 is least over
+// 0 <= x <= 9.4 (a linear programme for each p): 0.88.  Float takes ten coefficients and accurate exponentials and reciprocals.
+// 8192 x 4096, us (of what a copy of the same bytes takes): bf16 store 18.4 (0.84), load 18.5 (0.84), GELU 28.9 (0.89), its backward pass with gelu 38.9
+// (0.93); float 28.7 (0.90), 28.9 (0.89), 55.4 (0.83), 68.9 (0.97; with erfcf 71.7 and 90.8).  bf16 with erff, conversions and one value at a time:
+// 24.6, 24.8, 40.6, 57.4.
 // A thread moves kBatch vectors of 16 bytes, all loads before the first use.  A group is 4 (bf16) or 8 (float) neighbouring lanes, its
 // maximum 2 or 3 shuffles.  (kBatch 1, 2, 4: store 22.6, 18.5, 18.7; GELU 32.7, 28.9, 30.0; float 8192 x 1024 stored 12.6, 10.3, 10.3.)
 #include "float_pairs.cuh"
@@ -42,25 +43,36 @@ struct CheckpointParams {
 
 // gelu(z) and gelu'(z) of two values; every rounding is written out, so that no call's other outputs change them.  `tail` is the normal
 // distribution's beyond |z|, half of erfc(|z| / sqrt 2): taken as it is below zero, where 1/2 less what erf gives would cancel (4 % of gelu at -5).
-__device__ __forceinline__ void gelu_one(float z, float& act, float& slope) {
-  const float tail = __fmul_rn(0.5f, erfcf(__fmul_rn(fabsf(z), 0.70710678118654752440f)));
-  const float phi = z < 0.0f ? tail : __fsub_rn(1.0f, tail);
-  act = __fmul_rn(z, phi);
-  slope = fmaf(__fmul_rn(z, expf(__fmul_rn(__fmul_rn(-0.5f, z), z))), 0.39894228040143267794f, phi);
-}
-__device__ __forceinline__ void gelu_pair(float2 z, float2& act, float2& slope, float) {
-  gelu_one(z.x, act.x, slope.x);
-  gelu_one(z.y, act.y, slope.y);
-}
 __device__ __forceinline__ float one_from_zero_on(float z) {
   float b;
   asm("set.ge.f32.f32 %0, %1, 0f00000000;" : "=f"(b) : "f"(z));
   return b;
 }
+// From the tail and e = e^(-z^2 / 2).  Both are of |z| and b - tail, b = 1 from 0 on and else 0: gelu as it is, the slope but for its sign.
+__device__ __forceinline__ void gelu_from(float2 zf, f32x2 size, f32x2 tail, f32x2 e, float2& act, float2& slope) {
+  const f32x2 b = pair_of(one_from_zero_on(zf.x), one_from_zero_on(zf.y)), phi = fma2(tail, both(-1.0f), b);
+  act = floats_of(mul2(size, phi));
+  slope = floats_of(mul2(fma2(mul2(size, e), both(0.39894228040143267794f), phi), fma2(b, both(2.0f), both(-1.0f))));
+}
+__device__ __forceinline__ void gelu_pair(float2 zf, float2& act, float2& slope, float) {
+  const f32x2 size = pair_of(fabsf(zf.x), fabsf(zf.y));
+  const float2 arg = floats_of(mul2(mul2(size, both(-0.5f)), size)), den = floats_of(fma2(size, both(0.3889087439f), both(1.0f)));
+  const f32x2 e = pair_of(expf(arg.x), expf(arg.y)), t = pair_of(__frcp_rn(den.x), __frcp_rn(den.y));  // t = 1 / (1 + 0.55 |z| / sqrt 2)
+  // tail / e, to 9e-9 of itself up to |z| = 13.5 (interpolated at the Chebyshev nodes of t, relative to its values)
+  f32x2 q = fma2(t, both(0.02973128855f), both(-0.172106415f));
+  q = fma2(q, t, both(0.3993062079f));
+  q = fma2(q, t, both(-0.437952131f));
+  q = fma2(q, t, both(0.19097054f));
+  q = fma2(q, t, both(-0.05208843574f));
+  q = fma2(q, t, both(0.1025155559f));
+  q = fma2(q, t, both(0.1291147918f));
+  q = fma2(q, t, both(0.1553640366f));
+  q = fma2(q, t, both(0.1551445723f));
+  gelu_from(zf, size, mul2(mul2(q, t), e), e, act, slope);
+}
 __device__ __forceinline__ void gelu_pair(float2 zf, float2& act, float2& slope, bf16) {
-  const f32x2 z = pair_of(zf.x, zf.y);
-  const float2 arg = floats_of(mul2(mul2(z, z), both(-0.72134752044448170368f)));
-  const float2 den = floats_of(fma2(pair_of(fabsf(zf.x), fabsf(zf.y)), both(0.28991378f), both(1.0f)));
+  const f32x2 size = pair_of(fabsf(zf.x), fabsf(zf.y));
+  const float2 arg = floats_of(mul2(mul2(size, size), both(-0.72134752044448170368f))), den = floats_of(fma2(size, both(0.28991378f), both(1.0f)));
   float2 ef, tf;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ef.x) : "f"(arg.x));  // e^(-z^2 / 2)
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ef.y) : "f"(arg.y));
@@ -73,12 +85,7 @@ __device__ __forceinline__ void gelu_pair(float2 zf, float2& act, float2& slope,
   q = fma2(q, t, both(0.1820728296f));
   q = fma2(q, t, both(0.0998823909f));
   q = fma2(q, t, both(0.1169299858f));
-  const f32x2 tail = mul2(mul2(q, t), e);
-  // Both are of |z| and b - tail, b = 1 from 0 on and else 0: gelu as it is, the slope but for its sign
-  const f32x2 b = pair_of(one_from_zero_on(zf.x), one_from_zero_on(zf.y)), size = pair_of(fabsf(zf.x), fabsf(zf.y));
-  const f32x2 phi = fma2(tail, both(-1.0f), b);
-  act = floats_of(mul2(size, phi));
-  slope = floats_of(mul2(fma2(mul2(size, e), both(0.39894228040143267794f), phi), fma2(b, both(2.0f), both(-1.0f))));
+  gelu_from(zf, size, mul2(mul2(q, t), e), e, act, slope);
 }
 
 // Bits of the largest magnitude of a vector, as a float's
