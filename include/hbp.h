@@ -361,9 +361,11 @@ hbp_status hbp_context_rotary(hbp_ctx* ctx, const hbp_rotary_spec* spec, int64_t
  *  heads     query head h reads key / value head h / (q_heads / kv_heads); q_heads is a multiple of kv_heads.
  *  offsets   device int32 [sequences + 1]: sequence b is rows offsets[b] .. offsets[b + 1] - 1 of the tensors; q_len (kv_len) is then
  *            the longest of them.  NULL: all sequences are q_len (kv_len) long, one after the other.  Empty sequences are
- *            allowed.  Rows of q_rows (kv_rows) in no sequence are neither read nor written.
+ *            allowed.  Rows of q_rows (kv_rows) in no sequence are not written (but see fresh), and what they hold changes no
+ *            result; they may be read.
  *  causal    query i of n sees keys 0 .. i + (kv_n - n): the last query sees the last key.
- * A query that sees no key has output 0, log-sum-exp -infinity and gradient 0.  A sequence whose offsets decrease, leave the tensor or
+ * A query that sees no key has output 0, log-sum-exp -infinity and gradient 0.  A value that is not finite stays within its sequence and the heads
+ * of its key head, but may make NaN of any row there, also of one that does not see it: what is not seen is multiplied by 0.  A sequence whose offsets decrease, leave the tensor or
  * span more than q_len (kv_len) rows is skipped, and *status (device int32, may be NULL; zeroed by the caller) becomes
  * HBP_ERR_INVALID_ARG; a bounded wait that runs out makes it HBP_ERR_TIMEOUT and leaves outputs incomplete.
  * head_dim up to 128, a multiple of 16 bytes.  Inputs may be broadcast (strides of 0) and share memory; outputs overlap neither themselves nor anything
@@ -401,7 +403,8 @@ hbp_status hbp_attention_backward(const hbp_attention* a, const hbp_heads* d_o, 
  * scales [rows][(d + 31) / 32] (uint8) are e + 127.  Every stored value is a bf16 number: reading it back is exact in both dtypes,
  * and is off by at most 2^(e-1) from x (2^e where x is 63.5 * 2^122 or more: 2^128 is no float).  A group that holds an infinity or a NaN has scale 255 and is read back as NaN throughout.
  * ld* are elements between rows of the dtype tensors (>= d, multiples of 16 bytes); codes and scales have none.  codes 16-byte
- * aligned.  rows may be 0.
+ * aligned.  rows may be 0.  Outputs overlap nothing but what is named here.  gelu is off by 2e-4 of itself in bf16 (before the rounding to
+ * it), by (2 z^2 + 20) 2^-24 of itself in float; so is gelu' for z <= -3, elsewhere by 1e-6.
  *  store          codes, scales of x
  *  load           x of codes, scales
  *  gelu           act = gelu(z) from z itself (act may be z), and z's codes and scales

@@ -63,7 +63,7 @@ __device__ __forceinline__ SeqPair sequence_pair(const hbp_attention& a, int b) 
 }
 // Ragged batches of up to a warp's lanes of sequences are taken longest walks first (over_keys: walks over the keys, else over the queries), so that
 // no long walk begins when the others are nearly done: w.b, a place in that order, becomes the sequence.  12 sequences of up to 509 queries and 1301
-// keys, 10 heads of 80, forward: 33 against 42 us in the batch's order.  More sequences even out by themselves.
+// keys, 10 heads of 80, forward: 33 against 42 us in the batch's order.  (More sequences are taken in the batch's order; another one was not tried.)
 __device__ __forceinline__ SeqPair sequence_pair(const hbp_attention& a, BlockOf& w, bool over_keys) {
   const int n = a.sequences;
   if ((a.q_offsets || a.kv_offsets) && n > 1 && n <= 32) {

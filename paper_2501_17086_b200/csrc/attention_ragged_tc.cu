@@ -43,8 +43,8 @@ using namespace tc;
 
 namespace {
 
-constexpr int BIG = 128;     // rows of a block; keys of a forward tile
-constexpr int SMALL = 64;    // rows of a backward tile, and of every copy
+constexpr int BIG = 128;     // rows of a block
+constexpr int SMALL = 64;    // rows of a tile that a block walks over, and of every copy
 constexpr int SUB = 64;      // channels of a run of tile rows (128 bytes)
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float kGrowth = 8.0f;  // log2 of how far a row's maximum may grow before what was summed is scaled
