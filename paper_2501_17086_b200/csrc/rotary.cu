@@ -8,7 +8,7 @@
 //    warp that read different frequencies from the constant bank would be served one after the other;
 //  - a thread keeps CV pairs of a row (two vectors of up to 16 bytes) and walks over heads: its cosines and sines stay in registers
 //    and a head costs two loads, the rotation and two stores.
-// bf16, 16384 rows, 12 + 12 heads of 64 (101 MB): 22.5 us (4.5 TB/s; 15.4 at the rate of a copy), 8192 rows, 32 + 8 heads of 128 (168 MB): 34.3.
+// bf16, 16384 rows, 12 + 12 heads of 64 (101 MB): 22.2 us (4.5 TB/s; 15.4 at the rate of a copy), 8192 rows, 32 + 8 heads of 128 (168 MB): 32.9.
 // With the angles in double and every thread forming its own: 34.8 and 49.6; the pairs of a block dealt out one by one
 // (280 instructions a unit): 26.6 and 36.9.  Blocks of 256 threads and 16 rows, which all start at once and wait at once: 24.6 and 48.0.
 // What is left are the instructions of a unit and the first wait of a block, for its positions.
