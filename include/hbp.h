@@ -404,7 +404,7 @@ hbp_status hbp_attention_backward(const hbp_attention* a, const hbp_heads* d_o, 
  * and is off by at most 2^(e-1) from x (2^e where x is 63.5 * 2^122 or more: 2^128 is no float).  A group that holds an infinity or a NaN has scale 255 and is read back as NaN throughout.
  * ld* are elements between rows of the dtype tensors (>= d, multiples of 16 bytes); codes and scales have none.  codes 16-byte
  * aligned.  rows may be 0.  Outputs overlap nothing but what is named here.  gelu is off by 2e-4 of itself in bf16 (before the rounding to
- * it), by (2 z^2 + 20) 2^-24 of itself in float; so is gelu' for z <= -3, elsewhere by 1e-6.
+ * it), by (3 z^2 + 25) 2^-24 of itself in float; so is gelu' for z <= -3, elsewhere by 1e-6.
  *  store          codes, scales of x
  *  load           x of codes, scales
  *  gelu           act = gelu(z) from z itself (act may be z), and z's codes and scales
