@@ -420,6 +420,88 @@ hbp_status hbp_checkpoint_gelu_backward(int32_t dtype, int64_t rows, int32_t d, 
                                         const void* d_act, int64_t ldd, void* dz, int64_t ldz, void* act, int64_t lda,
                                         void* cuda_stream);
 
+/* ---------------------------------------------------------------- a decoder's ends, and what joins its blocks
+ * What a training step has around the blocks of hbp_forward / hbp_backward, or of callers that run layers of their own: x0 from
+ * tokens and the table's gradient from g_0; norms and the residual update between blocks and after the last one; the loss, and with it delta,
+ * from the last state.  As above: no state, no allocation, calls on different streams are independent as long as their buffers are, all can be captured
+ * into a CUDA graph.  Pointers 16-byte aligned (tokens, targets: to their size), widths d and distances of rows multiples of 16 bytes.  Outputs
+ * overlap neither themselves nor anything else but what is named here.
+ *
+ * Tokens and targets are int32 (token_bytes, target_bytes 4) or int64 (8) on the device.  A negative one stands for none: padding.
+ * One that is vocab or more is taken for none, too, and sets *status (device int32, may be NULL; zeroed by the caller) to HBP_ERR_INVALID_ARG. */
+
+/* out[i] = scale * table[tokens[i]], rounded once to dtype; zeros where there is no token.  table [vocab] rows ldt elements apart (0: one row for
+ * all), out [rows] rows ldo apart. */
+hbp_status hbp_embedding(int32_t dtype, int64_t rows, int32_t vocab, int32_t d, const void* tokens, int32_t token_bytes, const void* table,
+                         int64_t ldt, float scale, void* out, int64_t ldo, int32_t* status, void* cuda_stream);
+
+/* d_table[v] = add[v] + scale * sum of d_out[i] over the rows i whose token is v: float [vocab][d], without gaps, as is add.  add NULL: zeros.
+ * add may be d_table itself; rows of tokens that do not occur are then not touched (a table that is the vocabulary matrix too: the gradient of
+ * hbp_cross_entropy_gradients is added to).  d_out: rows ldd apart (0: one row for all).  Rows are summed in float in a fixed order, by sorted tokens: runs agree bit
+ * for bit.  rows up to 2^30.  scratch: device memory of hbp_embedding_gradient_scratch_bytes bytes, not shared by calls that may overlap. */
+hbp_status hbp_embedding_gradient_scratch_bytes(int64_t rows, int32_t d, size_t* bytes);
+hbp_status hbp_embedding_gradient(int32_t dtype, int64_t rows, int32_t vocab, int32_t d, const void* tokens, int32_t token_bytes,
+                                  const void* d_out, int64_t ldd, float scale, const float* add, float* d_table, void* scratch,
+                                  size_t scratch_bytes, int32_t* status, void* cuda_stream);
+
+/* A residual update between two norms.  With x the stream and f a block's output, rows of d channels,
+ *   h = norm(f) * w_post (post != 0) or f,   x_new = gate * x + scale * h,   y = norm(x_new) * w_pre
+ * norm: LAYER (v - mean(v)) / sqrt(var(v) + eps), biased variance; RMS v / sqrt(mean(v^2) + eps).  w_post, gate, w_pre: [d] of dtype, NULL = ones.
+ * x_new is rounded once to dtype, and y is the norm of those stored values, in float and rounded once.  d up to 8192. */
+typedef enum { HBP_NORM_LAYER = 0, HBP_NORM_RMS = 1 } hbp_norm_kind;
+typedef struct {
+  int32_t dtype, kind;
+  int64_t rows;
+  int32_t d, post;
+  float eps;   /* >= 0 */
+  float scale;
+  const void *w_post, *gate, *w_pre;
+} hbp_norm;
+/* A tensor [rows][d]: rows `stride` elements apart (inputs: 0 = one row for all) */
+typedef struct {
+  void* x;
+  int64_t stride;
+} hbp_rows;
+
+/* f NULL: there is no update, y = norm(x) * w_pre (gate, x_new NULL, post 0).  y NULL: x_new alone.  An output may be x or f (same pointer
+ * and stride). */
+hbp_status hbp_norm_residual(const hbp_norm* n, const hbp_rows* x, const hbp_rows* f, const hbp_rows* x_new, const hbp_rows* y, void* cuda_stream);
+
+/* Gradients from those of y and of x_new as the layers behind use it (d_y or d_new may be NULL: zero).  x_new (with d_y): what hbp_norm_residual has stored (or x, where there was
+ * no update); f is read where post is set, x for da.  dx, df of dtype; dw_pre, dw_post, da [d] float (OVERWRITTEN), summed in a fixed order: runs agree bit for
+ * bit.  Any output may be NULL.  dx and df may be inputs (same pointer and stride).  scratch: device memory of
+ * hbp_norm_residual_scratch_bytes bytes where a [d] gradient is asked for, not shared by calls that may overlap. */
+hbp_status hbp_norm_residual_scratch_bytes(int64_t rows, int32_t d, size_t* bytes);
+hbp_status hbp_norm_residual_backward(const hbp_norm* n, const hbp_rows* d_y, const hbp_rows* d_new, const hbp_rows* x_new, const hbp_rows* f,
+                                      const hbp_rows* x, const hbp_rows* dx, const hbp_rows* df, float* dw_pre, float* dw_post, float* da,
+                                      void* scratch, size_t scratch_bytes, void* cuda_stream);
+
+/* Hidden states x [rows][d] (rows ldx apart) and a vocabulary matrix w [vocab][d] (ldw), both of dtype, and each row's target.  The logits
+ * z = x w^T, float sums of exact products (float data: of all but 2^-26 of them), are never in memory as such. */
+typedef struct {
+  int32_t dtype, vocab, d, target_bytes;
+  int64_t rows;
+  const void* x;
+  int64_t ldx;
+  const void* w;
+  int64_t ldw;
+  const void* targets;
+  int32_t* status; /* may be NULL; a bounded wait that runs out makes it HBP_ERR_TIMEOUT and leaves outputs incomplete */
+} hbp_vocabulary;
+
+/* loss[i] = log(sum_j exp(z_ij)) - z_i,target (float; 0 where there is no target, whatever x holds there).  A row that holds a value that is not
+ * finite makes its own loss NaN (or infinite), one of w that of every row.
+ * With gradients of sum_i d_loss[i * d_loss_stride] * loss[i] (d_loss float on the device, NULL: ones): dx [rows][d] of dtype (0 where there is no target) and
+ * dw [vocab][d] (OVERWRITTEN), float or, bf16 data, bf16 (dw_dtype); either may be NULL.  bf16: the probabilities' numerators and x times its row's
+ * factor are rounded to bf16 as operands of products whose sums are float.  In one call, as two products less are formed than by a backward pass
+ * of its own.  scratch: device memory, 256-byte aligned, not shared by calls that may overlap, of hbp_cross_entropy_scratch_bytes bytes, of
+ * which the numerators of up to 4 GiB are the most, or less (HBP_ERR_WORKSPACE if it is too little for 256 rows at a time): the rows are then
+ * taken in smaller pieces, and dw is added up over these in float. */
+hbp_status hbp_cross_entropy_scratch_bytes(const hbp_vocabulary* v, int32_t gradients, size_t* bytes);
+hbp_status hbp_cross_entropy(const hbp_vocabulary* v, float* loss, void* scratch, size_t scratch_bytes, void* cuda_stream);
+hbp_status hbp_cross_entropy_gradients(const hbp_vocabulary* v, const float* d_loss, int64_t d_loss_stride, float* loss, void* dx, int64_t lddx,
+                                       void* dw, int32_t dw_dtype, int64_t lddw, void* scratch, size_t scratch_bytes, void* cuda_stream);
+
 const char* hbp_status_string(hbp_status s);
 void hbp_destroy(hbp_ctx* ctx);
 

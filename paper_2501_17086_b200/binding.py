@@ -27,6 +27,8 @@ EXPORTS = ["hbp_workspace_bytes", "hbp_create", "hbp_workspace_bytes_checkpointe
            "hbp_compare_scratch_bytes", "hbp_compare", "hbp_iterate", "hbp_add_carry", "hbp_param_grads",
            "hbp_rotary", "hbp_context_rotary", "hbp_attention_forward", "hbp_attention_scratch_bytes", "hbp_attention_backward",
            "hbp_checkpoint_store", "hbp_checkpoint_load", "hbp_checkpoint_gelu", "hbp_checkpoint_gelu_backward",
+           "hbp_embedding", "hbp_embedding_gradient", "hbp_embedding_gradient_scratch_bytes", "hbp_norm_residual", "hbp_norm_residual_backward",
+           "hbp_norm_residual_scratch_bytes", "hbp_cross_entropy", "hbp_cross_entropy_gradients", "hbp_cross_entropy_scratch_bytes",
            "hbp_status_string", "hbp_destroy"]
 
 
@@ -66,6 +68,21 @@ class hbp_attention(C.Structure):  # (``fresh``, the four bytes before ``status`
                 ("q_offsets", C.c_void_p), ("kv_offsets", C.c_void_p), ("scale", C.c_float), ("status", C.c_void_p)]
 
 
+class hbp_norm(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("kind", C.c_int32), ("rows", C.c_int64), ("d", C.c_int32), ("post", C.c_int32), ("eps", C.c_float),
+                ("scale", C.c_float), ("w_post", C.c_void_p), ("gate", C.c_void_p), ("w_pre", C.c_void_p)]
+
+
+class hbp_rows(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("stride", C.c_int64)]
+
+
+class hbp_vocabulary(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("vocab", C.c_int32), ("d", C.c_int32), ("target_bytes", C.c_int32), ("rows", C.c_int64), ("x", C.c_void_p),
+                ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("targets", C.c_void_p), ("status", C.c_void_p)]
+
+
+NORM_KINDS = {"layer": 0, "rms": 1}
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "by_parts": 2}
 
@@ -108,6 +125,15 @@ def _load():
     lib.hbp_checkpoint_load.argtypes = [i32, i64, i32, vp, vp, vp, i64, vp]
     lib.hbp_checkpoint_gelu.argtypes = [i32, i64, i32, vp, i64, vp, i64, vp, vp, vp]
     lib.hbp_checkpoint_gelu_backward.argtypes = [i32, i64, i32, vp, vp, vp, i64, vp, i64, vp, i64, vp]
+    lib.hbp_embedding.argtypes = [i32, i64, i32, i32, vp, i32, vp, i64, C.c_float, vp, i64, vp, vp]
+    lib.hbp_embedding_gradient_scratch_bytes.argtypes = [i64, i32, C.POINTER(sz)]
+    lib.hbp_embedding_gradient.argtypes = [i32, i64, i32, i32, vp, i32, vp, i64, C.c_float, vp, vp, vp, sz, vp, vp]
+    lib.hbp_norm_residual.argtypes = [vp] * 6
+    lib.hbp_norm_residual_scratch_bytes.argtypes = [i64, i32, C.POINTER(sz)]
+    lib.hbp_norm_residual_backward.argtypes = [vp] * 12 + [sz, vp]
+    lib.hbp_cross_entropy_scratch_bytes.argtypes = [vp, i32, C.POINTER(sz)]
+    lib.hbp_cross_entropy.argtypes = [vp, vp, vp, sz, vp]
+    lib.hbp_cross_entropy_gradients.argtypes = [vp, vp, i64, vp, vp, i64, vp, i32, i64, vp, sz, vp]
     lib.hbp_sync_status.argtypes = [vp, vp]
     lib.hbp_profile_enable.argtypes = [vp, i32]
     lib.hbp_profile_read.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(i64)]
@@ -442,11 +468,11 @@ def rotary_spec(rotary_dim, base=10000.0, layout="half", scaling="none", factor=
                            slow, amplitude)
 
 
-def _choice(table, name):
+def _choice(table, name, what="rotary"):
     try:
         return table[name]
     except (KeyError, TypeError):
-        raise HbpError(6, f"rotary: {name!r} is none of {', '.join(table)}") from None
+        raise HbpError(6, f"{what}: {name!r} is none of {', '.join(table)}") from None
 
 
 def rotary(q, k=None, positions=None, first=0, period=0, rotary_dim=None, base=10000.0, layout="half", scaling="none", factor=1.0,
@@ -506,3 +532,54 @@ def checkpoint_gelu_backward(d_act, codes, scales, with_act=False, dz=None, act=
     """dz = d_act * gelu'(z8) (``dz`` may be d_act itself) from the z that checkpoint_gelu kept, and with ``with_act`` (or
     ``act`` given) gelu(z8) too, the operand of the following product's weight gradient: dz, or (dz, act)."""
     return _calls.checkpoint_gelu_backward(d_act, codes, scales, with_act, dz, act)
+
+
+# ---- a decoder's ends, and what joins its blocks: as above ------------------------------------------------------------------
+def embedding(tokens, table, scale=1.0, out=None, status=None):
+    """scale * table[tokens]: see hbp_embedding.  tokens int32 or int64 [rows], table [vocab, channels]; a negative token gives zeros, and so does
+    one beyond the table, which sets ``status`` (int32 [1], zeroed by the caller)."""
+    return _calls.embedding(tokens, table, scale, out, status)
+
+
+def embedding_gradient(tokens, d_out, vocab, scale=1.0, add=None, d_table=None, scratch=None, status=None):
+    """The gradient of embedding's table, float [vocab, channels], from that of its output: see hbp_embedding_gradient.  It is added to ``add``
+    where given; with ``d_table`` the same tensor, rows of tokens that do not occur are not touched."""
+    return _calls.embedding_gradient(tokens, d_out, vocab, scale, add, d_table, scratch, status)
+
+
+def norm_residual(x, f=None, kind="layer", eps=1e-5, post=False, w_post=None, gate=None, scale=1.0, w_pre=None, with_y=True, x_new=None, y=None):
+    """(x_new, y): x_new = gate * x + scale * h with h = f, or (``post``) norm(f) * w_post, and y = norm(x_new) * w_pre: see hbp_norm_residual.
+    x, f [rows, channels]; weights [channels] of their type, or None for ones; kind "layer" or "rms".  Without f, x_new is x itself.
+    x_new and y may be given, x and f among them.  ``with_y`` False: y is None."""
+    return _calls.norm_residual(x, f, _choice(NORM_KINDS, kind, "norm_residual"), eps, post, w_post, gate, scale, w_pre, with_y, x_new, y)
+
+
+def norm_residual_backward(d_y, x_new, f=None, x=None, d_new=None, kind="layer", eps=1e-5, post=False, w_post=None, gate=None, scale=1.0, w_pre=None,
+                           with_dx=True, with_df=True, with_weights=True, dx=None, df=None, scratch=None):
+    """(dx, df, dw_pre, dw_post, da): the gradients of norm_residual's x, f, and float ones of w_pre, w_post and gate (None for those that are not
+    given, or without ``with_weights``), from those of y and of x_new (d_y or d_new may be None): see hbp_norm_residual_backward.
+    ``f`` is needed with ``post``, ``x`` for the gate's gradient.  Of a norm without an update: x_new is its x, with_df False."""
+    return _calls.norm_residual_backward(d_y, x_new, f, x, d_new, _choice(NORM_KINDS, kind, "norm_residual_backward"), eps, post, w_post, gate, scale, w_pre,
+                                         with_dx, with_df, with_weights, dx, df, scratch)
+
+
+def cross_entropy(x, w, targets, loss=None, scratch=None, status=None):
+    """The softmax cross entropy of every row, float [rows]: x [rows, channels] against the vocabulary matrix w [vocab, channels], targets int32 or
+    int64 [rows], negative where a row has none (its loss is 0): see hbp_cross_entropy."""
+    return _calls.cross_entropy(x, w, targets, status, loss, scratch)
+
+
+def cross_entropy_gradients(x, w, targets, d_loss=None, with_dx=True, with_dw=True, dw_dtype=torch.float32, loss=None, dx=None, dw=None, scratch=None,
+                            status=None):
+    """(loss, dx, dw): cross_entropy and the gradients of sum(d_loss * loss), d_loss float [rows] (None: ones): see hbp_cross_entropy_gradients.
+    dw is float, or bf16 for bf16 data if ``dw_dtype`` (or ``dw``) says so; what is not asked for is None.  ``scratch`` (uint8, 256-byte aligned) of less than
+    cross_entropy_scratch_bytes makes it take the rows in smaller pieces."""
+    return _calls.cross_entropy_gradients(x, w, targets, status, d_loss, with_dx, with_dw, _dtype_code(dw_dtype) == HBP_F32, loss, dx, dw, scratch)
+
+
+def cross_entropy_scratch_bytes(dtype, rows, vocab, channels, gradients=True) -> int:
+    """Bytes of the scratch that cross_entropy and cross_entropy_gradients make themselves if not given any."""
+    v = hbp_vocabulary(_dtype_code(dtype), vocab, channels, 8, rows)
+    n = C.c_size_t(0)
+    _check(lib.hbp_cross_entropy_scratch_bytes(C.addressof(v), int(gradients), C.byref(n)), "hbp_cross_entropy_scratch_bytes")
+    return n.value

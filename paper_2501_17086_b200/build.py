@@ -15,7 +15,8 @@ LIB = os.path.join(HERE, "libhbp.so")
 CALLS = os.path.join(HERE, "_calls.so")
 CALLS_FOR = os.path.join(HERE, "_build", "calls.for")  # what the extension module was built against
 SOURCES = ["hbp_api.cu", "gemm_simt.cu", "gemm_tc.cu", "gemm_f32.cu", "gemm_parts.cu", "gemm_cell.cu", "few_rows.cu", "scan.cu", "scan_static.cu", "scan_ring.cu", "attention.cu", "attention_tc.cu", "rnn.cu", "rnn_persistent.cu", "rnn_cluster.cu", "cell_cluster.cu", "gru.cu", "lstm.cu", "diag.cu", "rotary.cu",
-           "checkpoint.cu", "attention_ragged.cu", "attention_ragged_tc.cu"]
+           "checkpoint.cu", "attention_ragged.cu", "attention_ragged_tc.cu",
+           "embedding.cu", "norm_residual.cu", "cross_entropy.cu"]
 
 
 def _built_for() -> str:

@@ -1,4 +1,4 @@
-// Marshalling of the short calls (binding.py: rotary, attention_*, checkpoint_*) as an extension module: checks of the tensors, their
+// Marshalling of the short calls (binding.py: rotary, attention_*, checkpoint_*, embedding*, norm_residual*, cross_entropy*) as an extension module: checks of the tensors, their
 // pointers, strides and sizes, new outputs, the current stream, and the call of the C ABI.  A launch or two of these take some
 // microseconds; the same steps in Python with ctypes took 10 to 20 (rotary positions of one token 13.3 us a call, of which the
 // launch and two allocations are 5; a checkpoint stored 9.8; attention with its backward pass 38).  Nothing is computed
@@ -392,10 +392,257 @@ PyObject* checkpoint_gelu_backward(PyObject*, PyObject* const* a, Py_ssize_t n) 
   CALL_END
 }
 
+// ---- a decoder's ends, and what joins its blocks
+// int32 or int64 [rows] without gaps: its element's bytes
+int32_t whole_numbers(const Call& c, const at::Tensor& t, const char* what) {
+  const int32_t bytes = t.scalar_type() == at::kInt ? 4 : t.scalar_type() == at::kLong ? 8 : 0;
+  if (!bytes || t.dim() != 1 || !t.is_contiguous()) refuse(HBP_ERR_SHAPE, c.name, what);
+  return bytes;
+}
+int32_t* status_of(Call& c, PyObject* o) {
+  const at::Tensor* status = c.maybe(o, "status is no tensor");
+  if (status && (status->scalar_type() != at::kInt || status->numel() < 1)) refuse(HBP_ERR_SHAPE, c.name, "status: wanted an int32 tensor");
+  return status ? status->data_ptr<int32_t>() : nullptr;
+}
+// device memory for a call: given, or new
+struct Memory {
+  at::Tensor t;
+  Memory(Call& c, PyObject* o, size_t bytes, const at::Tensor& like) {
+    if (o != Py_None) {
+      t = c.tensor(o, "scratch is no tensor");
+      if (!t.is_contiguous()) refuse(HBP_ERR_WORKSPACE, c.name, "scratch is not contiguous");
+    } else if (bytes) {
+      t = at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
+    }
+  }
+  void* at() const { return t.defined() ? t.data_ptr() : nullptr; }
+  size_t bytes() const { return t.defined() ? t.nbytes() : 0; }
+};
+const at::Tensor* weight(Call& c, PyObject* o, const at::Tensor& x, const char* what) {
+  const at::Tensor* w = c.maybe(o, what);
+  if (w && (w->dim() != 1 || w->size(0) != x.size(1) || !w->is_contiguous() || w->scalar_type() != x.scalar_type())) refuse(HBP_ERR_SHAPE, c.name, what);
+  return w;
+}
+hbp_rows rows_of(Call& c, const at::Tensor& t) { return {t.data_ptr(), c.apart(t)}; }
+
+// tokens, table, scale, out, status
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN
+  wanted(n, 5, "embedding");
+  Call c("embedding");
+  const at::Tensor &tokens = c.tensor(a[0], "tokens are no tensor"), &table = c.tensor(a[1], "table is no tensor");
+  const int32_t bytes = whole_numbers(c, tokens, "tokens: wanted int32 or int64 [rows]"), type = c.dtype(table);
+  const int64_t ldt = c.apart(table), rows = tokens.size(0);
+  int32_t* status = status_of(c, a[4]);
+  const at::Tensor* given = c.maybe(a[3], "out is no tensor");
+  if (given && (given->dim() != 2 || given->size(0) != rows || given->size(1) != table.size(1) || given->scalar_type() != table.scalar_type()))
+    refuse(HBP_ERR_SHAPE, c.name, "out: wanted [rows, channels] of the table's type");
+  const at::Tensor out = given ? *given : at::empty({rows, table.size(1)}, table.options());
+  check(unlocked(hbp_embedding, type, rows, c.narrow(table.size(0)), c.narrow(table.size(1)), tokens.data_ptr(), bytes, table.data_ptr(), ldt, (float)c.real(a[2]),
+                 out.data_ptr(), c.apart(out), status, c.stream()),
+        "hbp_embedding");
+  return THPVariable_Wrap(out);
+  CALL_END
+}
+
+// tokens, d_out, vocab, scale, add, d_table, scratch, status
+PyObject* embedding_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN
+  wanted(n, 8, "embedding_gradient");
+  Call c("embedding_gradient");
+  const at::Tensor &tokens = c.tensor(a[0], "tokens are no tensor"), &d_out = c.tensor(a[1], "d_out is no tensor");
+  const int32_t bytes = whole_numbers(c, tokens, "tokens: wanted int32 or int64 [rows]"), type = c.dtype(d_out), vocab = c.whole32(a[2]);
+  const int64_t ldd = c.apart(d_out), rows = tokens.size(0), d = d_out.size(1);
+  if (d_out.size(0) != rows) refuse(HBP_ERR_SHAPE, c.name, "d_out: wanted a row for each token");
+  if (vocab < 0) refuse(HBP_ERR_SHAPE, c.name, "a negative number of tokens");
+  auto like = [&](const at::Tensor& t, const char* what) {
+    if (t.dim() != 2 || t.size(0) != vocab || t.size(1) != d || !t.is_contiguous() || t.scalar_type() != at::kFloat) refuse(HBP_ERR_SHAPE, c.name, what);
+  };
+  const at::Tensor *add = c.maybe(a[4], "add is no tensor"), *given = c.maybe(a[5], "d_table is no tensor");
+  if (add) like(*add, "add: wanted float [vocab, channels]");
+  if (given) like(*given, "d_table: wanted float [vocab, channels]");
+  int32_t* status = status_of(c, a[7]);
+  const at::Tensor out = given ? *given : at::empty({vocab, d}, d_out.options().dtype(at::kFloat));
+  size_t need = 0;
+  check(hbp_embedding_gradient_scratch_bytes(rows, c.narrow(d), &need), "hbp_embedding_gradient_scratch_bytes");
+  const Memory scratch(c, a[6], need, d_out);
+  check(unlocked(hbp_embedding_gradient, type, rows, vocab, c.narrow(d), tokens.data_ptr(), bytes, d_out.data_ptr(), ldd, (float)c.real(a[3]),
+                 add ? add->data_ptr<float>() : nullptr, out.data_ptr<float>(), scratch.at(), scratch.bytes(), status, c.stream()),
+        "hbp_embedding_gradient");
+  return THPVariable_Wrap(out);
+  CALL_END
+}
+
+// a[0..6]: kind, eps, post, w_post, gate, scale, w_pre
+hbp_norm norm_of(Call& c, const at::Tensor& x, PyObject* const* a) {
+  if (x.dim() != 2) refuse(HBP_ERR_SHAPE, c.name, "wanted [rows, channels]");
+  hbp_norm s = {};
+  s.dtype = c.dtype(x);
+  s.kind = c.whole32(a[0]);
+  s.rows = x.size(0);
+  s.d = c.narrow(x.size(1));
+  s.post = c.truth(a[2]);
+  s.eps = (float)c.real(a[1]);
+  s.scale = (float)c.real(a[5]);
+  const at::Tensor *post = weight(c, a[3], x, "w_post: wanted [channels] of x's type"), *gate = weight(c, a[4], x, "gate: wanted [channels] of x's type"),
+                   *pre = weight(c, a[6], x, "w_pre: wanted [channels] of x's type");
+  s.w_post = post ? post->data_ptr() : nullptr;
+  s.gate = gate ? gate->data_ptr() : nullptr;
+  s.w_pre = pre ? pre->data_ptr() : nullptr;
+  return s;
+}
+at::Tensor rows_output(Call& c, PyObject* o, const at::Tensor& x, const char* what) { return o == Py_None ? packed_like(x) : c.output(o, x, what); }
+PyObject* none() { Py_RETURN_NONE; }
+PyObject* wrapped(const at::Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : none(); }
+
+// x, f, (as norm_of), with_y, x_new, y
+PyObject* norm_residual(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN
+  wanted(n, 12, "norm_residual");
+  Call c("norm_residual");
+  const at::Tensor& x = c.tensor(a[0], "x is no tensor");
+  const at::Tensor* f = c.maybe(a[1], "f is no tensor");
+  const hbp_norm s = norm_of(c, x, a + 2);
+  if (f) c.alike(*f, x, "f is not like x");
+  if (!f && a[10] != Py_None) refuse(HBP_ERR_INVALID_ARG, c.name, "x_new without a block's output f");
+  const hbp_rows xr = rows_of(c, x), fr = f ? rows_of(c, *f) : hbp_rows{};
+  const at::Tensor x_new = f ? rows_output(c, a[10], x, "x_new is not like x") : at::Tensor();
+  const bool with_y = a[11] != Py_None || c.truth(a[9]);
+  const at::Tensor y = with_y ? rows_output(c, a[11], x, "y is not like x") : at::Tensor();
+  const hbp_rows nr = f ? rows_of(c, x_new) : hbp_rows{}, yr = with_y ? rows_of(c, y) : hbp_rows{};
+  check(unlocked(hbp_norm_residual, &s, &xr, &fr, &nr, &yr, c.stream()), "hbp_norm_residual");
+  PyObject *p = wrapped(f ? x_new : x), *q = p ? wrapped(y) : nullptr, *t = q ? PyTuple_Pack(2, p, q) : nullptr;
+  Py_XDECREF(p);
+  Py_XDECREF(q);
+  return t;
+  CALL_END
+}
+
+// d_y, x_new, f, x, d_new, (as norm_of), with_dx, with_df, with_weights, dx, df, scratch
+PyObject* norm_residual_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN
+  wanted(n, 18, "norm_residual_backward");
+  Call c("norm_residual_backward");
+  const at::Tensor *d_y = c.maybe(a[0], "d_y is no tensor"), *x_new = c.maybe(a[1], "x_new is no tensor"), *f = c.maybe(a[2], "f is no tensor"),
+                   *x = c.maybe(a[3], "x is no tensor"), *d_new = c.maybe(a[4], "d_new is no tensor");
+  if (!d_y && !d_new) refuse(HBP_ERR_INVALID_ARG, c.name, "neither d_y nor d_new is given");
+  const at::Tensor& like = d_y ? *d_y : *d_new;
+  const hbp_norm s = norm_of(c, like, a + 5);
+  hbp_rows in[5];
+  const at::Tensor* t[5] = {d_y, d_new, x_new, f, x};
+  for (int i = 0; i < 5; ++i) {
+    if (t[i]) c.alike(*t[i], like, "the tensors differ in shape or type");
+    in[i] = t[i] ? rows_of(c, *t[i]) : hbp_rows{};
+  }
+  const bool weights = c.truth(a[14]);
+  const at::Tensor dx = a[15] != Py_None || c.truth(a[12]) ? rows_output(c, a[15], like, "dx is not like d_y") : at::Tensor();
+  const at::Tensor df = a[16] != Py_None || c.truth(a[13]) ? rows_output(c, a[16], like, "df is not like d_y") : at::Tensor();
+  auto vector = [&](bool want) { return want ? at::empty({like.size(1)}, like.options().dtype(at::kFloat)) : at::Tensor(); };
+  const at::Tensor pre = vector(weights && s.w_pre && d_y), post = vector(weights && s.w_post && s.post), da = vector(weights && s.gate);
+  const hbp_rows dxr = dx.defined() ? rows_of(c, dx) : hbp_rows{}, dfr = df.defined() ? rows_of(c, df) : hbp_rows{};
+  auto floats = [](const at::Tensor& v) { return v.defined() ? v.data_ptr<float>() : nullptr; };
+  size_t need = 0;
+  if (pre.defined() || post.defined() || da.defined()) check(hbp_norm_residual_scratch_bytes(s.rows, s.d, &need), "hbp_norm_residual_scratch_bytes");
+  const Memory scratch(c, a[17], need, like);
+  check(unlocked(hbp_norm_residual_backward, &s, &in[0], &in[1], &in[2], &in[3], &in[4], &dxr, &dfr, floats(pre), floats(post), floats(da), scratch.at(),
+                 scratch.bytes(), c.stream()),
+        "hbp_norm_residual_backward");
+  const at::Tensor* out[5] = {&dx, &df, &pre, &post, &da};
+  PyObject* all = PyTuple_New(5);
+  for (int i = 0; all && i < 5; ++i) {
+    PyObject* o = wrapped(*out[i]);
+    if (!o) {
+      Py_DECREF(all);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(all, i, o);
+  }
+  return all;
+  CALL_END
+}
+
+// x, w, targets, status
+hbp_vocabulary vocabulary_of(Call& c, PyObject* const* a) {
+  const at::Tensor &x = c.tensor(a[0], "x is no tensor"), &w = c.tensor(a[1], "w is no tensor"), &targets = c.tensor(a[2], "targets are no tensor");
+  hbp_vocabulary v = {};
+  v.dtype = c.dtype(x);
+  v.ldx = c.apart(x);
+  v.ldw = c.apart(w);
+  if (w.size(1) != x.size(1) || w.scalar_type() != x.scalar_type()) refuse(HBP_ERR_SHAPE, c.name, "w: wanted [vocab, channels] of x's width and type");
+  v.target_bytes = whole_numbers(c, targets, "targets: wanted int32 or int64 [rows]");
+  if (targets.size(0) != x.size(0)) refuse(HBP_ERR_SHAPE, c.name, "targets: wanted one for each row");
+  v.vocab = c.narrow(w.size(0));
+  v.d = c.narrow(x.size(1));
+  v.rows = x.size(0);
+  v.x = x.data_ptr();
+  v.w = w.data_ptr();
+  v.targets = targets.data_ptr();
+  v.status = status_of(c, a[3]);
+  return v;
+}
+at::Tensor losses(Call& c, PyObject* o, const at::Tensor& x) {
+  if (o == Py_None) return at::empty({x.size(0)}, x.options().dtype(at::kFloat));
+  const at::Tensor& t = c.tensor(o, "loss is no tensor");
+  if (t.dim() != 1 || t.size(0) != x.size(0) || !t.is_contiguous() || t.scalar_type() != at::kFloat) refuse(HBP_ERR_SHAPE, c.name, "loss: wanted float [rows]");
+  return t;
+}
+Memory vocabulary_scratch(Call& c, PyObject* o, const hbp_vocabulary& v, bool gradients, const at::Tensor& x) {
+  size_t need = 0;
+  check(hbp_cross_entropy_scratch_bytes(&v, gradients, &need), "hbp_cross_entropy_scratch_bytes");
+  return Memory(c, o, need, x);
+}
+
+// x, w, targets, status, loss, scratch
+PyObject* cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN
+  wanted(n, 6, "cross_entropy");
+  Call c("cross_entropy");
+  const hbp_vocabulary v = vocabulary_of(c, a);
+  const at::Tensor& x = THPVariable_Unpack(a[0]);
+  const at::Tensor loss = losses(c, a[4], x);
+  const Memory scratch = vocabulary_scratch(c, a[5], v, false, x);
+  check(unlocked(hbp_cross_entropy, &v, loss.data_ptr<float>(), scratch.at(), scratch.bytes(), c.stream()), "hbp_cross_entropy");
+  return THPVariable_Wrap(loss);
+  CALL_END
+}
+
+// x, w, targets, status, d_loss, with_dx, with_dw, dw float or not, loss, dx, dw, scratch
+PyObject* cross_entropy_gradients(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN
+  wanted(n, 12, "cross_entropy_gradients");
+  Call c("cross_entropy_gradients");
+  const hbp_vocabulary v = vocabulary_of(c, a);
+  const at::Tensor &x = THPVariable_Unpack(a[0]), &w = THPVariable_Unpack(a[1]);
+  const at::Tensor* d_loss = c.maybe(a[4], "d_loss is no tensor");
+  if (d_loss && (d_loss->dim() != 1 || d_loss->size(0) != v.rows || d_loss->scalar_type() != at::kFloat)) refuse(HBP_ERR_SHAPE, c.name, "d_loss: wanted float [rows]");
+  const at::Tensor loss = losses(c, a[8], x);
+  const at::Tensor dx = a[9] != Py_None || c.truth(a[5]) ? rows_output(c, a[9], x, "dx is not like x") : at::Tensor();
+  at::Tensor dw;
+  if (a[10] != Py_None) {
+    dw = c.tensor(a[10], "dw is no tensor");
+    if (dw.sizes() != w.sizes()) refuse(HBP_ERR_SHAPE, c.name, "dw is not like w");
+  } else if (c.truth(a[6])) {
+    dw = at::empty(w.sizes(), w.options().dtype(c.truth(a[7]) ? at::kFloat : at::kBFloat16));
+  }
+  const Memory scratch = vocabulary_scratch(c, a[11], v, true, x);
+  check(unlocked(hbp_cross_entropy_gradients, &v, d_loss ? d_loss->data_ptr<float>() : nullptr, d_loss ? d_loss->stride(0) : (int64_t)0, loss.data_ptr<float>(),
+                 dx.defined() ? dx.data_ptr() : nullptr, dx.defined() ? c.apart(dx) : (int64_t)0, dw.defined() ? dw.data_ptr() : nullptr,
+                 dw.defined() ? c.dtype(dw) : (int32_t)HBP_F32, dw.defined() ? c.apart(dw) : (int64_t)0, scratch.at(), scratch.bytes(), c.stream()),
+        "hbp_cross_entropy_gradients");
+  PyObject *p = wrapped(loss), *q = p ? wrapped(dx) : nullptr, *r = q ? wrapped(dw) : nullptr, *t = r ? PyTuple_Pack(3, p, q, r) : nullptr;
+  Py_XDECREF(p);
+  Py_XDECREF(q);
+  Py_XDECREF(r);
+  return t;
+  CALL_END
+}
+
 #define FAST(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {{"set_error", set_error, METH_O, nullptr}, FAST(rotary),          FAST(attention_forward),
                           FAST(attention_backward),                  FAST(checkpoint_store), FAST(checkpoint_load),
-                          FAST(checkpoint_gelu),                     FAST(checkpoint_gelu_backward), {nullptr, nullptr, 0, nullptr}};
+                          FAST(checkpoint_gelu),                     FAST(checkpoint_gelu_backward),
+                          FAST(embedding), FAST(embedding_gradient), FAST(norm_residual), FAST(norm_residual_backward), FAST(cross_entropy),
+                          FAST(cross_entropy_gradients), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,602 @@
+// Softmax cross entropy of hidden states x [rows][d] against a vocabulary matrix w [vocab][d] (hbp_cross_entropy), and with its
+// gradients (hbp_cross_entropy_gradients).  z = x w^T is never in memory as such.
+//
+// With t a row's target and r a number near its largest logit, e_j = exp(z_j - r):
+//   S' = sum over j != t of e_j,   S = S' + e_t,   loss = log(S) - (z_t - r),   dz_j = g e_j / S (j != t),   dz_t = -g S' / S
+// so that neither a small loss nor its gradient is a difference of like numbers.  Taking r = z_t, which a dot product a row gives
+// beforehand, makes e_t = 1 and loss = log1p(S').
+//
+// bf16, three products of 2 rows vocab d flop instead of the four of a backward pass that forms the logits again:
+//   1. target_kernel   z_t by a warp a row
+//   2. gemm_tc, EPI_EXP: e rounded to bf16 into E [rows][vocab] (0 at the target), in float each row's sums and its largest logit
+//   3. finish_kernel   S', loss, the row's factor s = g / S; E at the target becomes -S'; s x, rounded to bf16
+//   4. gemm_tc, EPI_ROWS: dx = s (E w)          5. gemm_tc: dw = E^T (s x)
+// s is a number a row, which is why E needs no second pass: it comes out of the sum over the vocabulary in 4, and goes into the other
+// operand in 5.  E and s x are rounded to bf16, the operands' type: 2^-9 of each of their values at most, as a rounding of dz would be.  A row whose largest logit is more than
+// kFar above the target's (a loss of 40) would leave the range that bf16 and float sums of e have: finish_kernel then takes r = the largest logit,
+// and 2 and 3 run again; their launches return at once where no row asked for that.
+// The forward pass alone is 1 to 3 without E.
+//
+// float: products of operands in three bf16 parts (gemm_parts.cu); the logits of a piece of the rows lie in scratch, and
+// one pass over them forms dz, in parts.
+//
+// E has a piece of the rows at a time where it would be more than kPieceBytes, or than the scratch that the caller has.
+#include <math.h>
+
+#include <algorithm>
+
+#include "float_parts.cuh"
+#include "tc_common.cuh"
+
+namespace hbp {
+
+namespace {
+
+constexpr float kFar = 40.0f;
+constexpr size_t kPieceBytes = (size_t)4 << 30;
+constexpr int kPairs = 74;  // of CTAs, that a B200 runs at a time
+
+struct Targets {
+  const void* t;
+  int bytes;
+  __device__ __forceinline__ int64_t operator[](int64_t i) const { return bytes == 8 ? ((const int64_t*)t)[i] : (int64_t)((const int32_t*)t)[i]; }
+  // the column, -1 for a row that is ignored
+  __device__ __forceinline__ int column(int64_t i, int vocab, int* status) const {
+    const int64_t v = (*this)[i];
+    if (v >= vocab && status) *status = (int)HBP_ERR_INVALID_ARG;
+    return v < 0 || v >= vocab ? -1 : (int)v;
+  }
+};
+
+// ------------------------------------------------------------------------------------------- bf16
+struct RowData {
+  int64_t rows;
+  int vocab, d;
+  const bf16* x;
+  int64_t ldx;
+  const bf16* w;
+  int64_t ldw;
+  Targets targets;
+  int* status;
+  int* target;  // [rows]
+  float *zt, *ref, *factor;
+  float2* parts;  // [slots][rows]
+  int slots;
+  int* redo;
+  bool again;  // the second time, for rows whose reference was too low
+  const float* d_loss;
+  int64_t d_loss_stride;
+  float* loss;
+  bf16* E;  // not of the forward pass alone
+  int64_t ldE;
+  bf16* xs;
+};
+
+__global__ void __launch_bounds__(256) target_kernel(const RowData p) {
+  chain_next();
+  chain_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.redo = 0;
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (row >= p.rows) return;
+  const int t = p.targets.column(row, p.vocab, p.status);
+  float z = 0.0f;
+  if (t >= 0) {
+    const bf16 *x = p.x + row * p.ldx, *w = p.w + (int64_t)t * p.ldw;
+#pragma unroll 4
+    for (int c = lane * 8; c < p.d; c += 256) {
+      float a[8], b[8];
+      tc::unpack8(*reinterpret_cast<const uint4*>(x + c), a);
+      tc::unpack8(*reinterpret_cast<const uint4*>(w + c), b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z = fmaf(a[e], b[e], z);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+  }
+  if (lane == 0) {
+    p.target[row] = t;
+    p.zt[row] = z;
+    p.ref[row] = isfinite(z) ? z : 0.0f;
+  }
+}
+
+constexpr int kFinishWarps = 16;
+
+// 32 rows a block: the lanes' rows, the row sums of the tiles shared by the warps.
+__global__ void __launch_bounds__(32 * kFinishWarps) finish_kernel(const RowData p) {
+  __shared__ float sums[kFinishWarps][32], mosts[kFinishWarps][32], factors[32];
+  chain_next();
+  chain_wait();
+  if (p.again && *(const volatile int*)p.redo == 0) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t row0 = (int64_t)blockIdx.x * 32, row = row0 + lane;
+  float sum = 0.0f, most = -INFINITY;
+  if (row < p.rows) {
+#pragma unroll 8
+    for (int k = warp; k < p.slots; k += kFinishWarps) {
+      const float2 v = p.parts[(int64_t)k * p.rows + row];
+      sum += v.x;
+      most = fmaxf(most, v.y);
+    }
+  }
+  sums[warp][lane] = sum;
+  mosts[warp][lane] = most;
+  __syncthreads();
+  if (warp == 0) {
+    for (int k = 1; k < kFinishWarps; ++k) {
+      sum += sums[k][lane];
+      most = fmaxf(most, mosts[k][lane]);
+    }
+    float factor = 0.0f;
+    if (row < p.rows) {
+      const int t = p.target[row];
+      const float zt = p.zt[row], ref = p.ref[row];
+      float loss = 0.0f;
+      if (t >= 0) {
+        if (!p.again && most - ref > kFar) {
+          p.ref[row] = most;
+          *p.redo = 1;
+        }
+        const bool at_target = zt == ref;
+        const float total = sum + (at_target ? 1.0f : expf(zt - ref));
+        loss = at_target ? log1pf(sum) : logf(total) - (zt - ref);
+        if (p.E) {
+          factor = (p.d_loss ? p.d_loss[row * p.d_loss_stride] : 1.0f) / total;
+          const bf16 e = __float2bfloat16_rn(-sum);
+          p.E[row * p.ldE + t] = e;
+          // the largest term of most rows' gradients, with its rounding taken out again: the others share a 2^-9, as large as their own
+          const float kept = __bfloat162float(e);
+          if (sum > 0.0f && isfinite(kept)) factor *= sum / -kept;
+        }
+      }
+      p.loss[row] = loss;
+      if (p.E) p.factor[row] = factor;
+    }
+    factors[lane] = factor;
+  }
+  if (!p.xs) return;
+  __syncthreads();
+  const int per_row = p.d / 8;
+  const int64_t left = p.rows - row0;
+  const int n = (int)(left < 32 ? left : 32) * per_row;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += 32 * kFinishWarps) {
+    const int r = i / per_row, c = (i - r * per_row) * 8;
+    float f[8];
+    tc::unpack8(*reinterpret_cast<const uint4*>(p.x + (row0 + r) * p.ldx + c), f);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = factors[r] != 0.0f ? f[e] * factors[r] : 0.0f;  // (a row that is ignored may hold anything)
+    *reinterpret_cast<uint4*>(p.xs + (row0 + r) * p.d + c) = tc::pack8(f);
+  }
+}
+
+// out (rows ld apart, bf16) = factor[row] * the sum of `splits` [rows][d], in their order; eight channels a thread
+__global__ void __launch_bounds__(256) narrow_kernel(const float* in, int splits, const float* factor, bf16* out, int64_t ld, int64_t rows, int d) {
+  chain_next();
+  chain_wait();
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, n = rows * d;
+  if (i >= n) return;
+  float f[8] = {};
+#pragma unroll 4
+  for (int k = 0; k < splits; ++k) {
+    const float4 a = __ldcs(reinterpret_cast<const float4*>(in + k * n + i)), b = __ldcs(reinterpret_cast<const float4*>(in + k * n + i + 4));
+    f[0] += a.x; f[1] += a.y; f[2] += a.z; f[3] += a.w;
+    f[4] += b.x; f[5] += b.y; f[6] += b.z; f[7] += b.w;
+  }
+  const int64_t row = i / d;
+  if (factor) {
+    const float s = factor[row];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = s != 0.0f ? f[e] * s : 0.0f;
+  }
+  *reinterpret_cast<uint4*>(out + row * ld + (i - row * d)) = tc::pack8(f);
+}
+
+// ------------------------------------------------------------------------------------------- float
+// rows of src, ld apart -> planes; zeros for rows without a target (they may hold anything), where targets are given
+__global__ void __launch_bounds__(256) split_rows_kernel(const float* src, int64_t ld, Planes dst, int64_t rows, int d, Targets targets, int vocab) {
+  chain_next();
+  chain_wait();
+  const int per_row = d / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
+  if (row >= rows) return;
+  const int c = (int)(i - row * per_row) * 4;
+  const bool there = !targets.t || targets.column(row, vocab, nullptr) >= 0;
+  store_parts4(dst.p + row * dst.ld + c, dst.plane, there ? *reinterpret_cast<const float4*>(src + row * ld + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+}
+
+struct LogitsData {
+  const float* z;  // [rows][ldz], ldz a multiple of 4
+  int64_t ldz;
+  int vocab;
+  Targets targets;
+  int* status;
+  const float* d_loss;
+  int64_t d_loss_stride;
+  float* loss;
+  Planes dz;  // not of the forward pass alone
+};
+
+constexpr int kRowThreads = 512;
+
+// A block a row, which it reads once for the sum (twice where the target is far from the largest logit), and once more for dz.
+__global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p) {
+  __shared__ float sums[kRowThreads / 32], mosts[kRowThreads / 32];
+  chain_next();
+  chain_wait();
+  const int64_t row = blockIdx.x;
+  const float* z = p.z + row * p.ldz;
+  const int t = p.targets.column(row, p.vocab, threadIdx.x == 0 ? p.status : nullptr), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float zt = t >= 0 ? z[t] : 0.0f;
+  float ref = isfinite(zt) ? zt : 0.0f, sum = 0.0f, most = -INFINITY;
+  if (t >= 0) {
+    for (int again = 0; again < 2; ++again) {
+      sum = 0.0f;
+      for (int c = threadIdx.x * 4; c < p.vocab; c += kRowThreads * 4) {
+        const float4 q = *reinterpret_cast<const float4*>(z + c);
+        const float v[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < p.vocab && c + e != t) {
+            most = fmaxf(most, v[e]);
+            sum += expf(v[e] - ref);
+          }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      }
+      __syncthreads();
+      if (lane == 0) {
+        sums[warp] = sum;
+        mosts[warp] = most;
+      }
+      __syncthreads();
+      sum = 0.0f;
+      for (int k = 0; k < kRowThreads / 32; ++k) {
+        sum += sums[k];
+        most = fmaxf(most, mosts[k]);
+      }
+      if (!(most - ref > kFar)) break;
+      ref = most;
+    }
+  }
+  const bool at_target = zt == ref;
+  const float total = sum + (at_target ? 1.0f : expf(zt - ref));
+  if (threadIdx.x == 0) p.loss[row] = t < 0 ? 0.0f : at_target ? log1pf(sum) : logf(total) - (zt - ref);
+  if (!p.dz.p) return;
+  const float factor = t < 0 ? 0.0f : (p.d_loss ? p.d_loss[row * p.d_loss_stride] : 1.0f) / total;
+  bf16* out = p.dz.p + row * p.dz.ld;
+  for (int c = threadIdx.x * 4; c < p.vocab; c += kRowThreads * 4) {
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (factor != 0.0f) {
+      const float4 q = *reinterpret_cast<const float4*>(z + c);
+      v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = c + e >= p.vocab ? 0.0f : factor * (c + e == t ? -sum : expf(v[e] - ref));
+    }
+    store_parts4(out + c, p.dz.plane, make_float4(v[0], v[1], v[2], v[3]));
+  }
+}
+
+// ------------------------------------------------------------------------------------------- host
+size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+int64_t plane_ld(int64_t cols) { return cols < 256 ? (cols + 15) / 16 * 16 : (cols + 63) / 64 * 64; }
+
+// How many ways dx's contraction over the vocabulary is split, so that its few tiles fill the waves of CTA pairs: 8192 rows of 768 channels are 96 tiles,
+// 1.3 waves that take the time of 2, and split in three 3.9 of 4.  In blocks of 64: a tile's own, 8 for its beginning and end, and the partial
+// sums, which cost what 8 bytes an element do (512 clocks a block; 3.4 bytes a clock and pair from memory).
+int dx_splits(int64_t rows, int vocab, int d) {
+  const bool pair = rows > 128;
+  const int64_t tile = pair ? 256 : 128, tiles = (rows + tile - 1) / tile * ((d + 255) / 256), at_once = pair ? kPairs : 2 * kPairs, blocks = (vocab + 63) / 64;
+  const double sums = 8.0 * (double)rows * d / (at_once * (pair ? 44.0 : 22.0) * 512);
+  int best = 1;
+  double least = 0;
+  for (int n = 1; n <= 32 && (n == 1 || blocks / n >= 8); ++n) {
+    const double cost = (double)((tiles * n + at_once - 1) / at_once) * ((blocks + n - 1) / n + 8) + (n > 1 ? n * sums + 10 : 0);
+    if (n == 1 || cost < 0.97 * least) {
+      best = n;
+      least = cost;
+    }
+  }
+  return best;
+}
+
+// The scratch of pieces of `piece` rows.
+struct Plan {
+  int64_t piece;
+  int splits = 1;
+  int64_t ldE = 0;  // bf16: of E; float: of the logits
+  size_t target, zt, ref, factor, words, parts = 0, E = 0, xs = 0, partial = 0, dwf = 0, xp = 0, wp = 0, ep = 0;
+  size_t bytes = 0;
+  Planes x, w, e;  // float: strides alone
+  Plan(int dtype, int64_t rows, int vocab, int d, bool grads, bool dw_bf16, int64_t n) : piece(n) {
+    auto take = [&](size_t b) {
+      const size_t at = bytes;
+      bytes += up(b);
+      return at;
+    };
+    words = take(256);
+    target = take(n * 4);
+    zt = take(n * 4);
+    ref = take(n * 4);
+    factor = take(n * 4);
+    if (dtype == HBP_BF16) {
+      ldE = ((int64_t)vocab + 63) / 64 * 64;
+      parts = take((size_t)2 * ((vocab + 127) / 128) * n * 8);
+      if (grads) {
+        E = take((size_t)n * ldE * 2);
+        xs = take((size_t)n * d * 2);
+        splits = dx_splits(n, vocab, d);
+        if (splits > 1) partial = take((size_t)splits * n * d * 4);
+        if (dw_bf16 && n < rows) dwf = take((size_t)vocab * d * 4);
+      }
+      return;
+    }
+    ldE = ((int64_t)vocab + 3) / 4 * 4;
+    x.ld = w.ld = plane_ld(d);
+    e.ld = plane_ld(vocab);
+    x.plane = n * x.ld;
+    w.plane = vocab * w.ld;
+    e.plane = n * e.ld;
+    xp = take((size_t)3 * x.plane * 2);
+    wp = take((size_t)3 * w.plane * 2);
+    E = take((size_t)n * ldE * 4);
+    if (grads) ep = take((size_t)3 * e.plane * 2);
+  }
+};
+constexpr int64_t kLeastPiece = 256;
+// what grows with rows times vocab: bytes a row
+size_t row_bytes(int dtype, int vocab, bool grads) { return dtype == HBP_BF16 ? (grads ? (size_t)vocab * 2 : (size_t)(vocab + 127) / 128 * 16) : (size_t)vocab * (grads ? 10 : 4); }
+
+int64_t wanted_piece(int dtype, int64_t rows, int vocab, bool grads) {
+  const size_t b = row_bytes(dtype, vocab, grads);
+  int64_t n = (int64_t)(kPieceBytes / b) / kLeastPiece * kLeastPiece;
+  if (n < kLeastPiece) n = kLeastPiece;
+  if (n >= rows) return rows;
+  const int64_t pieces = (rows + n - 1) / n;  // of like size
+  n = ((rows + pieces - 1) / pieces + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
+  return n < rows ? n : rows;
+}
+
+struct Call {
+  const hbp_vocabulary* v;
+  const float* d_loss = nullptr;
+  int64_t d_loss_stride = 0;
+  float* loss = nullptr;
+  void* dx = nullptr;
+  int64_t lddx = 0;
+  void* dw = nullptr;
+  int dw_dtype = 0;
+  int64_t lddw = 0;
+  bool grads = false;
+  uint8_t* scratch = nullptr;
+  bool dw_bf16() const { return dw && dw_dtype == HBP_BF16; }
+};
+
+bool run_bf16(Launcher& lc, const Call& c, const Plan& plan, int* status) {
+  const hbp_vocabulary& v = *c.v;
+  uint8_t* s = c.scratch;
+  const bool pieces = plan.piece < v.rows;
+  for (int64_t lo = 0; lo < v.rows; lo += plan.piece) {
+    const int64_t n = v.rows - lo < plan.piece ? v.rows - lo : plan.piece;
+    RowData p = {};
+    p.rows = n;
+    p.vocab = v.vocab; p.d = v.d;
+    p.x = (const bf16*)v.x + lo * v.ldx; p.ldx = v.ldx;
+    p.w = (const bf16*)v.w; p.ldw = v.ldw;
+    p.targets = {(const uint8_t*)v.targets + lo * v.target_bytes, v.target_bytes};
+    p.status = v.status;
+    p.target = (int*)(s + plan.target);
+    p.zt = (float*)(s + plan.zt);
+    p.ref = (float*)(s + plan.ref);
+    p.factor = (float*)(s + plan.factor);
+    p.parts = (float2*)(s + plan.parts);
+    p.redo = (int*)(s + plan.words);
+    p.d_loss = c.d_loss ? c.d_loss + lo * c.d_loss_stride : nullptr;
+    p.d_loss_stride = c.d_loss_stride;
+    p.loss = c.loss + lo;
+    if (c.grads) {
+      p.E = (bf16*)(s + plan.E);
+      p.ldE = plan.ldE;
+      if (c.dw) p.xs = (bf16*)(s + plan.xs);
+    }
+    launch_chained(lc, target_kernel, dim3((unsigned)((n + 7) / 8)), 256, 0, 1, p);
+    GemmArgs g;
+    g.M = (int)n; g.N = v.vocab; g.K = v.d;
+    g.in_dtype = HBP_BF16;
+    g.A = p.x; g.a_sm = v.ldx; g.a_sk = 1;
+    g.B = p.w; g.b_sn = v.ldw; g.b_sk = 1;
+    g.epi = EPI_EXP;
+    g.D = p.E; g.ldd = p.ldE;
+    g.row_f = p.ref; g.target = p.target; g.row_parts = p.parts; g.slots_out = &p.slots;
+    for (int again = 0; again < 2; ++again) {
+      p.again = again != 0;
+      g.redo = again ? p.redo : nullptr;
+      if (!gemm_tc(lc, g, status)) return false;
+      launch_chained(lc, finish_kernel, dim3((unsigned)((n + 31) / 32)), 32 * kFinishWarps, 0, 1, p);
+    }
+    if (c.dx) {
+      GemmArgs b;
+      b.M = (int)n; b.N = v.d; b.K = v.vocab;
+      b.in_dtype = HBP_BF16;
+      b.A = p.E; b.a_sm = p.ldE; b.a_sk = 1;
+      b.B = p.w; b.b_sn = 1; b.b_sk = v.ldw;
+      bf16* dx = (bf16*)c.dx + lo * c.lddx;
+      const int splits = std::min(plan.splits, dx_splits(n, v.vocab, v.d));  // (the last piece is smaller, and its memory the others')
+      if (splits > 1) {
+        b.splitk = splits;
+        b.wide = true;
+        b.partial = (float*)(s + plan.partial);
+        b.d_f32 = true;
+        b.D = b.partial; b.ldd = v.d;
+        int made = 1;
+        b.splits_out = &made;
+        if (!gemm_tc(lc, b, status)) return false;
+        launch_chained(lc, narrow_kernel, dim3((unsigned)((n * v.d / 8 + 255) / 256)), 256, 0, 1, (const float*)b.partial, made, p.factor, dx, c.lddx, n, v.d);
+      } else {
+        b.epi = EPI_ROWS;
+        b.row_f = p.factor;
+        b.D = dx; b.ldd = c.lddx;
+        if (!gemm_tc(lc, b, status)) return false;
+      }
+    }
+    if (c.dw) {
+      GemmArgs b;
+      b.M = v.vocab; b.N = v.d; b.K = (int)n;
+      b.in_dtype = HBP_BF16;
+      b.A = p.E; b.a_sm = 1; b.a_sk = p.ldE;
+      b.B = p.xs; b.b_sn = 1; b.b_sk = v.d;
+      const bool narrow_after = pieces && c.dw_bf16();
+      b.d_f32 = narrow_after || !c.dw_bf16();
+      b.D = narrow_after ? (void*)(s + plan.dwf) : c.dw;
+      b.ldd = narrow_after ? v.d : c.lddw;
+      if (lo) b.epi = EPI_ACCUM;
+      if (!gemm_tc(lc, b, status)) return false;
+      if (narrow_after && lo + n == v.rows)
+        launch_chained(lc, narrow_kernel, dim3((unsigned)(((int64_t)v.vocab * v.d / 8 + 255) / 256)), 256, 0, 1, (const float*)b.D, 1, (const float*)nullptr, (bf16*)c.dw,
+                       c.lddw, (int64_t)v.vocab, v.d);
+    }
+  }
+  return true;
+}
+
+bool run_f32(Launcher& lc, const Call& c, const Plan& plan, int* status) {
+  const hbp_vocabulary& v = *c.v;
+  uint8_t* s = c.scratch;
+  Planes x = plan.x, w = plan.w, e = plan.e;
+  x.p = (bf16*)(s + plan.xp);
+  w.p = (bf16*)(s + plan.wp);
+  auto split = [&](const float* src, int64_t ld, const Planes& P, int64_t rows, const Targets& targets) {
+    launch_chained(lc, split_rows_kernel, dim3((unsigned)((rows * (v.d / 4) + 255) / 256)), 256, 0, 1, src, ld, P, rows, v.d, targets, v.vocab);
+  };
+  split((const float*)v.w, v.ldw, w, v.vocab, Targets{nullptr, 8});
+  for (int64_t lo = 0; lo < v.rows; lo += plan.piece) {
+    const int64_t n = v.rows - lo < plan.piece ? v.rows - lo : plan.piece;
+    const Targets targets = {(const uint8_t*)v.targets + lo * v.target_bytes, v.target_bytes};
+    split((const float*)v.x + lo * v.ldx, v.ldx, x, n, targets);
+    PartsGemm g;
+    g.M = (int)n; g.N = v.vocab; g.K = v.d;
+    g.A = x; g.B = w;
+    g.D = (float*)(s + plan.E); g.ldd = plan.ldE;
+    if (!gemm_parts(lc, g, status)) return false;
+    LogitsData p = {};
+    p.z = g.D; p.ldz = plan.ldE;
+    p.vocab = v.vocab;
+    p.targets = targets;
+    p.status = v.status;
+    p.d_loss = c.d_loss ? c.d_loss + lo * c.d_loss_stride : nullptr;
+    p.d_loss_stride = c.d_loss_stride;
+    p.loss = c.loss + lo;
+    if (c.grads) {
+      e.p = (bf16*)(s + plan.ep);
+      p.dz = e;
+    }
+    launch_chained(lc, logits_kernel, dim3((unsigned)n), kRowThreads, 0, 1, p);
+    if (c.dx) {
+      PartsGemm b;
+      b.M = (int)n; b.N = v.d; b.K = v.vocab;
+      b.A = e; b.B = w;
+      b.b_mn = true;
+      b.D = (float*)c.dx + lo * c.lddx; b.ldd = c.lddx;
+      if (!gemm_parts(lc, b, status)) return false;
+    }
+    if (c.dw) {
+      PartsGemm b;
+      b.M = v.vocab; b.N = v.d; b.K = (int)n;
+      b.A = e; b.B = x;
+      b.a_mn = b.b_mn = true;
+      b.D = (float*)c.dw; b.ldd = c.lddw;
+      if (lo) {
+        b.epi = EPI_RESID;
+        b.E = (const float*)c.dw; b.lde = c.lddw;
+      }
+      if (!gemm_parts(lc, b, status)) return false;
+    }
+  }
+  return true;
+}
+
+hbp_status check(const hbp_vocabulary* v) {
+  if (!v) return HBP_ERR_INVALID_ARG;
+  if (v->dtype != HBP_F32 && v->dtype != HBP_BF16) return HBP_ERR_DTYPE;
+  const int k = v->dtype == HBP_F32 ? 4 : 8;
+  // (columns and rows of tiles are 32-bit numbers, a little beyond the last ones too)
+  if (v->rows < 0 || v->rows > (1 << 30) || v->vocab <= 0 || v->vocab > (1 << 30) || v->d <= 0 || v->d % k || v->d > (1 << 24)) return HBP_ERR_SHAPE;
+  if (v->target_bytes != 4 && v->target_bytes != 8) return HBP_ERR_INVALID_ARG;
+  if (((uintptr_t)v->targets % v->target_bytes) || ((uintptr_t)v->status & 3u)) return HBP_ERR_SHAPE;
+  return HBP_OK;
+}
+bool bad_rows(const void* t, int64_t ld, int d, int v) { return ((uintptr_t)t & 15u) || ld % v || ld < d; }
+
+hbp_status call(Call& c, void* scratch, size_t bytes, void* stream) {
+  const hbp_vocabulary& v = *c.v;
+  const int k = v.dtype == HBP_F32 ? 4 : 8;
+  if (!v.w || (v.rows && (!v.x || !v.targets || !c.loss))) return HBP_ERR_INVALID_ARG;
+  if (bad_rows(v.w, v.ldw, v.d, k) || (v.rows && bad_rows(v.x, v.ldx, v.d, k)) || ((uintptr_t)c.loss & 3u)) return HBP_ERR_SHAPE;
+  Launcher lc;
+  lc.stream = (cudaStream_t)stream;
+  if (v.rows == 0) {
+    if (!c.dw) return HBP_OK;
+    const size_t es = c.dw_bf16() ? 2 : 4;
+    return cudaMemset2DAsync(c.dw, c.lddw * es, 0, v.d * es, v.vocab, lc.stream) == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
+  }
+  int64_t n = wanted_piece(v.dtype, v.rows, v.vocab, c.grads);
+  auto plan_of = [&](int64_t piece) { return Plan(v.dtype, v.rows, v.vocab, v.d, c.grads, c.dw_bf16(), piece); };
+  if (!scratch || ((uintptr_t)scratch & 255u)) return HBP_ERR_WORKSPACE;
+  while (plan_of(n).bytes > bytes) {  // smaller pieces for less memory
+    if (n <= kLeastPiece) return HBP_ERR_WORKSPACE;
+    n = (n / 2 + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
+  }
+  const Plan plan = plan_of(n);
+  c.scratch = (uint8_t*)scratch;
+  int* status = v.status ? v.status : (int*)(c.scratch + plan.words) + 1;
+  const bool ok = v.dtype == HBP_BF16 ? run_bf16(lc, c, plan, status) : run_f32(lc, c, plan, status);
+  return ok && lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
+}
+
+}  // namespace
+
+}  // namespace hbp
+
+using namespace hbp;
+
+extern "C" hbp_status hbp_cross_entropy_scratch_bytes(const hbp_vocabulary* v, int32_t gradients, size_t* bytes) {
+  if (!bytes) return HBP_ERR_INVALID_ARG;
+  const hbp_status st = check(v);
+  if (st != HBP_OK) return st;
+  const bool grads = gradients != 0;
+  *bytes = v->rows ? Plan(v->dtype, v->rows, v->vocab, v->d, grads, true, wanted_piece(v->dtype, v->rows, v->vocab, grads)).bytes : 0;
+  return HBP_OK;
+}
+
+extern "C" hbp_status hbp_cross_entropy(const hbp_vocabulary* v, float* loss, void* scratch, size_t scratch_bytes, void* cuda_stream) {
+  const hbp_status st = check(v);
+  if (st != HBP_OK) return st;
+  Call c;
+  c.v = v;
+  c.loss = loss;
+  return call(c, scratch, scratch_bytes, cuda_stream);
+}
+
+extern "C" hbp_status hbp_cross_entropy_gradients(const hbp_vocabulary* v, const float* d_loss, int64_t d_loss_stride, float* loss, void* dx, int64_t lddx,
+                                                  void* dw, int32_t dw_dtype, int64_t lddw, void* scratch, size_t scratch_bytes, void* cuda_stream) {
+  const hbp_status st = check(v);
+  if (st != HBP_OK) return st;
+  const int k = v->dtype == HBP_F32 ? 4 : 8;
+  if (!dx && !dw) return HBP_ERR_INVALID_ARG;
+  if (dw && dw_dtype != HBP_F32 && !(dw_dtype == HBP_BF16 && v->dtype == HBP_BF16)) return HBP_ERR_DTYPE;
+  if (d_loss_stride < 0 || ((uintptr_t)d_loss & 3u) || (dx && v->rows && bad_rows(dx, lddx, v->d, k)) || (dw && bad_rows(dw, lddw, v->d, dw_dtype == HBP_F32 ? 4 : 8)))
+    return HBP_ERR_SHAPE;
+  Call c;
+  c.v = v;
+  c.d_loss = d_loss;
+  c.d_loss_stride = d_loss_stride;
+  c.loss = loss;
+  c.dx = dx; c.lddx = lddx;
+  c.dw = dw; c.dw_dtype = dw_dtype; c.lddw = lddw;
+  c.grads = true;
+  return call(c, scratch, scratch_bytes, cuda_stream);
+}

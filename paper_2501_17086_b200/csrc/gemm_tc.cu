@@ -71,7 +71,21 @@ struct TcParams {
   int* status;
   uint64_t wait_limit_ns;  // limit of every barrier wait
   int stall;               // self-test of the bounded waits only.  1: the first stage is armed and nothing copied; 2: B copied, nothing armed
+  // EPI_EXP, EPI_ROWS
+  const float* row_f;
+  const int* target;
+  float2* row_parts;
+  const int* redo;
+  int panel;  // row blocks that share a column block's copies
 };
+
+// EPI_EXP: tiles go down `panel` row blocks of one column block, then on to the next one: w is far too large for L2, those rows of x
+// are not.  (Along the columns, as everywhere else, each row block would read all of w again: 4096 x 50021 x 1024 read 1.6 GB.)
+__device__ __forceinline__ void panel_tile(const TcParams& p, int r, int& m, int& n) {
+  const int per_panel = p.panel * p.n_tiles, first = r / per_panel * p.panel, q = r % per_panel, rows = min(p.panel, p.m_tiles - first);
+  m = first + q % rows;
+  n = q / rows;
+}
 
 // ------------------------------------------------------------------------------------------- epilogue math
 // Two floats in one 64-bit register: one instruction does both (the forward GELU is bound by how many it issues).
@@ -155,9 +169,48 @@ __device__ __forceinline__ void residual_chunk(const TcParams& p, int b, int row
   }
 }
 
+// EPI_EXP on 64 columns of a row, from `col` on: z -> exp(z - ref), 0 for the target's column and those behind the last; what that adds to the
+// row's sum and largest z.
+__device__ __forceinline__ void exp_chunk(float* v, int col, int N, int target, float ref, float& sum, float& most) {
+  const uint32_t at = (uint32_t)(target - col);
+  if (__any_sync(0xffffffffu, at < 64u)) {
+#pragma unroll
+    for (int i = 0; i < 64; ++i) v[i] = at == (uint32_t)i ? -INFINITY : v[i];
+  }
+  if (col + 64 > N) {
+#pragma unroll
+    for (int i = 0; i < 64; ++i) v[i] = col + i >= N ? -INFINITY : v[i];
+  }
+  // the difference first: a product with log2(e) of each, and one rounding less, would be off by |z| 2^-24
+  const f32x2 less = both(-ref), log2e = both(1.44269504088896340736f);
+  f32x2 s2[2] = {both(0.0f), both(0.0f)};
+  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < 64; i += 4) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] = fmaxf(m[k], v[i + k]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float* e = v + i + 2 * k;
+      f32x2 d;
+      asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack2(e[0], e[1])), "l"(less));
+      unpack2(mul2(d, log2e), e[0], e[1]);
+      asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[0]));
+      asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[1]));
+      asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s2[k]) : "l"(pack2(e[0], e[1])));
+    }
+  }
+  most = fmaxf(fmaxf(most, fmaxf(m[0], m[1])), fmaxf(m[2], m[3]));
+  float s0, s1, t0, t1;
+  unpack2(s2[0], s0, s1);
+  unpack2(s2[1], t0, t1);
+  sum += (s0 + s1) + (t0 + t1);
+}
+
 // ------------------------------------------------------------------------------------------- kernel
+// kRows: the epilogues EPI_EXP and EPI_ROWS, which know their row, and launches that may turn out to be needless; else the others.
 // kNarrow: tiles of p.n_mma columns; else of 256, whose constants the compiler folds (a run-time width costs the large products 2 to 4 %)
-template <bool kPair, bool kTf32, bool kNarrow>
+template <bool kPair, bool kTf32, bool kNarrow, bool kRows = false>
 __global__ void __launch_bounds__(THREADS, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1,
@@ -175,7 +228,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   // issues the MMAs, its peer's tile loads signal the leader's barriers
   const uint32_t rank = kPair ? cluster_ctarank() : 0u;
   const bool leader = rank == 0;
-  const int first_tile = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
+  int first_tile = kPair ? (int)(blockIdx.x >> 1) : (int)blockIdx.x;
   const int tile_step = kPair ? (int)(gridDim.x >> 1) : (int)gridDim.x;
   extern __shared__ uint8_t smem_raw[];
   // the swizzled tiles need 1024-byte alignment
@@ -232,6 +285,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const uint32_t tmem_base = *tmem_slot;
   chain_next();
   chain_wait();
+  if (kRows && p.redo && *(const volatile int*)p.redo == 0) first_tile = p.num_tiles;  // (every role, of both CTAs, finds no tile)
   const int tiles_per_batch = p.m_tiles * p.n_tiles;
   // per element size: elements per 128-byte row (= K elements per stage), bytes of one MN-major block
   const int row_elems = kTf32 ? 32 : 64;
@@ -248,7 +302,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const int zc = tile / tiles_per_batch, r = tile % tiles_per_batch;
         const int b = zc % p.batch, split = zc / p.batch;
         // n fastest: a wave shares few A row-panels.  This CTA's rows of A and (pair) its half of B's columns
-        const int m0 = (r / p.n_tiles) * TILE_M + (int)rank * BM, n0 = (r % p.n_tiles) * tile_n + (kPair ? (int)rank * b_rows : 0);
+        int mt = r / p.n_tiles, nt = r % p.n_tiles;
+        if (kRows && p.panel) panel_tile(p, r, mt, nt);
+        const int m0 = mt * TILE_M + (int)rank * BM, n0 = nt * tile_n + (kPair ? (int)rank * b_rows : 0);
         const int kb_lo = split * p.kb_per_split, kb_hi = min(p.k_blocks, kb_lo + p.kb_per_split);
         for (int seg = 0; seg < p.segs && ok; ++seg) {
           const CUtensorMap* mA = seg == 0 ? &tmA : (seg == 1 ? &tmA1 : &tmA2);
@@ -388,7 +444,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     for (int tile = first_tile; tile < p.num_tiles; tile += tile_step) {
       // b indexes the outputs: with split-K it is split * batch + batch entry (partial sums [split][batch][M][N])
       const int b = tile / tiles_per_batch, r = tile % tiles_per_batch;
-      const int m0 = (r / p.n_tiles) * TILE_M + (int)rank * BM, n0 = (r % p.n_tiles) * tile_n;  // this CTA's 128 rows
+      int mt = r / p.n_tiles, nt = r % p.n_tiles;
+      if (kRows && p.panel) panel_tile(p, r, mt, nt);
+      const int m0 = mt * TILE_M + (int)rank * BM, n0 = nt * tile_n;  // this CTA's 128 rows
       const int row0 = m0 + quarter * 32, colw = n0 + half * half_cols;
       // chunk c of E goes through buffer c % EPI_BUFS, where the result replaces it
       auto load_e = [&](int c) {
@@ -402,6 +460,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         load_e(0);
         if (EPI_BUFS > 1 && nchunks > 1) load_e(1);
       }
+      // (kRows) this lane's row
+      const bool row_in = kRows && row0 + lane < p.M;
+      const float row_f = row_in ? p.row_f[row0 + lane] : 0.0f;
+      const int target = row_in && p.epi == EPI_EXP ? p.target[row0 + lane] : -1;
+      float row_total = 0.0f, row_most = -INFINITY;
       if (!mbar_wait(accf_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit_ns)) break;
       tc_fence_after();
       const uint32_t tsrc = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + half * half_cols);
@@ -434,6 +497,19 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             if (lane == 0) release_acc(acc);
           }
           const int col = colw + c * cw;
+          if (kRows && p.epi == EPI_EXP) {
+            exp_chunk(v, col, p.N, target, row_f, row_total, row_most);
+            if (!p.D) continue;
+            if (__any_sync(0xffffffffu, target < 0)) {
+#pragma unroll
+              for (int i = 0; i < 64; ++i) v[i] = target >= 0 ? v[i] : 0.0f;  // (a row that is ignored may hold anything)
+            }
+          }
+          if (kRows && p.epi == EPI_ROWS) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+              if (i < cw) v[i] = row_f != 0.0f ? v[i] * row_f : 0.0f;
+          }
           // the buffer this chunk goes through; without E the oldest one, once its last copy out has read it
           const uint32_t bi = has_e ? (uint32_t)(c % EPI_BUFS) : next_buf;
           uint32_t buf = buf0 + bi * EPI_BUF_BYTES;
@@ -516,6 +592,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
         if (!ok) break;
       }
+      if (kRows && p.epi == EPI_EXP && row_in)
+        p.row_parts[(int64_t)(nt * 2 + half) * p.M + row0 + lane] = make_float2(row_total, row_most);
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
     if (lane == 0) {
@@ -570,7 +648,7 @@ bool make_map(CUtensorMap* tm, const void* base, int extent_mn, int K, int batch
 // one.  In tiles of 256 / 128 columns: 2664 x 512 x 2048 15.8 / 14.5 us, 2664 x 512 x 1536 13.5 / 12.2, 1000 x 768 x 3072 20.0 / 18.7; but
 // 2664 x 2048 x 512 11.9 / 13.5 and 8192 x 1024 x 4096 48.8 / 79, where there are enough.
 int pair_tile_width(const GemmArgs& g, int k_blocks, int pairs) {
-  const int per_col = g.epi == EPI_GELU_FWD ? 24 : g.epi == EPI_MUL || g.epi == EPI_STORE_LN || g.epi == EPI_ACCUM ? 14 : 8;
+  const int per_col = g.epi == EPI_GELU_FWD ? 24 : g.epi == EPI_MUL || g.epi == EPI_STORE_LN || g.epi == EPI_ACCUM || g.epi == EPI_EXP ? 14 : 8;
   const int64_t rows = (int64_t)((g.M + 255) / 256) * g.batch;
   int64_t best = 0;
   int width = BN;
@@ -645,14 +723,17 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   if (!f32 && g.A2) return false;
   if (g.M <= 0 || g.N <= 0 || g.K <= 0 || g.batch <= 0) return false;
   const int vec = f32 ? 4 : 8;  // elements per 16 bytes
-  if (g.N % vec) return false;
-  if (g.epi != EPI_STORE && g.epi != EPI_GELU_FWD && g.epi != EPI_MUL && g.epi != EPI_RESID && g.epi != EPI_STORE_LN &&
+  const bool by_rows = g.epi == EPI_EXP || g.epi == EPI_ROWS;
+  if (g.N % vec && g.epi != EPI_EXP) return false;
+  if (by_rows && (f32 || g.batch != 1 || g.splitk > 1 || !g.row_f)) return false;
+  if (g.epi == EPI_EXP && (g.d_f32 || !g.target || !g.row_parts)) return false;
+  if (!by_rows && g.epi != EPI_STORE && g.epi != EPI_GELU_FWD && g.epi != EPI_MUL && g.epi != EPI_RESID && g.epi != EPI_STORE_LN &&
       g.epi != EPI_ADD && g.epi != EPI_ACCUM)
     return false;
   if (g.epi == EPI_ADD && (!g.E || !(g.d_f32 || g.in_dtype == HBP_F32) || g.splitk > 1)) return false;  // float outputs only
   if (g.epi == EPI_STORE_LN && (!g.stats || !g.E)) return false;
   const bool out_f32 = g.d_f32 || f32;
-  if (out_f32 && g.epi != EPI_STORE && g.epi != EPI_ADD && g.epi != EPI_ACCUM) return false;
+  if (out_f32 && g.epi != EPI_STORE && g.epi != EPI_ADD && g.epi != EPI_ACCUM && g.epi != EPI_ROWS) return false;
   if (g.epi == EPI_ACCUM && (!g.d_f32 || f32 || g.splitk > 1)) return false;
   if (g.splitk > 1 && (g.epi != EPI_STORE || !out_f32 || !g.partial || g.ldd != g.N || (g.batch > 1 && g.d_sb != (int64_t)g.M * g.N)))
     return false;
@@ -666,12 +747,12 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   if (!operand_ok(B0, b_sn, b_sk, g.b_sb, g.batch, &b_mn, vec)) return false;
   // K may be ragged where it is no operand's contiguous index (weight gradients of any number of rows): the copies fill rows past its end
   // with zeros.  Weight gradients of 2500 rows went to the CUDA cores for that: 6 layers 1800 (5000), exact pass 49.4 -> 1.3 ms.
-  if (g.K % vec && !(a_mn && b_mn)) return false;
+  // (Nor does it matter where rows of K are whole vectors apart, as operand_ok has seen to.)
+  if (f32 && g.K % vec) return false;
   if (f32 && (!aligned16(g.A_lo) || !aligned16(g.B_lo))) return false;
   // 32-bit MN-major operands need a shared-memory layout of their own that this kernel does not build:
   // float operands must be K-major (the callers write the split copies that way)
   if (f32 && (a_mn || b_mn || g.batch != 1)) return false;
-  if (a_mn && g.M % vec) return false;
   // epilogue operands: 16-byte vectors
   const int dv = out_f32 ? 4 : 8;
   if (!aligned16(g.D) || g.ldd % dv || g.d_sb % dv) return false;
@@ -693,7 +774,9 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   const bool pair = lc.gemm_pair && sms >= 2 && g.M > BM && !narrow && !f32;
   const int row_elems = f32 ? 32 : 64;
   const int k_blocks = (g.K + row_elems - 1) / row_elems;
-  const int n_mma = narrow ? (g.N <= 64 ? 64 : 128) : pair ? pair_tile_width(g, k_blocks, sms / 2) : BN;
+  // (EPI_EXP: two of its row sums a tile; a split product fills the pairs by its splits)
+  int n_mma = narrow ? (g.N <= 64 ? 64 : 128) : pair ? (g.splitk > 1 && g.wide ? BN : pair_tile_width(g, k_blocks, sms / 2)) : BN;
+  if (pair && g.epi == EPI_EXP && n_mma < 128) n_mma = 128;
   const int b_rows = pair ? n_mma / 2 : n_mma;
   CUtensorMap tmA, tmB;
   if (!make_map(&tmA, A0, g.M, g.K, g.batch, a_sm, a_sk, g.a_sb, a_mn, BM, f32)) return false;
@@ -719,7 +802,7 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
     if (g.batch > 1 && g.d_sb <= 0) return false;
     if (splits > 1) {
       if (!make_map_epi(&tmD, g.partial, true, g.M, g.N, g.batch * splits, g.N, (int64_t)g.M * g.N)) return false;
-    } else if (!make_map_epi(&tmD, g.D, out_f32, g.M, g.N, g.batch, g.ldd, g.d_sb)) return false;
+    } else if (g.D && !make_map_epi(&tmD, g.D, out_f32, g.M, g.N, g.batch, g.ldd, g.d_sb)) return false;
     if (g.epi == EPI_GELU_FWD && !make_map_epi(&tmD2, g.D2, false, g.M, g.N, g.batch, g.ldd2, g.d2_sb)) return false;
     if ((g.epi == EPI_MUL || g.epi == EPI_STORE_LN) && !make_map_epi(&tmE, g.E, false, g.M, g.N, g.batch, g.lde, g.e_sb))
       return false;
@@ -732,7 +815,9 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   if (!attr_set) {
     bool ok = true;
     for (auto kernel : {gemm_tc_kernel<false, false, false>, gemm_tc_kernel<false, false, true>, gemm_tc_kernel<false, true, false>,
-                        gemm_tc_kernel<false, true, true>, gemm_tc_kernel<true, false, false>, gemm_tc_kernel<true, false, true>})
+                        gemm_tc_kernel<false, true, true>, gemm_tc_kernel<true, false, false>, gemm_tc_kernel<true, false, true>,
+                        gemm_tc_kernel<false, false, false, true>, gemm_tc_kernel<false, false, true, true>,
+                        gemm_tc_kernel<true, false, false, true>, gemm_tc_kernel<true, false, true, true>})
       ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) == cudaSuccess;
     if (!ok) {
       cudaGetLastError();
@@ -767,14 +852,25 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   p.status = status_word;
   p.wait_limit_ns = g.wait_limit_ns ? g.wait_limit_ns : WAIT_LIMIT_NS;
   p.stall = g.test_stall;
+  p.row_f = g.row_f; p.target = g.target; p.row_parts = g.row_parts; p.redo = g.redo;
+  if (g.slots_out) *g.slots_out = 2 * p.n_tiles;
+  p.panel = 0;
+  if (g.epi == EPI_EXP) {  // rows of x of 32 MB, a quarter of L2
+    const int64_t fits = (32 << 20) / ((int64_t)(pair ? 256 : BM) * g.K * 2);
+    p.panel = (int)(fits < 1 ? 1 : fits < p.m_tiles ? fits : p.m_tiles);
+  }
   const bool full = n_mma == BN;
   const int workers = pair ? sms / 2 : sms;
   auto kernel = pair ? (full ? gemm_tc_kernel<true, false, false> : gemm_tc_kernel<true, false, true>)
                      : (f32 ? (full ? gemm_tc_kernel<false, true, false> : gemm_tc_kernel<false, true, true>)
                             : (full ? gemm_tc_kernel<false, false, false> : gemm_tc_kernel<false, false, true>));
+  if (by_rows)
+    kernel = pair ? (full ? gemm_tc_kernel<true, false, false, true> : gemm_tc_kernel<true, false, true, true>)
+                  : (full ? gemm_tc_kernel<false, false, false, true> : gemm_tc_kernel<false, false, true, true>);
   launch_chained(lc, kernel, dim3((pair ? 2 : 1) * (p.num_tiles < workers ? p.num_tiles : workers)), THREADS, SMEM_BYTES, pair ? 2 : 1, tmA, tmB,
                  tmA1, tmB1, tmA2, tmB2, tmD, tmD2, tmE, p);
-  if (splits > 1) reduce_splitk(lc, g.partial, (float*)g.D, splits, (int64_t)g.batch * g.M * g.N);
+  if (g.splits_out) *g.splits_out = splits;
+  else if (splits > 1) reduce_splitk(lc, g.partial, (float*)g.D, splits, (int64_t)g.batch * g.M * g.N);
   return true;
 }
 

@@ -22,6 +22,8 @@ enum Epilogue {
   EPI_STORE_LN = 6,  // D = acc, plus per-row partial sums (sum acc, sum acc * E[m,n]) per 64 columns -> stats
   EPI_ADD = 7,       // D = acc + E[m,n]   (u_t + delta_t: the scan then reads one tensor less)
   EPI_ACCUM = 8,     // D += acc, D float (bf16 operands on the tensor cores only: gemm_tc; gemm() does not take it)
+  EPI_EXP = 9,         // D = exp(acc - row_f[m]), 0 at n = target[m] and in rows whose target is negative (bf16; no D: not stored); row_parts (gemm_tc only)
+  EPI_ROWS = 10,       // D = acc * row_f[m], 0 where that is 0 (gemm_tc only)
   EPI_RNN_FWD = 5,   // c = tanh(acc + E[m,n]);  D2 = 1 - c^2;  D = gate[n] * E2[m,n] + c
 };
 
@@ -55,6 +57,15 @@ struct GemmArgs {
   // fp32 accumulation, the small terms first).
   const float *A_hi = nullptr, *A_lo = nullptr, *B_hi = nullptr, *B_lo = nullptr;
   int64_t hl_a_sm = 0, hl_a_sk = 0, hl_b_sn = 0, hl_b_sk = 0;
+  // EPI_EXP, EPI_ROWS: a number a row; the column of each row that is left out; per tile and half of its columns [slots][M] the row's (sum of
+  // what D receives, largest acc) without that column; where the number of those slots goes (host); a device word without which, 0, the launch does nothing
+  const float* row_f = nullptr;
+  const int* target = nullptr;
+  float2* row_parts = nullptr;
+  int* slots_out = nullptr;
+  const int* redo = nullptr;
+  bool wide = false;   // splitk > 1: tiles of full width
+  int* splits_out = nullptr;  // gemm_tc: where the number of splits goes, whose partial sums are then left to the caller (one: it went to D)
   int splitk = 1;      // > 1: partial sums to `partial` [splitk][batch][M][N], reduced in fixed order
   float* partial = nullptr;
   // self-test of the tensor-core kernel's bounded waits (hbp_selftest_wait_timeout): a wait limit other than the
