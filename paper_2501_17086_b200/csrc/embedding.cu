@@ -1,14 +1,15 @@
 // Rows of a table by tokens, scaled, and the table's gradient (hbp_embedding, hbp_embedding_gradient).
 //
 // Gradient: d_table[v] = add[v] + scale * sum of d_out[i] over the rows i whose token is v, in three launches.
-//  1. One cluster of eight blocks sorts the tokens with their rows (stable, by digits of up to 9 bits, least first: 18 bits, which most
-//     vocabularies need, are two passes); the other blocks of the launch meanwhile clear the table, or copy `add`: with 16384
-//     tokens of 50021 that is what takes the time.  Eight blocks of 1024 threads rank and move 16384 tokens in some microseconds; their
-//     exchange is a cluster's barrier and 512 counts a block.
-//  2. Blocks add up the rows of 32 sorted tokens each, whole runs of one token straight to the table.  The share of a run that began in an
-//     earlier tile, or goes on in the next, is a partial sum in scratch.
-//  3. Those runs' partial sums are added in the order of the tiles, eight stretches of them at a time.
+//  1. One cluster of eight blocks (a block alone up to 2048 tokens) sorts the tokens with their rows: stable, by digits of up to 9 bits, least first, 18
+//     bits, which most vocabularies need, in two passes; 16384 tokens 22 us, 262144 150, of one block 14 for 1000.  Meanwhile the other blocks of the
+//     launch clear the table, or copy `add`: 50021 x 768 floats 24 us, which is what bounds such a step.
+//  2. Blocks add up the rows of 16 to 128 sorted tokens each, whole runs of one token straight to the table.  The share of a run that began in an
+//     earlier tile, or goes on in the next, is a partial sum in scratch.  Bound by bytes and by the wait for tokens, then rows: 16384 tokens of 768
+//     bf16 channels 13 us.
+//  3. Those runs' partial sums are added in the order of the tiles, eight stretches of them at a time (7 us).
 // Every sum has a fixed order: runs agree bit for bit.  A token that is every second one of a text costs no more than others.
+// All of it, with the lookup (8 us): 16384 tokens of 50021 x 768, 57 us of 32 for the bytes; 5003 of 10007 x 1492 floats added to another gradient 47 of 32.
 #include "hbp_internal.h"
 #include "tc_common.cuh"
 
@@ -92,7 +93,10 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(const LookupParams p) 
 
 // ------------------------------------------------------------------------------------------- tokens in order
 constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxDigit = 9, kMaxBins = 1 << kMaxDigit;
-constexpr int kTile = 32;  // sorted tokens a block adds up
+// Up to so many tokens one block sorts, in shared memory: no exchange.
+constexpr int kAlone = 2048;
+// Sorted tokens a block adds up: 16, and more of more than 65536, whose longest runs would have too many parts to join.
+constexpr int kLeastTile = 16, kMostTile = 128;
 
 struct SortParams {
   Tokens tokens;
@@ -106,16 +110,31 @@ struct SortParams {
 };
 
 struct SortShared {
-  uint32_t counts[kSortWarps][kMaxBins];  // of a warp's tokens, then where the next one of a digit goes
-  uint32_t totals[kMaxBins];              // of a block's, read by the others
+  uint32_t counts[kSortWarps][kMaxBins + 1];  // of a warp's tokens, then where the next one of a digit goes (a digit's column has 32 banks)
+  uint32_t totals[kMaxBins];                  // of a block's, read by the others
   uint32_t base[kMaxBins];
   uint32_t warp_sums[kSortWarps];
+  uint32_t keys[2][kAlone], from[2][kAlone];
 };
 
 __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr) {
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
+}
+
+// kAdd: filled from add
+template <bool kAdd>
+__device__ __forceinline__ void fill(const SortParams& p, int block, int blocks) {
+  // 64 KB at a time, each block's own: 154 MB 24 us (38 with every thread's four vectors as far apart as the blocks together are wide)
+  for (int64_t i = ((int64_t)block * 4) * kSortThreads + threadIdx.x; i < p.vectors; i += (int64_t)blocks * 4 * kSortThreads) {
+    float4 v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = kAdd && i + u * kSortThreads < p.vectors ? __ldcs(p.add + i + u * kSortThreads) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u * kSortThreads < p.vectors) p.table[i + u * kSortThreads] = v[u];
+  }
 }
 
 __global__ void __launch_bounds__(kSortThreads, 1) sort_fill_kernel(const SortParams p) {
@@ -125,58 +144,71 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_fill_kernel(const SortPa
   chain_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (blockIdx.x >= kSortCtas) {
-    const int64_t step = (int64_t)(gridDim.x - kSortCtas) * kSortThreads;
-    const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int64_t i = (int64_t)(blockIdx.x - kSortCtas) * kSortThreads + tid; i < p.vectors; i += 4 * step) {
-      float4 v[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = p.add && i + u * step < p.vectors ? p.add[i + u * step] : zero;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (i + u * step < p.vectors) p.table[i + u * step] = v[u];
-    }
+    if (p.add) fill<true>(p, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
+    else fill<false>(p, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
     return;
   }
   const uint32_t rank = blockIdx.x;  // (the first cluster of the grid)
+  const bool alone = p.rows <= kAlone;
+  if (alone && rank) return;
   const uint32_t bins = 1u << p.digit;
-  // each warp of the cluster has a stretch of its own, in whole rounds of 32
-  const int64_t stretch = (p.rows + kSortCtas * kSortWarps * 32 - 1) / (kSortCtas * kSortWarps * 32) * 32;
+  // each warp has a stretch of its own, in whole rounds of 32
+  const int64_t warps = (alone ? 1 : kSortCtas) * kSortWarps, stretch = (p.rows + warps * 32 - 1) / (warps * 32) * 32;
   const int64_t lo = (int64_t)(rank * kSortWarps + warp) * stretch, hi = lo + stretch < p.rows ? lo + stretch : p.rows;
   for (int pass = 0; pass < p.passes; ++pass) {
     const int shift = pass * p.digit;
+    const bool last = pass == p.passes - 1;
     const uint32_t* keys_in = p.keys[(pass + 1) & 1];
     const uint32_t* from_in = p.from[(pass + 1) & 1];
-    uint32_t* keys_out = p.keys[pass & 1];
-    uint32_t* from_out = p.from[pass & 1];
+    uint32_t* keys_out = alone && !last ? s.keys[pass & 1] : p.keys[pass & 1];
+    uint32_t* from_out = alone && !last ? s.from[pass & 1] : p.from[pass & 1];
+    bool beyond = false;
     auto key_at = [&](int64_t i) {
-      if (pass) return __ldcg(keys_in + i);
+      if (pass) return alone ? s.keys[(pass + 1) & 1][i] : __ldcg(keys_in + i);
       const int64_t t = p.tokens[i];
-      if (t >= p.vocab && p.status) *p.status = (int)HBP_ERR_INVALID_ARG;
+      beyond = beyond || t >= p.vocab;
       return t < 0 || t >= p.vocab ? (uint32_t)p.vocab : (uint32_t)t;  // no token: behind all others
     };
+    auto row_at = [&](int64_t i) { return pass ? (alone ? s.from[(pass + 1) & 1][i] : __ldcg(from_in + i)) : (uint32_t)i; };
     for (uint32_t b = lane; b < bins; b += 32) s.counts[warp][b] = 0;
     __syncwarp();
-    for (int64_t i = lo + lane; i < hi; i += 32) atomicAdd(&s.counts[warp][(key_at(i) >> shift) & (bins - 1)], 1u);
-    __syncthreads();
-    uint32_t total = 0;
-    if (tid < (int)bins) {
-#pragma unroll 8
-      for (int w = 0; w < kSortWarps; ++w) {
-        const uint32_t c = s.counts[w][tid];
-        s.counts[w][tid] = total;
-        total += c;
-      }
-      s.totals[tid] = total;
+    constexpr int kAhead = 8;  // rounds asked for at once
+    for (int64_t i0 = lo + lane; i0 < hi; i0 += 32 * kAhead) {
+      uint32_t key[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) key[k] = i0 + 32 * k < hi ? key_at(i0 + 32 * k) : 0u;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + 32 * k < hi) atomicAdd(&s.counts[warp][(key[k] >> shift) & (bins - 1)], 1u);
     }
-    tc::cluster_sync_whole_warps();
+    if (beyond && p.status) *p.status = (int)HBP_ERR_INVALID_ARG;
+    __syncthreads();
+    // a warp takes every 32nd digit: its lanes the warps' counts, in their order
+    for (uint32_t b = warp; b < bins; b += kSortWarps) {
+      const uint32_t c = s.counts[lane][b];
+      uint32_t upto = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
+      }
+      s.counts[lane][b] = upto - c;
+      if (lane == 31) s.totals[b] = upto;
+    }
+    if (alone) __syncthreads();
+    else tc::cluster_sync_whole_warps();
     uint32_t all = 0, before = 0;
     if (tid < (int)bins) {
-      const uint32_t at = tc::smem_u32(&s.totals[tid]);
+      if (alone) {
+        all = s.totals[tid];
+      } else {
+        const uint32_t at = tc::smem_u32(&s.totals[tid]);
 #pragma unroll
-      for (uint32_t r = 0; r < kSortCtas; ++r) {
-        const uint32_t c = ld_cluster(tc::map_to_cta(at, r));
-        all += c;
-        before += r < rank ? c : 0;
+        for (uint32_t r = 0; r < kSortCtas; ++r) {
+          const uint32_t c = ld_cluster(tc::map_to_cta(at, r));
+          all += c;
+          before += r < rank ? c : 0;
+        }
       }
     }
     uint32_t upto = all;  // of the warp's digits, this one's included
@@ -189,24 +221,47 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_fill_kernel(const SortPa
     __syncthreads();
     if (tid < (int)bins) {
       uint32_t first = 0;
-      for (int w = 0; w < warp; ++w) first += s.warp_sums[w];
+#pragma unroll
+      for (int w = 0; w < kMaxBins / 32; ++w) first += w < warp ? s.warp_sums[w] : 0;
       s.base[tid] = first + upto - all + before;
     }
     __syncthreads();
-    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
-      const int64_t i = i0 + lane;
-      const bool in = i < hi;
-      const uint32_t key = in ? key_at(i) : 0u, digit = in ? (key >> shift) & (bins - 1) : bins;
-      const uint32_t row = in ? (pass ? __ldcg(from_in + i) : (uint32_t)i) : 0u;
-      const uint32_t alike = __match_any_sync(0xffffffffu, digit), below = __popc(alike & ((1u << lane) - 1u));
+    auto place = [&](bool in, uint32_t key) {
+      // the lanes that have the same digit, bit by bit (__match_any_sync takes a turn for each value among them: 1 us for 32 of them in all warps)
+      const uint32_t digit = (key >> shift) & (bins - 1);
+      uint32_t alike = __ballot_sync(0xffffffffu, in);
+      for (int b = 0; b < p.digit; ++b) {
+        const uint32_t set = __ballot_sync(0xffffffffu, (digit >> b) & 1u);
+        alike &= (digit >> b) & 1u ? set : ~set;
+      }
+      const uint32_t below = __popc(alike & ((1u << lane) - 1u));
       const uint32_t at = in ? s.base[digit] + s.counts[warp][digit] + below : 0u;
       __syncwarp();
       if (in && below == 0) s.counts[warp][digit] += __popc(alike);
       __syncwarp();
-      if (in) {
-        keys_out[at] = key;
-        from_out[at] = row;
+      return at;
+    };
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAhead) {
+      uint32_t key[kAhead], row[kAhead], at[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int64_t i = i0 + 32 * k + lane;
+        key[k] = i < hi ? key_at(i) : 0u;
+        row[k] = i < hi ? row_at(i) : 0u;
       }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + 32 * k < hi) at[k] = place(i0 + 32 * k + lane < hi, key[k]);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + 32 * k + lane < hi) {
+          keys_out[at[k]] = key[k];
+          from_out[at[k]] = row[k];
+        }
+    }
+    if (alone) {
+      __syncthreads();
+      continue;
     }
     tc::cluster_sync_whole_warps();  // what is written is seen by all; the totals have been read
   }
@@ -216,13 +271,21 @@ __global__ void __launch_bounds__(kSortThreads, 1) sort_fill_kernel(const SortPa
 struct SumParams {
   const uint32_t *keys, *from;  // tokens in order, and the rows that they are of
   int64_t rows, ldd, tiles;
+  int tile;
   const void* d_out;
   int vocab, d;
   float scale;
-  const float* add;
+  bool add;
   float* table;
   float *head, *tail;  // [tiles][d]: of a run that began in an earlier tile; of one that began here and goes on
 };
+
+// Four floats added to what the table has (`add`: it has been copied there, or is the table).  Each element is added to once a call, so the order of
+// these is no matter; nothing waits for what was there: a thread that read it lost a memory's latency at the end of each run, 65536 tokens, of
+// which 36 thousand differ, 88 us.
+__device__ __forceinline__ void add4(float* to, const float4& v) {
+  asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(to), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
 
 constexpr int kSumThreads = 128;
 constexpr uint32_t kNoKey = 0xffffffffu;
@@ -230,15 +293,15 @@ constexpr uint32_t kNoKey = 0xffffffffu;
 template <typename T>
 __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumParams p) {
   constexpr int V = Vec<T>::V, kAhead = 8;
-  __shared__ uint32_t key[kTile + 2], from[kTile];
+  __shared__ uint32_t key[kMostTile + 2], from[kMostTile];
   chain_next();
   chain_wait();
-  const int64_t first = (int64_t)blockIdx.x * kTile;
-  const int n = p.rows - first < kTile ? (int)(p.rows - first) : kTile, tid = threadIdx.x;
-  if (tid < kTile + 2) {  // (one before, one behind)
-    const int64_t i = first + tid - 1;
-    key[tid] = i >= 0 && i < p.rows ? p.keys[i] : kNoKey;
-    if (tid >= 1 && tid <= n) from[tid - 1] = p.from[i];
+  const int64_t first = (int64_t)blockIdx.x * p.tile;
+  const int n = p.rows - first < p.tile ? (int)(p.rows - first) : p.tile, tid = threadIdx.x;
+  for (int k = tid; k < p.tile + 2; k += kSumThreads) {  // (one before, one behind)
+    const int64_t i = first + k - 1;
+    key[k] = i >= 0 && i < p.rows ? p.keys[i] : kNoKey;
+    if (k >= 1 && k <= n) from[k - 1] = p.from[i];
   }
   __syncthreads();
   const int c = (int)(blockIdx.y * kSumThreads + tid) * V;
@@ -275,12 +338,9 @@ __global__ void __launch_bounds__(kSumThreads) sum_kernel(const SumParams p) {
       const bool add = p.add && !began_before && !goes_on;
 #pragma unroll
       for (int e = 0; e < V; e += 4) {
-        float4 o = add ? *reinterpret_cast<const float4*>(p.add + (int64_t)k * p.d + c + e) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        o.x = fmaf(scale, acc[e], o.x);
-        o.y = fmaf(scale, acc[e + 1], o.y);
-        o.z = fmaf(scale, acc[e + 2], o.z);
-        o.w = fmaf(scale, acc[e + 3], o.w);
-        *reinterpret_cast<float4*>(to + e) = o;
+        const float4 o = make_float4(scale * acc[e], scale * acc[e + 1], scale * acc[e + 2], scale * acc[e + 3]);
+        if (add) add4(to + e, o);
+        else *reinterpret_cast<float4*>(to + e) = o;
         acc[e] = acc[e + 1] = acc[e + 2] = acc[e + 3] = 0.0f;
       }
     }
@@ -296,23 +356,31 @@ __global__ void __launch_bounds__(32 * kJoinTiles) join_kernel(const SumParams p
   chain_next();
   chain_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (lane == 0) {
-    const int64_t tile = (int64_t)blockIdx.x * kJoinTiles + warp, at = tile * kTile, next = at + kTile;
+  {
+    const int64_t tile = (int64_t)blockIdx.x * kJoinTiles + warp, at = tile * p.tile, next = at + p.tile;
     int64_t end = -1;
     if (next < p.rows) {
-      const uint32_t k = p.keys[next];
-      if (k < (uint32_t)p.vocab && p.keys[next - 1] == k && !(at > 0 && p.keys[at - 1] == k)) {
-        int64_t lo = next, hi = p.rows;  // keys[lo] is k; hi is behind the run
-        while (hi - lo > 1) {
-          const int64_t mid = lo + (hi - lo) / 2;
-          if (p.keys[mid] == k) lo = mid;
-          else hi = mid;
+      const uint32_t k = p.keys[next], in = p.keys[next - 1], before = at > 0 ? p.keys[at - 1] : kNoKey;
+      if (k < (uint32_t)p.vocab && in == k && before != k) {
+        // the last tile whose first token is k: of 32 at a time, then of those between two of them
+        int64_t lo = tile + 1, hi = p.tiles - 1;  // lo is one, none is behind hi
+        for (int64_t step = 1; lo < hi;) {
+          const int64_t i = lo + step * (lane + 1);
+          const uint32_t same = __ballot_sync(0xffffffffu, i <= hi && p.keys[i * p.tile] == k);
+          const int n = __ffs(~same) - 1;  // (sorted: the first n; -1 for all)
+          lo += step * (n < 0 ? 32 : n);
+          if (n >= 0) {
+            hi = min(hi, lo + step - 1);
+            step = (hi - lo + 31) / 32;
+          } else {
+            step *= 32;
+          }
         }
-        end = lo / kTile;
-        token[warp] = k;
+        end = lo;
+        if (lane == 0) token[warp] = k;
       }
     }
-    last[warp] = end;
+    if (lane == 0) last[warp] = end;
   }
   __syncthreads();
   const int c = (int)(blockIdx.y * 32 + lane) * 4;
@@ -323,7 +391,7 @@ __global__ void __launch_bounds__(32 * kJoinTiles) join_kernel(const SumParams p
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (c < p.d) {
       if (warp == 0) sum = *reinterpret_cast<const float4*>(p.tail + tile * p.d + c);
-#pragma unroll 8
+#pragma unroll 16
       for (int64_t i = lo; i < hi; ++i) {
         const float4 v = *reinterpret_cast<const float4*>(p.head + i * p.d + c);
         sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
@@ -337,13 +405,10 @@ __global__ void __launch_bounds__(32 * kJoinTiles) join_kernel(const SumParams p
         const float4 v = part[g][lane];
         sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
       }
-      const int64_t at = (int64_t)token[w] * p.d + c;
-      float4 o = p.add ? *reinterpret_cast<const float4*>(p.add + at) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      o.x = fmaf(p.scale, sum.x, o.x);
-      o.y = fmaf(p.scale, sum.y, o.y);
-      o.z = fmaf(p.scale, sum.z, o.z);
-      o.w = fmaf(p.scale, sum.w, o.w);
-      *reinterpret_cast<float4*>(p.table + at) = o;
+      float* to = p.table + (int64_t)token[w] * p.d + c;
+      const float4 o = make_float4(p.scale * sum.x, p.scale * sum.y, p.scale * sum.z, p.scale * sum.w);
+      if (p.add) add4(to, o);
+      else *reinterpret_cast<float4*>(to) = o;
     }
     __syncthreads();
   }
@@ -369,9 +434,12 @@ bool bad_rows(const void* t, int64_t ld, int d, int v, bool input) { return ((ui
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 struct Scratch {
   size_t list, sums, bytes;  // of a list of the sorted tokens; of a list of partial sums; of all
+  int tile;
   int64_t tiles;
   Scratch(int64_t rows, int d) {
-    tiles = (rows + kTile - 1) / kTile;
+    for (tile = kLeastTile; tile < kMostTile && rows > 4096 * (int64_t)tile; tile *= 2) {
+    }
+    tiles = (rows + tile - 1) / tile;
     list = up((size_t)rows * 4);
     sums = up((size_t)tiles * d * 4);
     bytes = 4 * list + 2 * sums;
@@ -458,9 +526,9 @@ extern "C" hbp_status hbp_embedding_gradient(int32_t dtype, int64_t rows, int32_
   s.table = (float4*)d_table;
   s.add = (const float4*)add;
   s.vectors = in_place ? 0 : (int64_t)vocab * d / 4;
-  // clusters of eight that fill a GPU with one block an SM, and no more than have a quarter of a block's round each
-  const int64_t wanted = (s.vectors + kSortThreads * kSortCtas - 1) / (kSortThreads * kSortCtas), most = tc::sm_count() / kSortCtas - 1;
-  const int fill = (int)(wanted < most ? wanted : most > 0 ? most : 1);
+  // as many clusters beside the first as run at a time (15 in all: 18 took two turns, 154 MB 40 us), and no more than have 64 KB a block
+  const int64_t wanted = (s.vectors + 4 * kSortThreads * kSortCtas - 1) / (4 * kSortThreads * kSortCtas);
+  const int fill = (int)(wanted < 14 ? wanted : 14);
   Launcher lc;
   lc.stream = (cudaStream_t)cuda_stream;
   launch_chained(lc, sort_fill_kernel, dim3(kSortCtas * (1 + fill)), kSortThreads, sizeof(SortShared), kSortCtas, s);
@@ -468,11 +536,11 @@ extern "C" hbp_status hbp_embedding_gradient(int32_t dtype, int64_t rows, int32_
     SumParams p;
     const int last = (s.passes - 1) & 1;
     p.keys = s.keys[last]; p.from = s.from[last];
-    p.rows = rows; p.ldd = ldd; p.tiles = need.tiles;
+    p.rows = rows; p.ldd = ldd; p.tiles = need.tiles; p.tile = need.tile;
     p.d_out = d_out;
     p.vocab = vocab; p.d = d;
     p.scale = scale;
-    p.add = add;
+    p.add = add != nullptr;
     p.table = d_table;
     p.head = (float*)(at + 4 * need.list);
     p.tail = (float*)(at + 4 * need.list + need.sums);
