@@ -12,6 +12,7 @@
 // fixed order.
 #include <type_traits>
 
+#include "float_pairs.cuh"
 #include "hbp_internal.h"
 #include "tc_common.cuh"
 
@@ -22,11 +23,13 @@ namespace {
 struct Rows {
   const void* x;
   int64_t ld;
+  int64_t step;  // from a group's row to its next, in elements
 };
 
 struct NormParams {
   int64_t rows;
   int d, per_row, threads;  // vectors a row; threads that hold one
+  int stages;  // rows of a group under way
   float eps, scale, inv_d;
   const void *w_post, *gate, *w_pre;
   Rows x, f, x_new, y;                 // forward: x_new and y are written
@@ -36,7 +39,7 @@ struct NormParams {
 };
 
 template <typename T>
-struct Vec {
+struct Channels {
   static constexpr int V = 16 / (int)sizeof(T);
   static __device__ __forceinline__ void widen(const uint4& r, float* f) {
     if constexpr (sizeof(T) == 2) {
@@ -52,11 +55,14 @@ struct Vec {
 };
 
 constexpr int kMaxWarps = 16;  // of a block
+// What the warps of a row exchange: two buffers in turn, so that one barrier a sum is enough.
+struct Exchange {
+  float part[2][kMaxWarps][4];
+};
 
-// Sums of K values over the threads of a row, in every one of them.  Rows of more than a warp use a barrier of their own; two buffers in
-// turn, so that one barrier a sum is enough.
+// Sums of K values over the threads of a row, in every one of them.  Rows of more than a warp use a barrier of their own.
 template <int K>
-__device__ __forceinline__ void row_sum(float (&v)[K], int threads, int group, float (*buf)[kMaxWarps][4], int& turn) {
+__device__ __forceinline__ void row_sum(float (&v)[K], int threads, int group, Exchange& x, int& turn) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
@@ -65,30 +71,111 @@ __device__ __forceinline__ void row_sum(float (&v)[K], int threads, int group, f
   const int warp = threadIdx.x >> 5, warps = threads >> 5;
   if ((threadIdx.x & 31) == 0)
 #pragma unroll
-    for (int k = 0; k < K; ++k) buf[turn][warp][k] = v[k];
+    for (int k = 0; k < K; ++k) x.part[turn][warp][k] = v[k];
   asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
+  // a lane takes a warp's: adding up eight warps' is three times the instructions for every thread
+  const int lane = threadIdx.x & 31;
+  const float4 q = lane < warps ? *reinterpret_cast<const float4*>(x.part[turn][group * warps + lane]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const float part[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = 0.0f;
-  for (int w = 0; w < warps; ++w)
+  for (int k = 0; k < K; ++k) v[k] = part[k];
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += buf[turn][group * warps + w][k];
+  for (int o = kMaxWarps / 2; o > 0; o >>= 1)
+    if (o < warps) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    }
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = __shfl_sync(0xffffffffu, v[k], 0);
   turn ^= 1;
 }
 
+// Vectors of rows on their way: a thread copies its own into its own place of shared memory, so that it waits for nobody to have them and registers
+// hold none of them.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_made() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+// A vector of 16 bytes as pairs of floats
 template <typename T>
-__device__ __forceinline__ uint4 load(const Rows& r, int64_t row, int c) {
-  return *reinterpret_cast<const uint4*>((const T*)r.x + row * r.ld + c);
+__device__ __forceinline__ void pairs_of(const uint4& r, f32x2 (&p)[8 / sizeof(T)]) {
+#pragma unroll
+  for (int e = 0; e < (int)(8 / sizeof(T)); ++e) p[e] = widen2(reinterpret_cast<const T*>(&r) + 2 * e);
 }
 template <typename T>
-__device__ __forceinline__ void store(const Rows& r, int64_t row, int c, const float* f) {
-  *reinterpret_cast<uint4*>((T*)r.x + row * r.ld + c) = Vec<T>::narrow(f);
+__device__ __forceinline__ uint4 vector_of(const f32x2 (&p)[8 / sizeof(T)]) {
+  uint4 r;
+#pragma unroll
+  for (int e = 0; e < (int)(8 / sizeof(T)); ++e) narrow2(p[e], reinterpret_cast<T*>(&r) + 2 * e);
+  return r;
 }
-// weights of one vector of channels, or ones
+__device__ __forceinline__ float total(f32x2 v) {
+  const float2 f = floats_of(v);
+  return f.x + f.y;
+}
+
+__device__ __forceinline__ void copies_wait_but(int left) {
+  if (left >= 3) copies_wait<3>();
+  else if (left == 2) copies_wait<2>();
+  else if (left == 1) copies_wait<1>();
+  else copies_wait<0>();
+}
+
+constexpr int kMostStages = 4;  // rows of a group under way
+
+// a weight's vector of channels, or ones
 template <typename T>
-__device__ __forceinline__ void weights(const void* w, int c, float* f) {
-  constexpr int V = Vec<T>::V;
+__device__ __forceinline__ void weights(const void* w, int c, f32x2 (&p)[8 / sizeof(T)]) {
   if (w) {
-    Vec<T>::widen(*reinterpret_cast<const uint4*>((const T*)w + c), f);
+    pairs_of<T>(*reinterpret_cast<const uint4*>((const T*)w + c), p);
+  } else {
+#pragma unroll
+    for (int e = 0; e < (int)(8 / sizeof(T)); ++e) p[e] = both(1.0f);
+  }
+}
+
+// Less the mean (0 without kLayer) and 1 / sqrt(mean square + eps) of a row's values.
+template <int NV, int H, bool kLayer>
+__device__ __forceinline__ float2 statistics(const f32x2 (&v)[NV][H], const bool (&in)[NV], const NormParams& p, int group, Exchange& buf, int& turn) {
+  float m[1] = {0.0f};
+  if (kLayer) {
+    f32x2 s = both(0.0f);
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+      if (in[u])
+#pragma unroll
+        for (int e = 0; e < H; ++e) s = add2(s, v[u][e]);
+    m[0] = total(s);
+    row_sum(m, p.threads, group, buf, turn);
+    m[0] *= -p.inv_d;
+  }
+  f32x2 s = both(0.0f);
+  const f32x2 less = both(m[0]);
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+    if (in[u])
+#pragma unroll
+      for (int e = 0; e < H; ++e) {
+        const f32x2 c = kLayer ? add2(v[u][e], less) : v[u][e];
+        s = fma2(c, c, s);
+      }
+  float q[1] = {total(s)};
+  row_sum(q, p.threads, group, buf, turn);
+  return make_float2(m[0], 1.0f / sqrtf(fmaf(q[0], p.inv_d, p.eps)));
+}
+
+// ------------------------------------------------------------------------------------------- forward
+// float: a group of threads a row, loaded as it comes, near a copy's rate (16384 x 2048, both norms 92 us of 82 for the bytes; copied ahead by groups that walk over
+// the rows, and in pairs of floats, as bf16 below, 107).
+__device__ __forceinline__ uint4 row_vector(const Rows& r, int64_t row, int c) { return *reinterpret_cast<const uint4*>((const float*)r.x + row * r.ld + c); }
+// weights of one vector of channels, or ones
+__device__ __forceinline__ void row_weights(const void* w, int c, float* f) {
+  constexpr int V = Channels<float>::V;
+  if (w) {
+    Channels<float>::widen(*reinterpret_cast<const uint4*>((const float*)w + c), f);
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e) f[e] = 1.0f;
@@ -97,8 +184,7 @@ __device__ __forceinline__ void weights(const void* w, int c, float* f) {
 
 // Mean (0 without kLayer) and 1 / sqrt(mean square + eps) of a row's values.  Channels beyond d hold zeros.
 template <int NV, int V, bool kLayer>
-__device__ __forceinline__ float2 statistics(const float (&v)[NV][V], const bool (&in)[NV], const NormParams& p, int group, float (*buf)[kMaxWarps][4],
-                                             int& turn) {
+__device__ __forceinline__ float2 row_statistics(const float (&v)[NV][V], const bool (&in)[NV], const NormParams& p, int group, Exchange& buf, int& turn) {
   float m[1] = {0.0f};
   if (kLayer) {
 #pragma unroll
@@ -118,12 +204,11 @@ __device__ __forceinline__ float2 statistics(const float (&v)[NV][V], const bool
   return make_float2(m[0], 1.0f / sqrtf(fmaf(q[0], p.inv_d, p.eps)));
 }
 
-// ------------------------------------------------------------------------------------------- forward
 // kBlock: the block's output and the update, else only the norm of the stream.
-template <typename T, int NV, bool kLayer, bool kBlock, bool kPost>
-__global__ void __launch_bounds__(512) norm_forward_kernel(const NormParams p) {
-  constexpr int V = Vec<T>::V;
-  __shared__ float buf[2][kMaxWarps][4];
+template <int NV, bool kLayer, bool kBlock, bool kPost>
+__global__ void __launch_bounds__(512) norm_row_kernel(const NormParams p) {
+  constexpr int V = Channels<float>::V;
+  __shared__ __align__(16) Exchange buf;
   chain_next();
   chain_wait();
   int turn = 0;
@@ -139,187 +224,410 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormParams p) {
     in[u] = c < p.d;
     x[u] = f[u] = make_uint4(0, 0, 0, 0);
     if (in[u]) {
-      x[u] = load<T>(p.x, row, c);
-      if (kBlock) f[u] = load<T>(p.f, row, c);
+      x[u] = row_vector(p.x, row, c);
+      if (kBlock) f[u] = row_vector(p.f, row, c);
     }
   }
   if (kBlock) {
     float2 s = make_float2(0.0f, 1.0f);
 #pragma unroll
-    for (int u = 0; u < NV; ++u) Vec<T>::widen(f[u], v[u]);
-    if (kPost) s = statistics<NV, V, kLayer>(v, in, p, group, buf, turn);
+    for (int u = 0; u < NV; ++u) Channels<float>::widen(f[u], v[u]);
+    if (kPost) s = row_statistics<NV, V, kLayer>(v, in, p, group, buf, turn);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int c = (t + u * p.threads) * V;
       if (!in[u]) continue;
       float w[V], g[V], xf[V];
-      weights<T>(kPost ? p.w_post : nullptr, c, w);
-      weights<T>(p.gate, c, g);
-      Vec<T>::widen(x[u], xf);
+      row_weights(kPost ? p.w_post : nullptr, c, w);
+      row_weights(p.gate, c, g);
+      Channels<float>::widen(x[u], xf);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float h = kPost ? (v[u][e] - s.x) * s.y * w[e] : v[u][e];
         v[u][e] = fmaf(p.scale, h, g[e] * xf[e]);
       }
-      x[u] = Vec<T>::narrow(v[u]);
-      *reinterpret_cast<uint4*>((T*)p.x_new.x + row * p.x_new.ld + c) = x[u];
+      x[u] = Channels<float>::narrow(v[u]);
+      *reinterpret_cast<uint4*>((float*)p.x_new.x + row * p.x_new.ld + c) = x[u];
     }
     if (!p.y.x) return;
   }
 #pragma unroll
-  for (int u = 0; u < NV; ++u) Vec<T>::widen(x[u], v[u]);  // the stream as it is stored
-  const float2 s = statistics<NV, V, kLayer>(v, in, p, group, buf, turn);
+  for (int u = 0; u < NV; ++u) Channels<float>::widen(x[u], v[u]);  // the stream as it is stored
+  const float2 s = row_statistics<NV, V, kLayer>(v, in, p, group, buf, turn);
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
     const int c = (t + u * p.threads) * V;
     if (!in[u]) continue;
     float w[V];
-    weights<T>(p.w_pre, c, w);
+    row_weights(p.w_pre, c, w);
 #pragma unroll
     for (int e = 0; e < V; ++e) v[u][e] = (v[u][e] - s.x) * s.y * w[e];
-    store<T>(p.y, row, c, v[u]);
+    *reinterpret_cast<uint4*>((float*)p.y.x + row * p.y.ld + c) = Channels<float>::narrow(v[u]);
   }
 }
 
-// ------------------------------------------------------------------------------------------- backward
-template <typename T, int NV, bool kLayer, bool kPost>
-__global__ void __launch_bounds__(512) norm_backward_kernel(const NormParams p) {
-  constexpr int V = Vec<T>::V;
-  __shared__ float buf[2][kMaxWarps][4];
-  extern __shared__ float sums[];  // [3][d]: of a block's groups
+// bf16: groups of 32 to 512 threads walk over the rows, a grid apart.  (A block for every eight rows of 768 channels, which read them when it
+// came, had both norms' 16384 rows in 31 us, so 25; for every four, in 39: blocks cost that much to come and go.)
+template <int NV, bool kLayer, bool kBlock, bool kPost>
+__global__ void __launch_bounds__(512) norm_forward_kernel(const NormParams p) {
+  typedef bf16 T;
+  constexpr int V = Channels<T>::V, H = V / 2;
+  __shared__ __align__(16) Exchange buf;
+  extern __shared__ float4 dynamic[];  // [stages][x, f][NV][threads of the block]
   chain_next();
   chain_wait();
   int turn = 0;
   const int groups = blockDim.x / p.threads, group = threadIdx.x / p.threads, t = threadIdx.x - group * p.threads;
-  float dw_pre[NV][V], dw_post[NV][V], da[NV][V];
+  const uint32_t slab = NV * blockDim.x * 16, row_bytes = (kBlock ? 2 : 1) * slab, mine = tc::smem_u32(dynamic) + threadIdx.x * 16;
+  const uint32_t end = mine + p.stages * row_bytes;
+  bool in[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) in[u] = (t + u * p.threads) * V < p.d;
+  const int64_t step = (int64_t)gridDim.x * groups, first = (int64_t)blockIdx.x * groups + group;
+  auto at = [&](const Rows& r) { return (const T*)r.x + first * r.ld + t * V; };
+  const T *a_x = at(p.x), *a_f = at(p.f);
+  T *o_new = (T*)at(p.x_new), *o_y = (T*)at(p.y);
+  int64_t asked = first;
+  uint32_t to = mine, from = mine;
+  auto ask = [&]() {
+    if (asked < p.rows) {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        if (!in[u]) continue;
+        const uint32_t place = to + u * blockDim.x * 16;
+        copy16(place, a_x + u * p.threads * V);
+        if (kBlock) copy16(place + slab, a_f + u * p.threads * V);
+      }
+      a_x += p.x.step;
+      a_f += p.f.step;
+      asked += step;
+    }
+    to = to + row_bytes == end ? mine : to + row_bytes;
+    copies_made();
+  };
+  for (int s = 0; s < p.stages - 1; ++s) ask();
+  for (int64_t row = first; row < p.rows; row += step) {
+    ask();  // into the place of the row before, which this thread is done with
+    copies_wait_but(p.stages - 1);
+    const uint32_t here = from;
+    from = from + row_bytes == end ? mine : from + row_bytes;
+    f32x2 v[NV][H];
+    if (kBlock) {
+      float2 s = make_float2(0.0f, 1.0f);
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+        if (in[u]) pairs_of<T>(tc::ld_shared16(here + slab + u * blockDim.x * 16), v[u]);
+      if (kPost) s = statistics<NV, H, kLayer>(v, in, p, group, buf, turn);
+      const f32x2 less = both(s.x), r = both(s.y), scale = both(p.scale);
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        if (!in[u]) continue;
+        const int c = (t + u * p.threads) * V;
+        f32x2 x[H], w[H];
+        if (kPost) {
+          weights<T>(p.w_post, c, w);
+#pragma unroll
+          for (int e = 0; e < H; ++e) v[u][e] = mul2(mul2(kLayer ? add2(v[u][e], less) : v[u][e], r), w[e]);
+        }
+        pairs_of<T>(tc::ld_shared16(here + u * blockDim.x * 16), x);
+        if (p.gate) {
+          weights<T>(p.gate, c, w);
+#pragma unroll
+          for (int e = 0; e < H; ++e) x[e] = mul2(x[e], w[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < H; ++e) v[u][e] = fma2(v[u][e], scale, x[e]);
+        const uint4 stored = vector_of<T>(v[u]);
+        *reinterpret_cast<uint4*>(o_new + u * p.threads * V) = stored;
+        pairs_of<T>(stored, v[u]);  // the stream as it is stored
+      }
+      o_new += p.x_new.step;
+      if (!p.y.x) continue;
+    } else {
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+        if (in[u]) pairs_of<T>(tc::ld_shared16(here + u * blockDim.x * 16), v[u]);
+    }
+    const float2 s = statistics<NV, H, kLayer>(v, in, p, group, buf, turn);
+    const f32x2 less = both(s.x), r = both(s.y);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      if (!in[u]) continue;
+      f32x2 w[H];
+      weights<T>(p.w_pre, (t + u * p.threads) * V, w);
+#pragma unroll
+      for (int e = 0; e < H; ++e) v[u][e] = mul2(mul2(kLayer ? add2(v[u][e], less) : v[u][e], r), w[e]);
+      *reinterpret_cast<uint4*>(o_y + u * p.threads * V) = vector_of<T>(v[u]);
+    }
+    o_y += p.y.step;
+  }
+}
+
+// ------------------------------------------------------------------------------------------- backward
+// Whether threads of few registers keep the weights in shared memory (five floats of 8192 channels leave no room there)
+template <typename T>
+constexpr bool kShares = sizeof(T) == 2;
+
+// A vector that is used more than once: as floats, or as it came where registers are short (two vectors a thread and more).
+template <typename T, bool kFloats>
+struct Kept {
+  static constexpr int H = 8 / sizeof(T);
+  f32x2 v[kFloats ? H : 1];
+  uint4 r;
+  __device__ __forceinline__ void set(const uint4& raw) {
+    if constexpr (kFloats) pairs_of<T>(raw, v);
+    else r = raw;
+  }
+  __device__ __forceinline__ void get(f32x2 (&p)[H]) const {
+    if constexpr (kFloats) {
+#pragma unroll
+      for (int e = 0; e < H; ++e) p[e] = v[e];
+    } else {
+      pairs_of<T>(r, p);
+    }
+  }
+};
+
+// Rows are on their way up to three before they are used, as in the forward pass (16384 x 2048 bf16, both norms and a gate: loaded when they are used 171 us, ahead 118,
+// where the bytes take 72).  Then it is the instructions, 76 a channel, and the way of a row through its sums, two or three that wait for all of its warps: 16
+// channels a thread instead of 8 halve what a row costs beside its channels, pointers walk along with the rows, lanes share the warps' sums; and four rows are
+// under way an SM where weights of bf16 rows are read from shared memory again instead of holding registers (208 of these: 122 us): 103 us.  float: values that are
+// used again stay in registers, 6.2 TB/s.  Groups walk over the rows, a grid apart.
+// kFew: 128 registers a thread, for rows of more than 256 threads, or twice the rows under way.  kAll: both gradients arrive and both are wanted.
+template <typename T, int NV, bool kLayer, bool kPost, bool kFew, bool kAll>
+__global__ void __launch_bounds__(kFew ? 512 : 256) norm_backward_kernel(const NormParams p) {
+  constexpr int V = Channels<T>::V, H = V / 2;
+  constexpr bool kFloats = !kFew, kShared = kShares<T> && kFew;
+  typedef Kept<T, kFloats> Vector;
+  __shared__ __align__(16) Exchange buf;
+  extern __shared__ float4 dynamic[];  // [stages][tensors][NV][threads of the block]; at the end [3][d], the sums of the block's groups
+  chain_next();
+  chain_wait();
+  int turn = 0;
+  const int groups = blockDim.x / p.threads, group = threadIdx.x / p.threads, t = threadIdx.x - group * p.threads;
+  const bool has_y = kAll || p.d_y.x, has_new = kAll || p.d_new.x;
+  // the tensors' places in a stage
+  const int at_new = has_y ? 2 : 0, at_f = at_new + has_new, at_x = at_f + kPost, tensors = at_x + p.want_gate;
+  const uint32_t slab = NV * blockDim.x * 16, row_bytes = tensors * slab, mine = tc::smem_u32(dynamic) + threadIdx.x * 16;
+  f32x2 dw_pre[NV][H], dw_post[NV][H], da[NV][H];
+  Vector w_pre[NV], w_post[NV], gate[NV];  // (kShared: in shared memory)
+  const uint32_t weights_at = mine + p.stages * row_bytes;
   bool in[NV];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
-    in[u] = (t + u * p.threads) * V < p.d;
+    const int c = (t + u * p.threads) * V;
+    in[u] = c < p.d;
 #pragma unroll
-    for (int e = 0; e < V; ++e) dw_pre[u][e] = dw_post[u][e] = da[u][e] = 0.0f;
+    for (int e = 0; e < H; ++e) dw_pre[u][e] = dw_post[u][e] = da[u][e] = both(0.0f);
+    float ones[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) ones[e] = 1.0f;
+    auto keep = [&](Vector& v, const void* w, int which) {
+      const uint4 raw = in[u] && w ? *reinterpret_cast<const uint4*>((const T*)w + c) : Channels<T>::narrow(ones);
+      if constexpr (!kShared) v.set(raw);
+      else tc::st_shared16(weights_at + (which * NV + u) * blockDim.x * 16, raw);
+    };
+    keep(w_pre[u], p.w_pre, 0);
+    if (kPost) keep(w_post[u], p.w_post, 1);
+    keep(gate[u], p.gate, 2);
   }
-  for (int64_t row = (int64_t)blockIdx.x * groups + group; row < p.rows; row += (int64_t)gridDim.x * groups) {
-    uint4 dy[NV], dn[NV], xn[NV], f[NV], x[NV];
+  auto weight = [&](const Vector& v, int which, int u, f32x2 (&w)[H]) {
+    if constexpr (!kShared) v.get(w);
+    else pairs_of<T>(tc::ld_shared16(weights_at + (which * NV + u) * blockDim.x * 16), w);
+  };
+  const int64_t step = (int64_t)gridDim.x * groups, first = (int64_t)blockIdx.x * groups + group;
+  // where this thread's first vector is: of the row to ask for next, and of the outputs' row
+  auto at = [&](const Rows& r) { return (const T*)r.x + first * r.ld + t * V; };
+  const T *a_dy = at(p.d_y), *a_xn = at(p.x_new), *a_dn = at(p.d_new), *a_f = at(p.f), *a_x = at(p.x);
+  T *o_dx = (T*)at(p.dx), *o_df = (T*)at(p.df);
+  int64_t asked = first;
+  uint32_t to = mine;
+  const uint32_t end = mine + p.stages * row_bytes;
+  auto ask = [&]() {
+    if (asked < p.rows) {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        if (!in[u]) continue;
+        const int c = u * p.threads * V;
+        uint32_t place = to + u * blockDim.x * 16;
+        auto one = [&](const T* from) {
+          copy16(place, from + c);
+          place += slab;
+        };
+        if (has_y) {
+          one(a_dy);
+          one(a_xn);
+        }
+        if (has_new) one(a_dn);
+        if (kPost) one(a_f);
+        if (p.want_gate) one(a_x);
+      }
+      a_dy += p.d_y.step;
+      a_xn += p.x_new.step;
+      a_dn += p.d_new.step;
+      a_f += p.f.step;
+      a_x += p.x.step;
+      asked += step;
+    }
+    to = to + row_bytes == end ? mine : to + row_bytes;
+    copies_made();
+  };
+  for (int s = 0; s < p.stages - 1; ++s) ask();
+  uint32_t from = mine;
+  for (int64_t row = first; row < p.rows; row += step) {
+    ask();  // into the place of the row before, which this thread is done with
+    copies_wait_but(p.stages - 1);
+    const uint32_t here = from;
+    from = from + row_bytes == end ? mine : from + row_bytes;
+    auto held = [&](int i, int u) { return tc::ld_shared16(here + i * slab + u * blockDim.x * 16); };
+    Vector xn[NV], f[NV], a[NV];  // a = dy * w_pre
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int c = (t + u * p.threads) * V;
-      dy[u] = dn[u] = xn[u] = f[u] = x[u] = make_uint4(0, 0, 0, 0);
       if (!in[u]) continue;
-      if (p.d_y.x) {
-        dy[u] = load<T>(p.d_y, row, c);
-        xn[u] = load<T>(p.x_new, row, c);
-      }
-      if (p.d_new.x) dn[u] = load<T>(p.d_new, row, c);
-      if (kPost) f[u] = load<T>(p.f, row, c);
-      if (p.want_gate) x[u] = load<T>(p.x, row, c);
+      if (has_y) xn[u].set(held(1, u));
+      if (kPost) f[u].set(held(at_f, u));
     }
     // means of the stream and the block's output
     float mean[2] = {0.0f, 0.0f};
     if (kLayer) {
+      f32x2 m0 = both(0.0f), m1 = both(0.0f), v[H];
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        float a[V], b[V];
-        Vec<T>::widen(xn[u], a);
-        Vec<T>::widen(f[u], b);
+        if (!in[u]) continue;
+        if (has_y) {
+          xn[u].get(v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          mean[0] += a[e];
-          if (kPost) mean[1] += b[e];
+          for (int e = 0; e < H; ++e) m0 = add2(m0, v[e]);
+        }
+        if (kPost) {
+          f[u].get(v);
+#pragma unroll
+          for (int e = 0; e < H; ++e) m1 = add2(m1, v[e]);
         }
       }
+      mean[0] = total(m0);
+      mean[1] = total(m1);
       row_sum(mean, p.threads, group, buf, turn);
       mean[0] *= p.inv_d;
       mean[1] *= p.inv_d;
     }
-    // sums of squares around them, and of a = dy * w_pre and a times the centred stream
-    float q[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const f32x2 less = both(-mean[0]), less_f = both(-mean[1]);
+    // sums of squares around them, of a times the centred stream, and of a
+    constexpr int Q = kLayer ? 4 : kPost ? 3 : 2;
+    float q[4];
+    {
+      f32x2 s[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      if (!in[u]) continue;
-      float a[V], v[V], w[V];
-      Vec<T>::widen(dy[u], a);
-      Vec<T>::widen(xn[u], v);
-      weights<T>(p.w_pre, (t + u * p.threads) * V, w);
+      for (int u = 0; u < NV; ++u) {
+        f32x2 v[H], w[H], g[H];
+        if (!in[u]) continue;
+        if (has_y) {
+          pairs_of<T>(held(0, u), g);
+          xn[u].get(v);
+          weight(w_pre[u], 0, u, w);
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float cx = v[e] - mean[0], g = a[e] * w[e];
-        q[0] = fmaf(cx, cx, q[0]);
-        q[1] = fmaf(g, cx, q[1]);
-        q[2] += g;
+          for (int e = 0; e < H; ++e) {
+            const f32x2 cx = kLayer ? add2(v[e], less) : v[e], aw = mul2(g[e], w[e]);
+            if constexpr (kFloats) a[u].v[e] = aw;
+            s[0] = fma2(cx, cx, s[0]);
+            s[1] = fma2(aw, cx, s[1]);
+            if (kLayer) s[3] = add2(s[3], aw);
+          }
+        }
+        if (kPost) {
+          f[u].get(v);
+#pragma unroll
+          for (int e = 0; e < H; ++e) {
+            const f32x2 cf = kLayer ? add2(v[e], less_f) : v[e];
+            s[2] = fma2(cf, cf, s[2]);
+          }
+        }
       }
-      if (kPost) {
-        Vec<T>::widen(f[u], v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) q[3] = fmaf(v[e] - mean[1], v[e] - mean[1], q[3]);
-      }
+      for (int k = 0; k < 4; ++k) q[k] = total(s[k]);
     }
-    row_sum(q, p.threads, group, buf, turn);
-    const float r = 1.0f / sqrtf(fmaf(q[0], p.inv_d, p.eps)), along = q[1] * r * p.inv_d, flat = kLayer ? q[2] * p.inv_d : 0.0f;
-    const float rf = kPost ? 1.0f / sqrtf(fmaf(q[3], p.inv_d, p.eps)) : 1.0f;
+    row_sum(*reinterpret_cast<float(*)[Q]>(q), p.threads, group, buf, turn);
+    const float r = 1.0f / sqrtf(fmaf(q[0], p.inv_d, p.eps)), along = q[1] * r * p.inv_d, flat = kLayer ? q[3] * p.inv_d : 0.0f;
+    const float rf = kPost ? 1.0f / sqrtf(fmaf(q[2], p.inv_d, p.eps)) : 1.0f;
+    const f32x2 r2 = both(r), rf2 = both(rf), along2 = both(-along), flat2 = both(-flat), scale = both(p.scale);
     // the gradient of the new stream; what it gives
-    float g[NV][V], b[2] = {0.0f, 0.0f};
+    f32x2 g[NV][H], b0 = both(0.0f), b1 = both(0.0f);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int c = (t + u * p.threads) * V;
       if (!in[u]) continue;
-      float a[V], v[V], w[V], fv[V], wp[V];
-      Vec<T>::widen(dn[u], g[u]);
-      if (p.d_y.x) {
-        Vec<T>::widen(dy[u], a);
-        Vec<T>::widen(xn[u], v);
-        weights<T>(p.w_pre, c, w);
+      f32x2 v[H], w[H], y[H];
+      if (has_new) {
+        pairs_of<T>(held(at_new, u), g[u]);
+      } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float xhat = (v[e] - mean[0]) * r;
-          dw_pre[u][e] = fmaf(a[e], xhat, dw_pre[u][e]);
-          g[u][e] = fmaf(fmaf(-xhat, along, fmaf(a[e], w[e], -flat)), r, g[u][e]);
+        for (int e = 0; e < H; ++e) g[u][e] = both(0.0f);
+      }
+      if (has_y) {
+        pairs_of<T>(held(0, u), y);
+        xn[u].get(v);
+        if constexpr (!kFloats) weight(w_pre[u], 0, u, w);
+#pragma unroll
+        for (int e = 0; e < H; ++e) {
+          const f32x2 xhat = mul2(kLayer ? add2(v[e], less) : v[e], r2);
+          dw_pre[u][e] = fma2(y[e], xhat, dw_pre[u][e]);
+          f32x2 aw;
+          if constexpr (kFloats) aw = a[u].v[e];
+          else aw = mul2(y[e], w[e]);
+          if (kLayer) aw = add2(aw, flat2);
+          g[u][e] = fma2(fma2(xhat, along2, aw), r2, g[u][e]);
         }
       }
       if (p.want_gate) {
-        Vec<T>::widen(x[u], v);
+        pairs_of<T>(held(at_x, u), v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) da[u][e] = fmaf(g[u][e], v[e], da[u][e]);
+        for (int e = 0; e < H; ++e) da[u][e] = fma2(g[u][e], v[e], da[u][e]);
       }
+      if (kAll || p.dx.x) {
+        weight(gate[u], 2, u, w);
+#pragma unroll
+        for (int e = 0; e < H; ++e) v[e] = mul2(g[u][e], w[e]);
+        *reinterpret_cast<uint4*>(o_dx + u * p.threads * V) = vector_of<T>(v);
+      }
+#pragma unroll
+      for (int e = 0; e < H; ++e) g[u][e] = mul2(g[u][e], scale);  // of h
       if (kPost) {
-        Vec<T>::widen(f[u], fv);
-        weights<T>(p.w_post, c, wp);
-      }
-      if (p.dx.x) {
-        weights<T>(p.gate, c, w);
+        f[u].get(v);
+        weight(w_post[u], 1, u, w);
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = g[u][e] * w[e];
-        store<T>(p.dx, row, c, v);
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) g[u][e] *= p.scale;  // of h
-      if (kPost) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float fhat = (fv[e] - mean[1]) * rf;
-          dw_post[u][e] = fmaf(g[u][e], fhat, dw_post[u][e]);
-          g[u][e] *= wp[e];
-          b[0] = fmaf(g[u][e], fhat, b[0]);
-          b[1] += g[u][e];
+        for (int e = 0; e < H; ++e) {
+          const f32x2 fhat = mul2(kLayer ? add2(v[e], less_f) : v[e], rf2);
+          dw_post[u][e] = fma2(g[u][e], fhat, dw_post[u][e]);
+          g[u][e] = mul2(g[u][e], w[e]);
+          b0 = fma2(g[u][e], fhat, b0);
+          if (kLayer) b1 = add2(b1, g[u][e]);
         }
       }
     }
-    if (!p.df.x) continue;
-    if (kPost) row_sum(b, p.threads, group, buf, turn);
-    const float along_f = b[0] * p.inv_d, flat_f = kLayer ? b[1] * p.inv_d : 0.0f;
+    o_dx += p.dx.step;
+    if (!kAll && !p.df.x) continue;
+    float b[2] = {total(b0), total(b1)};
+    if (kPost) row_sum(*reinterpret_cast<float(*)[kLayer ? 2 : 1]>(b), p.threads, group, buf, turn);
+    const f32x2 along_f = both(-b[0] * p.inv_d), flat_f = both(kLayer ? -b[1] * p.inv_d : 0.0f);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       if (!in[u]) continue;
       if (kPost) {
-        float fv[V];
-        Vec<T>::widen(f[u], fv);
+        f32x2 v[H];
+        f[u].get(v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) g[u][e] = (g[u][e] - flat_f - (fv[e] - mean[1]) * rf * along_f) * rf;
+        for (int e = 0; e < H; ++e) {
+          const f32x2 fhat = mul2(kLayer ? add2(v[e], less_f) : v[e], rf2);
+          g[u][e] = mul2(fma2(fhat, along_f, kLayer ? add2(g[u][e], flat_f) : g[u][e]), rf2);
+        }
       }
-      store<T>(p.df, row, (t + u * p.threads) * V, g[u]);
+      *reinterpret_cast<uint4*>(o_df + u * p.threads * V) = vector_of<T>(g[u]);
     }
+    o_df += p.df.step;
   }
   if (!p.partial) return;
+  copies_wait<0>();
+  __syncthreads();  // the stages are done with
+  float* sums = reinterpret_cast<float*>(dynamic);
   for (int k = 0; k < groups; ++k) {  // the groups' sums, one after the other
     if (k == group) {
 #pragma unroll
@@ -327,19 +635,23 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormParams p) 
         const int c = (t + u * p.threads) * V;
         if (!in[u]) continue;
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          sums[c + e] = k ? sums[c + e] + dw_pre[u][e] : dw_pre[u][e];
-          sums[p.d + c + e] = k ? sums[p.d + c + e] + dw_post[u][e] : dw_post[u][e];
-          sums[2 * p.d + c + e] = k ? sums[2 * p.d + c + e] + da[u][e] : da[u][e];
+        for (int e = 0; e < H; ++e) {
+          auto put = [&](int which, f32x2 v) {
+            f32x2* to = reinterpret_cast<f32x2*>(sums + which * p.d + c + 2 * e);
+            *to = k ? add2(*to, v) : v;
+          };
+          put(0, dw_pre[u][e]);
+          put(1, dw_post[u][e]);
+          put(2, da[u][e]);
         }
       }
     }
     __syncthreads();
   }
-  float* to = p.partial + (int64_t)blockIdx.x * 3 * p.d;
+  float* out = p.partial + (int64_t)blockIdx.x * 3 * p.d;
   for (int i = threadIdx.x * 4; i < 3 * p.d; i += blockDim.x * 4) {
     const int k = i / p.d;
-    if (k == 0 ? p.want_pre : k == 1 ? p.want_post : p.want_gate) *reinterpret_cast<float4*>(to + i) = *reinterpret_cast<const float4*>(sums + i);
+    if (k == 0 ? p.want_pre : k == 1 ? p.want_post : p.want_gate) *reinterpret_cast<float4*>(out + i) = *reinterpret_cast<const float4*>(sums + i);
   }
 }
 
@@ -378,41 +690,61 @@ __global__ void __launch_bounds__(256) weight_sums_kernel(const WeightSums p) {
 
 // ------------------------------------------------------------------------------------------- host
 constexpr int kMaxWidth = 8192;
+constexpr int kMostShared = 224 << 10;
 
-// Vectors a thread holds, and threads a row (whole warps).  Rows of up to 128 vectors (forward; 32 backward, whose threads hold the weights' sums
-// too) are a warp's: no barriers.
-void split_of(int per_row, bool backward, int* nv, int* threads) {
-  if (per_row <= 32) *nv = 1;
-  else if (!backward && per_row <= 64) *nv = 2;
-  else if (!backward && per_row <= 128) *nv = 4;
-  else if (backward && per_row <= 256) *nv = 1;
-  else *nv = per_row <= 1024 ? 2 : 4;
+// Vectors a thread holds, and threads a row (whole warps).  Forward: rows of up to 128 vectors are a warp's: no barriers.  Backward: 8 to 16
+// channels, as threads hold three sums a channel too.
+void split_of(int per_row, bool backward, bool f32, int* nv, int* threads) {
+  if (backward) *nv = per_row <= 32 ? 1 : f32 ? (per_row <= 512 ? 2 : 4) : 2;
+  else *nv = per_row <= 32 ? 1 : per_row <= 64 ? 2 : per_row <= 128 ? 4 : per_row <= 1024 ? 2 : 4;
   *threads = ((per_row + *nv - 1) / *nv + 31) / 32 * 32;
 }
 
-// Blocks of `threads` threads and `smem` bytes that an SM runs at once, by the kernel's registers (looked up once, as its leave for the
-// widest rows' shared memory is asked for); 0: an error.
-int blocks_at_once(const void* kernel, int& registers, int threads, size_t smem) {
+// Blocks of `threads` threads that an SM runs at once, by the kernel's registers (looked up once, as its leave for the widest rows' shared
+// memory is asked for); 0: an error.
+int blocks_at_once(const void* kernel, int& registers, int threads) {
   if (registers == 0) {
     cudaFuncAttributes a;
     if (cudaFuncGetAttributes(&a, kernel) != cudaSuccess ||
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 3 * kMaxWidth * 4) != cudaSuccess) {
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) != cudaSuccess) {
       cudaGetLastError();
       return 0;
     }
     registers = (a.numRegs + 7) / 8 * 8;
   }
-  const int by_regs = 65536 / registers / threads, by_threads = 2048 / threads, by_smem = (int)((227 << 10) / (smem + 2048));
-  const int n = by_regs < by_threads ? by_regs : by_threads, m = n < by_smem ? n : by_smem;
-  return m > 0 ? m : 1;
+  const int by_regs = 65536 / registers / threads, by_threads = 2048 / threads, n = by_regs < by_threads ? by_regs : by_threads;
+  return n > 0 ? n : 1;
 }
 
+// Dynamic shared memory of each of so many blocks on an SM
+size_t room(int blocks) { return (size_t)(226 << 10) / blocks - 2048; }
+
 template <typename T, int NV, bool kLayer>
-void forward(Launcher& lc, const NormParams& p, bool post) {
-  const int groups = p.threads >= 256 ? 1 : 256 / p.threads;
-  auto kernel = !p.f.x ? norm_forward_kernel<T, NV, kLayer, false, false>
-                       : post ? norm_forward_kernel<T, NV, kLayer, true, true> : norm_forward_kernel<T, NV, kLayer, true, false>;
-  launch_chained(lc, kernel, dim3((unsigned)((p.rows + groups - 1) / groups)), groups * p.threads, 0, 1, p);
+void forward(Launcher& lc, NormParams& p, bool post) {
+  const int groups = p.threads >= 256 ? 1 : 256 / p.threads, kind = !p.f.x ? 0 : post ? 2 : 1;
+  const int64_t wanted = (p.rows + groups - 1) / groups;
+  if constexpr (sizeof(T) == 4) {
+    auto kernel = kind == 0 ? norm_row_kernel<NV, kLayer, false, false> : kind == 2 ? norm_row_kernel<NV, kLayer, true, true> : norm_row_kernel<NV, kLayer, true, false>;
+    launch_chained(lc, kernel, dim3((unsigned)wanted), groups * p.threads, 0, 1, p);
+  } else {
+    auto kernel = kind == 0 ? norm_forward_kernel<NV, kLayer, false, false>
+                            : kind == 2 ? norm_forward_kernel<NV, kLayer, true, true> : norm_forward_kernel<NV, kLayer, true, false>;
+    static PerDevice<int> registers[3];
+    int per_sm = blocks_at_once((const void*)kernel, registers[kind].here(), groups * p.threads);
+    if (per_sm == 0) {
+      lc.err = cudaErrorInvalidValue;
+      return;
+    }
+    if (per_sm > 4) per_sm = 4;  // (65536 x 256: 22 us, five 25)
+    // two rows under way a group, if need be with fewer blocks
+    const size_t stage = (size_t)(p.f.x ? 2 : 1) * NV * groups * p.threads * 16;
+    while (per_sm > 1 && room(per_sm) < 2 * stage) --per_sm;
+    const size_t fits = room(per_sm) / stage;  // (32 KB are the most that a row takes)
+    p.stages = (int)(fits < kMostStages ? fits : kMostStages);
+    const int64_t most = (int64_t)per_sm * tc::sm_count(), blocks = wanted < most ? wanted : most;
+    for (Rows* r : {&p.x, &p.f, &p.x_new, &p.y}) r->step = r->ld * blocks * groups;
+    launch_chained(lc, kernel, dim3((unsigned)blocks), groups * p.threads, p.stages * stage, 1, p);
+  }
 }
 
 constexpr int kMostBlocks = 4;     // an SM, backward: each leaves 12 d bytes for the second launch
@@ -421,17 +753,37 @@ constexpr int kMostPartials = 640;  // and all of them together
 template <typename T, int NV, bool kLayer>
 int backward(Launcher& lc, NormParams& p, bool post) {
   const int groups = p.threads >= 256 ? 1 : 256 / p.threads;
-  auto kernel = post ? norm_backward_kernel<T, NV, kLayer, true> : norm_backward_kernel<T, NV, kLayer, false>;
-  const size_t smem = p.partial ? (size_t)3 * p.d * 4 : 0;
-  static PerDevice<int> registers[2];
-  int per_sm = blocks_at_once((const void*)kernel, registers[post].here(), groups * p.threads, smem);
+  const bool few = sizeof(T) == 2 ? NV == 2 : p.threads > 256, all = p.d_y.x && p.d_new.x && p.dx.x && p.df.x;
+  auto pick = [&](auto of_few) {
+    constexpr bool kFew = decltype(of_few)::value;
+    return post ? (all ? norm_backward_kernel<T, NV, kLayer, true, kFew, true> : norm_backward_kernel<T, NV, kLayer, true, kFew, false>)
+                : (all ? norm_backward_kernel<T, NV, kLayer, false, kFew, true> : norm_backward_kernel<T, NV, kLayer, false, kFew, false>);
+  };
+  void (*kernel)(NormParams);
+  if constexpr (sizeof(T) == 4 && NV == 4) kernel = few ? pick(std::true_type()) : pick(std::false_type());
+  else kernel = pick(std::integral_constant<bool, sizeof(T) == 2 && NV == 2>());
+  static PerDevice<int> registers[8];
+  int per_sm = blocks_at_once((const void*)kernel, registers[4 * all + 2 * few + post].here(), groups * p.threads);
   if (per_sm == 0) {
     lc.err = cudaErrorInvalidValue;
     return 0;
   }
   if (per_sm > kMostBlocks) per_sm = kMostBlocks;
+  // as many rows under way as the blocks of an SM have shared memory for; fewer blocks where not even one fits
+  const int tensors = (p.d_y.x ? 2 : 0) + (p.d_new.x != nullptr) + post + p.want_gate;
+  const size_t stage = (size_t)tensors * NV * groups * p.threads * 16, sums = p.partial ? (size_t)3 * p.d * 4 : 0;
+  const size_t weights = few && kShares<T> ? (size_t)3 * NV * groups * p.threads * 16 : 0;
+  while (per_sm > 1 && (room(per_sm) < stage + weights || room(per_sm) < sums)) --per_sm;
+  const size_t fits = (room(per_sm) - weights) / stage;
+  p.stages = (int)(fits < kMostStages ? fits : kMostStages);
+  if (p.stages < 1) {  // (5 * 32 KB are the most that a row takes)
+    lc.err = cudaErrorInvalidValue;
+    return 0;
+  }
+  const size_t rows = p.stages * stage + weights, smem = rows > sums ? rows : sums;
   const int64_t wanted = (p.rows + groups - 1) / groups, at_once = (int64_t)per_sm * tc::sm_count(), most = at_once < kMostPartials ? at_once : kMostPartials;
   const int blocks = (int)(wanted < most ? wanted : most);
+  for (Rows* r : {&p.x, &p.f, &p.x_new, &p.d_y, &p.d_new, &p.dx, &p.df}) r->step = r->ld * blocks * groups;
   launch_chained(lc, kernel, dim3(blocks), groups * p.threads, smem, 1, p);
   return blocks;
 }
@@ -448,11 +800,11 @@ hbp_status check(const hbp_norm* n) {
 }
 // a tensor's rows, none if it is not given
 bool rows_of(const hbp_norm& n, const hbp_rows* t, bool input, Rows* r) {
-  *r = {nullptr, 0};
+  *r = {nullptr, 0, 0};
   if (!t || !t->x) return true;
   const int v = n.dtype == HBP_F32 ? 4 : 8;
   if (((uintptr_t)t->x & 15u) || t->stride % v || (t->stride < n.d && !(input && t->stride == 0) && n.rows > 1)) return false;
-  *r = {t->x, t->stride};
+  *r = {t->x, t->stride, 0};
   return true;
 }
 // an output that lies on an input has to lie on it row by row
@@ -463,7 +815,7 @@ NormParams params_of(const hbp_norm& n, bool backward, int* nv) {
   p.rows = n.rows;
   p.d = n.d;
   p.per_row = n.d / (n.dtype == HBP_F32 ? 4 : 8);
-  split_of(p.per_row, backward, nv, &p.threads);
+  split_of(p.per_row, backward, n.dtype == HBP_F32, nv, &p.threads);
   p.eps = n.eps;
   p.scale = n.scale;
   p.inv_d = (float)(1.0 / n.d);
@@ -551,7 +903,10 @@ extern "C" hbp_status hbp_norm_residual_backward(const hbp_norm* n, const hbp_ro
   p.partial = sums ? (float*)scratch : nullptr;
   WeightSums w = {(const float*)scratch, 0, n->d, {dw_pre, dw_post, da}};
   if (n->rows)
-    w.blocks = by_variant(*n, nv, [&](auto t, auto v, auto layer) { return backward<decltype(t), decltype(v)::value, decltype(layer)::value>(lc, p, post); });
+    w.blocks = by_variant(*n, nv, [&](auto t, auto v, auto layer) {
+      if constexpr (sizeof(t) == 2 && decltype(v)::value == 4) return 0;  // (rows of bf16 have 1024 vectors at most)
+      else return backward<decltype(t), decltype(v)::value, decltype(layer)::value>(lc, p, post);
+    });
   if (sums) launch_chained(lc, weight_sums_kernel, dim3((n->d + 127) / 128, 3), 256, 0, 1, w);
   return lc.err == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
 }
