@@ -15,7 +15,7 @@
 // operand in 5.  E and s x are rounded to bf16, the operands' type: 2^-9 of each of their values at most, as a rounding of dz would be.  A row whose largest logit is more than
 // kFar above the target's (a loss of 40) would leave the range that bf16 and float sums of e have: finish_kernel then takes r = the largest logit,
 // and 2 and 3 run again; their launches return at once where no row asked for that.
-// The forward pass alone is 1 to 3 without E.
+// The forward pass alone has no E: the product sums exp(z - its largest), takes z_t out on the way, and loss_kernel joins what its tiles have.
 //
 // float: products of operands in three bf16 parts (gemm_parts.cu); the logits of a piece of the rows lie in scratch, and
 // one pass over them forms dz, in parts.
@@ -67,7 +67,7 @@ struct RowData {
   const float* d_loss;
   int64_t d_loss_stride;
   float* loss;
-  bf16* E;  // not of the forward pass alone
+  bf16* E;
   int64_t ldE;
   bf16* xs;
 };
@@ -141,17 +141,15 @@ __global__ void __launch_bounds__(32 * kFinishWarps) finish_kernel(const RowData
         const bool at_target = zt == ref;
         const float total = sum + (at_target ? 1.0f : expf(zt - ref));
         loss = at_target ? log1pf(sum) : logf(total) - (zt - ref);
-        if (p.E) {
-          factor = (p.d_loss ? p.d_loss[row * p.d_loss_stride] : 1.0f) / total;
-          const bf16 e = __float2bfloat16_rn(-sum);
-          p.E[row * p.ldE + t] = e;
-          // the largest term of most rows' gradients, with its rounding taken out again: the others share a 2^-9, as large as their own
-          const float kept = __bfloat162float(e);
-          if (sum > 0.0f && isfinite(kept)) factor *= sum / -kept;
-        }
+        factor = (p.d_loss ? p.d_loss[row * p.d_loss_stride] : 1.0f) / total;
+        const bf16 e = __float2bfloat16_rn(-sum);
+        p.E[row * p.ldE + t] = e;
+        // the largest term of most rows' gradients, with its rounding taken out again: the others share it, as large as their own
+        const float kept = __bfloat162float(e);
+        if (sum > 0.0f && isfinite(kept)) factor *= sum / -kept;
       }
       p.loss[row] = loss;
-      if (p.E) p.factor[row] = factor;
+      p.factor[row] = factor;
     }
     factors[lane] = factor;
   }
@@ -169,6 +167,56 @@ __global__ void __launch_bounds__(32 * kFinishWarps) finish_kernel(const RowData
     for (int e = 0; e < 8; ++e) f[e] = factors[r] != 0.0f ? f[e] * factors[r] : 0.0f;  // (a row that is ignored may hold anything)
     *reinterpret_cast<uint4*>(p.xs + (row0 + r) * p.d + c) = tc::pack8(f);
   }
+}
+
+// The forward pass alone: sums of exp(z - largest) of the tiles, joined the same way.
+__global__ void __launch_bounds__(32 * kFinishWarps) loss_kernel(const RowData p) {
+  __shared__ float2 joined[kFinishWarps][32];
+  chain_next();
+  chain_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+  float2 s = make_float2(0.0f, -INFINITY);
+  // eight sums at a time: their exponentials wait for one maximum, not for each other
+  auto join = [&](const float2 (&v)[8]) {
+    float top = s.y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i].y);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    s.x *= __expf(s.y - ref);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s.x = fmaf(v[i].x, __expf(v[i].y - ref), s.x);
+    s.y = top;
+  };
+  const float2 empty = make_float2(0.0f, -INFINITY);
+  float2 v[8];
+  for (int k = warp; k < p.slots; k += 8 * kFinishWarps) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int slot = k + i * kFinishWarps;
+      v[i] = row < p.rows && slot < p.slots ? p.parts[(int64_t)slot * p.rows + row] : empty;
+    }
+    join(v);
+  }
+  joined[warp][lane] = s;
+  __syncthreads();
+  if (warp || row >= p.rows) return;
+  s = empty;
+#pragma unroll
+  for (int k = 0; k < kFinishWarps; k += 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = joined[k + i][lane];
+    join(v);
+  }
+  const int t = p.targets.column(row, p.vocab, p.status);
+  float loss = 0.0f;
+  if (t >= 0) {
+    const float above = s.y - p.zt[row];
+    if (p.zt[row] == INFINITY) loss = NAN;
+    else if (above <= kFar) loss = log1pf(s.x * expf(above));
+    else loss = logf(s.x + expf(-above)) + above;
+  }
+  p.loss[row] = loss;
 }
 
 // out (rows ld apart, bf16) = factor[row] * the sum of `splits` [rows][d], in their order; eight channels a thread
@@ -194,22 +242,38 @@ __global__ void __launch_bounds__(256) narrow_kernel(const float* in, int splits
 }
 
 // ------------------------------------------------------------------------------------------- float
-// rows of src, ld apart -> planes; zeros for rows without a target (they may hold anything), where targets are given
-__global__ void __launch_bounds__(256) split_rows_kernel(const float* src, int64_t ld, Planes dst, int64_t rows, int d, Targets targets, int vocab) {
+// rows of src, ld apart -> planes; zeros for those behind the last, and for rows without a target (they may hold anything), where targets are given
+__global__ void __launch_bounds__(256) split_rows_kernel(const float* src, int64_t ld, Planes dst, int64_t rows, int64_t all, int d, Targets targets, int vocab) {
   chain_next();
   chain_wait();
   const int per_row = d / 4;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per_row;
-  if (row >= rows) return;
+  if (row >= all) return;
   const int c = (int)(i - row * per_row) * 4;
-  const bool there = !targets.t || targets.column(row, vocab, nullptr) >= 0;
+  const bool there = row < rows && (!targets.t || targets.column(row, vocab, nullptr) >= 0);
   store_parts4(dst.p + row * dst.ld + c, dst.plane, there ? *reinterpret_cast<const float4*>(src + row * ld + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+}
+
+// out (rows ld apart) = the sum of `splits` [rows][d], in their order; four channels a thread
+__global__ void __launch_bounds__(256) sum_splits_kernel(const float* in, int splits, float* out, int64_t ld, int64_t rows, int d) {
+  chain_next();
+  chain_wait();
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = rows * d;
+  if (i >= n) return;
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int k = 0; k < splits; ++k) {
+    const float4 v = __ldcs(reinterpret_cast<const float4*>(in + k * n + i));
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  const int64_t row = i / d;
+  *reinterpret_cast<float4*>(out + row * ld + (i - row * d)) = s;
 }
 
 struct LogitsData {
   const float* z;  // [rows][ldz], ldz a multiple of 4
   int64_t ldz;
-  int vocab;
+  int vocab, columns;  // of dz: zeros behind the vocabulary
   Targets targets;
   int* status;
   const float* d_loss;
@@ -269,9 +333,9 @@ __global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p)
   if (!p.dz.p) return;
   const float factor = t < 0 ? 0.0f : (p.d_loss ? p.d_loss[row * p.d_loss_stride] : 1.0f) / total;
   bf16* out = p.dz.p + row * p.dz.ld;
-  for (int c = threadIdx.x * 4; c < p.vocab; c += kRowThreads * 4) {
+  for (int c = threadIdx.x * 4; c < p.columns; c += kRowThreads * 4) {
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (factor != 0.0f) {
+    if (factor != 0.0f && c < p.vocab) {
       const float4 q = *reinterpret_cast<const float4*>(z + c);
       v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
 #pragma unroll
@@ -304,10 +368,35 @@ int dx_splits(int64_t rows, int vocab, int d) {
   return best;
 }
 
+// The same for float: 12 instructions a block of 32, of n_tile / 2 clocks each and 40 at least, tiles of 256 x 32 to 192 (gemm_parts.cu), and what is
+// read for a tile, of which the pairs get 50 bytes a clock: 1901 rows of 520 channels, whose 72 tiles of 64 columns read the probabilities nine times over, 177 us,
+// split in three XXX.
+int dx_splits_f32(int64_t rows, int vocab, int d) {
+  const int64_t m_tiles = (rows + 255) / 256, blocks = (vocab + 31) / 32;
+  int best = 1;
+  double least = 0;
+  for (int n = 1; n <= 32 && (n == 1 || blocks / n >= 16); ++n) {
+    double cost = 0;
+    for (int w = 32; w <= 192; w += 32) {
+      const int64_t tiles = m_tiles * ((d + w - 1) / w) * n;
+      const int issue = 12 * (w / 2 > 40 ? w / 2 : 40), read = (256 + w) * 32 * 6 / 50, block = issue > read ? issue : read;
+      const double c = (double)((tiles + kPairs - 1) / kPairs) * ((double)((blocks + n - 1) / n) * block + 1500 + 12 * w);
+      if (cost == 0 || c < cost) cost = c;
+    }
+    if (n > 1) cost += n * 8.0 * (double)rows * d / (kPairs * 44.0) + 5000;
+    if (n == 1 || cost < 0.97 * least) {
+      best = n;
+      least = cost;
+    }
+  }
+  return best;
+}
+
 // The scratch of pieces of `piece` rows.
 struct Plan {
   int64_t piece;
-  int splits = 1;
+  int splits = 1;   // of dx's contraction; float: in chunks of so many columns
+  int chunk = 0;
   int64_t ldE = 0;  // bf16: of E; float: of the logits
   size_t target, zt, ref, factor, words, parts = 0, E = 0, xs = 0, partial = 0, dwf = 0, xp = 0, wp = 0, ep = 0;
   size_t bytes = 0;
@@ -336,15 +425,20 @@ struct Plan {
       return;
     }
     ldE = ((int64_t)vocab + 3) / 4 * 4;
+    if (grads) splits = dx_splits_f32(n, vocab, d);
+    chunk = splits > 1 ? ((vocab + splits - 1) / splits + 63) / 64 * 64 : vocab;
     x.ld = w.ld = plane_ld(d);
-    e.ld = plane_ld(vocab);
+    e.ld = splits > 1 ? (int64_t)splits * chunk : plane_ld(vocab);
     x.plane = n * x.ld;
-    w.plane = vocab * w.ld;
+    w.plane = (int64_t)splits * chunk * w.ld;
     e.plane = n * e.ld;
+    e.sb = chunk;
+    w.sb = (int64_t)chunk * w.ld;
     xp = take((size_t)3 * x.plane * 2);
     wp = take((size_t)3 * w.plane * 2);
     E = take((size_t)n * ldE * 4);
     if (grads) ep = take((size_t)3 * e.plane * 2);
+    if (splits > 1) partial = take((size_t)splits * n * d * 4);
   }
 };
 constexpr int64_t kLeastPiece = 256;
@@ -403,15 +497,23 @@ bool run_bf16(Launcher& lc, const Call& c, const Plan& plan, int* status) {
       p.ldE = plan.ldE;
       if (c.dw) p.xs = (bf16*)(s + plan.xs);
     }
-    launch_chained(lc, target_kernel, dim3((unsigned)((n + 7) / 8)), 256, 0, 1, p);
     GemmArgs g;
     g.M = (int)n; g.N = v.vocab; g.K = v.d;
     g.in_dtype = HBP_BF16;
     g.A = p.x; g.a_sm = v.ldx; g.a_sk = 1;
     g.B = p.w; g.b_sn = v.ldw; g.b_sk = 1;
     g.epi = EPI_EXP;
+    g.row_parts = p.parts; g.slots_out = &p.slots;
+    if (!c.grads) {
+      g.target = (const int*)p.targets.t; g.target_bytes = v.target_bytes;
+      g.row_z = p.zt;
+      if (!gemm_tc(lc, g, status)) return false;
+      launch_chained(lc, loss_kernel, dim3((unsigned)((n + 31) / 32)), 32 * kFinishWarps, 0, 1, p);
+      continue;
+    }
+    launch_chained(lc, target_kernel, dim3((unsigned)((n + 7) / 8)), 256, 0, 1, p);
     g.D = p.E; g.ldd = p.ldE;
-    g.row_f = p.ref; g.target = p.target; g.row_parts = p.parts; g.slots_out = &p.slots;
+    g.row_f = p.ref; g.target = p.target;
     for (int again = 0; again < 2; ++again) {
       p.again = again != 0;
       g.redo = again ? p.redo : nullptr;
@@ -469,14 +571,15 @@ bool run_f32(Launcher& lc, const Call& c, const Plan& plan, int* status) {
   Planes x = plan.x, w = plan.w, e = plan.e;
   x.p = (bf16*)(s + plan.xp);
   w.p = (bf16*)(s + plan.wp);
-  auto split = [&](const float* src, int64_t ld, const Planes& P, int64_t rows, const Targets& targets) {
-    launch_chained(lc, split_rows_kernel, dim3((unsigned)((rows * (v.d / 4) + 255) / 256)), 256, 0, 1, src, ld, P, rows, v.d, targets, v.vocab);
+  auto split = [&](const float* src, int64_t ld, const Planes& P, int64_t rows, int64_t all, const Targets& targets) {
+    launch_chained(lc, split_rows_kernel, dim3((unsigned)((all * (v.d / 4) + 255) / 256)), 256, 0, 1, src, ld, P, rows, all, v.d, targets, v.vocab);
   };
-  split((const float*)v.w, v.ldw, w, v.vocab, Targets{nullptr, 8});
+  const int64_t columns = (int64_t)plan.splits * plan.chunk;
+  split((const float*)v.w, v.ldw, w, v.vocab, columns, Targets{nullptr, 8});
   for (int64_t lo = 0; lo < v.rows; lo += plan.piece) {
     const int64_t n = v.rows - lo < plan.piece ? v.rows - lo : plan.piece;
     const Targets targets = {(const uint8_t*)v.targets + lo * v.target_bytes, v.target_bytes};
-    split((const float*)v.x + lo * v.ldx, v.ldx, x, n, targets);
+    split((const float*)v.x + lo * v.ldx, v.ldx, x, n, n, targets);
     PartsGemm g;
     g.M = (int)n; g.N = v.vocab; g.K = v.d;
     g.A = x; g.B = w;
@@ -484,7 +587,7 @@ bool run_f32(Launcher& lc, const Call& c, const Plan& plan, int* status) {
     if (!gemm_parts(lc, g, status)) return false;
     LogitsData p = {};
     p.z = g.D; p.ldz = plan.ldE;
-    p.vocab = v.vocab;
+    p.vocab = v.vocab; p.columns = (int)columns;
     p.targets = targets;
     p.status = v.status;
     p.d_loss = c.d_loss ? c.d_loss + lo * c.d_loss_stride : nullptr;
@@ -497,11 +600,17 @@ bool run_f32(Launcher& lc, const Call& c, const Plan& plan, int* status) {
     launch_chained(lc, logits_kernel, dim3((unsigned)n), kRowThreads, 0, 1, p);
     if (c.dx) {
       PartsGemm b;
-      b.M = (int)n; b.N = v.d; b.K = v.vocab;
+      b.M = (int)n; b.N = v.d; b.K = plan.chunk;
+      b.batch = plan.splits;  // (chunks of the contraction; behind the vocabulary there are zeros)
       b.A = e; b.B = w;
       b.b_mn = true;
-      b.D = (float*)c.dx + lo * c.lddx; b.ldd = c.lddx;
+      float* dx = (float*)c.dx + lo * c.lddx;
+      b.D = plan.splits > 1 ? (float*)(s + plan.partial) : dx;
+      b.ldd = plan.splits > 1 ? v.d : c.lddx;
+      b.d_sb = n * v.d;
       if (!gemm_parts(lc, b, status)) return false;
+      if (plan.splits > 1)
+        launch_chained(lc, sum_splits_kernel, dim3((unsigned)((n * v.d / 4 + 255) / 256)), 256, 0, 1, (const float*)b.D, plan.splits, dx, c.lddx, n, v.d);
     }
     if (c.dw) {
       PartsGemm b;

@@ -74,7 +74,9 @@ struct TcParams {
   // EPI_EXP, EPI_ROWS
   const float* row_f;
   const int* target;
+  int target_bytes;
   float2* row_parts;
+  float* row_z;
   const int* redo;
   int panel;  // row blocks that share a column block's copies
 };
@@ -205,6 +207,48 @@ __device__ __forceinline__ void exp_chunk(float* v, int col, int N, int target, 
   unpack2(s2[0], s0, s1);
   unpack2(s2[1], t0, t1);
   sum += (s0 + s1) + (t0 + t1);
+}
+
+// The same where the terms are not kept (EPI_EXP without D): sum is of exp(z - most), whatever the reference would have been, and the target's logit is
+// taken out.
+__device__ __forceinline__ void sum_chunk(float* v, int col, int N, int target, float& z, float& sum, float& most) {
+  const uint32_t at = (uint32_t)(target - col);
+  if (__any_sync(0xffffffffu, at < 64u)) {
+#pragma unroll
+    for (int i = 0; i < 64; ++i) {
+      z = at == (uint32_t)i ? v[i] : z;
+      v[i] = at == (uint32_t)i ? -INFINITY : v[i];
+    }
+  }
+  if (col + 64 > N) {
+#pragma unroll
+    for (int i = 0; i < 64; ++i) v[i] = col + i >= N ? -INFINITY : v[i];
+  }
+  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < 64; i += 4)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] = fmaxf(m[k], v[i + k]);
+  const float top = fmaxf(fmaxf(most, fmaxf(m[0], m[1])), fmaxf(m[2], m[3]));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  const f32x2 less = both(-ref), log2e = both(1.44269504088896340736f);
+  f32x2 s2[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+  for (int i = 0; i < 64; i += 2) {
+    f32x2 d;
+    float e0, e1;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack2(v[i], v[i + 1])), "l"(less));
+    unpack2(mul2(d, log2e), e0, e1);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e0));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e1));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s2[i / 2 & 1]) : "l"(pack2(e0, e1)));
+  }
+  float s0, s1, t0, t1, scale = (most - ref) * 1.44269504088896340736f;
+  unpack2(s2[0], s0, s1);
+  unpack2(s2[1], t0, t1);
+  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(scale));
+  sum = fmaf(sum, scale, (s0 + s1) + (t0 + t1));
+  most = top;
 }
 
 // ------------------------------------------------------------------------------------------- kernel
@@ -462,9 +506,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       }
       // (kRows) this lane's row
       const bool row_in = kRows && row0 + lane < p.M;
-      const float row_f = row_in ? p.row_f[row0 + lane] : 0.0f;
-      const int target = row_in && p.epi == EPI_EXP ? p.target[row0 + lane] : -1;
-      float row_total = 0.0f, row_most = -INFINITY;
+      const float row_f = row_in && p.row_f ? p.row_f[row0 + lane] : 0.0f;
+      int target = -1;
+      if (row_in && p.epi == EPI_EXP)  // (int32, or the low half of int64 where the high one is 0)
+        target = p.target_bytes == 8 && p.target[2 * (int64_t)(row0 + lane) + 1] != 0 ? -1 : p.target[(int64_t)(p.target_bytes / 4) * (row0 + lane)];
+      float row_total = 0.0f, row_most = -INFINITY, row_z = 0.0f;
       if (!mbar_wait(accf_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit_ns)) break;
       tc_fence_after();
       const uint32_t tsrc = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + half * half_cols);
@@ -498,8 +544,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
           }
           const int col = colw + c * cw;
           if (kRows && p.epi == EPI_EXP) {
+            if (!p.D) {
+              sum_chunk(v, col, p.N, target, row_z, row_total, row_most);
+              continue;
+            }
             exp_chunk(v, col, p.N, target, row_f, row_total, row_most);
-            if (!p.D) continue;
             if (__any_sync(0xffffffffu, target < 0)) {
 #pragma unroll
               for (int i = 0; i < 64; ++i) v[i] = target >= 0 ? v[i] : 0.0f;  // (a row that is ignored may hold anything)
@@ -592,8 +641,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
         if (!ok) break;
       }
-      if (kRows && p.epi == EPI_EXP && row_in)
+      if (kRows && p.epi == EPI_EXP && row_in) {
         p.row_parts[(int64_t)(nt * 2 + half) * p.M + row0 + lane] = make_float2(row_total, row_most);
+        if (!p.D && target >= colw && target < min(colw + my_cols, p.N)) p.row_z[row0 + lane] = row_z;
+      }
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
     if (lane == 0) {
@@ -725,8 +776,9 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   const int vec = f32 ? 4 : 8;  // elements per 16 bytes
   const bool by_rows = g.epi == EPI_EXP || g.epi == EPI_ROWS;
   if (g.N % vec && g.epi != EPI_EXP) return false;
-  if (by_rows && (f32 || g.batch != 1 || g.splitk > 1 || !g.row_f)) return false;
-  if (g.epi == EPI_EXP && (g.d_f32 || !g.target || !g.row_parts)) return false;
+  if (by_rows && (f32 || g.batch != 1 || g.splitk > 1)) return false;
+  if (g.epi == EPI_ROWS && !g.row_f) return false;
+  if (g.epi == EPI_EXP && (g.d_f32 || !g.target || !g.row_parts || (g.D ? !g.row_f : !g.row_z))) return false;
   if (!by_rows && g.epi != EPI_STORE && g.epi != EPI_GELU_FWD && g.epi != EPI_MUL && g.epi != EPI_RESID && g.epi != EPI_STORE_LN &&
       g.epi != EPI_ADD && g.epi != EPI_ACCUM)
     return false;
@@ -852,7 +904,7 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   p.status = status_word;
   p.wait_limit_ns = g.wait_limit_ns ? g.wait_limit_ns : WAIT_LIMIT_NS;
   p.stall = g.test_stall;
-  p.row_f = g.row_f; p.target = g.target; p.row_parts = g.row_parts; p.redo = g.redo;
+  p.row_f = g.row_f; p.target = g.target; p.target_bytes = g.target_bytes; p.row_parts = g.row_parts; p.row_z = g.row_z; p.redo = g.redo;
   if (g.slots_out) *g.slots_out = 2 * p.n_tiles;
   p.panel = 0;
   if (g.epi == EPI_EXP) {  // rows of x of 32 MB, a quarter of L2

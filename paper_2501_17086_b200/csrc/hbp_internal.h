@@ -22,7 +22,9 @@ enum Epilogue {
   EPI_STORE_LN = 6,  // D = acc, plus per-row partial sums (sum acc, sum acc * E[m,n]) per 64 columns -> stats
   EPI_ADD = 7,       // D = acc + E[m,n]   (u_t + delta_t: the scan then reads one tensor less)
   EPI_ACCUM = 8,     // D += acc, D float (bf16 operands on the tensor cores only: gemm_tc; gemm() does not take it)
-  EPI_EXP = 9,         // D = exp(acc - row_f[m]), 0 at n = target[m] and in rows whose target is negative (bf16; no D: not stored); row_parts (gemm_tc only)
+  // D = exp(acc - row_f[m]), 0 at n = target[m] and in rows without a target (bf16); row_parts.  Without D: row_parts, their sums those of
+  // exp(acc - largest), and row_z[m] = acc at the target.  (gemm_tc only)
+  EPI_EXP = 9,
   EPI_ROWS = 10,       // D = acc * row_f[m], 0 where that is 0 (gemm_tc only)
   EPI_RNN_FWD = 5,   // c = tanh(acc + E[m,n]);  D2 = 1 - c^2;  D = gate[n] * E2[m,n] + c
 };
@@ -60,8 +62,10 @@ struct GemmArgs {
   // EPI_EXP, EPI_ROWS: a number a row; the column of each row that is left out; per tile and half of its columns [slots][M] the row's (sum of
   // what D receives, largest acc) without that column; where the number of those slots goes (host); a device word without which, 0, the launch does nothing
   const float* row_f = nullptr;
-  const int* target = nullptr;
+  const int* target = nullptr;  // numbers of target_bytes; negative or (8 bytes) 2^31 and more: none
+  int target_bytes = 4;
   float2* row_parts = nullptr;
+  float* row_z = nullptr;
   int* slots_out = nullptr;
   const int* redo = nullptr;
   bool wide = false;   // splitk > 1: tiles of full width
