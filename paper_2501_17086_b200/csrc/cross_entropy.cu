@@ -414,7 +414,7 @@ struct Plan {
     factor = take(n * 4);
     if (dtype == HBP_BF16) {
       ldE = ((int64_t)vocab + 63) / 64 * 64;
-      parts = take((size_t)2 * ((vocab + 127) / 128) * n * 8);
+      parts = take(((size_t)(vocab + 63) / 64 + 3) * n * 8);  // (slots of 64 columns, of whole tiles of up to 256)
       if (grads) {
         E = take((size_t)n * ldE * 2);
         xs = take((size_t)n * d * 2);
@@ -443,7 +443,7 @@ struct Plan {
 };
 constexpr int64_t kLeastPiece = 256;
 // what grows with rows times vocab: bytes a row
-size_t row_bytes(int dtype, int vocab, bool grads) { return dtype == HBP_BF16 ? (grads ? (size_t)vocab * 2 : (size_t)(vocab + 127) / 128 * 16) : (size_t)vocab * (grads ? 10 : 4); }
+size_t row_bytes(int dtype, int vocab, bool grads) { return dtype == HBP_BF16 ? (grads ? (size_t)vocab * 2 : ((size_t)(vocab + 63) / 64 + 3) * 8) : (size_t)vocab * (grads ? 10 : 4); }
 
 int64_t wanted_piece(int dtype, int64_t rows, int vocab, bool grads) {
   const size_t b = row_bytes(dtype, vocab, grads);

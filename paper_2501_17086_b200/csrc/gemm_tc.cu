@@ -3,7 +3,7 @@
 //
 //   D(m, n) = sum_k A(m, k) B(n, k), fp32 accumulate, batched (one launch covers all layers of a group).
 //
-// Persistent kernel, one CTA per SM, 384 threads:
+// Persistent kernel, one CTA per SM, 384 threads (EPI_EXP: 640, 16 epilogue warps):
 //   warps 0, 10 TMA producers of A and of B (one lane each): fill a ring of {A 128x64, B 128x64 (pairs) or 256x64} bf16 tiles.  (One
 //               producer of both held the narrow tiles back, and MN-major operands, which come as two copies a stage: 2664 x 512 x
 //               2048 16.4 -> 15.8 us, in tiles of 128 columns 15.7 -> 14.5; 8192 x 1024 x 4096 50.4 -> 48.8)
@@ -19,6 +19,8 @@
 // Every wait on an mbarrier is bounded: after ~4 s it raises a shared abort flag, records
 // HBP_ERR_TIMEOUT in the status word, and all roles drain and leave through the common exit that
 // frees the tensor memory.
+#include <type_traits>
+
 #include "ring_drain.cuh"
 #include "tc_common.cuh"
 
@@ -37,18 +39,25 @@ constexpr int A_BYTES = BM * BK * 2;
 // 1115 -> 1174 TFLOP/s, but an epilogue that waits for each of its copies).  Float operands run on single CTAs only: the float
 // products of 32 units and more that pairs would take are the bf16 kernels' (gemm_parts.cu, gemm_cell.cu).
 constexpr int PAIR_STAGE_BYTES = A_BYTES + 128 * BK * 2;
-template <bool kPair>
+// EPI_EXP has 16 epilogue warps of 64 columns, a buffer each: what they do is long for the products of a short contraction, and of eight warps two share a
+// scheduler, which leaves it idle two thirds of the time (the loss of 16384 x 50021 x 64: 482 us, so 372; of 256 channels 250 and 201 for 8192 rows, from 768 on the same).
+enum Rows { kNoRows = 0, kExpRows = 1, kScaledRows = 2 };  // EPI_EXP; EPI_ROWS
+template <bool kPair, int kRows>
 struct Mode {
   static constexpr int kTileM = kPair ? 256 : 128;
-  static constexpr int kEpiBufs = kPair ? 2 : 1;  // staging buffers per epilogue warp
-  static constexpr int kRingBytes = (kEpiBufs == 2 ? 5 : 6) * PAIR_STAGE_BYTES;  // single CTAs: 4, 6 or 8 stages
+  static constexpr int kEpiWarps = kRows == kExpRows ? 16 : 8;
+  static constexpr int kEpiBufs = kPair && kRows != kExpRows ? 2 : 1;  // staging buffers per epilogue warp
+  static constexpr int kRingBytes = (kPair || kRows == kExpRows ? 5 : 6) * PAIR_STAGE_BYTES;  // single CTAs: 4, 6 or 8 stages (EPI_EXP: 3, 5, 6)
+  static constexpr int kThreads = 128 + 32 * kEpiWarps;
 };
-constexpr int MAX_STAGES = 8;
-constexpr int EPI_WARPS = 8, kProducerB = 2 + EPI_WARPS, THREADS = 64 + 32 * EPI_WARPS + 64;
+constexpr int MAX_STAGES = 8, MAX_EPI_WARPS = 16;
 constexpr uint32_t TMEM_COLS = 512;
 constexpr int EPI_BUF_BYTES = 4096;  // 32 rows x 128 bytes
-constexpr int SMEM_BYTES = Mode<true>::kRingBytes + 2 * EPI_WARPS * EPI_BUF_BYTES + 1024 /*alignment slack*/ + 512 /*barriers*/;
-static_assert(Mode<false>::kRingBytes + EPI_WARPS * EPI_BUF_BYTES == Mode<true>::kRingBytes + 2 * EPI_WARPS * EPI_BUF_BYTES, "one size");
+constexpr int SMEM_BYTES = Mode<true, kNoRows>::kRingBytes + 2 * 8 * EPI_BUF_BYTES + 1024 /*alignment slack*/ + 512 /*barriers*/;
+template <bool kPair, int kRows>
+constexpr int kUsed = Mode<kPair, kRows>::kRingBytes + Mode<kPair, kRows>::kEpiWarps * Mode<kPair, kRows>::kEpiBufs * EPI_BUF_BYTES;
+static_assert(kUsed<true, kNoRows> == kUsed<false, kNoRows> && kUsed<true, kNoRows> == kUsed<true, kExpRows> && kUsed<true, kNoRows> == kUsed<false, kExpRows>, "one size");
+static_assert(8 * (2 * MAX_STAGES + 5 + 2 * MAX_EPI_WARPS) + 8 <= 512, "barriers");
 
 struct TcParams {
   int M, N, K, batch;
@@ -78,15 +87,17 @@ struct TcParams {
   float2* row_parts;
   float* row_z;
   const int* redo;
-  int panel;  // row blocks that share a column block's copies
+  // EPI_EXP: row blocks that share a column block's copies; those of the last such panel; tiles of a panel
+  int panel;
+  Divider by_panel, by_last, by_tiles;
 };
 
 // EPI_EXP: tiles go down `panel` row blocks of one column block, then on to the next one: w is far too large for L2, those rows of x
 // are not.  (Along the columns, as everywhere else, each row block would read all of w again: 4096 x 50021 x 1024 read 1.6 GB.)
 __device__ __forceinline__ void panel_tile(const TcParams& p, int r, int& m, int& n) {
-  const int per_panel = p.panel * p.n_tiles, first = r / per_panel * p.panel, q = r % per_panel, rows = min(p.panel, p.m_tiles - first);
-  m = first + q % rows;
-  n = q / rows;
+  const int k = (int)p.by_tiles((uint32_t)r), first = k * p.panel, q = r - k * (p.panel * p.n_tiles), rows = min(p.panel, p.m_tiles - first);
+  n = (int)(rows == p.panel ? p.by_panel((uint32_t)q) : p.by_last((uint32_t)q));
+  m = first + q - n * rows;
 }
 
 // ------------------------------------------------------------------------------------------- epilogue math
@@ -171,102 +182,78 @@ __device__ __forceinline__ void residual_chunk(const TcParams& p, int b, int row
   }
 }
 
-// EPI_EXP on 64 columns of a row, from `col` on: z -> exp(z - ref), 0 for the target's column and those behind the last; what that adds to the
-// row's sum and largest z.
-__device__ __forceinline__ void exp_chunk(float* v, int col, int N, int target, float ref, float& sum, float& most) {
-  const uint32_t at = (uint32_t)(target - col);
-  if (__any_sync(0xffffffffu, at < 64u)) {
-#pragma unroll
-    for (int i = 0; i < 64; ++i) v[i] = at == (uint32_t)i ? -INFINITY : v[i];
-  }
-  if (col + 64 > N) {
-#pragma unroll
-    for (int i = 0; i < 64; ++i) v[i] = col + i >= N ? -INFINITY : v[i];
-  }
-  // the difference first: a product with log2(e) of each, and one rounding less, would be off by |z| 2^-24
-  const f32x2 less = both(-ref), log2e = both(1.44269504088896340736f);
-  f32x2 s2[2] = {both(0.0f), both(0.0f)};
-  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-  for (int i = 0; i < 64; i += 4) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) m[k] = fmaxf(m[k], v[i + k]);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      float* e = v + i + 2 * k;
-      f32x2 d;
-      asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack2(e[0], e[1])), "l"(less));
-      unpack2(mul2(d, log2e), e[0], e[1]);
-      asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[0]));
-      asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e[1]));
-      asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s2[k]) : "l"(pack2(e[0], e[1])));
-    }
-  }
-  most = fmaxf(fmaxf(most, fmaxf(m[0], m[1])), fmaxf(m[2], m[3]));
-  float s0, s1, t0, t1;
-  unpack2(s2[0], s0, s1);
-  unpack2(s2[1], t0, t1);
-  sum += (s0 + s1) + (t0 + t1);
+// The largest of three
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
-
-// The same where the terms are not kept (EPI_EXP without D): sum is of exp(z - most), whatever the reference would have been, and the target's logit is
-// taken out.
-__device__ __forceinline__ void sum_chunk(float* v, int col, int N, int target, float& z, float& sum, float& most) {
+// EPI_EXP on 32 columns of a row, from `col` on.  Without the target's column, whose z is taken out, and those behind the last, v becomes exp(z - ref) and
+// sum grows by that; most: the largest z.  kKeep: v is kept, ref is given; else sum is of exp(z - most) whatever ref is.
+template <bool kKeep>
+__device__ __forceinline__ void exp_chunk(float* v, int col, int N, int target, float ref, float& z, float& sum, float& most) {
   const uint32_t at = (uint32_t)(target - col);
-  if (__any_sync(0xffffffffu, at < 64u)) {
+  if (__any_sync(0xffffffffu, at < 32u)) {
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
+    for (int i = 0; i < 32; ++i) {
       z = at == (uint32_t)i ? v[i] : z;
       v[i] = at == (uint32_t)i ? -INFINITY : v[i];
     }
   }
-  if (col + 64 > N) {
+  if (col + 32 > N) {
 #pragma unroll
-    for (int i = 0; i < 64; ++i) v[i] = col + i >= N ? -INFINITY : v[i];
+    for (int i = 0; i < 32; ++i) v[i] = col + i >= N ? -INFINITY : v[i];
   }
-  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  float m[4] = {most, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-  for (int i = 0; i < 64; i += 4)
+  for (int i = 0; i < 32; i += 8)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) m[k] = fmaxf(m[k], v[i + k]);
-  const float top = fmaxf(fmaxf(most, fmaxf(m[0], m[1])), fmaxf(m[2], m[3]));
-  const float ref = top == -INFINITY ? 0.0f : top;
+    for (int k = 0; k < 4; ++k) m[k] = max3(m[k], v[i + 2 * k], v[i + 2 * k + 1]);
+  const float top = fmaxf(max3(m[0], m[1], m[2]), m[3]);
+  float scale = 1.0f;
+  if (!kKeep) {
+    ref = top == -INFINITY ? 0.0f : top;
+    scale = (most - ref) * 1.44269504088896340736f;
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(scale));
+  }
+  most = top;
+  // the difference first: a product with log2(e) of each, and one rounding less, would be off by |z| 2^-24
   const f32x2 less = both(-ref), log2e = both(1.44269504088896340736f);
   f32x2 s2[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
-  for (int i = 0; i < 64; i += 2) {
+  for (int i = 0; i < 32; i += 2) {
     f32x2 d;
-    float e0, e1;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(pack2(v[i], v[i + 1])), "l"(less));
-    unpack2(mul2(d, log2e), e0, e1);
-    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e0));
-    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(e1));
-    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s2[i / 2 & 1]) : "l"(pack2(e0, e1)));
+    unpack2(mul2(d, log2e), v[i], v[i + 1]);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(v[i]));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(v[i + 1]));
+    asm("add.rn.f32x2 %0, %0, %1;" : "+l"(s2[i / 2 & 1]) : "l"(pack2(v[i], v[i + 1])));
   }
-  float s0, s1, t0, t1, scale = (most - ref) * 1.44269504088896340736f;
+  float s0, s1, t0, t1;
   unpack2(s2[0], s0, s1);
   unpack2(s2[1], t0, t1);
-  asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(scale));
-  sum = fmaf(sum, scale, (s0 + s1) + (t0 + t1));
-  most = top;
+  const float more = (s0 + s1) + (t0 + t1);
+  sum = kKeep ? sum + more : fmaf(sum, scale, more);
 }
 
 // ------------------------------------------------------------------------------------------- kernel
 // kRows: the epilogues EPI_EXP and EPI_ROWS, which know their row, and launches that may turn out to be needless; else the others.
 // kNarrow: tiles of p.n_mma columns; else of 256, whose constants the compiler folds (a run-time width costs the large products 2 to 4 %)
-template <bool kPair, bool kTf32, bool kNarrow, bool kRows = false>
-__global__ void __launch_bounds__(THREADS, 1)
+template <bool kPair, bool kTf32, bool kNarrow, int kRows = kNoRows>
+__global__ void __launch_bounds__(Mode<kPair, kRows>::kThreads, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                const __grid_constant__ CUtensorMap tmA1, const __grid_constant__ CUtensorMap tmB1,
                const __grid_constant__ CUtensorMap tmA2, const __grid_constant__ CUtensorMap tmB2,
                const __grid_constant__ CUtensorMap tmD, const __grid_constant__ CUtensorMap tmD2,
                const __grid_constant__ CUtensorMap tmE, const TcParams p) {
+  typedef Mode<kPair, kRows> M;
+  constexpr int EPI_WARPS = M::kEpiWarps, kProducerB = 2 + EPI_WARPS;
   constexpr int kFullB = kPair ? BN / 2 : BN, kFullStage = A_BYTES + kFullB * 128;
   const int STAGE_BYTES = kNarrow ? (int)p.stage_bytes : kFullStage;
-  const int STAGES = kNarrow ? p.stages : Mode<kPair>::kRingBytes / kFullStage;
+  const int STAGES = kNarrow ? p.stages : M::kRingBytes / kFullStage;
   const int b_rows = kNarrow ? p.b_rows : kFullB;
-  constexpr int RING_BYTES = Mode<kPair>::kRingBytes, EPI_BUFS = Mode<kPair>::kEpiBufs;
-  constexpr int TILE_M = Mode<kPair>::kTileM;
+  constexpr int RING_BYTES = M::kRingBytes, EPI_BUFS = M::kEpiBufs;
+  constexpr int TILE_M = M::kTileM;
   const int tile_n = kNarrow ? p.n_mma : BN;
   // pair mode: rank of this CTA in its pair; the even CTA (leader) owns the pipeline's full barriers and
   // issues the MMAs, its peer's tile loads signal the leader's barriers
@@ -343,11 +330,17 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
       uint32_t phase = 0;
       bool ok = true;
       for (int tile = first_tile; tile < p.num_tiles && ok; tile += tile_step) {
-        const int zc = tile / tiles_per_batch, r = tile % tiles_per_batch;
+        const bool in_panels = kRows == kExpRows;  // (one batch entry, one split)
+        const int zc = in_panels ? 0 : tile / tiles_per_batch, r = in_panels ? tile : tile % tiles_per_batch;
         const int b = zc % p.batch, split = zc / p.batch;
         // n fastest: a wave shares few A row-panels.  This CTA's rows of A and (pair) its half of B's columns
-        int mt = r / p.n_tiles, nt = r % p.n_tiles;
-        if (kRows && p.panel) panel_tile(p, r, mt, nt);
+        int mt, nt;
+        if (in_panels) {
+          panel_tile(p, r, mt, nt);
+        } else {
+          mt = r / p.n_tiles;
+          nt = r % p.n_tiles;
+        }
         const int m0 = mt * TILE_M + (int)rank * BM, n0 = nt * tile_n + (kPair ? (int)rank * b_rows : 0);
         const int kb_lo = split * p.kb_per_split, kb_hi = min(p.k_blocks, kb_lo + p.kb_per_split);
         for (int seg = 0; seg < p.segs && ok; ++seg) {
@@ -466,7 +459,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     }
   } else if (warp < kProducerB) {
     // ------------------------------------------------------------------ epilogue
-    const int quarter = warp & 3, half = (warp - 2) >> 2, ew = warp - 2;
+    const int quarter = warp & 3, half = (warp - 2) >> 2, ew = warp - 2;  // (EPI_EXP: half is one of four parts of 64 columns)
     const uint32_t buf0 = epi_base + ew * EPI_BUFS * EPI_BUF_BYTES;
     uint32_t e_phase = 0;    // bit i: parity of the next load into buffer i
     uint32_t e_pending = 0;  // lane 0, bit i: a load into buffer i is in flight
@@ -477,19 +470,34 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const bool has_e = p.epi == EPI_MUL || p.epi == EPI_STORE_LN || p.epi == EPI_ADD;
     const int cw = p.d_f32 ? 32 : 64;      // accumulator columns per staged chunk (128 bytes of output per row)
     // columns of this warp's half (the first has the odd 64)
-    const int half_cols = (tile_n + 127) / 128 * 64, my_cols = half ? tile_n - half_cols : half_cols;
-    const int nchunks = (my_cols + cw - 1) / cw;
+    const int half_cols = kRows == kExpRows ? 64 : (tile_n + 127) / 128 * 64;
+    const int my_cols = kRows == kExpRows ? min(64, tile_n - 64 * half) : half ? tile_n - half_cols : half_cols;
+    const int nchunks = my_cols > 0 ? (my_cols + cw - 1) / cw : 0;
     const uint32_t acce_target[2] = {kPair ? map_to_cta(acce_bar(0), 0) : acce_bar(0),
                                      kPair ? map_to_cta(acce_bar(1), 0) : acce_bar(1)};
     auto release_acc = [&](int a) {
       if (kPair) mbar_arrive_cluster(acce_target[a]);
       else mbar_arrive(acce_bar(a));
     };
+    float next_f = 0.0f;
+    int next_target = -1;
+    auto ask_row = [&](int row) {
+      next_f = row < p.M && p.row_f ? p.row_f[row] : 0.0f;
+      next_target = -1;
+      if (row < p.M && kRows == kExpRows)  // (int32, or the low half of int64 where the high one is 0)
+        next_target = p.target_bytes == 8 && p.target[2 * (int64_t)row + 1] != 0 ? -1 : p.target[(int64_t)(p.target_bytes / 4) * row];
+    };
     for (int tile = first_tile; tile < p.num_tiles; tile += tile_step) {
       // b indexes the outputs: with split-K it is split * batch + batch entry (partial sums [split][batch][M][N])
-      const int b = tile / tiles_per_batch, r = tile % tiles_per_batch;
-      int mt = r / p.n_tiles, nt = r % p.n_tiles;
-      if (kRows && p.panel) panel_tile(p, r, mt, nt);
+      const bool in_panels = kRows == kExpRows;
+      const int b = in_panels ? 0 : tile / tiles_per_batch, r = in_panels ? tile : tile % tiles_per_batch;
+      int mt, nt;
+      if (in_panels) {
+        panel_tile(p, r, mt, nt);
+      } else {
+        mt = r / p.n_tiles;
+        nt = r % p.n_tiles;
+      }
       const int m0 = mt * TILE_M + (int)rank * BM, n0 = nt * tile_n;  // this CTA's 128 rows
       const int row0 = m0 + quarter * 32, colw = n0 + half * half_cols;
       // chunk c of E goes through buffer c % EPI_BUFS, where the result replaces it
@@ -504,12 +512,17 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         load_e(0);
         if (EPI_BUFS > 1 && nchunks > 1) load_e(1);
       }
-      // (kRows) this lane's row
+      // (kRows) this lane's row.  What it has is asked for a tile ahead: an epilogue that is behind the products would wait for it.
       const bool row_in = kRows && row0 + lane < p.M;
-      const float row_f = row_in && p.row_f ? p.row_f[row0 + lane] : 0.0f;
-      int target = -1;
-      if (row_in && p.epi == EPI_EXP)  // (int32, or the low half of int64 where the high one is 0)
-        target = p.target_bytes == 8 && p.target[2 * (int64_t)(row0 + lane) + 1] != 0 ? -1 : p.target[(int64_t)(p.target_bytes / 4) * (row0 + lane)];
+      if (kRows && tile == first_tile) ask_row(row0 + lane);
+      const float row_f = next_f;
+      const int target = next_target;
+      if (kRows && tile + tile_step < p.num_tiles) {
+        int nm, nn;
+        if (in_panels) panel_tile(p, tile + tile_step, nm, nn);
+        else nm = (tile + tile_step) / p.n_tiles;  // (one batch entry)
+        ask_row(nm * TILE_M + (int)rank * BM + quarter * 32 + lane);
+      }
       float row_total = 0.0f, row_most = -INFINITY, row_z = 0.0f;
       if (!mbar_wait(accf_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit_ns)) break;
       tc_fence_after();
@@ -518,6 +531,39 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         tc_fence_before();
         __syncwarp();
         if (lane == 0) release_acc(acc);
+      } else if (kRows == kExpRows) {
+        const bool ignored = __any_sync(0xffffffffu, target < 0);
+        const uint32_t buf = buf0;
+#pragma unroll 1
+        for (int c = 0; c < 64; c += 32) {
+          float v[32];
+          tc_ld32(tsrc + c, v);
+          if (c) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) release_acc(acc);
+          }
+          if (!p.D) {
+            exp_chunk<false>(v, colw + c, p.N, target, row_f, row_z, row_total, row_most);
+            continue;
+          }
+          exp_chunk<true>(v, colw + c, p.N, target, row_f, row_z, row_total, row_most);
+          if (ignored) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = target >= 0 ? v[i] : 0.0f;  // (a row that is ignored may hold anything)
+          }
+          if (c == 0) {  // the tile before has left the buffer
+            if (lane == 0) tma_store_wait_read();
+            __syncwarp();
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) st_shared16(swz(buf, lane, c / 8 + u), pack8(v + 8 * u));
+        }
+        if (p.D) {
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) tma_store_3d(&tmD, buf, colw, row0, b);
+        }
       } else if (!staged) {
 #pragma unroll 1
         for (int c = 0; c < (my_cols + 31) / 32; ++c) {
@@ -543,18 +589,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             if (lane == 0) release_acc(acc);
           }
           const int col = colw + c * cw;
-          if (kRows && p.epi == EPI_EXP) {
-            if (!p.D) {
-              sum_chunk(v, col, p.N, target, row_z, row_total, row_most);
-              continue;
-            }
-            exp_chunk(v, col, p.N, target, row_f, row_total, row_most);
-            if (__any_sync(0xffffffffu, target < 0)) {
-#pragma unroll
-              for (int i = 0; i < 64; ++i) v[i] = target >= 0 ? v[i] : 0.0f;  // (a row that is ignored may hold anything)
-            }
-          }
-          if (kRows && p.epi == EPI_ROWS) {
+          if (kRows == kScaledRows) {
 #pragma unroll
             for (int i = 0; i < 64; ++i)
               if (i < cw) v[i] = row_f != 0.0f ? v[i] * row_f : 0.0f;
@@ -641,8 +676,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
         if (!ok) break;
       }
-      if (kRows && p.epi == EPI_EXP && row_in) {
-        p.row_parts[(int64_t)(nt * 2 + half) * p.M + row0 + lane] = make_float2(row_total, row_most);
+      if (kRows == kExpRows && row_in && my_cols > 0) {
+        p.row_parts[(int64_t)(nt * (tile_n / 64) + half) * p.M + row0 + lane] = make_float2(row_total, row_most);
         if (!p.D && target >= colw && target < min(colw + my_cols, p.N)) p.row_z[row0 + lane] = row_z;
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
@@ -868,8 +903,10 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
     bool ok = true;
     for (auto kernel : {gemm_tc_kernel<false, false, false>, gemm_tc_kernel<false, false, true>, gemm_tc_kernel<false, true, false>,
                         gemm_tc_kernel<false, true, true>, gemm_tc_kernel<true, false, false>, gemm_tc_kernel<true, false, true>,
-                        gemm_tc_kernel<false, false, false, true>, gemm_tc_kernel<false, false, true, true>,
-                        gemm_tc_kernel<true, false, false, true>, gemm_tc_kernel<true, false, true, true>})
+                        gemm_tc_kernel<false, false, false, kExpRows>, gemm_tc_kernel<false, false, true, kExpRows>,
+                        gemm_tc_kernel<true, false, false, kExpRows>, gemm_tc_kernel<true, false, true, kExpRows>,
+                        gemm_tc_kernel<false, false, false, kScaledRows>, gemm_tc_kernel<false, false, true, kScaledRows>,
+                        gemm_tc_kernel<true, false, false, kScaledRows>, gemm_tc_kernel<true, false, true, kScaledRows>})
       ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) == cudaSuccess;
     if (!ok) {
       cudaGetLastError();
@@ -890,7 +927,9 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   // stages sized by the B tile that a CTA loads (in blocks of 64 columns where it is MN-major): a narrow tile's ring is deeper, as the
   // bytes in flight, not the stage count, hide the load latency
   p.stage_bytes = A_BYTES + (b_mn ? (b_rows + 63) / 64 * 64 : b_rows) * 128;
-  const int ring = pair ? Mode<true>::kRingBytes : Mode<false>::kRingBytes;
+  // (EPI_EXP without D on single CTAs, few rows: it is the bytes under way that count, and nothing is staged)
+  const bool all_ring = g.epi == EPI_EXP && !g.D && !pair;
+  const int ring = all_ring ? kUsed<false, kExpRows> : pair || g.epi == EPI_EXP ? Mode<true, kNoRows>::kRingBytes : Mode<false, kNoRows>::kRingBytes;
   p.stages = ring / (int)p.stage_bytes < MAX_STAGES ? ring / (int)p.stage_bytes : MAX_STAGES;
   p.slots = gemm_tc_stats_slots(g.N);
   p.splits = splits; p.kb_per_split = kb_per_split;
@@ -905,21 +944,29 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   p.wait_limit_ns = g.wait_limit_ns ? g.wait_limit_ns : WAIT_LIMIT_NS;
   p.stall = g.test_stall;
   p.row_f = g.row_f; p.target = g.target; p.target_bytes = g.target_bytes; p.row_parts = g.row_parts; p.row_z = g.row_z; p.redo = g.redo;
-  if (g.slots_out) *g.slots_out = 2 * p.n_tiles;
+  if (g.slots_out) *g.slots_out = p.n_tiles * (n_mma / 64);
   p.panel = 0;
   if (g.epi == EPI_EXP) {  // rows of x of 32 MB, a quarter of L2
     const int64_t fits = (32 << 20) / ((int64_t)(pair ? 256 : BM) * g.K * 2);
     p.panel = (int)(fits < 1 ? 1 : fits < p.m_tiles ? fits : p.m_tiles);
+    p.by_panel = divider((uint32_t)p.panel);
+    p.by_last = divider((uint32_t)((p.m_tiles - 1) % p.panel + 1));
+    p.by_tiles = divider((uint32_t)(p.panel * p.n_tiles));
   }
-  const bool full = n_mma == BN;
+  const bool full = n_mma == BN && !all_ring;
   const int workers = pair ? sms / 2 : sms;
   auto kernel = pair ? (full ? gemm_tc_kernel<true, false, false> : gemm_tc_kernel<true, false, true>)
                      : (f32 ? (full ? gemm_tc_kernel<false, true, false> : gemm_tc_kernel<false, true, true>)
                             : (full ? gemm_tc_kernel<false, false, false> : gemm_tc_kernel<false, false, true>));
-  if (by_rows)
-    kernel = pair ? (full ? gemm_tc_kernel<true, false, false, true> : gemm_tc_kernel<true, false, true, true>)
-                  : (full ? gemm_tc_kernel<false, false, false, true> : gemm_tc_kernel<false, false, true, true>);
-  launch_chained(lc, kernel, dim3((pair ? 2 : 1) * (p.num_tiles < workers ? p.num_tiles : workers)), THREADS, SMEM_BYTES, pair ? 2 : 1, tmA, tmB,
+  auto of_rows = [&](auto kind) {
+    constexpr int k = decltype(kind)::value;
+    return pair ? (full ? gemm_tc_kernel<true, false, false, k> : gemm_tc_kernel<true, false, true, k>)
+                : (full ? gemm_tc_kernel<false, false, false, k> : gemm_tc_kernel<false, false, true, k>);
+  };
+  if (g.epi == EPI_EXP) kernel = of_rows(std::integral_constant<int, kExpRows>());
+  if (g.epi == EPI_ROWS) kernel = of_rows(std::integral_constant<int, kScaledRows>());
+  const int threads = g.epi == EPI_EXP ? Mode<true, kExpRows>::kThreads : Mode<true, kNoRows>::kThreads;
+  launch_chained(lc, kernel, dim3((pair ? 2 : 1) * (p.num_tiles < workers ? p.num_tiles : workers)), threads, SMEM_BYTES, pair ? 2 : 1, tmA, tmB,
                  tmA1, tmB1, tmA2, tmB2, tmD, tmD2, tmE, p);
   if (g.splits_out) *g.splits_out = splits;
   else if (splits > 1) reduce_splitk(lc, g.partial, (float*)g.D, splits, (int64_t)g.batch * g.M * g.N);

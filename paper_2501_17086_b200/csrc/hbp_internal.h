@@ -59,7 +59,7 @@ struct GemmArgs {
   // fp32 accumulation, the small terms first).
   const float *A_hi = nullptr, *A_lo = nullptr, *B_hi = nullptr, *B_lo = nullptr;
   int64_t hl_a_sm = 0, hl_a_sk = 0, hl_b_sn = 0, hl_b_sk = 0;
-  // EPI_EXP, EPI_ROWS: a number a row; the column of each row that is left out; per tile and half of its columns [slots][M] the row's (sum of
+  // EPI_EXP, EPI_ROWS: a number a row; the column of each row that is left out; per 64 columns [slots][M] the row's (sum of
   // what D receives, largest acc) without that column; where the number of those slots goes (host); a device word without which, 0, the launch does nothing
   const float* row_f = nullptr;
   const int* target = nullptr;  // numbers of target_bytes; negative or (8 bytes) 2^31 and more: none
