@@ -15,7 +15,7 @@
 // operand in 5.  E and s x are rounded to bf16, the operands' type: 2^-9 of each of their values at most, as a rounding of dz would be.  A row whose largest logit is more than
 // kFar above the target's (a loss of 40) would leave the range that bf16 and float sums of e have: finish_kernel then takes r = the largest logit,
 // and 2 and 3 run again; their launches return at once where no row asked for that.
-// The forward pass alone has no E: the product sums exp(z - its largest), takes z_t out on the way, and loss_kernel joins what its tiles have.
+// The forward pass alone has no E: the product sums exp(z - its largest) without z_t, and loss_kernel joins what its tiles have.
 //
 // float: products of operands in three bf16 parts (gemm_parts.cu); the logits of a piece of the rows lie in scratch, and
 // one pass over them forms dz, in parts.
@@ -72,6 +72,24 @@ struct RowData {
   bf16* xs;
 };
 
+// A row's logit of its target t >= 0, by a warp: a float dot product.  (The tensor core's sum is truncated, and would take ten times the error to a loss.)
+__device__ __forceinline__ float target_logit(const RowData& p, int64_t row, int t) {
+  const int lane = threadIdx.x & 31;
+  const bf16 *x = p.x + row * p.ldx, *w = p.w + (int64_t)t * p.ldw;
+  float z = 0.0f;
+#pragma unroll 4
+  for (int c = lane * 8; c < p.d; c += 256) {
+    float a[8], b[8];
+    tc::unpack8(*reinterpret_cast<const uint4*>(x + c), a);
+    tc::unpack8(*reinterpret_cast<const uint4*>(w + c), b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) z = fmaf(a[e], b[e], z);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+  return z;
+}
+
 __global__ void __launch_bounds__(256) target_kernel(const RowData p) {
   chain_next();
   chain_wait();
@@ -80,20 +98,7 @@ __global__ void __launch_bounds__(256) target_kernel(const RowData p) {
   const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= p.rows) return;
   const int t = p.targets.column(row, p.vocab, p.status);
-  float z = 0.0f;
-  if (t >= 0) {
-    const bf16 *x = p.x + row * p.ldx, *w = p.w + (int64_t)t * p.ldw;
-#pragma unroll 4
-    for (int c = lane * 8; c < p.d; c += 256) {
-      float a[8], b[8];
-      tc::unpack8(*reinterpret_cast<const uint4*>(x + c), a);
-      tc::unpack8(*reinterpret_cast<const uint4*>(w + c), b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z = fmaf(a[e], b[e], z);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-  }
+  const float z = t >= 0 ? target_logit(p, row, t) : 0.0f;
   if (lane == 0) {
     p.target[row] = t;
     p.zt[row] = z;
@@ -172,10 +177,17 @@ __global__ void __launch_bounds__(32 * kFinishWarps) finish_kernel(const RowData
 // The forward pass alone: sums of exp(z - largest) of the tiles, joined the same way.
 __global__ void __launch_bounds__(32 * kFinishWarps) loss_kernel(const RowData p) {
   __shared__ float2 joined[kFinishWarps][32];
+  __shared__ float logits[32];
   chain_next();
   chain_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t row = (int64_t)blockIdx.x * 32 + lane;
+  const int64_t row0 = (int64_t)blockIdx.x * 32, row = row0 + lane;
+#pragma unroll
+  for (int r = warp; r < 32; r += kFinishWarps) {
+    const int t = row0 + r < p.rows ? p.targets.column(row0 + r, p.vocab, p.status) : -1;
+    const float z = t >= 0 ? target_logit(p, row0 + r, t) : 0.0f;
+    if (lane == 0) logits[r] = z;
+  }
   float2 s = make_float2(0.0f, -INFINITY);
   // eight sums at a time: their exponentials wait for one maximum, not for each other
   auto join = [&](const float2 (&v)[8]) {
@@ -208,11 +220,10 @@ __global__ void __launch_bounds__(32 * kFinishWarps) loss_kernel(const RowData p
     for (int i = 0; i < 8; ++i) v[i] = joined[k + i][lane];
     join(v);
   }
-  const int t = p.targets.column(row, p.vocab, p.status);
   float loss = 0.0f;
-  if (t >= 0) {
-    const float above = s.y - p.zt[row];
-    if (p.zt[row] == INFINITY) loss = NAN;
+  if (p.targets.column(row, p.vocab, nullptr) >= 0) {
+    const float zt = logits[lane], above = s.y - zt;
+    if (zt == INFINITY) loss = NAN;
     else if (above <= kFar) loss = log1pf(s.x * expf(above));
     else loss = logf(s.x + expf(-above)) + above;
   }
@@ -506,7 +517,6 @@ bool run_bf16(Launcher& lc, const Call& c, const Plan& plan, int* status) {
     g.row_parts = p.parts; g.slots_out = &p.slots;
     if (!c.grads) {
       g.target = (const int*)p.targets.t; g.target_bytes = v.target_bytes;
-      g.row_z = p.zt;
       if (!gemm_tc(lc, g, status)) return false;
       launch_chained(lc, loss_kernel, dim3((unsigned)((n + 31) / 32)), 32 * kFinishWarps, 0, 1, p);
       continue;

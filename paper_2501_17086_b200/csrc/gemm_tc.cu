@@ -85,7 +85,6 @@ struct TcParams {
   const int* target;
   int target_bytes;
   float2* row_parts;
-  float* row_z;
   const int* redo;
   // EPI_EXP: row blocks that share a column block's copies; those of the last such panel; tiles of a panel
   int panel;
@@ -188,17 +187,14 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// EPI_EXP on 32 columns of a row, from `col` on.  Without the target's column, whose z is taken out, and those behind the last, v becomes exp(z - ref) and
+// EPI_EXP on 32 columns of a row, from `col` on.  Without the target's column and those behind the last, v becomes exp(z - ref) and
 // sum grows by that; most: the largest z.  kKeep: v is kept, ref is given; else sum is of exp(z - most) whatever ref is.
 template <bool kKeep>
-__device__ __forceinline__ void exp_chunk(float* v, int col, int N, int target, float ref, float& z, float& sum, float& most) {
+__device__ __forceinline__ void exp_chunk(float* v, int col, int N, int target, float ref, float& sum, float& most) {
   const uint32_t at = (uint32_t)(target - col);
   if (__any_sync(0xffffffffu, at < 32u)) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      z = at == (uint32_t)i ? v[i] : z;
-      v[i] = at == (uint32_t)i ? -INFINITY : v[i];
-    }
+    for (int i = 0; i < 32; ++i) v[i] = at == (uint32_t)i ? -INFINITY : v[i];
   }
   if (col + 32 > N) {
 #pragma unroll
@@ -523,7 +519,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         else nm = (tile + tile_step) / p.n_tiles;  // (one batch entry)
         ask_row(nm * TILE_M + (int)rank * BM + quarter * 32 + lane);
       }
-      float row_total = 0.0f, row_most = -INFINITY, row_z = 0.0f;
+      float row_total = 0.0f, row_most = -INFINITY;
       if (!mbar_wait(accf_bar(acc), acc_phase, abort_flag, p.status, p.wait_limit_ns)) break;
       tc_fence_after();
       const uint32_t tsrc = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN + half * half_cols);
@@ -544,10 +540,10 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             if (lane == 0) release_acc(acc);
           }
           if (!p.D) {
-            exp_chunk<false>(v, colw + c, p.N, target, row_f, row_z, row_total, row_most);
+            exp_chunk<false>(v, colw + c, p.N, target, row_f, row_total, row_most);
             continue;
           }
-          exp_chunk<true>(v, colw + c, p.N, target, row_f, row_z, row_total, row_most);
+          exp_chunk<true>(v, colw + c, p.N, target, row_f, row_total, row_most);
           if (ignored) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = target >= 0 ? v[i] : 0.0f;  // (a row that is ignored may hold anything)
@@ -676,10 +672,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         }
         if (!ok) break;
       }
-      if (kRows == kExpRows && row_in && my_cols > 0) {
+      if (kRows == kExpRows && row_in && my_cols > 0)
         p.row_parts[(int64_t)(nt * (tile_n / 64) + half) * p.M + row0 + lane] = make_float2(row_total, row_most);
-        if (!p.D && target >= colw && target < min(colw + my_cols, p.N)) p.row_z[row0 + lane] = row_z;
-      }
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
     if (lane == 0) {
@@ -813,7 +807,7 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   if (g.N % vec && g.epi != EPI_EXP) return false;
   if (by_rows && (f32 || g.batch != 1 || g.splitk > 1)) return false;
   if (g.epi == EPI_ROWS && !g.row_f) return false;
-  if (g.epi == EPI_EXP && (g.d_f32 || !g.target || !g.row_parts || (g.D ? !g.row_f : !g.row_z))) return false;
+  if (g.epi == EPI_EXP && (g.d_f32 || !g.target || !g.row_parts || (g.D && !g.row_f))) return false;
   if (!by_rows && g.epi != EPI_STORE && g.epi != EPI_GELU_FWD && g.epi != EPI_MUL && g.epi != EPI_RESID && g.epi != EPI_STORE_LN &&
       g.epi != EPI_ADD && g.epi != EPI_ACCUM)
     return false;
@@ -943,7 +937,7 @@ bool gemm_tc(Launcher& lc, const GemmArgs& g, int* status_word) {
   p.status = status_word;
   p.wait_limit_ns = g.wait_limit_ns ? g.wait_limit_ns : WAIT_LIMIT_NS;
   p.stall = g.test_stall;
-  p.row_f = g.row_f; p.target = g.target; p.target_bytes = g.target_bytes; p.row_parts = g.row_parts; p.row_z = g.row_z; p.redo = g.redo;
+  p.row_f = g.row_f; p.target = g.target; p.target_bytes = g.target_bytes; p.row_parts = g.row_parts; p.redo = g.redo;
   if (g.slots_out) *g.slots_out = p.n_tiles * (n_mma / 64);
   p.panel = 0;
   if (g.epi == EPI_EXP) {  // rows of x of 32 MB, a quarter of L2

@@ -22,8 +22,8 @@ enum Epilogue {
   EPI_STORE_LN = 6,  // D = acc, plus per-row partial sums (sum acc, sum acc * E[m,n]) per 64 columns -> stats
   EPI_ADD = 7,       // D = acc + E[m,n]   (u_t + delta_t: the scan then reads one tensor less)
   EPI_ACCUM = 8,     // D += acc, D float (bf16 operands on the tensor cores only: gemm_tc; gemm() does not take it)
-  // D = exp(acc - row_f[m]), 0 at n = target[m] and in rows without a target (bf16); row_parts.  Without D: row_parts, their sums those of
-  // exp(acc - largest), and row_z[m] = acc at the target.  (gemm_tc only)
+  // D = exp(acc - row_f[m]), 0 at n = target[m] and in rows without a target (bf16); row_parts.  Without D: row_parts alone, their sums those of
+  // exp(acc - largest).  (gemm_tc only)
   EPI_EXP = 9,
   EPI_ROWS = 10,       // D = acc * row_f[m], 0 where that is 0 (gemm_tc only)
   EPI_RNN_FWD = 5,   // c = tanh(acc + E[m,n]);  D2 = 1 - c^2;  D = gate[n] * E2[m,n] + c
@@ -65,7 +65,6 @@ struct GemmArgs {
   const int* target = nullptr;  // numbers of target_bytes; negative or (8 bytes) 2^31 and more: none
   int target_bytes = 4;
   float2* row_parts = nullptr;
-  float* row_z = nullptr;
   int* slots_out = nullptr;
   const int* redo = nullptr;
   bool wide = false;   // splitk > 1: tiles of full width
