@@ -489,8 +489,9 @@ typedef struct {
   int32_t* status; /* may be NULL; a bounded wait that runs out makes it HBP_ERR_TIMEOUT and leaves outputs incomplete */
 } hbp_vocabulary;
 
-/* loss[i] = log(sum_j exp(z_ij)) - z_i,target (float; 0 where there is no target, whatever x holds there).  A row that holds a value that is not
- * finite makes its own loss NaN (or infinite), one of w that of every row.
+/* loss[i] = log(sum_j exp(z_ij)) - z_i,target (float; 0 where there is no target, whatever x holds there), to its last digits however small it is: it is
+ * formed without the difference.  A row that has a target and holds a value that is not finite makes its own loss NaN (or infinite) and with it its dx and all of
+ * dw; one of w does so to every row.
  * With gradients of sum_i d_loss[i * d_loss_stride] * loss[i] (d_loss float on the device, NULL: ones): dx [rows][d] of dtype (0 where there is no target) and
  * dw [vocab][d] (OVERWRITTEN), float or, bf16 data, bf16 (dw_dtype); either may be NULL.  bf16: the probabilities' numerators and x times its row's
  * factor are rounded to bf16 as operands of products whose sums are float.  In one call, as two products less are formed than by a backward pass

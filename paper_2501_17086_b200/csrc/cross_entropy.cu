@@ -24,6 +24,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "float_parts.cuh"
 #include "tc_common.cuh"
@@ -107,28 +108,37 @@ __global__ void __launch_bounds__(256) target_kernel(const RowData p) {
 }
 
 constexpr int kFinishWarps = 16;
+// Rows a block: a quarter of a warp has a slot of all of them at a time.  (With 32 the 16 rows of a short call are one block's, 10 us instead of 4; 8192 rows take 29 us and 31.)
+constexpr int kFinishRows = 8, kSlotStep = kFinishWarps * 32 / kFinishRows;
 
-// 32 rows a block: the lanes' rows, the row sums of the tiles shared by the warps.
 __global__ void __launch_bounds__(32 * kFinishWarps) finish_kernel(const RowData p) {
-  __shared__ float sums[kFinishWarps][32], mosts[kFinishWarps][32], factors[32];
+  __shared__ float sums[kFinishWarps][kFinishRows], mosts[kFinishWarps][kFinishRows], factors[kFinishRows];
   chain_next();
   chain_wait();
   if (p.again && *(const volatile int*)p.redo == 0) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t row0 = (int64_t)blockIdx.x * 32, row = row0 + lane;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_block = lane % kFinishRows;
+  const int64_t row0 = (int64_t)blockIdx.x * kFinishRows, row = row0 + in_block;
   float sum = 0.0f, most = -INFINITY;
   if (row < p.rows) {
 #pragma unroll 8
-    for (int k = warp; k < p.slots; k += kFinishWarps) {
+    for (int k = threadIdx.x / kFinishRows; k < p.slots; k += kSlotStep) {
       const float2 v = p.parts[(int64_t)k * p.rows + row];
       sum += v.x;
       most = fmaxf(most, v.y);
     }
   }
-  sums[warp][lane] = sum;
-  mosts[warp][lane] = most;
+#pragma unroll
+  for (int o = kFinishRows; o < 32; o <<= 1) {
+    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+  }
+  if (lane < kFinishRows) {
+    sums[warp][lane] = sum;
+    mosts[warp][lane] = most;
+  }
   __syncthreads();
-  if (warp == 0) {
+  if (threadIdx.x < kFinishRows) {
+#pragma unroll
     for (int k = 1; k < kFinishWarps; ++k) {
       sum += sums[k][lane];
       most = fmaxf(most, mosts[k][lane]);
@@ -162,7 +172,7 @@ __global__ void __launch_bounds__(32 * kFinishWarps) finish_kernel(const RowData
   __syncthreads();
   const int per_row = p.d / 8;
   const int64_t left = p.rows - row0;
-  const int n = (int)(left < 32 ? left : 32) * per_row;
+  const int n = (int)(left < kFinishRows ? left : kFinishRows) * per_row;
 #pragma unroll 4
   for (int i = threadIdx.x; i < n; i += 32 * kFinishWarps) {
     const int r = i / per_row, c = (i - r * per_row) * 8;
@@ -176,50 +186,53 @@ __global__ void __launch_bounds__(32 * kFinishWarps) finish_kernel(const RowData
 
 // The forward pass alone: sums of exp(z - largest) of the tiles, joined the same way.
 __global__ void __launch_bounds__(32 * kFinishWarps) loss_kernel(const RowData p) {
-  __shared__ float2 joined[kFinishWarps][32];
-  __shared__ float logits[32];
+  __shared__ float2 joined[kFinishWarps][kFinishRows];
+  __shared__ float logits[kFinishRows];
   chain_next();
   chain_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t row0 = (int64_t)blockIdx.x * 32, row = row0 + lane;
-#pragma unroll
-  for (int r = warp; r < 32; r += kFinishWarps) {
-    const int t = row0 + r < p.rows ? p.targets.column(row0 + r, p.vocab, p.status) : -1;
-    const float z = t >= 0 ? target_logit(p, row0 + r, t) : 0.0f;
-    if (lane == 0) logits[r] = z;
+  const int64_t row0 = (int64_t)blockIdx.x * kFinishRows, row = row0 + lane % kFinishRows;
+  if (warp < kFinishRows) {
+    const int t = row0 + warp < p.rows ? p.targets.column(row0 + warp, p.vocab, p.status) : -1;
+    const float z = t >= 0 ? target_logit(p, row0 + warp, t) : 0.0f;
+    if (lane == 0) logits[warp] = z;
   }
   float2 s = make_float2(0.0f, -INFINITY);
-  // eight sums at a time: their exponentials wait for one maximum, not for each other
-  auto join = [&](const float2 (&v)[8]) {
+  // several sums at a time: their exponentials wait for one maximum, not for each other
+  auto join = [&](auto& v, auto count) {
+    constexpr int n = decltype(count)::value;
     float top = s.y;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i].y);
+    for (int i = 0; i < n; ++i) top = fmaxf(top, v[i].y);
     const float ref = top == -INFINITY ? 0.0f : top;
     s.x *= __expf(s.y - ref);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s.x = fmaf(v[i].x, __expf(v[i].y - ref), s.x);
+    for (int i = 0; i < n; ++i) s.x = fmaf(v[i].x, __expf(v[i].y - ref), s.x);
     s.y = top;
   };
   const float2 empty = make_float2(0.0f, -INFINITY);
-  float2 v[8];
-  for (int k = warp; k < p.slots; k += 8 * kFinishWarps) {
+  for (int k = threadIdx.x / kFinishRows; k < p.slots; k += 8 * kSlotStep) {
+    float2 v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int slot = k + i * kFinishWarps;
+      const int slot = k + i * kSlotStep;
       v[i] = row < p.rows && slot < p.slots ? p.parts[(int64_t)slot * p.rows + row] : empty;
     }
-    join(v);
+    join(v, std::integral_constant<int, 8>());
   }
-  joined[warp][lane] = s;
+#pragma unroll
+  for (int o = kFinishRows; o < 32; o <<= 1) {
+    const float2 v[1] = {make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o))};
+    join(v, std::integral_constant<int, 1>());
+  }
+  if (lane < kFinishRows) joined[warp][lane] = s;
   __syncthreads();
-  if (warp || row >= p.rows) return;
+  if (threadIdx.x >= kFinishRows || row >= p.rows) return;
   s = empty;
+  float2 v[kFinishWarps];
 #pragma unroll
-  for (int k = 0; k < kFinishWarps; k += 8) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = joined[k + i][lane];
-    join(v);
-  }
+  for (int k = 0; k < kFinishWarps; ++k) v[k] = joined[k][lane];
+  join(v, std::integral_constant<int, kFinishWarps>());
   float loss = 0.0f;
   if (p.targets.column(row, p.vocab, nullptr) >= 0) {
     const float zt = logits[lane], above = s.y - zt;
@@ -237,7 +250,7 @@ __global__ void __launch_bounds__(256) narrow_kernel(const float* in, int splits
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, n = rows * d;
   if (i >= n) return;
   float f[8] = {};
-#pragma unroll 4
+#pragma unroll 8
   for (int k = 0; k < splits; ++k) {
     const float4 a = __ldcs(reinterpret_cast<const float4*>(in + k * n + i)), b = __ldcs(reinterpret_cast<const float4*>(in + k * n + i + 4));
     f[0] += a.x; f[1] += a.y; f[2] += a.z; f[3] += a.w;
@@ -272,7 +285,7 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const float* in, int sp
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = rows * d;
   if (i >= n) return;
   float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
+#pragma unroll 8
   for (int k = 0; k < splits; ++k) {
     const float4 v = __ldcs(reinterpret_cast<const float4*>(in + k * n + i));
     s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -295,7 +308,8 @@ struct LogitsData {
 
 constexpr int kRowThreads = 512;
 
-// A block a row, which it reads once for the sum (twice where the target is far from the largest logit), and once more for dz.
+// A block a row, which it reads once for the sum (twice where the target is far from the largest logit), and once more for dz.  Instructions bound it, expf half of
+// them; a row's exponentials held in registers in between took as long (1901 rows of 8111: 44 us, 49; 94 where a thread holds 64).
 __global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p) {
   __shared__ float sums[kRowThreads / 32], mosts[kRowThreads / 32];
   chain_next();
@@ -380,8 +394,8 @@ int dx_splits(int64_t rows, int vocab, int d) {
 }
 
 // The same for float: 12 instructions a block of 32, of n_tile / 2 clocks each and 40 at least, tiles of 256 x 32 to 192 (gemm_parts.cu), and what is
-// read for a tile, of which the pairs get 50 bytes a clock: 1901 rows of 520 channels, whose 72 tiles of 64 columns read the probabilities nine times over, 177 us,
-// split in three XXX.
+// read for a tile, of which the pairs get 50 bytes a clock: for 1901 rows of 520 channels 72 tiles of 64 columns read the probabilities nine times over and took 1.5
+// times as long as the product of the logits, of as many operations; split in three they take as long.
 int dx_splits_f32(int64_t rows, int vocab, int d) {
   const int64_t m_tiles = (rows + 255) / 256, blocks = (vocab + 31) / 32;
   int best = 1;
@@ -508,6 +522,7 @@ bool run_bf16(Launcher& lc, const Call& c, const Plan& plan, int* status) {
       p.ldE = plan.ldE;
       if (c.dw) p.xs = (bf16*)(s + plan.xs);
     }
+    const dim3 blocks((unsigned)((n + kFinishRows - 1) / kFinishRows));
     GemmArgs g;
     g.M = (int)n; g.N = v.vocab; g.K = v.d;
     g.in_dtype = HBP_BF16;
@@ -518,7 +533,7 @@ bool run_bf16(Launcher& lc, const Call& c, const Plan& plan, int* status) {
     if (!c.grads) {
       g.target = (const int*)p.targets.t; g.target_bytes = v.target_bytes;
       if (!gemm_tc(lc, g, status)) return false;
-      launch_chained(lc, loss_kernel, dim3((unsigned)((n + 31) / 32)), 32 * kFinishWarps, 0, 1, p);
+      launch_chained(lc, loss_kernel, blocks, 32 * kFinishWarps, 0, 1, p);
       continue;
     }
     launch_chained(lc, target_kernel, dim3((unsigned)((n + 7) / 8)), 256, 0, 1, p);
@@ -528,7 +543,7 @@ bool run_bf16(Launcher& lc, const Call& c, const Plan& plan, int* status) {
       p.again = again != 0;
       g.redo = again ? p.redo : nullptr;
       if (!gemm_tc(lc, g, status)) return false;
-      launch_chained(lc, finish_kernel, dim3((unsigned)((n + 31) / 32)), 32 * kFinishWarps, 0, 1, p);
+      launch_chained(lc, finish_kernel, blocks, 32 * kFinishWarps, 0, 1, p);
     }
     if (c.dx) {
       GemmArgs b;
