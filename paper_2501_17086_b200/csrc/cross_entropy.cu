@@ -12,7 +12,7 @@
 //   3. finish_kernel   S', loss, the row's factor s = g / S; E at the target becomes -S'; s x, rounded to bf16
 //   4. gemm_tc, EPI_ROWS: dx = s (E w)          5. gemm_tc: dw = E^T (s x)
 // s is a number a row, which is why E needs no second pass: it comes out of the sum over the vocabulary in 4, and goes into the other
-// operand in 5.  E and s x are rounded to bf16, the operands' type: 2^-9 of each of their values at most, as a rounding of dz would be.  A row whose largest logit is more than
+// operand in 5.  E and s x are rounded to bf16, the operands' type: 2^-8 of each of their values at most, as a rounding of dz would be.  A row whose largest logit is more than
 // kFar above the target's (a loss of 40) would leave the range that bf16 and float sums of e have: finish_kernel then takes r = the largest logit,
 // and 2 and 3 run again; their launches return at once where no row asked for that.
 // The forward pass alone has no E: the product sums exp(z - its largest) without z_t, and loss_kernel joins what its tiles have.
@@ -680,11 +680,12 @@ hbp_status call(Call& c, void* scratch, size_t bytes, void* stream) {
   int64_t n = wanted_piece(v.dtype, v.rows, v.vocab, c.grads);
   auto plan_of = [&](int64_t piece) { return Plan(v.dtype, v.rows, v.vocab, v.d, c.grads, c.dw_bf16(), piece); };
   if (!scratch || ((uintptr_t)scratch & 255u)) return HBP_ERR_WORKSPACE;
-  while (plan_of(n).bytes > bytes) {  // smaller pieces for less memory
+  Plan plan = plan_of(n);
+  while (plan.bytes > bytes) {  // smaller pieces for less memory
     if (n <= kLeastPiece) return HBP_ERR_WORKSPACE;
     n = (n / 2 + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
+    plan = plan_of(n);
   }
-  const Plan plan = plan_of(n);
   c.scratch = (uint8_t*)scratch;
   int* status = v.status ? v.status : (int*)(c.scratch + plan.words) + 1;
   const bool ok = v.dtype == HBP_BF16 ? run_bf16(lc, c, plan, status) : run_f32(lc, c, plan, status);

@@ -1,5 +1,8 @@
 """The operators at a decoder's ends and between its blocks used together, captured, on several streams, and at sizes beyond 32 bits."""
 import math
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -132,6 +135,30 @@ def test_captured_and_replayed(B, dtype):
         want = again()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), seed
+
+
+FIRST = """
+import sys
+sys.path[:0] = sys.argv[1:3]
+import torch
+from paper_2501_17086_b200 import binding as B
+from test_gpu_decoder_ends import all_calls
+for dtype in (torch.float32, torch.bfloat16):
+    t, call = all_calls(B, dtype)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    graph.replay()
+    want = call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want)), dtype
+"""
+
+
+def test_a_process_whose_first_calls_are_captured():
+    here = os.path.dirname(os.path.abspath(__file__))
+    subprocess.run([sys.executable, "-c", FIRST, os.path.dirname(here), here], check=True, timeout=300)
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
