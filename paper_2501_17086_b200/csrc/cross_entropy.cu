@@ -18,7 +18,7 @@
 // The forward pass alone has no E: the product sums exp(z - its largest) without z_t, and loss_kernel joins what its tiles have.
 //
 // float: products of operands in three bf16 parts (gemm_parts.cu); the logits of a piece of the rows lie in scratch, and
-// one pass over them forms dz, in parts.
+// one pass over them forms dz, in parts.  Few rows take w as it is, in float: what bounds them is its bytes, and in parts it is 16 a value to write and read instead of 4.
 //
 // E has a piece of the rows at a time where it would be more than kPieceBytes, or than the scratch that the caller has.
 #include <math.h>
@@ -26,6 +26,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "float_pairs.cuh"
 #include "float_parts.cuh"
 #include "tc_common.cuh"
 
@@ -294,6 +295,23 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const float* in, int sp
   *reinterpret_cast<float4*>(out + row * ld + (i - row * d)) = s;
 }
 
+__device__ __forceinline__ int cluster_blocks() {
+  uint32_t n;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return (int)n;
+}
+__device__ __forceinline__ int cluster_block() {
+  uint32_t n;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(n));
+  return (int)n;
+}
+__device__ __forceinline__ float2 cluster_load(const float2* p, int block) {
+  const uint32_t at = tc::map_to_cta((uint32_t)__cvta_generic_to_shared(p), block);
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+  return v;
+}
+
 struct LogitsData {
   const float* z;  // [rows][ldz], ldz a multiple of 4
   int64_t ldz;
@@ -303,26 +321,33 @@ struct LogitsData {
   const float* d_loss;
   int64_t d_loss_stride;
   float* loss;
-  Planes dz;  // not of the forward pass alone
+  Planes dz;         // not of the forward pass alone: in parts,
+  float* dz_f;       // or as floats in the logits' place
 };
 
 constexpr int kRowThreads = 512;
 
-// A block a row, which it reads once for the sum (twice where the target is far from the largest logit), and once more for dz.  Instructions bound it, expf half of
-// them; a row's exponentials held in registers in between took as long (1901 rows of 8111: 44 us, 49; 94 where a thread holds 64).
+// A block a row, or a cluster of up to eight where there are few rows; each reads its columns once for the sum (twice where the target is far from the largest logit),
+// and once more for dz.  Instructions bound it, expf half of them; a row's exponentials held in registers in between took as long (1901 rows of 8111: 44 us, 49; 94
+// where a thread holds 64).
 __global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p) {
   __shared__ float sums[kRowThreads / 32], mosts[kRowThreads / 32];
+  __shared__ float2 blocks[2];
   chain_next();
   chain_wait();
-  const int64_t row = blockIdx.x;
+  const int shares = cluster_blocks(), share = cluster_block();
+  const int64_t row = blockIdx.x / shares;
   const float* z = p.z + row * p.ldz;
-  const int t = p.targets.column(row, p.vocab, threadIdx.x == 0 ? p.status : nullptr), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const bool first = threadIdx.x == 0 && share == 0;
+  const int t = p.targets.column(row, p.vocab, first ? p.status : nullptr), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t from = ((int64_t)share * kRowThreads + threadIdx.x) * 4, step = (int64_t)shares * kRowThreads * 4;
   const float zt = t >= 0 ? z[t] : 0.0f;
   float ref = isfinite(zt) ? zt : 0.0f, sum = 0.0f, most = -INFINITY;
   if (t >= 0) {
     for (int again = 0; again < 2; ++again) {
       sum = 0.0f;
-      for (int c = threadIdx.x * 4; c < p.vocab; c += kRowThreads * 4) {
+#pragma unroll 4
+      for (int64_t c = from; c < p.vocab; c += step) {
         const float4 q = *reinterpret_cast<const float4*>(z + c);
         const float v[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -348,17 +373,27 @@ __global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p)
         sum += sums[k];
         most = fmaxf(most, mosts[k]);
       }
+      if (shares > 1) {  // (a place a turn: nobody waits for the others to have read)
+        if (threadIdx.x == 0) blocks[again] = make_float2(sum, most);
+        tc::cluster_sync();
+        sum = 0.0f;
+        for (int k = 0; k < shares; ++k) {
+          const float2 q = cluster_load(&blocks[again], k);
+          sum += q.x;
+          most = fmaxf(most, q.y);
+        }
+      }
       if (!(most - ref > kFar)) break;
       ref = most;
     }
+    if (shares > 1) tc::cluster_sync();  // (the others read this block's; and the target's logit may be written over)
   }
   const bool at_target = zt == ref;
   const float total = sum + (at_target ? 1.0f : expf(zt - ref));
-  if (threadIdx.x == 0) p.loss[row] = t < 0 ? 0.0f : at_target ? log1pf(sum) : logf(total) - (zt - ref);
-  if (!p.dz.p) return;
+  if (first) p.loss[row] = t < 0 ? 0.0f : at_target ? log1pf(sum) : logf(total) - (zt - ref);
+  if (!p.dz.p && !p.dz_f) return;
   const float factor = t < 0 ? 0.0f : (p.d_loss ? p.d_loss[row * p.d_loss_stride] : 1.0f) / total;
-  bf16* out = p.dz.p + row * p.dz.ld;
-  for (int c = threadIdx.x * 4; c < p.columns; c += kRowThreads * 4) {
+  for (int64_t c = from; c < p.columns; c += step) {
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (factor != 0.0f && c < p.vocab) {
       const float4 q = *reinterpret_cast<const float4*>(z + c);
@@ -366,8 +401,259 @@ __global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p)
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = c + e >= p.vocab ? 0.0f : factor * (c + e == t ? -sum : expf(v[e] - ref));
     }
-    store_parts4(out + c, p.dz.plane, make_float4(v[0], v[1], v[2], v[3]));
+    const float4 dz = make_float4(v[0], v[1], v[2], v[3]);
+    if (p.dz_f) *reinterpret_cast<float4*>(p.dz_f + row * p.ldz + c) = dz;
+    else store_parts4(p.dz.p + row * p.dz.ld + c, p.dz.plane, dz);
   }
+}
+
+// How many blocks a row, so that few rows fill the GPU: two an SM, of one turn of its threads at least.
+int logit_shares(int64_t rows, int vocab) {
+  int n = 1;
+  while (n < 8 && rows * 2 * n <= 4 * kPairs && (int64_t)2 * n * kRowThreads * 4 <= vocab) n *= 2;
+  return n;
+}
+
+// ------------------------------------------------------------------------------------------- float, few rows
+constexpr int kFewAtOnce = 16, kFewTile = 64;  // rows of x, rows of w
+constexpr int kFewSteps = 32, kFewPitch = kFewSteps + 4, kFewStages = 3, kFewThreads = 256;
+
+__device__ __forceinline__ void copy_or_zero(float* to, const float* from, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_made() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+struct alignas(16) Pairs2 {
+  f32x2 a, b;
+};
+
+// z [rows][ldz]: 16 x 64 of it a block of two warps, 4 x 4 a thread, the sums of even and odd channels and of each 32 apart (8 + d / 64 units of 2^-23 at most); 32 channels at a time by asynchronous copies, two steps
+// ahead.  Rows of shared memory are 36 floats apart: the eight rows of w that a warp reads at once lie in different banks.  (16 rows of 131072 x 2048: 259 us with
+// all of the loss, of 163 for w's bytes; w straight into registers, a row a warp, 696.)
+__global__ void __launch_bounds__(64) few_logits_kernel(const float* x, int64_t ldx, int rows, const float* w, int64_t ldw, int vocab, int d, float* z, int64_t ldz) {
+  constexpr int kRows = kFewTile + kFewAtOnce;
+  __shared__ __align__(16) float shared[kFewStages][kRows * kFewPitch];
+  chain_next();
+  chain_wait();
+  const int tid = threadIdx.x, i0 = blockIdx.y * kFewAtOnce, piece = tid % 8 * 4;
+  const int64_t j0 = (int64_t)blockIdx.x * kFewTile;
+  const int steps = (d + kFewSteps - 1) / kFewSteps;
+  const float* from[kRows / 8];
+  uint32_t there = 0;
+#pragma unroll
+  for (int q = 0; q < kRows / 8; ++q) {
+    const int row = q * 8 + tid / 8;
+    const bool of_w = q < kFewTile / 8, in = of_w ? j0 + row < vocab : i0 + row - kFewTile < rows;
+    from[q] = !in ? w : of_w ? w + (j0 + row) * ldw : x + (int64_t)(i0 + row - kFewTile) * ldx;
+    there |= (uint32_t)in << q;
+  }
+  auto copy = [&](int step) {
+    float* to = shared[step % kFewStages] + tid / 8 * kFewPitch + piece;
+    const int k = step * kFewSteps + piece;
+#pragma unroll
+    for (int q = 0; q < kRows / 8; ++q) copy_or_zero(to + q * 8 * kFewPitch, from[q] + (k < d ? k : 0), (there >> q & 1) && k < d);
+  };
+#pragma unroll
+  for (int i = 0; i < kFewStages - 1; ++i) {
+    if (i < steps) copy(i);
+    copies_made();
+  }
+  const int column = tid % 8 + tid / 32 * 32, row = tid / 8 % 4;
+  f32x2 all[4][4];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) all[i / 4][i % 4] = both(0.0f);
+  for (int step = 0; step < steps; ++step) {
+    copies_wait<kFewStages - 2>();
+    __syncthreads();
+    if (step + kFewStages - 1 < steps) copy(step + kFewStages - 1);
+    copies_made();
+    const float* at = shared[step % kFewStages];
+    f32x2 v[4][4];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i / 4][i % 4] = both(0.0f);
+#pragma unroll
+    for (int k = 0; k < kFewSteps; k += 4) {
+      Pairs2 a[4], b[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        a[e] = *reinterpret_cast<const Pairs2*>(at + (column + e * 8) * kFewPitch + k);
+        b[e] = *reinterpret_cast<const Pairs2*>(at + (kFewTile + row + e * 4) * kFewPitch + k);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = fma2(b[i].b, a[j].b, fma2(b[i].a, a[j].a, v[i][j]));
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) all[i / 4][i % 4] = add2(all[i / 4][i % 4], v[i / 4][i % 4]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = floats_of(all[i][j]);
+      if (i0 + row + i * 4 < rows && j0 + column + j * 8 < vocab) z[(int64_t)(i0 + row + i * 4) * ldz + j0 + column + j * 8] = f.x + f.y;
+    }
+}
+
+// The two gradients' blocks: `width` threads of four channels each, the rows of w among the 256 / width groups of them; as many blocks as there are to be of columns and
+// stretches of the vocabulary.
+struct FewSplit {
+  int width, columns, per, splits;
+  FewSplit(int vocab, int d, int blocks) {
+    const int vectors = d / 4;
+    for (width = 4; width < 64 && width < vectors;) width *= 2;
+    columns = (vectors + width - 1) / width;
+    const int wanted = std::max(1, blocks / columns);
+    per = (int)((((int64_t)vocab + wanted - 1) / wanted + kFewTile - 1) / kFewTile) * kFewTile;
+    splits = (vocab + per - 1) / per;
+  }
+};
+
+// dz of 64 columns and 16 rows: [column][row], each twice, as the factor of a pair of channels.  Asked for a tile ahead.
+struct FewTiles {
+  static constexpr int kEach = kFewTile * kFewAtOnce / kFewThreads;
+  float next[kEach];
+  __device__ __forceinline__ void ask(const float* dz, int64_t ldz, int rows, int64_t j0, int end) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int i = e * (kFewThreads / kFewTile) + threadIdx.x / kFewTile;
+      const int64_t j = j0 + threadIdx.x % kFewTile;
+      next[e] = i < rows && j < end ? dz[i * ldz + j] : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void put(f32x2 (&tile)[kFewTile][kFewAtOnce + 2]) const {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) tile[threadIdx.x % kFewTile][e * (kFewThreads / kFewTile) + threadIdx.x / kFewTile] = both(next[e]);
+  }
+};
+
+// partial [splits][rows][d] of dx = dz w: a thread has four channels of 16 rows, all there are; the groups' sums are joined in shared memory.  (16 rows of
+// 131072 x 2048: 385 us, of 163 for w's bytes; 16 rows of 32003 x 1024 75, of 20.  Sums of whole blocks, without the groups, were 4 times the bytes to join.)
+__global__ void __launch_bounds__(kFewThreads, 2) few_dx_kernel(const float* dz, int64_t ldz, int rows, const float* w, int64_t ldw, int vocab, int d, int width, int per, float* partial) {
+  __shared__ __align__(16) f32x2 tile[kFewTile][kFewAtOnce + 2];
+  __shared__ float4 groups_sums[4][kFewThreads];
+  chain_next();
+  chain_wait();
+  const int groups = kFewThreads / width, group = threadIdx.x / width, at = threadIdx.x % width, c0 = blockIdx.x * width * 4, c = c0 + at * 4;
+  const int64_t lo = (int64_t)blockIdx.y * per;
+  const int end = (int)(lo + per < vocab ? lo + per : vocab);
+  f32x2 acc[kFewAtOnce][2];
+#pragma unroll
+  for (int i = 0; i < kFewAtOnce; ++i) acc[i][0] = acc[i][1] = both(0.0f);
+  FewTiles tiles;
+  tiles.ask(dz, ldz, rows, lo, end);
+  for (int64_t j0 = lo; j0 < end; j0 += kFewTile) {
+    __syncthreads();
+    tiles.put(tile);
+    __syncthreads();
+    if (j0 + kFewTile < end) tiles.ask(dz, ldz, rows, j0 + kFewTile, end);
+    if (c >= d) continue;
+    const int n = (int)(end - j0 < kFewTile ? end - j0 : kFewTile);
+    const float* from = w + j0 * ldw + c;
+#pragma unroll 8
+    for (int j = group; j < n; j += groups) {
+      const float4 f = __ldcs(reinterpret_cast<const float4*>(from + (int64_t)j * ldw));
+      const f32x2 b[2] = {pair_of(f.x, f.y), pair_of(f.z, f.w)};
+#pragma unroll
+      for (int i = 0; i < kFewAtOnce; i += 2) {
+        const Pairs2 g = *reinterpret_cast<const Pairs2*>(&tile[j][i]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          acc[i][h] = fma2(g.a, b[h], acc[i][h]);
+          acc[i + 1][h] = fma2(g.b, b[h], acc[i + 1][h]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < kFewAtOnce; q += 4) {
+    if (q) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 a = floats_of(acc[q + i][0]), b = floats_of(acc[q + i][1]);
+      groups_sums[i][threadIdx.x] = make_float4(a.x, a.y, b.x, b.y);
+    }
+    __syncthreads();
+    const int i = threadIdx.x / width;  // (its row of the four)
+    if (i < 4 && q + i < rows && c < d) {
+      float4 s = groups_sums[i][at];
+      for (int k = 1; k < groups; ++k) {
+        const float4 v = groups_sums[i][k * width + at];
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+      *reinterpret_cast<float4*>(partial + ((int64_t)blockIdx.y * rows + q + i) * d + c) = s;
+    }
+  }
+}
+
+// dw = dz^T x: a thread has four channels of the rows of x and writes those of one row of dw after the other (16 rows of 131072 x 2048: 297 us, of 163; as a product
+// in parts 245, and dz and x to write in parts.  32 rows, the second 16 added to what the first wrote: 941, which is why 16 are the most).
+__global__ void __launch_bounds__(kFewThreads, 2) few_dw_kernel(const float* dz, int64_t ldz, int rows, const float* x, int64_t ldx, Targets targets, int vocab, int d, int width, int per,
+                                                                 float* dw, int64_t lddw) {
+  __shared__ __align__(16) f32x2 tile[kFewTile][kFewAtOnce + 2];
+  chain_next();
+  chain_wait();
+  const int groups = kFewThreads / width, group = threadIdx.x / width, c = (blockIdx.x * width + threadIdx.x % width) * 4;
+  const int64_t lo = (int64_t)blockIdx.y * per;
+  const int end = (int)(lo + per < vocab ? lo + per : vocab);
+  f32x2 v[kFewAtOnce][2];
+#pragma unroll
+  for (int i = 0; i < kFewAtOnce; ++i) {
+    float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    // (a row that is ignored may hold anything)
+    if (i < rows && c < d && targets.column(i, vocab, nullptr) >= 0) f = *reinterpret_cast<const float4*>(x + i * ldx + c);
+    v[i][0] = pair_of(f.x, f.y);
+    v[i][1] = pair_of(f.z, f.w);
+  }
+  FewTiles tiles;
+  tiles.ask(dz, ldz, rows, lo, end);
+  for (int64_t j0 = lo; j0 < end; j0 += kFewTile) {
+    __syncthreads();
+    tiles.put(tile);
+    __syncthreads();
+    if (j0 + kFewTile < end) tiles.ask(dz, ldz, rows, j0 + kFewTile, end);
+    if (c >= d) continue;
+    const int n = (int)(end - j0 < kFewTile ? end - j0 : kFewTile);
+    for (int j = group; j < n; j += groups) {
+      f32x2 s[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+      for (int i = 0; i < kFewAtOnce; i += 2) {
+        const Pairs2 g = *reinterpret_cast<const Pairs2*>(&tile[j][i]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) s[h] = fma2(g.b, v[i + 1][h], fma2(g.a, v[i][h], s[h]));
+      }
+      const float2 a = floats_of(s[0]), b = floats_of(s[1]);
+      __stcs(reinterpret_cast<float4*>(dw + (j0 + j) * lddw + c), make_float4(a.x, a.y, b.x, b.y));
+    }
+  }
+}
+
+// out (rows ld apart) = the sum of many splits of few elements: 32 x 4 channels a block, its eight warps an eighth of the splits each
+__global__ void __launch_bounds__(256) sum_many_kernel(const float* in, int splits, float* out, int64_t ld, int rows, int d) {
+  __shared__ float4 part[8][32];
+  chain_next();
+  chain_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (splits + 7) / 8, end = min(splits, (warp + 1) * per);
+  const int64_t n = (int64_t)rows * d, i = ((int64_t)blockIdx.x * 32 + lane) * 4;
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (i < n)
+#pragma unroll 8
+    for (int k = warp * per; k < end; ++k) {
+      const float4 v = __ldcs(reinterpret_cast<const float4*>(in + k * n + i));
+      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+    }
+  part[warp][lane] = s;
+  __syncthreads();
+  if (warp || i >= n) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) {
+    const float4 v = part[k][lane];
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  const int64_t row = i / d;
+  *reinterpret_cast<float4*>(out + row * ld + (i - row * d)) = s;
 }
 
 // ------------------------------------------------------------------------------------------- host
@@ -417,9 +703,15 @@ int dx_splits_f32(int64_t rows, int vocab, int d) {
   return best;
 }
 
+// float, up to so many rows: products of w as it is.  Before and now, 16 rows of 32003 x 1024: the loss 157 and 59 us, gradients 293 and 150; of 131072 x 2048 960 and
+// 259, 1909 and 881; of 5003 x 512 37 and 27, 72 and 73.  32 rows take w twice, by way of L2: the loss 138 and 76, 930 and 485 us; gradients would be 260 and 290.
+bool few_rows(int64_t rows, bool grads) { return rows <= (grads ? 1 : 2) * kFewAtOnce; }
+constexpr int kFewBlocks = 4 * kPairs;  // of the gradients: two an SM
+
 // The scratch of pieces of `piece` rows.
 struct Plan {
   int64_t piece;
+  bool few = false;
   int splits = 1;   // of dx's contraction; float: in chunks of so many columns
   int chunk = 0;
   int64_t ldE = 0;  // bf16: of E; float: of the logits
@@ -450,6 +742,12 @@ struct Plan {
       return;
     }
     ldE = ((int64_t)vocab + 3) / 4 * 4;
+    few = few_rows(rows, grads);
+    if (few) {  // (its one piece)
+      E = take((size_t)n * ldE * 4);
+      if (grads) partial = take((size_t)FewSplit(vocab, d, kFewBlocks).splits * n * d * 4);
+      return;
+    }
     if (grads) splits = dx_splits_f32(n, vocab, d);
     chunk = splits > 1 ? ((vocab + splits - 1) / splits + 63) / 64 * 64 : vocab;
     x.ld = w.ld = plane_ld(d);
@@ -590,6 +888,36 @@ bool run_bf16(Launcher& lc, const Call& c, const Plan& plan, int* status) {
   return true;
 }
 
+void run_few(Launcher& lc, const Call& c, const Plan& plan) {
+  const hbp_vocabulary& v = *c.v;
+  const int n = (int)v.rows;
+  const Targets targets = {v.targets, v.target_bytes};
+  float* z = (float*)(c.scratch + plan.E);
+  const int64_t ldz = plan.ldE;
+  launch_chained(lc, few_logits_kernel, dim3((unsigned)((v.vocab + kFewTile - 1) / kFewTile), (unsigned)((n + kFewAtOnce - 1) / kFewAtOnce)), 64, 0, 1,
+                 (const float*)v.x, v.ldx, n, (const float*)v.w, v.ldw, v.vocab, v.d, z, ldz);
+  LogitsData p = {};
+  p.z = z; p.ldz = ldz;
+  p.vocab = p.columns = v.vocab;
+  p.targets = targets;
+  p.status = v.status;
+  p.d_loss = c.d_loss;
+  p.d_loss_stride = c.d_loss_stride;
+  p.loss = c.loss;
+  if (c.grads) p.dz_f = z;
+  const int shares = logit_shares(n, v.vocab);
+  launch_chained(lc, logits_kernel, dim3((unsigned)(n * shares)), kRowThreads, 0, shares, p);
+  const FewSplit f(v.vocab, v.d, kFewBlocks);
+  if (c.dx) {
+    float* partial = (float*)(c.scratch + plan.partial);
+    launch_chained(lc, few_dx_kernel, dim3(f.columns, f.splits), kFewThreads, 0, 1, (const float*)z, ldz, n, (const float*)v.w, v.ldw, v.vocab, v.d, f.width, f.per, partial);
+    launch_chained(lc, sum_many_kernel, dim3((unsigned)(((int64_t)n * v.d / 4 + 31) / 32)), 256, 0, 1, (const float*)partial, f.splits, (float*)c.dx, c.lddx, n, v.d);
+  }
+  if (c.dw)
+    launch_chained(lc, few_dw_kernel, dim3(f.columns, f.splits), kFewThreads, 0, 1, (const float*)z, ldz, n, (const float*)v.x, v.ldx, targets, v.vocab, v.d, f.width, f.per,
+                   (float*)c.dw, c.lddw);
+}
+
 bool run_f32(Launcher& lc, const Call& c, const Plan& plan, int* status) {
   const hbp_vocabulary& v = *c.v;
   uint8_t* s = c.scratch;
@@ -599,6 +927,10 @@ bool run_f32(Launcher& lc, const Call& c, const Plan& plan, int* status) {
   auto split = [&](const float* src, int64_t ld, const Planes& P, int64_t rows, int64_t all, const Targets& targets) {
     launch_chained(lc, split_rows_kernel, dim3((unsigned)((all * (v.d / 4) + 255) / 256)), 256, 0, 1, src, ld, P, rows, all, v.d, targets, v.vocab);
   };
+  if (plan.few) {
+    run_few(lc, c, plan);
+    return true;
+  }
   const int64_t columns = (int64_t)plan.splits * plan.chunk;
   split((const float*)v.w, v.ldw, w, v.vocab, columns, Targets{nullptr, 8});
   for (int64_t lo = 0; lo < v.rows; lo += plan.piece) {
@@ -622,7 +954,8 @@ bool run_f32(Launcher& lc, const Call& c, const Plan& plan, int* status) {
       e.p = (bf16*)(s + plan.ep);
       p.dz = e;
     }
-    launch_chained(lc, logits_kernel, dim3((unsigned)n), kRowThreads, 0, 1, p);
+    const int shares = logit_shares(n, v.vocab);
+    launch_chained(lc, logits_kernel, dim3((unsigned)(n * shares)), kRowThreads, 0, shares, p);
     if (c.dx) {
       PartsGemm b;
       b.M = (int)n; b.N = v.d; b.K = plan.chunk;

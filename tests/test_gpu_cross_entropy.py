@@ -231,3 +231,31 @@ def test_gradients_against_differences(B):
     a, b = dx.double() * sx, dw.double() * sw
     # 1e-6 of the terms: the gradients' bound above; h^2 of third derivatives (1e-10 times some hundreds) and the difference's 2^-52 / h are less
     assert abs(float(a.sum() + b.sum()) - slope) <= 2e-6 * float(a.abs().sum() + b.abs().sum())
+
+
+# Few rows of float data: sums of 32 channels, 16 multiplications each, joined one by one, are within the bound of a logit above; a gradient's sums, of the stretches of
+# a block's threads, the threads and the blocks, have vocab / 16 steps at most; dw's 16.
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 32, 33])
+@pytest.mark.parametrize("d,vocab", [(4, 3), (4, 20011), (68, 2100), (260, 64), (1100, 4097), (2052, 20011)])
+def test_few_rows_of_float_data(B, n, d, vocab):
+    c = Case(n, d, vocab, torch.float32, n + d, 5.0, pad=4, ignored=0.2)
+    c.t[-1] = c.t[-1].clamp_min(0)
+    if n > 2:
+        c.t[1] = -1
+        c.x[1] = float("nan")
+    check(c, B.cross_entropy(c.x, c.w, c.t))
+    loss, dx, dw = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss)
+    check(c, loss, dx, dw, c.d_loss)
+    again = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss)
+    assert torch.equal(again[0], loss) and torch.equal(again[1], dx) and torch.equal(again[2], dw)
+
+
+@pytest.mark.parametrize("n", [1, 7, 30])
+def test_few_rows_far_below_the_largest_logit(B, n):
+    """A row's columns lie with several blocks, which agree on another reference."""
+    c = Case(n, 128, 20011, torch.float32, 11, ignored=0.0)
+    c.x[: (n + 1) // 2] *= 300.0
+    check(c, B.cross_entropy(c.x, c.w, c.t))
+    loss, dx, dw = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss)
+    assert float(loss.max()) > 40
+    check(c, loss, dx, dw, c.d_loss)
