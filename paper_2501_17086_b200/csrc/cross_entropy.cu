@@ -330,24 +330,25 @@ constexpr int kRowThreads = 512;
 // A block a row, or a cluster of up to eight where there are few rows; each reads its columns once for the sum (twice where the target is far from the largest logit),
 // and once more for dz.  Instructions bound it, expf half of them; a row's exponentials held in registers in between took as long (1901 rows of 8111: 44 us, 49; 94
 // where a thread holds 64).
+template <bool kClusters>
 __global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p) {
   __shared__ float sums[kRowThreads / 32], mosts[kRowThreads / 32];
   __shared__ float2 blocks[2];
   chain_next();
   chain_wait();
-  const int shares = cluster_blocks(), share = cluster_block();
+  const int shares = kClusters ? cluster_blocks() : 1, share = kClusters ? cluster_block() : 0;
   const int64_t row = blockIdx.x / shares;
   const float* z = p.z + row * p.ldz;
   const bool first = threadIdx.x == 0 && share == 0;
   const int t = p.targets.column(row, p.vocab, first ? p.status : nullptr), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t from = ((int64_t)share * kRowThreads + threadIdx.x) * 4, step = (int64_t)shares * kRowThreads * 4;
+  const int from = (share * kRowThreads + (int)threadIdx.x) * 4, step = shares * kRowThreads * 4;
   const float zt = t >= 0 ? z[t] : 0.0f;
   float ref = isfinite(zt) ? zt : 0.0f, sum = 0.0f, most = -INFINITY;
   if (t >= 0) {
     for (int again = 0; again < 2; ++again) {
       sum = 0.0f;
 #pragma unroll 4
-      for (int64_t c = from; c < p.vocab; c += step) {
+      for (int c = from; c < p.vocab; c += step) {
         const float4 q = *reinterpret_cast<const float4*>(z + c);
         const float v[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p)
         sum += sums[k];
         most = fmaxf(most, mosts[k]);
       }
-      if (shares > 1) {  // (a place a turn: nobody waits for the others to have read)
+      if (kClusters) {  // (a place a turn: nobody waits for the others to have read)
         if (threadIdx.x == 0) blocks[again] = make_float2(sum, most);
         tc::cluster_sync();
         sum = 0.0f;
@@ -386,14 +387,14 @@ __global__ void __launch_bounds__(kRowThreads) logits_kernel(const LogitsData p)
       if (!(most - ref > kFar)) break;
       ref = most;
     }
-    if (shares > 1) tc::cluster_sync();  // (the others read this block's; and the target's logit may be written over)
+    if (kClusters) tc::cluster_sync();  // (the others read this block's; and the target's logit may be written over)
   }
   const bool at_target = zt == ref;
   const float total = sum + (at_target ? 1.0f : expf(zt - ref));
   if (first) p.loss[row] = t < 0 ? 0.0f : at_target ? log1pf(sum) : logf(total) - (zt - ref);
   if (!p.dz.p && !p.dz_f) return;
   const float factor = t < 0 ? 0.0f : (p.d_loss ? p.d_loss[row * p.d_loss_stride] : 1.0f) / total;
-  for (int64_t c = from; c < p.columns; c += step) {
+  for (int c = from; c < p.columns; c += step) {
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (factor != 0.0f && c < p.vocab) {
       const float4 q = *reinterpret_cast<const float4*>(z + c);
@@ -906,7 +907,7 @@ void run_few(Launcher& lc, const Call& c, const Plan& plan) {
   p.loss = c.loss;
   if (c.grads) p.dz_f = z;
   const int shares = logit_shares(n, v.vocab);
-  launch_chained(lc, logits_kernel, dim3((unsigned)(n * shares)), kRowThreads, 0, shares, p);
+  launch_chained(lc, shares > 1 ? logits_kernel<true> : logits_kernel<false>, dim3((unsigned)(n * shares)), kRowThreads, 0, shares, p);
   const FewSplit f(v.vocab, v.d, kFewBlocks);
   if (c.dx) {
     float* partial = (float*)(c.scratch + plan.partial);
@@ -955,7 +956,7 @@ bool run_f32(Launcher& lc, const Call& c, const Plan& plan, int* status) {
       p.dz = e;
     }
     const int shares = logit_shares(n, v.vocab);
-    launch_chained(lc, logits_kernel, dim3((unsigned)(n * shares)), kRowThreads, 0, shares, p);
+    launch_chained(lc, shares > 1 ? logits_kernel<true> : logits_kernel<false>, dim3((unsigned)(n * shares)), kRowThreads, 0, shares, p);
     if (c.dx) {
       PartsGemm b;
       b.M = (int)n; b.N = v.d; b.K = plan.chunk;
