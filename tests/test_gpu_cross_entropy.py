@@ -259,3 +259,49 @@ def test_few_rows_far_below_the_largest_logit(B, n):
     loss, dx, dw = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss)
     assert float(loss.max()) > 40
     check(c, loss, dx, dw, c.d_loss)
+
+
+@pytest.mark.parametrize("n", [6, 16])
+def test_few_rows_of_strided_outputs_parts_and_bad_rows(B, n):
+    c = Case(n, 132, 4500, torch.float32, 21, pad=12, ignored=0.0)
+    loss, dx, dw = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss)
+    a = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss, with_dw=False)
+    b = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss, with_dx=False)
+    assert a[2] is None and b[1] is None and torch.equal(a[1], dx) and torch.equal(b[2], dw)
+    out, wide = torch.full((n, 140), 5.0, device="cuda"), torch.full((4500, 140), 5.0, device="cuda")
+    B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss, dx=out[:, 4:136], dw=wide[:, 4:136])
+    assert torch.equal(out[:, 4:136], dx) and torch.equal(wide[:, 4:136], dw)
+    assert all(bool((t[:, :4] == 5).all() and (t[:, 136:] == 5).all()) for t in (out, wide))
+    x = c.x.clone()
+    x[2, 7] = float("nan")
+    others = torch.arange(n, device="cuda") != 2
+    bad = B.cross_entropy_gradients(x, c.w, c.t, d_loss=c.d_loss)
+    assert bool(bad[0][2].isnan()) and bool(bad[1][2].isnan().all()) and bool(bad[2].isnan().all())
+    assert torch.equal(bad[0][others], loss[others]) and torch.equal(bad[1][others], dx[others])
+    # a target beyond the vocabulary is none, and reported
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    c.t[2] = 4500
+    beyond = B.cross_entropy_gradients(x, c.w, c.t, d_loss=c.d_loss, status=status)
+    c.t[2] = -1
+    none = B.cross_entropy_gradients(x, c.w, c.t, d_loss=c.d_loss)
+    assert int(status) != 0 and all(torch.equal(p, q) for p, q in zip(beyond, none))
+    check(c, *none, c.d_loss)
+
+
+def test_few_rows_captured_and_replayed(B):
+    """Replays read what the tensors hold then."""
+    c, other = Case(9, 260, 20011, torch.float32, 31), Case(9, 260, 20011, torch.float32, 32)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss)
+    for source in (c, other):
+        c.x.copy_(source.x)
+        c.w.copy_(source.w)
+        c.t.copy_(source.t)
+        graph.replay()
+        check(c, *got, c.d_loss)
