@@ -787,7 +787,7 @@ int sm_count() {
   int& n = count.here();
   if (n == 0) {
     cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, current_device());
-    if (n <= 0) n = 1;
+    if (n < 2) n = 2;  // (no device: a launch says so; callers divide by pairs)
   }
   return n;
 }
