@@ -496,8 +496,9 @@ typedef struct {
  * dw [vocab][d] (OVERWRITTEN), float or, bf16 data, bf16 (dw_dtype); either may be NULL.  bf16: the probabilities' numerators and x times its row's
  * factor are rounded to bf16 as operands of products whose sums are float.  In one call, as two products less are formed than by a backward pass
  * of its own.  scratch: device memory, 256-byte aligned, not shared by calls that may overlap, of hbp_cross_entropy_scratch_bytes bytes, of
- * which the numerators of up to 4 GiB are the most, or less (HBP_ERR_WORKSPACE if it is too little for 256 rows at a time): the rows are then
- * taken in smaller pieces, and dw is added up over these in float. */
+ * which the numerators of up to 4 GiB are the most, or less (HBP_ERR_WORKSPACE if it is too little for 256 rows at a time): dx's sums are then
+ * split in fewer parts, or the rows taken in smaller pieces, and dw is added up over these in float.  What is enough for some number of rows is enough for
+ * any smaller one, of the same vocab and d. */
 hbp_status hbp_cross_entropy_scratch_bytes(const hbp_vocabulary* v, int32_t gradients, size_t* bytes);
 hbp_status hbp_cross_entropy(const hbp_vocabulary* v, float* loss, void* scratch, size_t scratch_bytes, void* cuda_stream);
 hbp_status hbp_cross_entropy_gradients(const hbp_vocabulary* v, const float* d_loss, int64_t d_loss_stride, float* loss, void* dx, int64_t lddx,

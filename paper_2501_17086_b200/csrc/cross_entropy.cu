@@ -661,6 +661,8 @@ __global__ void __launch_bounds__(256) sum_many_kernel(const float* in, int spli
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 int64_t plane_ld(int64_t cols) { return cols < 256 ? (cols + 15) / 16 * 16 : (cols + 63) / 64 * 64; }
 
+constexpr int kMostSplits = 32;  // of dx's contraction
+
 // How many ways dx's contraction over the vocabulary is split, so that its few tiles fill the waves of CTA pairs: 8192 rows of 768 channels are 96 tiles,
 // 1.3 waves that take the time of 2, and split in three 3.9 of 4.  In blocks of 64: a tile's own, 8 for its beginning and end, and the partial
 // sums, which cost what 8 bytes an element do (512 clocks a block; 3.4 bytes a clock and pair from memory).
@@ -670,7 +672,7 @@ int dx_splits(int64_t rows, int vocab, int d) {
   const double sums = 8.0 * (double)rows * d / (at_once * (pair ? 44.0 : 22.0) * 512);
   int best = 1;
   double least = 0;
-  for (int n = 1; n <= 32 && (n == 1 || blocks / n >= 8); ++n) {
+  for (int n = 1; n <= kMostSplits && (n == 1 || blocks / n >= 8); ++n) {
     const double cost = (double)((tiles * n + at_once - 1) / at_once) * ((blocks + n - 1) / n + 8) + (n > 1 ? n * sums + 10 : 0);
     if (n == 1 || cost < 0.97 * least) {
       best = n;
@@ -687,7 +689,7 @@ int dx_splits_f32(int64_t rows, int vocab, int d) {
   const int64_t m_tiles = (rows + 255) / 256, blocks = (vocab + 31) / 32;
   int best = 1;
   double least = 0;
-  for (int n = 1; n <= 32 && (n == 1 || blocks / n >= 16); ++n) {
+  for (int n = 1; n <= kMostSplits && (n == 1 || blocks / n >= 16); ++n) {
     double cost = 0;
     for (int w = 32; w <= 192; w += 32) {
       const int64_t tiles = m_tiles * ((d + w - 1) / w) * n;
@@ -709,7 +711,7 @@ int dx_splits_f32(int64_t rows, int vocab, int d) {
 bool few_rows(int64_t rows, bool grads) { return rows <= (grads ? 1 : 2) * kFewAtOnce; }
 constexpr int kFewBlocks = 4 * kPairs;  // of the gradients: two an SM
 
-// The scratch of pieces of `piece` rows.
+// The scratch of pieces of `piece` rows.  Without dx's partial sums it grows with the rows; with them it need not, as fewer rows have more splits.
 struct Plan {
   int64_t piece;
   bool few = false;
@@ -719,7 +721,8 @@ struct Plan {
   size_t target, zt, ref, factor, words, parts = 0, E = 0, xs = 0, partial = 0, dwf = 0, xp = 0, wp = 0, ep = 0;
   size_t bytes = 0;
   Planes x, w, e;  // float: strides alone
-  Plan(int dtype, int64_t rows, int vocab, int d, bool grads, bool dw_bf16, int64_t n) : piece(n) {
+  // n: rows of a piece; most: of dx's splits
+  Plan(int dtype, int64_t rows, int vocab, int d, bool grads, bool dx, bool dw_bf16, int64_t n, int most) : piece(n) {
     auto take = [&](size_t b) {
       const size_t at = bytes;
       bytes += up(b);
@@ -736,7 +739,7 @@ struct Plan {
       if (grads) {
         E = take((size_t)n * ldE * 2);
         xs = take((size_t)n * d * 2);
-        splits = dx_splits(n, vocab, d);
+        if (dx && most > 1) splits = std::min(most, dx_splits(n, vocab, d));
         if (splits > 1) partial = take((size_t)splits * n * d * 4);
         if (dw_bf16 && n < rows) dwf = take((size_t)vocab * d * 4);
       }
@@ -746,10 +749,10 @@ struct Plan {
     few = few_rows(rows, grads);
     if (few) {  // (its one piece)
       E = take((size_t)n * ldE * 4);
-      if (grads) partial = take((size_t)FewSplit(vocab, d, kFewBlocks).splits * n * d * 4);
+      if (grads && dx) partial = take((size_t)FewSplit(vocab, d, kFewBlocks).splits * n * d * 4);
       return;
     }
-    if (grads) splits = dx_splits_f32(n, vocab, d);
+    if (grads && dx && most > 1) splits = std::min(most, dx_splits_f32(n, vocab, d));
     chunk = splits > 1 ? ((vocab + splits - 1) / splits + 63) / 64 * 64 : vocab;
     x.ld = w.ld = plane_ld(d);
     e.ld = splits > 1 ? (int64_t)splits * chunk : plane_ld(vocab);
@@ -1012,13 +1015,17 @@ hbp_status call(Call& c, void* scratch, size_t bytes, void* stream) {
     return cudaMemset2DAsync(c.dw, c.lddw * es, 0, v.d * es, v.vocab, lc.stream) == cudaSuccess ? HBP_OK : HBP_ERR_CUDA;
   }
   int64_t n = wanted_piece(v.dtype, v.rows, v.vocab, c.grads);
-  auto plan_of = [&](int64_t piece) { return Plan(v.dtype, v.rows, v.vocab, v.d, c.grads, c.dw_bf16(), piece); };
+  auto plan_of = [&](int64_t piece, int most) { return Plan(v.dtype, v.rows, v.vocab, v.d, c.grads, c.dx != nullptr, c.dw_bf16(), piece, most); };
   if (!scratch || ((uintptr_t)scratch & 255u)) return HBP_ERR_WORKSPACE;
-  Plan plan = plan_of(n);
-  while (plan.bytes > bytes) {  // smaller pieces for less memory
+  Plan plan = plan_of(n, kMostSplits);
+  while (plan.bytes > bytes) {  // fewer splits for less memory (what is enough for more rows is then enough), then smaller pieces
+    if (plan.splits > 1) {
+      plan = plan_of(n, plan.splits - 1);
+      continue;
+    }
     if (n <= kLeastPiece) return HBP_ERR_WORKSPACE;
     n = (n / 2 + kLeastPiece - 1) / kLeastPiece * kLeastPiece;
-    plan = plan_of(n);
+    plan = plan_of(n, kMostSplits);
   }
   c.scratch = (uint8_t*)scratch;
   int* status = v.status ? v.status : (int*)(c.scratch + plan.words) + 1;
@@ -1037,7 +1044,7 @@ extern "C" hbp_status hbp_cross_entropy_scratch_bytes(const hbp_vocabulary* v, i
   const hbp_status st = check(v);
   if (st != HBP_OK) return st;
   const bool grads = gradients != 0;
-  *bytes = v->rows ? Plan(v->dtype, v->rows, v->vocab, v->d, grads, true, wanted_piece(v->dtype, v->rows, v->vocab, grads)).bytes : 0;
+  *bytes = v->rows ? Plan(v->dtype, v->rows, v->vocab, v->d, grads, true, true, wanted_piece(v->dtype, v->rows, v->vocab, grads), kMostSplits).bytes : 0;
   return HBP_OK;
 }
 
