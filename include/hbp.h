@@ -438,7 +438,7 @@ hbp_status hbp_embedding(int32_t dtype, int64_t rows, int32_t vocab, int32_t d, 
 /* d_table[v] = add[v] + scale * sum of d_out[i] over the rows i whose token is v: float [vocab][d], without gaps, as is add.  add NULL: zeros.
  * add may be d_table itself; rows of tokens that do not occur are then not touched (a table that is the vocabulary matrix too: the gradient of
  * hbp_cross_entropy_gradients is added to).  d_out: rows ldd apart (0: one row for all).  Rows are summed in float in a fixed order, by sorted tokens: runs agree bit
- * for bit.  rows up to 2^30.  scratch: device memory of hbp_embedding_gradient_scratch_bytes bytes, not shared by calls that may overlap. */
+ * for bit.  rows up to 2^30.  scratch: device memory of hbp_embedding_gradient_scratch_bytes bytes (enough for fewer rows too), not shared by calls that may overlap. */
 hbp_status hbp_embedding_gradient_scratch_bytes(int64_t rows, int32_t d, size_t* bytes);
 hbp_status hbp_embedding_gradient(int32_t dtype, int64_t rows, int32_t vocab, int32_t d, const void* tokens, int32_t token_bytes,
                                   const void* d_out, int64_t ldd, float scale, const float* add, float* d_table, void* scratch,

@@ -97,6 +97,7 @@ constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32
 constexpr int kAlone = 2048;
 // Sorted tokens a block adds up: 16, and more of more than 65536, whose longest runs would have too many parts to join.
 constexpr int kLeastTile = 16, kMostTile = 128;
+constexpr int64_t kTilesBefore = 4096;  // tiles there are before they grow
 
 struct SortParams {
   Tokens tokens;
@@ -434,15 +435,19 @@ bool bad_rows(const void* t, int64_t ld, int d, int v, bool input) { return ((ui
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 struct Scratch {
   size_t list, sums, bytes;  // of a list of the sorted tokens; of a list of partial sums; of all
+  size_t asked;              // of all, and as much as fewer rows take
   int tile;
   int64_t tiles;
   Scratch(int64_t rows, int d) {
-    for (tile = kLeastTile; tile < kMostTile && rows > 4096 * (int64_t)tile; tile *= 2) {
+    for (tile = kLeastTile; tile < kMostTile && rows > kTilesBefore * tile; tile *= 2) {
     }
     tiles = (rows + tile - 1) / tile;
     list = up((size_t)rows * 4);
     sums = up((size_t)tiles * d * 4);
     bytes = 4 * list + 2 * sums;
+    // (65537 rows have half the tiles that 65536 have: the most are those of the last number of rows that the smaller tiles are for)
+    const int64_t most = tile > kLeastTile && tiles < kTilesBefore ? kTilesBefore : tiles;
+    asked = 4 * list + 2 * up((size_t)most * d * 4);
   }
 };
 
@@ -482,7 +487,7 @@ extern "C" hbp_status hbp_embedding(int32_t dtype, int64_t rows, int32_t vocab, 
 extern "C" hbp_status hbp_embedding_gradient_scratch_bytes(int64_t rows, int32_t d, size_t* bytes) {
   if (!bytes) return HBP_ERR_INVALID_ARG;
   if (rows < 0 || rows > kMostRows || d <= 0) return HBP_ERR_SHAPE;
-  *bytes = Scratch(rows, d).bytes;
+  *bytes = Scratch(rows, d).asked;
   return HBP_OK;
 }
 

@@ -42,3 +42,32 @@ def test_scratch_of_many_rows_is_enough_for_fewer():
     env = {**os.environ, "CUDA_VISIBLE_DEVICES": "", "PYTHONPATH": ROOT}
     done = subprocess.run([sys.executable, "-c", CROSS_ENTROPY], env=env, capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr[-2000:]
+
+
+EMBEDDING_GRADIENT = """
+import ctypes as C
+import torch
+from paper_2501_17086_b200 import binding as B
+assert torch.cuda.device_count() == 0
+P, CUDA = 0x10000, 7
+def size(n, d):
+    need = C.c_size_t()
+    assert B.lib.hbp_embedding_gradient_scratch_bytes(n, d, C.byref(need)) == 0
+    return need.value
+ends = [1 << 16, 1 << 17, 1 << 18, 1 << 19, 1 << 20]
+rows = sorted({*range(0, 300), *range(300, 1 << 20, 4099), *ends, *(n + 1 for n in ends), *(n - 1 for n in ends), 1 << 30})
+for d in (8, 24, 768, 8192):
+    sizes = [size(n, d) for n in rows]
+    assert sizes == sorted(sizes), d
+    for n, more in zip(rows, sizes[1:]):
+        if n:
+            assert B.lib.hbp_embedding_gradient(1, n, 1000, d, P, 8, P, d, 1.0, None, P, P, more, None, None) == CUDA, (n, d)
+"""
+
+
+def test_scratch_of_many_tokens_is_enough_for_fewer():
+    from paper_2501_17086_b200.build import build_library
+    build_library()
+    env = {**os.environ, "CUDA_VISIBLE_DEVICES": "", "PYTHONPATH": ROOT}
+    done = subprocess.run([sys.executable, "-c", EMBEDDING_GRADIENT], env=env, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
