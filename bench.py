@@ -58,14 +58,14 @@ def config_of(w, k, touched_bytes=None):
 # profiles/.  An entry is used only while the kernel's sources still hash to the value recorded with the capture and
 # the workload has the captured shapes; otherwise the bench line carries "traffic": null.
 TRAFFIC = {
-    # gemm_tc_kernel, VJP pair (dA + dY): c5_small (4 layers x 16384 tokens): 2173.215 + 1055.258 and 2795.633 + 279.751 MB;
-    # c2_small (8 layers x 8192 tokens): 738.724 + 504.356 and 791.332 + 127.611 MB
+    # gemm_tc_kernel, VJP pair (dA + dY): c5_small (4 layers x 16384 tokens): 2264.449 + 1054.863 and 3119.740 + 280.220 MB;
+    # c2_small (8 layers x 8192 tokens): 738.993 + 503.645 and 795.009 + 128.615 MB
     "gemm_vjp": [
-        {"sources": ("gemm_tc.cu", "tc_common.cuh"), "sha256": "955801bc2fc09540", "shape": ("preln_mlp", "bf16", 2048, 8192),
-         "bytes_per_token_layer": (2173.215e6 + 1055.258e6 + 2795.633e6 + 279.751e6) / (4 * 16384),
+        {"sources": ("gemm_tc.cu", "tc_common.cuh"), "sha256": "cc41676afd347564", "shape": ("preln_mlp", "bf16", 2048, 8192),
+         "bytes_per_token_layer": (2264.449e6 + 1054.863e6 + 3119.740e6 + 280.220e6) / (4 * 16384),
          "profile": "profiles/gemm_tc_kernel_c5_small.md"},
-        {"sources": ("gemm_tc.cu", "tc_common.cuh"), "sha256": "955801bc2fc09540", "shape": ("preln_mlp", "bf16", 1024, 4096),
-         "bytes_per_token_layer": (738.724e6 + 504.356e6 + 791.332e6 + 127.611e6) / (8 * 8192),
+        {"sources": ("gemm_tc.cu", "tc_common.cuh"), "sha256": "cc41676afd347564", "shape": ("preln_mlp", "bf16", 1024, 4096),
+         "bytes_per_token_layer": (738.993e6 + 503.645e6 + 795.009e6 + 128.615e6) / (8 * 8192),
          "profile": "profiles/gemm_tc_kernel_c2_small.md"}],
     # scan_depth_lnstat_kernel: c5_small 605.050 MB read + 213.970 MB written for 4 steps x 16384 x 2048 elements; c2_small
     # 286.283 + 80.576 MB for 8 x 8192 x 1024 (the writes still in L2 when such a small launch ends are not in the counter)

@@ -25,7 +25,7 @@ enum Epilogue {
   // D = exp(acc - row_f[m]), 0 at n = target[m] and in rows without a target (bf16); row_parts.  Without D: row_parts alone, their sums those of
   // exp(acc - largest).  (gemm_tc only)
   EPI_EXP = 9,
-  EPI_ROWS = 10,       // D = acc * row_f[m], 0 where that is 0 (gemm_tc only)
+  EPI_ROWS = 10,       // D = acc * row_f[m], 0 where that is 0 (bf16; gemm_tc only)
   EPI_RNN_FWD = 5,   // c = tanh(acc + E[m,n]);  D2 = 1 - c^2;  D = gate[n] * E2[m,n] + c
 };
 
