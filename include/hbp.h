@@ -477,7 +477,8 @@ hbp_status hbp_norm_residual_backward(const hbp_norm* n, const hbp_rows* d_y, co
                                       void* scratch, size_t scratch_bytes, void* cuda_stream);
 
 /* Hidden states x [rows][d] (rows ldx apart) and a vocabulary matrix w [vocab][d] (ldw), both of dtype, and each row's target.  The logits
- * z = x w^T, float sums of exact products (float data: of all but 2^-26 of them), are never in memory as such. */
+ * z = x w^T are float sums of exact products (float data: of all but 2^-26 of them).  The forward pass of bf16 data holds none of them in memory; with gradients, 2 bytes for
+ * each of a piece of the rows; float data, 4 (with gradients 10 beyond 16 rows): see the scratch below. */
 typedef struct {
   int32_t dtype, vocab, d, target_bytes;
   int64_t rows;
@@ -491,14 +492,19 @@ typedef struct {
 
 /* loss[i] = log(sum_j exp(z_ij)) - z_i,target (float; 0 where there is no target, whatever x holds there), to its last digits however small it is: it is
  * formed without the difference.  A row that has a target and holds a value that is not finite makes its own loss NaN (or infinite) and with it its dx and all of
- * dw; one of w does so to every row.
+ * dw; one of w does so to every row, but that an infinity which makes a logit -infinity may leave that row's loss as it is.
  * With gradients of sum_i d_loss[i * d_loss_stride] * loss[i] (d_loss float on the device, NULL: ones): dx [rows][d] of dtype (0 where there is no target) and
  * dw [vocab][d] (OVERWRITTEN), float or, bf16 data, bf16 (dw_dtype); either may be NULL.  bf16: the probabilities' numerators and x times its row's
- * factor are rounded to bf16 as operands of products whose sums are float.  In one call, as two products less are formed than by a backward pass
- * of its own.  scratch: device memory, 256-byte aligned, not shared by calls that may overlap, of hbp_cross_entropy_scratch_bytes bytes, of
- * which the numerators of up to 4 GiB are the most, or less (HBP_ERR_WORKSPACE if it is too little for 256 rows at a time): dx's sums are then
- * split in fewer parts, or the rows taken in smaller pieces, and dw is added up over these in float.  What is enough for some number of rows is enough for
- * any smaller one, of the same vocab and d. */
+ * factor are rounded to bf16 as operands of products whose sums are float.  In one call, as one product less is formed than by a loss and a backward pass
+ * of its own.
+ * scratch: device memory, 256-byte aligned, not shared by calls that may overlap, of hbp_cross_entropy_scratch_bytes bytes:
+ *   - for each row and token: bf16 2 bytes (the numerators) with gradients, else 1/8; float 10 (logits; their gradients in three bf16 parts) with gradients, else 4.  4 GiB
+ *     at most, or what 256 rows take if that is more: the rows are taken in pieces;
+ *   - bf16, with gradients: 2 d bytes a row of a piece; up to 32 partial sums of dx, 4 d bytes a row each; of several pieces, 4 d vocab bytes for a bf16 dw;
+ *   - float: 6 d bytes a row of a piece and a token, and the partial sums; up to 16 rows (32 without gradients) 4 bytes for each row and token instead of all that, and with gradients partial
+ *     sums of 4 d bytes for each row and (at most) 64 tokens.
+ * With less than that many bytes dx is summed up in fewer parts, then the rows are taken in smaller pieces, dw being added up over these in float; HBP_ERR_WORKSPACE if
+ * it is too little for 256 rows at a time.  What is enough for some number of rows is enough for any smaller one, of the same vocab and d. */
 hbp_status hbp_cross_entropy_scratch_bytes(const hbp_vocabulary* v, int32_t gradients, size_t* bytes);
 hbp_status hbp_cross_entropy(const hbp_vocabulary* v, float* loss, void* scratch, size_t scratch_bytes, void* cuda_stream);
 hbp_status hbp_cross_entropy_gradients(const hbp_vocabulary* v, const float* d_loss, int64_t d_loss_stride, float* loss, void* dx, int64_t lddx,

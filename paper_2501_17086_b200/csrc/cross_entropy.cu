@@ -1,5 +1,6 @@
 // Softmax cross entropy of hidden states x [rows][d] against a vocabulary matrix w [vocab][d] (hbp_cross_entropy), and with its
-// gradients (hbp_cross_entropy_gradients).  z = x w^T is never in memory as such.
+// gradients (hbp_cross_entropy_gradients).  z = x w^T is not in memory with bf16 data, whose gradients keep a number of 2 bytes a logit instead; float logits are, of a
+// piece of the rows.
 //
 // With t a row's target and r a number near its largest logit, e_j = exp(z_j - r):
 //   S' = sum over j != t of e_j,   S = S' + e_t,   loss = log(S) - (z_t - r),   dz_j = g e_j / S (j != t),   dz_t = -g S' / S

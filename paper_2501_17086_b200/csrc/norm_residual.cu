@@ -389,7 +389,7 @@ struct Kept {
 };
 
 // Rows are on their way up to three before they are used, as in the forward pass (16384 x 2048 bf16, both norms and a gate: loaded when they are used 171 us, ahead 118,
-// where the bytes take 72).  Then it is the instructions, 76 a channel, and the way of a row through its sums, two or three that wait for all of its warps: 16
+// where the bytes take 72).  Then it is the instructions, 76 a channel then and 59 now, and the way of a row through its sums, two or three that wait for all of its warps: 16
 // channels a thread instead of 8 halve what a row costs beside its channels, pointers walk along with the rows, lanes share the warps' sums; and four rows are
 // under way an SM where weights of bf16 rows are read from shared memory again instead of holding registers (208 of these: 122 us): 103 us.  float: values that are
 // used again stay in registers, 6.2 TB/s.  Groups walk over the rows, a grid apart.
