@@ -45,3 +45,18 @@ def test_scratch_may_hold_anything(B, dtype, n, d, vocab):
         got.append(B.cross_entropy(c.x, c.w, c.t, scratch=scratch))
         first = first or got
         assert all(torch.equal(p, q) for p, q in zip(first, got)), fill
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_pieces_with_rows_far_below_the_largest_logit(B, dtype):
+    """Each piece has some, but the last; nothing behind the scratch is written."""
+    c = Case(1100, 128, 2003, dtype, 47)
+    c.x[:900:3] *= 300.0
+    size = B.cross_entropy_scratch_bytes(dtype, 256, 2003, 128) + 4 * 2003 * 128 + 256
+    scratch = torch.full((size + 4096,), 255, dtype=torch.uint8, device="cuda")
+    for dw_dtype in {torch.float32, dtype}:
+        got = B.cross_entropy_gradients(c.x, c.w, c.t, d_loss=c.d_loss, dw_dtype=dw_dtype, scratch=scratch[:size])
+        assert float(got[0].max()) > 60
+        check(c, *got, c.d_loss)
+    check(c, B.cross_entropy(c.x, c.w, c.t, scratch=scratch[:size]))
+    assert bool((scratch[size:] == 255).all())
